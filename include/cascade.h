@@ -43,7 +43,10 @@ extern "C" {
 #define CASCADE_ERR_UNSUPPORTED_SHAPE (-4) /* shape outside what the kernels handle (see cascade_shape) */
 #define CASCADE_ERR_CUDA (-5)              /* a CUDA runtime / driver call failed                      */
 #define CASCADE_ERR_TIMEOUT (-6)           /* a bounded device-side wait gave up (see cascade_check)   */
-#define CASCADE_ERR_OVERFLOW (-7)          /* cascade_kv_append: a cache has no room (see cascade_check) */
+#define CASCADE_ERR_OVERFLOW (-7)          /* cascade_kv_append, cascade_paged_tables: a cache or its page pool has
+                                              no room (see cascade_check)                                */
+#define CASCADE_ERR_BAD_PAGE (-8)          /* a paged call met a page, slot or length outside what it was given
+                                              (found on the device, see cascade_check)                   */
 
 /* ---- enums ------------------------------------------------------------------------------------- */
 #define CASCADE_F32 0
@@ -102,8 +105,8 @@ int cascade_destroy(cascade_ctx* ctx);
 int64_t cascade_workspace_bytes(const cascade_ctx* ctx);
 
 /* Reads the context's device-side error word (set when a bounded wait inside a kernel ran out) after
- * synchronising `stream`.  Returns CASCADE_OK, CASCADE_ERR_TIMEOUT, CASCADE_ERR_BAD_TREE, CASCADE_ERR_OVERFLOW or
- * CASCADE_ERR_CUDA, and clears the word. */
+ * synchronising `stream`.  Returns CASCADE_OK, CASCADE_ERR_TIMEOUT, CASCADE_ERR_BAD_TREE, CASCADE_ERR_BAD_PAGE,
+ * CASCADE_ERR_OVERFLOW or CASCADE_ERR_CUDA, and clears the word. */
 int cascade_check(cascade_ctx* ctx, void* stream);
 
 /* Number of kernels the most recent call on this context enqueued. */
@@ -397,6 +400,107 @@ int cascade_kv_append(cascade_ctx* ctx, const cascade_tree* tree, int32_t n_laye
  * Errors: CASCADE_ERR_INVALID_ARG (null pointers, n_rows < 1, top_k < 0, top_p outside (0, 1]). */
 int cascade_filter_logits(cascade_ctx* ctx, float* logits, int32_t n_rows, int32_t top_k, float top_p,
                           int32_t* kept_count, void* stream);
+
+/* ---- prompts: a paged KV cache ------------------------------------------------------------------- */
+/* A verification step reads a prefix cache; these calls fill one and read it while a prompt is taken in, chunk by
+ * chunk and for many requests of different lengths at once (the paper treats the prompt's pass as given).  The cache
+ * is a pool of pages; a request's token at position x lives in page block_table[r][x / page_size] at row
+ * x % page_size.  The dense prefix cache of cascade_verify_step ([R,prefix_cap,Hkv,D]) is the special case
+ * n_pages = R * prefix_cap / page_size, block_table[r][i] = r * (prefix_cap / page_size) + i: prompts written through
+ * these calls into such a pool can be verified against without a copy.
+ *   k_pages, v_pages [n_pages,page_size,Hkv,D] elem, page p starting page_stride elements after page p - 1
+ *              (page_stride >= page_size*Hkv*D; larger where keys and values of a page lie side by side in one pool);
+ *              16-byte aligned, page_stride a multiple of 16 bytes
+ *   page_size  a multiple of 8; n_pages * page_size < 2^31
+ *   block_table [n_req,table_stride] int32, DEVICE.  Entries behind a request's last page are never used.
+ * Device-resident lengths, pages and slots cannot be checked on the host.  A kernel that meets one outside its range
+ * leaves it out, touches nothing outside the buffers it was given, and cascade_check returns CASCADE_ERR_BAD_PAGE.
+ * All four calls allocate nothing, take their sizes from host arguments alone and can be recorded into a CUDA graph.
+ * The context must have been created on the current device (CASCADE_ERR_INVALID_ARG otherwise). */
+typedef struct {
+  void* k_pages;
+  void* v_pages;
+  int64_t page_stride;
+  int32_t n_pages, page_size;
+  const int32_t* block_table;
+  int32_t table_stride;
+} cascade_paged_cache;
+
+/* Block tables and slot map of the next pass, from the requests' lengths, in one kernel.
+ *   new_len [n_req]: how many tokens request r appends; negative: the request is finished and gives its pages back.
+ *   kv_len [n_req]: tokens it holds.  free_pages [n_pages], free_count [1]: a stack of free page ids, its top at
+ *   free_pages[free_count - 1].
+ * First the pages of finished requests are pushed, in request order and each table's order; then the pages that the
+ * others need (ceil((kv_len + new_len) / page_size) - ceil(kv_len / page_size) each) are popped one by one in the same
+ * order and written behind the pages each has.  Outputs:
+ *   block_table (updated in place: only entries behind a request's old pages are written), free_pages (pushed entries),
+ *   free_count_out [1], kv_len_out [n_req] (kv_len + new_len, 0 if finished) -- may be the same arrays as free_count and
+ *   kv_len; apart from that no two arguments may overlap;
+ *   q_begin [n_req+1]: request r's new tokens are rows q_begin[r] .. q_begin[r+1]-1 of the pass;
+ *   slot, pos [n_tok]: page * page_size + row, and the position in the request, of every new token; -1 in the rows
+ *   behind the last one (n_tok is the padded row count of the pass).
+ * A negative kv_len, lengths that pass the table's width or n_tok, a pool that runs out or over: nothing is taken or
+ * given back -- kv_len_out and free_count_out repeat the inputs, q_begin is all 0, slot and pos all -1, so that what is
+ * enqueued behind does nothing -- and cascade_check returns CASCADE_ERR_OVERFLOW.  A token whose page id is outside
+ * the pool gets slot -1 (CASCADE_ERR_BAD_PAGE).
+ * 1 <= n_req <= CASCADE_MAX_REQUESTS; n_tok >= 0.  All arrays int32, DEVICE. */
+#define CASCADE_MAX_REQUESTS 4096
+int cascade_paged_tables(cascade_ctx* ctx, int32_t n_req, int32_t n_tok, int32_t page_size, int32_t n_pages,
+                         const int32_t* new_len, const int32_t* kv_len, int32_t* block_table, int32_t table_stride,
+                         int32_t* free_pages, const int32_t* free_count, int32_t* kv_len_out, int32_t* free_count_out,
+                         int32_t* q_begin, int32_t* slot, int32_t* pos, void* stream);
+
+/* Writes the keys and values of a pass into their slots, rotary embedding included (half-split pairing: element i
+ * turns with element i + D/2 by pos * rope_base^(-2i/D), as cascade_verify_step rotates tree rows).
+ *   k, v [n_tok,Hkv,D] elem, rows k_stride / v_stride elements apart (>= Hkv*D: parts of a stacked projection);
+ *   q [n_tok,Hq,D] rows q_stride apart -> q_out rows q_out_stride apart, rotated; q_out may be q (same stride).
+ *   q = q_out = NULL: keys and values only.  rope_base = 0: no rotation (then q has to be NULL).
+ *   slot, pos [n_tok] int32 from cascade_paged_tables; a row with slot -1 is left out (its q_out row too).  No two rows
+ *   may name the same slot.  pos >= 0 for the others.
+ * block_table is not used.  All bases 16-byte aligned, strides multiples of 16 bytes. */
+int cascade_paged_append(cascade_ctx* ctx, const cascade_paged_cache* cache, int32_t n_tok, const void* q, int64_t q_stride,
+                         const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* slot,
+                         const int32_t* pos, float rope_base, void* q_out, int64_t q_out_stride, void* stream);
+
+/* Attention of the new tokens of every request over its pages.  Row i of request r (q row q_begin[r] + i) stands at
+ * position x = kv_len[r] - (q_begin[r+1] - q_begin[r]) + i, the keys of the pass being in the cache already, and sees key
+ * j iff j <= x and (window == 0 or j > x - window or j < sinks):
+ *     out[row,head,:] = sum_j softmax_j(softmax_scale * <q[row,head,:], k_j>) v_j ;   lse[row,head] = log sum_j exp(...)
+ * Query head `head` reads kv head head / (Hq / Hkv).  A row that sees no key (kv_len smaller than its new tokens) gets
+ * zeros and lse -inf.  What lies at keys a row does not see, NaN and infinities included, does not reach it.
+ *   q [n_tok,Hq,D] elem, rows q_stride apart; out [n_tok,Hq,D] elem, dense; lse [n_tok,Hq] float or NULL
+ *   q_begin [n_req+1], kv_len [n_req] int32, DEVICE: as cascade_paged_tables leaves them.  Rows of q behind
+ *   q_begin[n_req] are not read, the same rows of out and lse not written.
+ *   max_q, max_kv: no request has more new tokens / keys than this (host bounds that launch sizes come from; a
+ *   request beyond them is left out, CASCADE_ERR_BAD_PAGE).  1 <= n_req <= CASCADE_MAX_REQUESTS.
+ *   window >= 0 (0: none), sinks >= 0.  Softmax and accumulation are fp32. */
+int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* cache, int32_t n_req, int32_t n_tok, const void* q,
+                       int64_t q_stride, const int32_t* q_begin, const int32_t* kv_len, int32_t max_q, int32_t max_kv,
+                       int32_t window, int32_t sinks, float softmax_scale, void* out, float* lse, void* stream);
+
+/* ---- one token a row ------------------------------------------------------------------------------- */
+/* Draws a token from every row of logits (a drafter's proposals, or plain decoding), with the truncations of
+ * cascade_filter_logits and the min-p rule applied on the fly; the logits are only read.  With m the row's largest
+ * logit and w[v] = exp((logits[v] - m) / temperature):
+ *   top_k (0 < k < V): keep logits >= the k-th largest (ties stay);
+ *   top_p (< 1): of those keep a token iff the mass of the tokens with a strictly larger logit is < top_p of the mass of
+ *     what top_k kept (the largest always stays);
+ *   min_p (> 0): of those keep w[v] >= min_p;
+ *   token = the first v whose cumulative kept weight exceeds uniforms[row] * (total kept weight);
+ *   prob  = w[token] / (total kept weight) -- what Algorithm 2 wants as draft_p;   kept = how many tokens remained.
+ * temperature <= 0: the largest logit, lowest index first, prob 1, kept 1.  A logit of -inf or NaN is never kept; one of
+ * +inf weighs 1 against 0 for every finite one.  A row without any logit to keep: token -1, prob 0, kept 0.
+ *   logits [n_rows,V] float (logits_dtype CASCADE_F32) or bf16 (CASCADE_BF16), rows row_stride elements apart, V from the
+ *   context; aligned to its element.  uniforms [n_rows] float in [0,1) (larger counts as the largest float below 1,
+ *   negative and NaN as 0).
+ *   temperature, top_p, min_p [n_rows] float, top_k [n_rows] int32, DEVICE, or NULL: 1 / off / off / off for all rows.
+ *     Per row, off is top_k <= 0 or >= V, top_p >= 1 or NaN, min_p <= 0 or NaN; a NaN temperature counts as 0, +inf
+ *     weighs all finite logits alike; min_p above 1 counts as 1.
+ *   token_out [n_rows] int32; prob_out [n_rows] float or NULL; kept_out [n_rows] int32 or NULL.
+ * Weights are formed in 64 bits and summed in fixed point, so the draw does not depend on the order of additions. */
+int cascade_sample(cascade_ctx* ctx, const void* logits, int32_t logits_dtype, int64_t row_stride, int32_t n_rows,
+                   const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                   const float* uniforms, int32_t* token_out, float* prob_out, int32_t* kept_out, void* stream);
 
 /* ---- the drafter's training loss (outside the verification step) ---------------------------------- */
 /* Section 4.3, Eq. 4: the soft cross-entropy between the target distribution and the drafter's at every position k

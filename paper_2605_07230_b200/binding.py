@@ -17,11 +17,12 @@ LIB_PATH = os.path.join(_HERE, "libcascade.so")
 
 OK = 0
 ERR_INVALID_ARG, ERR_BAD_TREE, ERR_WORKSPACE, ERR_UNSUPPORTED_SHAPE, ERR_CUDA, ERR_TIMEOUT = -1, -2, -3, -4, -5, -6
-ERR_OVERFLOW = -7
+ERR_OVERFLOW, ERR_BAD_PAGE = -7, -8
 F32, BF16 = 0, 1
 USE_I, USE_C, CONV_DIST_SELF = 1, 2, 4
 SELECT_LONGEST, SELECT_FIRST_ACCEPT = 0, 1
 KERNEL_COUNT = 32
+MAX_REQUESTS = 4096
 
 EXPORTS = [
     "cascade_create", "cascade_destroy", "cascade_workspace_bytes", "cascade_check", "cascade_last_launch_count",
@@ -31,6 +32,7 @@ EXPORTS = [
     "cascade_verify_step_host", "cascade_accept_static", "cascade_bonus_token", "cascade_kv_append",
     "cascade_filter_logits", "cascade_set_wait_limit", "cascade_wait_probe",
     "cascade_tree_update_device", "cascade_tree_download", "cascade_drafter_loss",
+    "cascade_paged_tables", "cascade_paged_append", "cascade_paged_attn", "cascade_sample",
 ]
 
 
@@ -63,6 +65,11 @@ class Step(C.Structure):
         ("hidden_out", C.c_void_p), ("k_tree_out", C.c_void_p), ("v_tree_out", C.c_void_p),
         ("top_k", C.c_int32), ("top_p", C.c_float),
     ]
+
+
+class PagedCacheStruct(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_stride", C.c_int64), ("n_pages", C.c_int32),
+                ("page_size", C.c_int32), ("block_table", C.c_void_p), ("table_stride", C.c_int32)]
 
 
 _lib = None
@@ -110,6 +117,12 @@ def lib() -> C.CDLL:
         L.cascade_tree_update_device.argtypes = [vp, C.c_int32, C.c_int32, C.c_int32, vp, vp]
         L.cascade_tree_download.argtypes = [vp, vp, vp, vp, vp, vp]
         L.cascade_drafter_loss.argtypes = [vp, vp, vp, C.c_int32, C.c_int32, C.c_int32, C.c_float, C.c_float, vp, vp, vp, vp]
+        i32, i64, f32 = C.c_int32, C.c_int64, C.c_float
+        cache = C.POINTER(PagedCacheStruct)
+        L.cascade_paged_tables.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.cascade_paged_append.argtypes = [vp, cache, i32, vp, i64, vp, i64, vp, i64, vp, vp, f32, vp, i64, vp]
+        L.cascade_paged_attn.argtypes = [vp, cache, i32, i32, vp, i64, vp, vp, i32, i32, i32, i32, f32, vp, vp, vp]
+        L.cascade_sample.argtypes = [vp, vp, i32, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         L.cascade_set_wait_limit.argtypes = [vp, C.c_int64]
         L.cascade_wait_probe.argtypes = [vp, vp, vp]
         _lib = L
@@ -362,3 +375,131 @@ def cascade_drafter_loss(target_logits, draft_logits, feat, tau_seq, c, loss_out
     _check(lib().cascade_drafter_loss(_ptr(target_logits), _ptr(draft_logits), _ptr(feat), K, V, feat.shape[-1],
                                       float(tau_seq), float(c), _ptr(loss_out), _ptr(weight_out), _ptr(total_out),
                                       _stream()))
+
+
+# ---- paged cache and sampling -----------------------------------------------------------------------------------------
+# These calls sit in a decode loop where a launch lasts a few microseconds, so their checks stay short.
+
+
+def _elem(ctx):
+    return torch.bfloat16 if ctx.shape.dtype == BF16 else torch.float32
+
+
+def _vectors(dtype, n, **tensors):
+    """Dense tensors of n elements (None: not given)."""
+    for name, t in tensors.items():
+        if t is not None and (t.dtype != dtype or t.shape != (n,) or not t.is_contiguous()):
+            raise ValueError(f"{name}: expected a dense {dtype} tensor of {n} elements, got {t.dtype} {tuple(t.shape)}")
+
+
+def _rows(name, t, n, heads, D, dtype):
+    """Row stride of a [n,heads,D] tensor whose rows may lie apart (a part of a stacked projection)."""
+    if t.dtype != dtype or t.shape != (n, heads, D):
+        raise ValueError(f"{name}: expected {dtype} {(n, heads, D)}, got {t.dtype} {tuple(t.shape)}")
+    st = t.stride()
+    if st[2] != 1 or (heads > 1 and st[1] != D):
+        raise ValueError(f"{name}: heads and their elements must be dense, strides are {st}")
+    return heads * D if n == 1 else st[0]
+
+
+def _on_device(*tensors):
+    """Every tensor given lives on the current device."""
+    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"a tensor lives on {t.device}, not on the current CUDA device")
+
+
+class PagedCache:
+    """A cascade_paged_cache over [n_pages,page_size,Hkv,D] pools (pages may lie apart) and an int32 block table."""
+
+    def __init__(self, k_pages, v_pages, block_table):
+        if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or k_pages.dtype != v_pages.dtype:
+            raise ValueError("k_pages and v_pages must be [n_pages, page_size, Hkv, D] of one type and shape")
+        n_pages, page, Hkv, D = k_pages.shape
+        for t in (k_pages, v_pages):
+            if t.stride(3) != 1 or (Hkv > 1 and t.stride(2) != D) or (page > 1 and t.stride(1) != Hkv * D):
+                raise ValueError("the rows of a page must be dense")
+        if n_pages > 1 and k_pages.stride(0) != v_pages.stride(0):
+            raise ValueError("k_pages and v_pages must have the same page stride")
+        if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.stride(1) != 1:
+            raise ValueError("block_table must be int32 [n_req, width] with dense rows")
+        self.k_pages, self.v_pages, self.block_table = k_pages, v_pages, block_table
+        self.dtype, self.heads, self.n_req = k_pages.dtype, (Hkv, D), block_table.shape[0]
+        stride = k_pages.stride(0) if n_pages > 1 else page * Hkv * D
+        width = block_table.shape[1] if self.n_req == 1 else block_table.stride(0)
+        self.struct = PagedCacheStruct(k_pages.data_ptr(), v_pages.data_ptr(), stride, n_pages, page,
+                                       block_table.data_ptr(), width)
+
+    def _check(self, ctx):
+        sh = ctx.shape
+        if self.dtype != _elem(ctx) or self.heads != (sh.Hkv, sh.D):
+            raise ValueError("the pool's element type, key heads or head size are not the context's")
+
+
+def cascade_paged_tables(ctx, page_size, n_pages, new_len, kv_len, block_table, free_pages, free_count, kv_len_out,
+                         free_count_out, q_begin, slot, pos):
+    """Block tables, slot map and positions of the next pass; int32 device tensors (see include/cascade.h)."""
+    n_req, n_tok, i32 = new_len.shape[0], slot.shape[0], torch.int32
+    _vectors(i32, n_req, new_len=new_len, kv_len=kv_len, kv_len_out=kv_len_out)
+    _vectors(i32, n_pages, free_pages=free_pages)
+    _vectors(i32, 1, free_count=free_count, free_count_out=free_count_out)
+    _vectors(i32, n_req + 1, q_begin=q_begin)
+    _vectors(i32, n_tok, slot=slot, pos=pos)
+    if block_table.dtype != i32 or block_table.dim() != 2 or block_table.shape[0] != n_req or not block_table.is_contiguous():
+        raise ValueError(f"block_table: expected a dense int32 tensor of {n_req} rows")
+    _on_device(new_len, kv_len, block_table, free_pages, free_count, kv_len_out, free_count_out, q_begin, slot, pos)
+    _check(lib().cascade_paged_tables(ctx.handle, n_req, n_tok, page_size, n_pages, new_len.data_ptr(), kv_len.data_ptr(),
+                                      block_table.data_ptr(), block_table.shape[1], free_pages.data_ptr(), free_count.data_ptr(),
+                                      kv_len_out.data_ptr(), free_count_out.data_ptr(), q_begin.data_ptr(),
+                                      slot.data_ptr() if n_tok else None, pos.data_ptr() if n_tok else None, _stream()))
+
+
+def cascade_paged_append(ctx, cache, k, v, slot, pos, rope_base=0.0, q=None, q_out=None):
+    """Keys and values [n_tok,Hkv,D] (rotated unless rope_base is 0) into their slots; queries [n_tok,Hq,D] rotated."""
+    cache._check(ctx)
+    sh, e, n = ctx.shape, cache.dtype, slot.shape[0]
+    _vectors(torch.int32, n, slot=slot, pos=pos)
+    ks, vs = _rows("k", k, n, sh.Hkv, sh.D, e), _rows("v", v, n, sh.Hkv, sh.D, e)
+    qs = 0 if q is None else _rows("q", q, n, sh.Hq, sh.D, e)
+    qos = 0 if q_out is None else _rows("q_out", q_out, n, sh.Hq, sh.D, e)
+    _on_device(cache.k_pages, cache.v_pages, k, v, slot, pos, q, q_out)
+    _check(lib().cascade_paged_append(ctx.handle, C.byref(cache.struct), n, None if q is None else q.data_ptr(), qs,
+                                      k.data_ptr(), ks, v.data_ptr(), vs, slot.data_ptr(), pos.data_ptr(), rope_base,
+                                      None if q_out is None else q_out.data_ptr(), qos, _stream()))
+
+
+def cascade_paged_attn(ctx, cache, q, q_begin, kv_len, max_q, max_kv, out, softmax_scale, window=0, sinks=0, lse=None):
+    """Causal attention of each request's new tokens over its pages, optionally through a window beside sink tokens."""
+    cache._check(ctx)
+    sh, e, n_req, n = ctx.shape, cache.dtype, kv_len.shape[0], q.shape[0]
+    _vectors(torch.int32, n_req + 1, q_begin=q_begin)
+    _vectors(torch.int32, n_req, kv_len=kv_len)
+    if cache.n_req < n_req:
+        raise ValueError(f"block_table has {cache.n_req} rows for {n_req} requests")
+    qs = _rows("q", q, n, sh.Hq, sh.D, e)
+    if out.dtype != e or out.shape != (n, sh.Hq, sh.D) or not out.is_contiguous():
+        raise ValueError(f"out: expected a dense {e} tensor of {(n, sh.Hq, sh.D)}")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (n, sh.Hq) or not lse.is_contiguous()):
+        raise ValueError(f"lse: expected a dense float32 tensor of {(n, sh.Hq)}")
+    _on_device(cache.k_pages, cache.v_pages, cache.block_table, q, q_begin, kv_len, out, lse)
+    _check(lib().cascade_paged_attn(ctx.handle, C.byref(cache.struct), n_req, n, q.data_ptr(), qs, q_begin.data_ptr(),
+                                    kv_len.data_ptr(), max_q, max_kv, window, sinks, softmax_scale, out.data_ptr(),
+                                    None if lse is None else lse.data_ptr(), _stream()))
+
+
+def cascade_sample(ctx, logits, uniforms, token, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, kept=None):
+    """One token per row of [n_rows,V] float or bf16 logits (rows may lie apart); settings are device tensors per row."""
+    if logits.dim() != 2 or logits.shape[1] != ctx.shape.V or logits.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"logits: expected float32 or bfloat16 [n_rows, {ctx.shape.V}], got {logits.dtype} {tuple(logits.shape)}")
+    n, V = logits.shape
+    st = logits.stride()
+    if st[1] != 1:
+        raise ValueError("a row of logits must be dense")
+    _vectors(torch.float32, n, uniforms=uniforms, temperature=temperature, top_p=top_p, min_p=min_p, prob=prob)
+    _vectors(torch.int32, n, token=token, top_k=top_k, kept=kept)
+    _on_device(logits, uniforms, token, temperature, top_k, top_p, min_p, prob, kept)
+    p = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    _check(lib().cascade_sample(ctx.handle, logits.data_ptr(), F32 if logits.dtype == torch.float32 else BF16,
+                                V if n == 1 else st[0], n, p(temperature), p(top_k), p(top_p), p(min_p), p(uniforms),
+                                p(token), p(prob), p(kept), _stream()))

@@ -1,0 +1,74 @@
+// Causal attention of every request's new tokens over its paged cache: checks, and the kernel of the fp32 type.
+#include "paged.h"
+#include "paged_attn.cuh"
+
+namespace {
+
+constexpr int kWarps = 8;
+
+// One warp per (new token, query head).
+template <typename E, int D>
+__global__ void __launch_bounds__(kWarps * 32) k_paged_attn_row(const PagedAttnArgs a) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int i = blockIdx.x * kWarps + warp, head = blockIdx.y, r = blockIdx.z;
+  paged::Request rq;
+  if (!paged::load_request(a, r, &rq) || i >= rq.nq) return;
+  paged::attend_row<E, D>(a, r, rq.q0 + i, rq.kv - rq.nq + i, head, lane);
+}
+
+template <typename E, int D>
+int launch_row(const PagedAttnArgs& a, cudaStream_t s) {
+  k_paged_attn_row<E, D><<<dim3(cascade_detail::ceil_div(a.max_q, kWarps), a.Hq, a.n_req), kWarps * 32, 0, s>>>(a);
+  CASCADE_CUDA_TRY(cudaGetLastError());
+  return CASCADE_OK;
+}
+
+}  // namespace
+
+extern "C" int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* cache, int32_t n_req, int32_t n_tok,
+                                  const void* q, int64_t q_stride, const int32_t* q_begin, const int32_t* kv_len,
+                                  int32_t max_q, int32_t max_kv, int32_t window, int32_t sinks, float softmax_scale,
+                                  void* out, float* lse, void* stream) {
+  if (ctx == nullptr || q == nullptr || q_begin == nullptr || kv_len == nullptr || out == nullptr) return CASCADE_ERR_INVALID_ARG;
+  CASCADE_TRY(check_paged_cache(ctx, cache));
+  const cascade_shape& sh = ctx->shape;
+  const int es = sh.dtype == CASCADE_BF16 ? 2 : 4;
+  if (cache->block_table == nullptr || cache->table_stride < 1) return CASCADE_ERR_INVALID_ARG;
+  if (n_req < 1 || n_tok < 1 || max_q < 1 || max_kv < 0 || window < 0 || sinks < 0) return CASCADE_ERR_INVALID_ARG;
+  if (!(softmax_scale > 0.f) || softmax_scale > 3e38f) return CASCADE_ERR_INVALID_ARG;
+  if (q_stride < (int64_t)sh.Hq * sh.D || q_stride * es % 16 != 0) return CASCADE_ERR_INVALID_ARG;
+  if (((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15u) != 0 || (reinterpret_cast<uintptr_t>(lse) & 3u) != 0)
+    return CASCADE_ERR_INVALID_ARG;
+  if (n_req > CASCADE_MAX_REQUESTS) return CASCADE_ERR_UNSUPPORTED_SHAPE;
+  CASCADE_TRY(check_current_device(ctx));
+  PagedAttnArgs a;
+  a.n_req = n_req;
+  a.n_tok = n_tok;
+  a.Hq = sh.Hq;
+  a.Hkv = sh.Hkv;
+  a.page_size = cache->page_size;
+  a.n_pages = cache->n_pages;
+  a.table_stride = cache->table_stride;
+  a.max_q = max_q < n_tok ? max_q : n_tok;
+  a.max_kv = max_kv;
+  a.window = window;
+  a.sinks = sinks;
+  a.page_stride = cache->page_stride;
+  a.q_stride = q_stride;
+  a.q = q;
+  a.k = cache->k_pages;
+  a.v = cache->v_pages;
+  a.out = out;
+  a.lse = lse;
+  a.q_begin = q_begin;
+  a.kv_len = kv_len;
+  a.block_table = cache->block_table;
+  a.scale = softmax_scale;
+  a.err = ctx->dev_error;
+  a.wait_ns = ctx->wait_limit_ns;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  ctx->launches = 0;
+  KernelScope ks(ctx, K_PAGED_ATTN, s);
+  if (sh.dtype == CASCADE_BF16) return sh.D == 128 ? launch_row<__nv_bfloat16, 128>(a, s) : launch_row<__nv_bfloat16, 64>(a, s);
+  return sh.D == 128 ? launch_row<float, 128>(a, s) : launch_row<float, 64>(a, s);
+}
