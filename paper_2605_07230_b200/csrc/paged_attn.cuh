@@ -94,3 +94,7 @@ __device__ void attend_row(const PagedAttnArgs& a, int r, int row, int x, int he
 }
 
 }  // namespace paged
+
+// paged_attn_tc.cu: row blocks on the tensor cores (bf16).  `takes`: the group of query heads fits into a block.
+bool paged_attn_tc_takes(const PagedAttnArgs& a);
+int launch_paged_attn_tc(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_t s);

@@ -1,0 +1,497 @@
+// Causal attention of new tokens over a paged cache on the tensor cores (bf16): prompts and chunks.
+//
+// One persistent CTA per SM walks over work items: two blocks of up to 128 query rows of one (request, key head), a row
+// being (token, query head of the group), with all the key tiles (128 keys) that any of the rows sees.
+//   * warp 8 loads: every lane owns one box of a tile (32 / 64 / ... rows of one page and 64 elements), looks its page up one
+//     tile ahead and issues its own TMA copy; keys and values share one ring of five 32 KB stages;
+//   * warp 9 issues the products: S_w = Q_w K^T (128 x 128) and O_w += P_w V with P_w taken from tensor memory, block 0
+//     and block 1 in turn, so that one block's softmax runs beside the other's products;
+//   * warps 0-3 and 4-7: softmax of block 0 and block 1, one row per thread.  A row's scores come from tensor memory in
+//     one go, the weights 2^(s c - ref) go back as bf16 over the scores' own columns.  ref is the running maximum, raised
+//     only when a score passes it by more than 2^8: then the row's accumulator is rescaled in place (rare).
+// Weights are rounded to bf16 for the product (the tensor cores take both operands in one type, and the values are bf16);
+// the sums and accumulators stay fp32.
+// Rows of the last tile behind the request's last key hold whatever the page held before: their scores are masked, and
+// their values are set to zero in shared memory, since 0 x NaN would reach the sum.  A row whose result is not finite all
+// the same (a non-finite value at a key that another row of the block sees) is computed again by one warp from the keys
+// it sees alone.
+// Tensor bound for prompts; every wait is bounded (error word, normal teardown).
+#include "paged.h"
+#include "paged_attn.cuh"
+#include "tmap.h"
+
+namespace {
+
+constexpr int kTile = 128;        // keys per tile, rows per block
+constexpr int kThreads = 320;
+constexpr int kStages = 5;
+constexpr float kLazy = 8.f;      // log2 units
+
+template <int D>
+struct Cfg {
+  static constexpr int kHalves = D / 64;                 // 64-element column blocks of a tile
+  static constexpr int kTileBytes = kTile * D * 2;
+  static constexpr int kSmem = (2 + kStages) * kTileBytes + 1024;
+};
+
+struct TcArgs {
+  PagedAttnArgs a;
+  int G, tpb, box_rows;           // query heads a key head; tokens per row block; rows of a page box
+};
+
+// Items of the requests in order, Hkv x pairs of row blocks each; a whole warp walks forward through them, 32 requests
+// at a time.
+struct Cursor {
+  int chunk = -32, lane_items = 0, lane_first = 0, base = 0, total = 0;
+  __device__ __forceinline__ bool find(const TcArgs& p, int item, int lane, int* r, int* local) {
+    while (chunk < 0 || item >= base + total) {
+      base += total;
+      chunk += 32;
+      if (chunk >= p.a.n_req) return false;
+      paged::Request q;
+      lane_items = 0;
+      if (chunk + lane < p.a.n_req && paged::load_request(p.a, chunk + lane, &q))
+        lane_items = p.a.Hkv * ((q.nq + 2 * p.tpb - 1) / (2 * p.tpb));
+      int inc = lane_items;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+      }
+      lane_first = inc - lane_items;
+      total = __shfl_sync(0xffffffffu, inc, 31);
+    }
+    const int x = item - base;
+    const int who = __ffs(__ballot_sync(0xffffffffu, x >= lane_first && x < lane_first + lane_items)) - 1;
+    *r = chunk + who;
+    *local = x - __shfl_sync(0xffffffffu, lane_first, who);
+    return true;
+  }
+};
+
+struct Item {
+  int r, head, q0, nq, kv;    // request, key head, the request's first row, rows, keys
+  int tok[2];                 // first token of each block
+  int n[2], n_tiles;          // key tiles each block needs, tiles loaded
+  int n_sink, skip;           // tile i is i (i < n_sink) or i + skip
+  __device__ __forceinline__ int tile(int i) const { return i < n_sink ? i : i + skip; }
+};
+
+__device__ __forceinline__ void make_item(const TcArgs& p, int r, int local, Item* it) {
+  it->r = r;
+  it->q0 = p.a.q_begin[r];
+  it->nq = p.a.q_begin[r + 1] - it->q0;
+  it->kv = p.a.kv_len[r];
+  const int pairs = (it->nq + 2 * p.tpb - 1) / (2 * p.tpb);
+  it->head = local / pairs;
+  const int pair = pairs - 1 - local % pairs;   // the longest rows first
+  const int x0 = it->kv - it->nq;               // position of the request's first new token
+  it->tok[0] = pair * 2 * p.tpb;
+  it->tok[1] = it->tok[0] + p.tpb;
+  const int lo = paged::window_begin(x0 + it->tok[0], p.a.window);
+  const int lo_tile = max(lo, 0) / kTile;
+  it->n_sink = min((min(p.a.sinks, lo) + kTile - 1) / kTile, lo_tile);
+  it->skip = lo_tile - it->n_sink;
+  it->n_tiles = 0;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    it->n[w] = 0;
+    if (it->tok[w] < it->nq) {
+      const int last = x0 + min(it->nq, it->tok[w] + p.tpb) - 1;   // position of the block's last token
+      if (last >= 0) it->n[w] = last / kTile + 1 - it->skip;
+    }
+    it->n_tiles = max(it->n_tiles, it->n[w]);
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                const __grid_constant__ CUtensorMap tm_v, const TcArgs p) {
+  using C = Cfg<D>;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t q_full[2], q_empty[2], kv_full[kStages], kv_empty[kStages], s_full[2], p_full[2], o_full[2],
+      o_empty[2];
+  __shared__ uint32_t s_tmem_base;
+  __shared__ int s_abort;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
+  const uint32_t q_addr = smem_base, ring = smem_base + 2 * C::kTileBytes;
+  volatile int* abort_flag = &s_abort;
+  int* err = p.a.err;
+  const uint64_t wait_ns = p.a.wait_ns;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      ptx::mbar_init(&kv_full[i], 1);
+      ptx::mbar_init(&kv_empty[i], 1);
+    }
+    for (int w = 0; w < 2; ++w) {
+      ptx::mbar_init(&q_full[w], 1);
+      ptx::mbar_init(&q_empty[w], 1);
+      ptx::mbar_init(&s_full[w], 1);
+      ptx::mbar_init(&p_full[w], 128);
+      ptx::mbar_init(&o_full[w], 1);
+      ptx::mbar_init(&o_empty[w], 128);
+    }
+    s_abort = 0;
+    ptx::fence_mbar_init();
+  }
+  if (warp == 8 && lane == 0) {
+    ptx::prefetch_tmap(&tm_q);
+    ptx::prefetch_tmap(&tm_k);
+    ptx::prefetch_tmap(&tm_v);
+  }
+  if (warp == 9) {
+    ptx::tmem_alloc(&s_tmem_base, 512);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = s_tmem_base;   // S0, S1 at 0, 128; O0, O1 at 256, 384
+
+  Cursor cur;
+  int r, local;
+  Item it;
+  if (warp == 8) {
+    // ---------------- loads ----------------
+    const int n_box = kTile / p.box_rows;                       // boxes of a tile along the keys
+    const int box_i = lane % n_box, half = lane / n_box;        // this lane's box
+    const bool has_box = half < C::kHalves;
+    const uint32_t box_bytes = (uint32_t)p.box_rows * 128u;
+    int stage = 0, items[2] = {0, 0};
+    uint32_t ph = 0;
+    bool ok = true;
+    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &r, &local); item += gridDim.x) {
+      make_item(p, r, local, &it);
+      for (int w = 0; w < 2; ++w) {
+        if (it.n[w] == 0) continue;
+        if (items[w] > 0) ok = ok && ptx::mbar_wait(&q_empty[w], (items[w] - 1) & 1u, abort_flag, err, wait_ns);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        ++items[w];
+        if (lane == 0) {
+          ptx::mbar_arrive_expect_tx(&q_full[w], (uint32_t)(p.tpb * p.G) * 128u * C::kHalves);
+          for (int h = 0; h < C::kHalves; ++h)
+            ptx::tma_load_4d(smem + w * C::kTileBytes + h * (kTile * 128), &tm_q, h * 64, 0, it.head, it.q0 + it.tok[w], &q_full[w]);
+        }
+      }
+      const int32_t* table = p.a.block_table + (size_t)it.r * p.a.table_stride;
+      auto page_of = [&](int i, int* row) {                     // this lane's page in tile i (-1: nothing to load)
+        const int key = it.tile(i) * kTile + box_i * p.box_rows;
+        *row = key % p.a.page_size;
+        return has_box && key < it.kv ? table[key / p.a.page_size] : -1;
+      };
+      int row = 0, next_row = 0;
+      int page = it.n_tiles > 0 ? page_of(0, &row) : -1;
+      bool wanted = has_box && it.n_tiles > 0 && it.tile(0) * kTile + box_i * p.box_rows < it.kv;
+      for (int i = 0; ok && i < it.n_tiles; ++i) {
+        int next = -1;
+        bool next_wanted = false;
+        if (i + 1 < it.n_tiles) {
+          next = page_of(i + 1, &next_row);
+          next_wanted = has_box && it.tile(i + 1) * kTile + box_i * p.box_rows < it.kv;
+        }
+        const bool load = wanted && page >= 0 && page < p.a.n_pages;
+        if (wanted && !load) atomicOr(err, CASCADE_DEV_ERR_BAD_PAGE);
+        const uint32_t bytes = box_bytes * (uint32_t)__popc(__ballot_sync(0xffffffffu, load));
+        for (int kv = 0; kv < 2; ++kv) {
+          ok = ptx::mbar_wait(&kv_empty[stage], ph ^ 1u, abort_flag, err, wait_ns);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          if (lane == 0) ptx::mbar_arrive_expect_tx(&kv_full[stage], bytes);
+          __syncwarp();
+          if (load)
+            ptx::tma_load_4d(smem + (2 + stage) * C::kTileBytes + half * (kTile * 128) + box_i * box_bytes, kv == 0 ? &tm_k : &tm_v,
+                             half * 64, it.head, row, page, &kv_full[stage]);
+          if (++stage == kStages) {
+            stage = 0;
+            ph ^= 1u;
+          }
+        }
+        page = next;
+        row = next_row;
+        wanted = next_wanted;
+      }
+    }
+    // every stage and query tile has been given back before the CTA may end (the arrivals are asynchronous)
+    for (int i = 0; ok && i < kStages; ++i) {
+      ok = ptx::mbar_wait(&kv_empty[stage], ph ^ 1u, abort_flag, err, wait_ns);
+      if (++stage == kStages) {
+        stage = 0;
+        ph ^= 1u;
+      }
+    }
+    for (int w = 0; ok && w < 2; ++w)
+      if (items[w] > 0) ok = ptx::mbar_wait(&q_empty[w], (items[w] - 1) & 1u, abort_flag, err, wait_ns);
+  } else if (warp == 9) {
+    // ---------------- products ----------------
+    const uint32_t idesc_s = ptx::umma_idesc_bf16(128, kTile);
+    const uint32_t idesc_o = ptx::umma_idesc_bf16_b_mn(128, D);
+    int used[2] = {0, 0}, tiles[2] = {0, 0};   // items / tiles of each block so far
+    int stage = 0;                             // the next stage to be consumed; K(i) and V(i) alternate
+    uint32_t ph = 0;
+    bool ok = true;
+    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &r, &local); item += gridDim.x) {
+      make_item(p, r, local, &it);
+      if (lane == 0 && it.n_tiles > 0) {
+        auto wait = [&](uint64_t* bar, uint32_t parity) { ok = ok && ptx::mbar_wait(bar, parity, abort_flag, err, wait_ns); };
+        auto scores = [&](int w, int st) {
+          ptx::tc_fence_after();
+          const uint32_t k_addr = ring + st * C::kTileBytes;
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks) {
+            const uint32_t off = (ks >> 2) * (kTile * 128) + (ks & 3) * 32;
+            ptx::umma_bf16(tmem + w * 128, ptx::umma_desc_sw128(q_addr + w * C::kTileBytes + off), ptx::umma_desc_sw128(k_addr + off),
+                           idesc_s, ks != 0);
+          }
+          ptx::umma_commit(&s_full[w]);
+        };
+        auto advance = [&]() {
+          if (++stage == kStages) {
+            stage = 0;
+            ph ^= 1u;
+          }
+        };
+        wait(&kv_full[stage], ph);
+        for (int w = 0; w < 2 && ok; ++w) {
+          if (it.n[w] == 0) continue;
+          wait(&q_full[w], used[w] & 1u);
+          if (!ok) break;
+          scores(w, stage);
+          if (it.n[w] == 1) ptx::umma_commit(&q_empty[w]);
+        }
+        if (ok) ptx::umma_commit(&kv_empty[stage]);
+        advance();
+        for (int i = 0; ok && i < it.n_tiles; ++i) {
+          const int v_stage = stage;
+          wait(&kv_full[stage], ph);
+          advance();
+          const int k_stage = stage;
+          const bool more = i + 1 < it.n_tiles;
+          bool k_here = false;
+          for (int w = 0; w < 2 && ok; ++w) {
+            if (i >= it.n[w]) continue;
+            if (i == 0 && used[w] > 0) wait(&o_empty[w], (used[w] - 1) & 1u);
+            wait(&p_full[w], tiles[w] & 1u);
+            if (!ok) break;
+            ++tiles[w];
+            ptx::tc_fence_after();
+            const uint32_t v_addr = ring + v_stage * C::kTileBytes;
+#pragma unroll
+            for (int ks = 0; ks < kTile / 16; ++ks)
+              ptx::umma_bf16_ts(tmem + 256 + w * 128, tmem + w * 128 + ks * 8,
+                                ptx::umma_desc_sw128_strides(v_addr + ks * 2048, kTile * 128, 1024), idesc_o, (i | ks) != 0);
+            if (i + 1 == it.n[w]) ptx::umma_commit(&o_full[w]);
+            if (i + 1 < it.n[w]) {
+              if (!k_here) {
+                wait(&kv_full[k_stage], ph);
+                k_here = true;
+                if (!ok) break;
+              }
+              scores(w, k_stage);
+              if (i + 2 == it.n[w]) ptx::umma_commit(&q_empty[w]);
+            }
+          }
+          if (!ok) break;
+          ptx::umma_commit(&kv_empty[v_stage]);
+          if (more) {
+            ptx::umma_commit(&kv_empty[k_stage]);
+            advance();
+          }
+        }
+        for (int w = 0; w < 2; ++w) used[w] += it.n[w] > 0;
+      }
+      ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+    }
+  } else {
+    // ---------------- softmax, one row per thread ----------------
+    const int w = warp >> 2, rr = threadIdx.x & 127;           // row block, row
+    const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t t_s = tmem + w * 128 + lane_addr, t_o = tmem + 256 + w * 128 + lane_addr;
+    const int my_tok = rr / p.G, my_g = rr % p.G;
+    const bool in_block = rr < p.tpb * p.G;
+    const float c = p.a.scale * paged::kLog2e;
+    int tiles = 0, used = 0, kv_count = 0;                     // tiles / items of this block, ring stages of all items
+    bool ok = true;
+    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &r, &local); item += gridDim.x) {
+      make_item(p, r, local, &it);
+      const int tok = it.tok[w] + my_tok;
+      const bool live = in_block && tok < it.nq;
+      const int x = live ? it.kv - it.nq + tok : -1;           // position; -1: sees nothing
+      const int lo = paged::window_begin(x, p.a.window), n_sink = p.a.sinks;
+      const int n = it.n[w];
+      float ref = -INFINITY, l = 0.f;
+      for (int i = 0; i < n; ++i, ++tiles) {
+        const int k0 = it.tile(i) * kTile;
+        ok = ptx::mbar_wait(&s_full[w], tiles & 1u, abort_flag, err, wait_ns);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        ptx::tc_fence_after();
+        uint32_t s[kTile];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) ptx::tmem_ld32_async(t_s + 32 * q, s + 32 * q);
+        ptx::tmem_wait_ld();
+        const bool whole = k0 + kTile - 1 <= x && (k0 >= lo || k0 + kTile <= n_sink);
+        if (!__all_sync(0xffffffffu, whole)) {
+          const int hi_j = x - k0, lo_j = lo - k0, sink_j = n_sink - k0;
+#pragma unroll
+          for (int j = 0; j < kTile; ++j)
+            if (!(j <= hi_j && (j >= lo_j || j < sink_j))) s[j] = 0xff800000u;   // -inf
+        }
+        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < kTile; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(s[j]));
+        const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * c;
+        float alpha = 1.f;
+        if (m > ref + kLazy || (ref == -INFINITY && m > -INFINITY)) {
+          alpha = ref == -INFINITY ? 0.f : ptx::ex2(ref - m);
+          ref = m;
+        }
+        if (i > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
+          // the scores of tile i come after the output product of tile i - 1, so the accumulator is at rest
+          l *= alpha;
+#pragma unroll 1
+          for (int q = 0; q < D / 16; ++q) {
+            float t[16];
+            ptx::tmem_ld16(t_o + 16 * q, t);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) t[k] *= alpha;
+            ptx::tmem_st16(t_o + 16 * q, t);
+          }
+        }
+        const float minus = ref == -INFINITY ? 0.f : -ref;
+        float sum4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const float a = ptx::ex2(fmaf(__uint_as_float(s[32 * q + 2 * k]), c, minus));
+            const float b = ptx::ex2(fmaf(__uint_as_float(s[32 * q + 2 * k + 1]), c, minus));
+            sum4[k & 3] += a + b;
+            pk[k] = ptx::pack_bf16x2(a, b);
+          }
+          ptx::tmem_st16_async(t_s + 16 * q, pk);
+        }
+        l += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
+        // values behind the last key: zeros (block 0 does it while it takes part, its product comes first)
+        if (k0 + kTile > it.kv && (w == 0 || i >= it.n[0])) {
+          const int st = (kv_count + 2 * i + 1) % kStages;
+          const uint32_t st_ph = ((uint32_t)(kv_count + 2 * i + 1) / kStages) & 1u;
+          ok = ptx::mbar_wait(&kv_full[st], st_ph, abort_flag, err, wait_ns);
+          if (ok && k0 + rr >= it.kv) {
+            for (int h = 0; h < C::kHalves; ++h)
+              for (int k = 0; k < 8; ++k) ptx::st_shared_v4(ring + st * C::kTileBytes + h * (kTile * 128) + rr * 128 + k * 16, 0, 0, 0, 0);
+            ptx::fence_proxy_async_smem();
+          }
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+        }
+        ptx::tmem_wait_st();
+        ptx::tc_fence_before();
+        ptx::mbar_arrive(&p_full[w]);
+      }
+      kv_count += 2 * it.n_tiles;
+      if (!ok) break;
+      // ---- the rows' results ----
+      const int row = it.q0 + tok, head = it.head * p.G + my_g;
+      bool odd = false;                                        // something is not finite, or every visible score was -inf
+      if (n > 0) {
+        ok = ptx::mbar_wait(&o_full[w], used & 1u, abort_flag, err, wait_ns);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        ptx::tc_fence_after();
+        ++used;
+      }
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      odd = x >= 0 && !(l > 0.f && l < INFINITY);
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.a.out) + ((long long)row * p.a.Hq + head) * D;
+#pragma unroll 1
+      for (int q = 0; q < D / 32; ++q) {
+        uint32_t o[32];
+        if (n > 0) {
+          ptx::tmem_ld32_async(t_o + 32 * q, o);
+          ptx::tmem_wait_ld();
+        } else {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) o[k] = 0u;
+        }
+        float bad = 0.f;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) bad = fmaf(__uint_as_float(o[k]), 0.f, bad);   // NaN if any is not finite
+        odd = odd || (x >= 0 && bad != 0.f);
+        if (live) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            uint32_t v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float a = __uint_as_float(o[8 * k + 2 * e]) * inv, b = __uint_as_float(o[8 * k + 2 * e + 1]) * inv;
+              v[e] = x < 0 ? 0u : ptx::pack_bf16x2(a, b);
+            }
+            *reinterpret_cast<uint4*>(out + 32 * q + 8 * k) = make_uint4(v[0], v[1], v[2], v[3]);
+          }
+        }
+      }
+      if (n > 0) {
+        ptx::tc_fence_before();
+        ptx::mbar_arrive(&o_empty[w]);
+      }
+      if (live && p.a.lse != nullptr)
+        p.a.lse[(long long)row * p.a.Hq + head] = l > 0.f ? (ref + log2f(l)) * paged::kLn2 : -INFINITY;
+      __syncwarp();
+      for (uint32_t left = __ballot_sync(0xffffffffu, odd); left != 0u; left &= left - 1u) {
+        const int who = __ffs(left) - 1;
+        paged::attend_row<__nv_bfloat16, D>(p.a, it.r, __shfl_sync(0xffffffffu, row, who), __shfl_sync(0xffffffffu, x, who),
+                                            __shfl_sync(0xffffffffu, head, who), lane);
+      }
+    }
+  }
+  __syncwarp();
+  if (*abort_flag) __nanosleep(1000000);   // copies still in flight
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  if (warp == 9) ptx::tmem_dealloc(tmem, 512);
+}
+
+template <int D>
+int launch(cascade_ctx* ctx, const TcArgs& p, int n_items, cudaStream_t s) {
+  const PagedAttnArgs& a = p.a;
+  const uint64_t dq[4] = {(uint64_t)D, (uint64_t)p.G, (uint64_t)a.Hkv, (uint64_t)a.n_tok};
+  const uint64_t sq[3] = {(uint64_t)D, (uint64_t)p.G * D, (uint64_t)a.q_stride};
+  const uint32_t bq[4] = {64, (uint32_t)p.G, 1, (uint32_t)p.tpb};
+  const uint64_t dk[4] = {(uint64_t)D, (uint64_t)a.Hkv, (uint64_t)a.page_size, (uint64_t)a.n_pages};
+  const uint64_t sk[3] = {(uint64_t)D, (uint64_t)a.Hkv * D, (uint64_t)a.page_stride};
+  const uint32_t bk[4] = {64, 1, (uint32_t)p.box_rows, 1};
+  const CUtensorMap* mq = get_tmap_4d_bf16(ctx, a.q, dq, sq, bq);
+  const CUtensorMap* mk = get_tmap_4d_bf16(ctx, a.k, dk, sk, bk);
+  const CUtensorMap* mv = get_tmap_4d_bf16(ctx, a.v, dk, sk, bk);
+  if (mq == nullptr || mk == nullptr || mv == nullptr) return CASCADE_ERR_CUDA;
+  CASCADE_CUDA_TRY(cudaFuncSetAttribute(k_paged_attn_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::kSmem));
+  const int grid = n_items < ctx->sm_count ? n_items : ctx->sm_count;
+  k_paged_attn_tc<D><<<grid, kThreads, Cfg<D>::kSmem, s>>>(*mq, *mk, *mv, p);
+  CASCADE_CUDA_TRY(cudaGetLastError());
+  return CASCADE_OK;
+}
+
+}  // namespace
+
+bool paged_attn_tc_takes(const PagedAttnArgs& a) { return a.Hq / a.Hkv <= kTile; }
+
+int launch_paged_attn_tc(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_t s) {
+  TcArgs p;
+  p.a = a;
+  p.G = a.Hq / a.Hkv;
+  p.tpb = kTile / p.G;
+  p.box_rows = 8;
+  while (p.box_rows < kTile && a.page_size % (2 * p.box_rows) == 0) p.box_rows *= 2;
+  // no more items than this: a request's pairs of row blocks are at most ceil(tokens / (2 tpb))
+  const long long pairs = (long long)a.n_tok / (2 * p.tpb) + a.n_req;
+  const long long items = pairs * a.Hkv;
+  const int n_items = items > (1 << 20) ? (1 << 20) : (int)items;
+  return ctx->shape.D == 128 ? launch<128>(ctx, p, n_items, s) : launch<64>(ctx, p, n_items, s);
+}
