@@ -69,6 +69,7 @@ extern "C" int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* c
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   ctx->launches = 0;
   KernelScope ks(ctx, K_PAGED_ATTN, s);
+  if (sh.dtype == CASCADE_BF16 && paged_attn_rows_takes(a)) return launch_paged_attn_rows(ctx, a, s);
   if (sh.dtype == CASCADE_BF16 && paged_attn_tc_takes(a)) return launch_paged_attn_tc(ctx, a, s);
   if (sh.dtype == CASCADE_BF16) return sh.D == 128 ? launch_row<__nv_bfloat16, 128>(a, s) : launch_row<__nv_bfloat16, 64>(a, s);
   return sh.D == 128 ? launch_row<float, 128>(a, s) : launch_row<float, 64>(a, s);

@@ -98,3 +98,6 @@ __device__ void attend_row(const PagedAttnArgs& a, int r, int row, int x, int he
 // paged_attn_tc.cu: row blocks on the tensor cores (bf16).  `takes`: the group of query heads fits into a block.
 bool paged_attn_tc_takes(const PagedAttnArgs& a);
 int launch_paged_attn_tc(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_t s);
+// paged_attn_rows.cu: at most 16 rows a key head, warp-level products straight from memory (bf16).
+bool paged_attn_rows_takes(const PagedAttnArgs& a);
+int launch_paged_attn_rows(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_t s);
