@@ -2,11 +2,12 @@
 // heads of a key head are at most 16 rows.
 //
 // Memory-bound: every key and value is read once for all rows.  One CTA of four warps per (KV split, key head, request);
-// a warp takes 16 keys at a time straight from memory into the operand registers of warp-level matrix products
-// (m16n8k16, the 16 rows on M): the sum over a head's elements does not care for their order, so a lane's 16-byte pieces
-// of a key row serve as they come, and the values' 16-byte pieces give pairs of keys after one byte permute per register.
-// No shared memory, no barrier in the loop: the keys of the next 16 are requested as soon as the scores have used the
-// registers, the values as soon as the output has, and with three CTAs an SM keeps about 80 KB in flight.
+// a warp takes 16 keys at a time straight from memory into the operand registers of warp-level matrix products (m16n8k16).
+// Keys and values stand on M and the rows on N, in blocks of eight: S^T = K Q^T and O^T = V^T P^T.  The sum over a head's
+// elements does not care for their order, so a lane's 16-byte pieces of a key row serve as they come; the values' pieces
+// give pairs of keys after one byte permute per register, and the weights turn with one 8 x 8 transpose per eight keys.
+// No shared memory and no barrier in the loop: the keys of the next 16 are requested as soon as the scores have used the
+// registers, the values as soon as the output has; with up to eight rows three CTAs fit an SM, 96 KB in flight.
 // (The 5th-generation tensor cores want 128 rows and operands in shared memory; here they would multiply padding.)
 // Weights are 2^(s c - ref); ref is the running maximum, raised only when a score passes it by more than 2^8.  Weights are
 // rounded to bf16 for the product with the bf16 values, sums and accumulators stay fp32.
@@ -21,10 +22,11 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kRows = 16;
 constexpr int kChunk = 16;        // keys per step of a warp
 constexpr float kLazy = 8.f;
+constexpr int kSortMost = 256;    // requests that are ordered by length
 
 struct RowArgs {
   PagedAttnArgs a;
-  int G, splits;
+  int G, splits, sorted, max_rows;
   uint32_t page_mul;              // key / page_size = (key * page_mul) >> page_shift for keys below 2^31
   int page_shift;
 };
@@ -34,26 +36,51 @@ __device__ __forceinline__ uint4 ld_stream(const void* p) {
   asm volatile("ld.global.nc.L1::no_allocate.L2::256B.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
   return v;
 }
-__device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+// 8 x 8 transpose of 16-bit elements across the warp.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ void mma16816(float* c, const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads, 3) k_paged_attn_rows(const RowArgs p) {
-  constexpr int kQ = D / 32;                     // 16-byte pieces of a row per lane
-  constexpr int kJ = D / 64;
+// kNb: blocks of eight rows.
+template <int D, int kNb>
+__global__ void __launch_bounds__(kThreads, kNb == 1 ? 3 : 2) k_paged_attn_rows(const RowArgs p) {
+  constexpr int kQ = D / 32;                     // 16-byte pieces of a key row per lane
+  constexpr int kJ = D / 64;                     // 16-byte pieces of a value row per lane
+  constexpr int kO = D / 16;                     // output products
   constexpr int kX = D + 4;                      // floats per row of a partial result: outputs, reference, sum
-  __shared__ __align__(16) float s_part[kWarps][kRows][kX];
+  extern __shared__ __align__(16) float s_part[];  // [warp][row][kX], as many rows as the call has at most
   __shared__ int s_odd;
   const PagedAttnArgs& a = p.a;
+  const int part = p.max_rows * kX;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int split = blockIdx.x, kh = blockIdx.y, r = blockIdx.z;
+  const int split = blockIdx.x, kh = blockIdx.y;
+  int r = blockIdx.z;
+  if (p.sorted) {
+    // several waves of CTAs: the longest requests go first, so that the last wave is short (the z-th longest is found by
+    // counting who is longer; ties by index)
+    __shared__ int s_len[kSortMost], s_r;
+    for (int i = threadIdx.x; i < a.n_req; i += kThreads) s_len[i] = a.kv_len[i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.n_req; i += kThreads) {
+      const int mine = s_len[i];
+      int rank = 0;
+      for (int k = 0; k < a.n_req; ++k) rank += s_len[k] > mine || (s_len[k] == mine && k < i);
+      if (rank == r) s_r = i;
+    }
+    __syncthreads();
+    r = s_r;
+  }
   paged::Request rq;
   const bool valid = paged::load_request(a, r, &rq);
-  const int rows = valid ? rq.nq * p.G : 0;      // at most kRows
+  const int rows = valid ? rq.nq * p.G : 0;      // at most 8 kNb
   const int x0 = rq.kv - rq.nq;                  // position of the first new token
   if (threadIdx.x == 0) s_odd = 0;
 
@@ -69,31 +96,37 @@ __global__ void __launch_bounds__(kThreads, 3) k_paged_attn_rows(const RowArgs p
   const int c_end = min(n, (split + 1) * per);
   int c = split * per + warp;
 
-  // query fragments: lane (g, t) holds elements 32 j + 8 t .. + 7 of rows g and g + 8
-  uint32_t q_lo[kQ][4], q_hi[kQ][4];
+  // query fragments: lane (g, t) holds elements 32 j + 8 t .. + 7 of row 8 b + g
+  uint32_t q[kNb][kQ][4];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int row = g + 8 * h;
-    const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q);
-    if (row < rows) q += (long long)(rq.q0 + row / p.G) * a.q_stride + (kh * p.G + row % p.G) * D;
+  for (int b = 0; b < kNb; ++b) {
+    const int row = 8 * b + g;
+    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q);
+    if (row < rows) src += (long long)(rq.q0 + row / p.G) * a.q_stride + (kh * p.G + row % p.G) * D;
 #pragma unroll
     for (int j = 0; j < kQ; ++j) {
-      const uint4 v = row < rows ? *reinterpret_cast<const uint4*>(q + 32 * j + 8 * t) : make_uint4(0, 0, 0, 0);
-      uint32_t* dst = h == 0 ? q_lo[j] : q_hi[j];
-      dst[0] = v.x;
-      dst[1] = v.y;
-      dst[2] = v.z;
-      dst[3] = v.w;
+      const uint4 v = row < rows ? *reinterpret_cast<const uint4*>(src + 32 * j + 8 * t) : make_uint4(0, 0, 0, 0);
+      q[b][j][0] = v.x;
+      q[b][j][1] = v.y;
+      q[b][j][2] = v.z;
+      q[b][j][3] = v.w;
     }
   }
-  const int x_row[2] = {g < rows ? x0 + g / p.G : -1, g + 8 < rows ? x0 + (g + 8) / p.G : -1};
+  int x_row[kNb][2];                             // positions of rows 8 b + 2 t + i; -1: no such row
+#pragma unroll
+  for (int b = 0; b < kNb; ++b)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = 8 * b + 2 * t + i;
+      x_row[b][i] = row < rows ? x0 + row / p.G : -1;
+    }
 
   const int32_t* table = a.block_table + (size_t)r * a.table_stride;
   const __nv_bfloat16* k_base = static_cast<const __nv_bfloat16*>(a.k) + kh * D;
   const __nv_bfloat16* v_base = static_cast<const __nv_bfloat16*>(a.v) + kh * D;
   const int row_elems = a.Hkv * D;
   auto first_key = [&](int i) { return (i < n_sink ? i : i + skip) * kChunk; };
-  // element offsets of the two groups of 8 keys of a step (a group lies in one page); -1: nothing there
+  // element offset of a group of 8 keys (a group lies in one page); -1: nothing there
   auto page_off = [&](int key) -> long long {
     if (key >= rq.kv) return -1;
     const int pi = (int)(((unsigned long long)(uint32_t)key * p.page_mul) >> p.page_shift);
@@ -107,7 +140,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_paged_attn_rows(const RowArgs p
   uint4 kr[2][kQ], vr[4][kJ];
   auto load_k = [&](int key0, const long long* off) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < 2; ++h) {                // keys g and 8 + g
       const bool there = off[h] >= 0 && key0 + 8 * h + g < rq.kv;
       const __nv_bfloat16* src = k_base + (there ? off[h] : 0) + (there ? g : 0) * row_elems + 8 * t;
 #pragma unroll
@@ -116,7 +149,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_paged_attn_rows(const RowArgs p
   };
   auto load_v = [&](int key0, const long long* off) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {   // keys 2t, 2t + 1, 2t + 8, 2t + 9
+    for (int i = 0; i < 4; ++i) {                // keys 2t, 2t + 1, 2t + 8, 2t + 9
       const int in = 2 * t + (i & 1), h = i >> 1;
       const bool there = off[h] >= 0 && key0 + 8 * h + in < rq.kv;
       const __nv_bfloat16* src = v_base + (there ? off[h] : 0) + (there ? in : 0) * row_elems + 8 * g;
@@ -125,22 +158,22 @@ __global__ void __launch_bounds__(kThreads, 3) k_paged_attn_rows(const RowArgs p
     }
   };
 
-  float o[kJ][8][4];
+  float o[kNb][kO][4];
+  float ref[kNb][2], l[kNb][2];                  // of rows 8 b + 2 t + i
 #pragma unroll
-  for (int j = 0; j < kJ; ++j)
+  for (int b = 0; b < kNb; ++b) {
+    ref[b][0] = ref[b][1] = -INFINITY;
+    l[b][0] = l[b][1] = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) o[j][e][k] = 0.f;
-  float ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    for (int e = 0; e < kO; ++e) o[b][e][0] = o[b][e][1] = o[b][e][2] = o[b][e][3] = 0.f;
+  }
   const float sc = a.scale * paged::kLog2e;
 
-  long long off[2] = {-1, -1}, off_next[2] = {-1, -1};
+  long long off_next[2] = {-1, -1};
   int key0 = 0;
   if (c < c_end) {
     key0 = first_key(c);
-    off[0] = page_off(key0);
-    off[1] = page_off(key0 + 8);
+    const long long off[2] = {page_off(key0), page_off(key0 + 8)};
     load_k(key0, off);
     load_v(key0, off);
     if (c + kWarps < c_end) {
@@ -155,82 +188,81 @@ __global__ void __launch_bounds__(kThreads, 3) k_paged_attn_rows(const RowArgs p
       off_after[0] = page_off(first_key(c + 2 * kWarps));
       off_after[1] = page_off(first_key(c + 2 * kWarps) + 8);
     }
-    // scores: keys key0 + 8 h + (2t, 2t + 1), rows g and g + 8
-    float s[2][4];
+    // scores: s[b][2 h + i] is key key0 + 8 h + g, row 8 b + 2 t + i
+    float s[kNb][4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      s[h][0] = s[h][1] = s[h][2] = s[h][3] = 0.f;
+    for (int b = 0; b < kNb; ++b) s[b][0] = s[b][1] = s[b][2] = s[b][3] = 0.f;
 #pragma unroll
-      for (int j = 0; j < kQ; ++j) {
-        const uint32_t a0[4] = {q_lo[j][0], q_hi[j][0], q_lo[j][1], q_hi[j][1]};
-        const uint32_t a1[4] = {q_lo[j][2], q_hi[j][2], q_lo[j][3], q_hi[j][3]};
-        mma16816(s[h], a0, kr[h][j].x, kr[h][j].y);
-        mma16816(s[h], a1, kr[h][j].z, kr[h][j].w);
+    for (int j = 0; j < kQ; ++j) {
+      const uint32_t a0[4] = {kr[0][j].x, kr[1][j].x, kr[0][j].y, kr[1][j].y};
+      const uint32_t a1[4] = {kr[0][j].z, kr[1][j].z, kr[0][j].w, kr[1][j].w};
+#pragma unroll
+      for (int b = 0; b < kNb; ++b) {
+        mma16816(s[b], a0, q[b][j][0], q[b][j][1]);
+        mma16816(s[b], a1, q[b][j][2], q[b][j][3]);
       }
     }
     if (c + kWarps < c_end) load_k(next0, off_next);
-    // visibility: steps behind the first token's position or at a window's edge look closer
+    // steps behind the first token's position or at a window's edge look closer
     const bool edge = key0 + kChunk - 1 > x0 || (a.window > 0 && key0 < x0 + rq.nq - a.window);
+    uint32_t w[kNb][2];                          // the weights as the B operand
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int b = 0; b < kNb; ++b) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        float v = s[h][k] * sc;
+        float v = s[b][k] * sc;
         if (edge) {
-          const int j = key0 + 8 * h + 2 * t + (k & 1), x = x_row[k >> 1];
+          const int j = key0 + 8 * (k >> 1) + g, x = x_row[b][k & 1];
           const bool sees = j <= x && (j >= paged::window_begin(x, a.window) || j < a.sinks);
           v = sees ? v : -INFINITY;
         }
-        s[h][k] = v;
+        s[b][k] = v;
       }
-    // raise the reference where a score passes it by more than kLazy (or the row had none)
-    float mx[2];
-    bool raise = false;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      mx[i] = fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1]));
-      raise = raise || mx[i] > ref[i] + kLazy || (ref[i] == -INFINITY && mx[i] > -INFINITY);
-    }
-    if (__any_sync(0xffffffffu, raise)) {
+      // raise the reference where a score passes it by more than kLazy (or the row had none)
+      float mx[2];
+      bool raise = false;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
-        mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
-        float alpha = 1.f;
-        if (mx[i] > ref[i]) {
-          alpha = ref[i] == -INFINITY ? 0.f : ptx::ex2(ref[i] - mx[i]);
-          ref[i] = mx[i];
-        }
-        l[i] *= alpha;
+        mx[i] = fmaxf(s[b][i], s[b][2 + i]);
+        raise = raise || mx[i] > ref[b][i] + kLazy || (ref[b][i] == -INFINITY && mx[i] > -INFINITY);
+      }
+      if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
-        for (int j = 0; j < kJ; ++j)
+        for (int i = 0; i < 2; ++i) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            o[j][e][2 * i] *= alpha;
-            o[j][e][2 * i + 1] *= alpha;
+          for (int x = 4; x < 32; x <<= 1) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], x));
+          float alpha = 1.f;
+          if (mx[i] > ref[b][i]) {
+            alpha = ref[b][i] == -INFINITY ? 0.f : ptx::ex2(ref[b][i] - mx[i]);
+            ref[b][i] = mx[i];
           }
+          l[b][i] *= alpha;
+#pragma unroll
+          for (int e = 0; e < kO; ++e) {
+            o[b][e][i] *= alpha;
+            o[b][e][2 + i] *= alpha;
+          }
+        }
+      }
+      const float m0 = ref[b][0] == -INFINITY ? 0.f : ref[b][0], m1 = ref[b][1] == -INFINITY ? 0.f : ref[b][1];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float w0 = ptx::ex2(s[b][2 * h] - m0), w1 = ptx::ex2(s[b][2 * h + 1] - m1);
+        l[b][0] += w0;
+        l[b][1] += w1;
+        w[b][h] = transpose8(ptx::pack_bf16x2(w0, w1));
       }
     }
-    uint32_t w[4];   // the weights as the A operand: rows g, g + 8; keys 2t.., 2t + 8..
+    // outputs: product e holds elements 8 g + e and 64 + 8 g + e (D = 64: 8 g + e and 8 g + 4 + e) on its 16 rows
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int e = 0; e < kO; ++e) {
+      const int e1 = D == 128 ? e : e + 4, j1 = kJ - 1;
+      const uint32_t sel = (e & 1) ? 0x7632u : 0x5410u;
+      auto word = [&](int i, int j, int x) { return (x >> 1) == 0 ? vr[i][j].x : (x >> 1) == 1 ? vr[i][j].y : (x >> 1) == 2 ? vr[i][j].z : vr[i][j].w; };
+      const uint32_t av[4] = {__byte_perm(word(0, 0, e), word(1, 0, e), sel), __byte_perm(word(0, j1, e1), word(1, j1, e1), sel),
+                              __byte_perm(word(2, 0, e), word(3, 0, e), sel), __byte_perm(word(2, j1, e1), word(3, j1, e1), sel)};
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float m = ref[i] == -INFINITY ? 0.f : ref[i];
-        const float w0 = ptx::ex2(s[h][2 * i] - m), w1 = ptx::ex2(s[h][2 * i + 1] - m);
-        l[i] += w0 + w1;
-        w[2 * h + i] = ptx::pack_bf16x2(w0, w1);
-      }
-    // outputs: n index g of product (j, e) is element 64 j + 8 g + e
-#pragma unroll
-    for (int j = 0; j < kJ; ++j) {
-      const uint32_t v0[4] = {vr[0][j].x, vr[0][j].y, vr[0][j].z, vr[0][j].w}, v1[4] = {vr[1][j].x, vr[1][j].y, vr[1][j].z, vr[1][j].w};
-      const uint32_t v2[4] = {vr[2][j].x, vr[2][j].y, vr[2][j].z, vr[2][j].w}, v3[4] = {vr[3][j].x, vr[3][j].y, vr[3][j].z, vr[3][j].w};
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t sel = (e & 1) ? 0x7632u : 0x5410u;
-        mma16816(o[j][e], w, __byte_perm(v0[e >> 1], v1[e >> 1], sel), __byte_perm(v2[e >> 1], v3[e >> 1], sel));
-      }
+      for (int b = 0; b < kNb; ++b) mma16816(o[b][e], av, w[b][0], w[b][1]);
     }
     if (c + kWarps < c_end) load_v(next0, off_next);
     key0 = next0;
@@ -238,28 +270,33 @@ __global__ void __launch_bounds__(kThreads, 3) k_paged_attn_rows(const RowArgs p
     off_next[1] = off_after[1];
   }
 
-  // ---- the warps' partial results -> one per CTA (in s_part[0]) -> one per cluster ----
+  // ---- the warps' partial results -> one per CTA (in place of the first) -> one per cluster ----
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-    const int row = g + 8 * i;
-    if (row < rows) {
-      float* x = s_part[warp][row];
+  for (int b = 0; b < kNb; ++b)
 #pragma unroll
-      for (int j = 0; j < kJ; ++j)
+    for (int i = 0; i < 2; ++i) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q)      // n = 2t + q: elements 64 j + 16 t + 8 q + e
-#pragma unroll
-          for (int e = 0; e < 8; e += 4)
-            *reinterpret_cast<float4*>(x + 64 * j + 16 * t + 8 * q + e) =
-                make_float4(o[j][e][2 * i + q], o[j][e + 1][2 * i + q], o[j][e + 2][2 * i + q], o[j][e + 3][2 * i + q]);
-      if (t == 0) {
-        x[D] = ref[i];
-        x[D + 1] = l[i];
+      for (int x = 4; x < 32; x <<= 1) l[b][i] += __shfl_xor_sync(0xffffffffu, l[b][i], x);
+      const int row = 8 * b + 2 * t + i;
+      if (row < rows) {
+        float* x = s_part + warp * part + row * kX;
+        float4* lo = reinterpret_cast<float4*>(x + 8 * g);
+        if constexpr (D == 128) {
+          float4* hi = reinterpret_cast<float4*>(x + 64 + 8 * g);
+          lo[0] = make_float4(o[b][0][i], o[b][1][i], o[b][2][i], o[b][3][i]);
+          lo[1] = make_float4(o[b][4][i], o[b][5][i], o[b][6][i], o[b][7][i]);
+          hi[0] = make_float4(o[b][0][2 + i], o[b][1][2 + i], o[b][2][2 + i], o[b][3][2 + i]);
+          hi[1] = make_float4(o[b][4][2 + i], o[b][5][2 + i], o[b][6][2 + i], o[b][7][2 + i]);
+        } else {
+          lo[0] = make_float4(o[b][0][i], o[b][1][i], o[b][2][i], o[b][3][i]);
+          lo[1] = make_float4(o[b][0][2 + i], o[b][1][2 + i], o[b][2][2 + i], o[b][3][2 + i]);
+        }
+        if (g == 0) {
+          x[D] = ref[b][i];
+          x[D + 1] = l[b][i];
+        }
       }
     }
-  }
   __syncthreads();
   // element i of the CTA's rows, from `count` partial results `get(s, row, column)`
   auto merge = [&](int row, int col, int count, auto get, float* ref_out, float* sum_out) {
@@ -277,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_paged_attn_rows(const RowArgs p
     *sum_out = sum;
     return acc;
   };
-  auto here = [&](int s, int row, int col) { return s_part[s][row][col]; };
+  auto here = [&](int s, int row, int col) { return s_part[s * part + row * kX + col]; };
   const bool alone = p.splits == 1;
   auto finish = [&](int row, int col, float acc, float m, float sum) {
     const int x = x0 + row / p.G, tok = rq.q0 + row / p.G, head = kh * p.G + row % p.G;
@@ -295,21 +332,22 @@ __global__ void __launch_bounds__(kThreads, 3) k_paged_attn_rows(const RowArgs p
     }
   } else {
     // merge the CTA's warps into s_part[0] (each thread reads a column of all four before it writes)
-    float mine[kRows * D / kThreads], m_mine[kRows * D / kThreads], sum_mine[kRows * D / kThreads];
+    constexpr int kMine = 8 * kNb * D / kThreads;
+    float mine[kMine], m_mine[kMine], sum_mine[kMine];
 #pragma unroll
-    for (int k = 0; k < kRows * D / kThreads; ++k) {
+    for (int k = 0; k < kMine; ++k) {
       const int i = k * kThreads + threadIdx.x;
       if (i < rows * D) mine[k] = merge(i / D, i % D, kWarps, here, &m_mine[k], &sum_mine[k]);
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kRows * D / kThreads; ++k) {
+    for (int k = 0; k < kMine; ++k) {
       const int i = k * kThreads + threadIdx.x;
       if (i < rows * D) {
-        s_part[0][i / D][i % D] = mine[k];
+        s_part[i / D * kX + i % D] = mine[k];
         if (i % D == 0) {
-          s_part[0][i / D][D] = m_mine[k];
-          s_part[0][i / D][D + 1] = sum_mine[k];
+          s_part[i / D * kX + D] = m_mine[k];
+          s_part[i / D * kX + D + 1] = sum_mine[k];
         }
       }
     }
@@ -317,7 +355,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_paged_attn_rows(const RowArgs p
     ptx::cluster_arrive();
     ptx::cluster_wait();
     if (ptx::cluster_ctarank() == 0) {
-      const uint32_t base = ptx::smem_u32(&s_part[0][0][0]);
+      const uint32_t base = ptx::smem_u32(s_part);
       auto there = [&](int s, int row, int col) { return ptx::ld_cluster_f32(ptx::map_to_cta(base + (uint32_t)(row * kX + col) * 4u, (uint32_t)s)); };
       for (int i = threadIdx.x; i < rows * D; i += kThreads) {
         float m, sum;
@@ -353,11 +391,16 @@ int launch_paged_attn_rows(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_
   const long long units = (long long)a.n_req * a.Hkv;
   const int span = a.window > 0 && (long long)a.window + a.sinks + a.max_q < a.max_kv ? a.window + a.sinks + a.max_q : a.max_kv;
   const int steps = cascade_detail::ceil_div(span > 0 ? span : 1, kChunk * kWarps);
+  p.max_rows = a.max_q * p.G;
+  const bool two_blocks = p.max_rows > 8;
+  const long long resident = (two_blocks ? 2ll : 3ll) * ctx->sm_count;
   p.splits = 1;
-  while (p.splits < 8 && units * p.splits * 2 <= 3ll * ctx->sm_count && steps >= 2 * p.splits) p.splits *= 2;
+  while (p.splits < 8 && units * p.splits * 2 <= resident && steps >= 2 * p.splits) p.splits *= 2;
+  p.sorted = units * p.splits > resident && a.n_req <= kSortMost;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p.splits, a.Hkv, a.n_req);
   cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = (size_t)kWarps * p.max_rows * (ctx->shape.D + 4) * sizeof(float);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -367,8 +410,8 @@ int launch_paged_attn_rows(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   if (ctx->shape.D == 128)
-    CASCADE_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_paged_attn_rows<128>, p));
+    CASCADE_CUDA_TRY(two_blocks ? cudaLaunchKernelEx(&cfg, k_paged_attn_rows<128, 2>, p) : cudaLaunchKernelEx(&cfg, k_paged_attn_rows<128, 1>, p));
   else
-    CASCADE_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_paged_attn_rows<64>, p));
+    CASCADE_CUDA_TRY(two_blocks ? cudaLaunchKernelEx(&cfg, k_paged_attn_rows<64, 2>, p) : cudaLaunchKernelEx(&cfg, k_paged_attn_rows<64, 1>, p));
   return CASCADE_OK;
 }
