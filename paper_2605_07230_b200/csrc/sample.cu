@@ -2,11 +2,14 @@
 //
 //   w[v] = exp((l[v] - m) / T),  token = first v whose cumulative kept weight exceeds u * (total kept weight)
 //
-// One CTA per row.  The row's order-preserving 32-bit keys stay in shared memory (what does not fit is read again from
-// memory), so HBM sees each logit once.  Weights are formed in 64 bits (relative error 1e-12) and summed as 64-bit fixed
-// point: sums do not depend on the order of additions, and a draw differs from exact arithmetic only where u falls
-// within about 1e-11 of a boundary.  Thresholds are exact: a histogram over the range of keys still in question, 2048
-// equal steps of the key at a time, until a step holds a single key value.
+// One CTA per row.  The row's order-preserving 32-bit keys stay in shared memory as far as they fit (the rest is read again
+// through the L2), so HBM sees each logit once.  Weights are formed in 64 bits (relative error 1e-12) and summed as 64-bit
+// fixed point: sums do not depend on the order of additions, and a draw differs from exact arithmetic only where u falls
+// within about 1e-11 of a boundary.
+// Thresholds are exact.  A histogram over 2048 equal steps of the distance to the row's maximum (counts for top-k, weights
+// for the nucleus) finds the step in which the threshold lies; the few tokens of that step are then ranked among each
+// other.  Where a step holds too many different values (logits spread over more than 48 and the threshold far down, or
+// infinities), the search goes over the keys' own range instead, 2048 steps at a time.
 #include <cfloat>
 
 #include "cascade_internal.h"
@@ -15,11 +18,9 @@
 
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kWarps = kThreads / 32;
-constexpr int kBins = 2048;
-constexpr int kMaxGroups = 2048;           // groups of consecutive tokens with a weight sum each
-constexpr int kResident = 48 * 1024;       // keys kept in shared memory
+constexpr int kBins = 2048;                // steps of a histogram; groups of consecutive tokens with a weight sum each
+constexpr int kList = 1024;                // tokens of one step that are ranked directly
+constexpr float kReach = 48.f;             // how far below the maximum the histogram reaches (its last step takes the rest)
 
 __device__ __forceinline__ uint32_t order_key(float x) {
   const uint32_t u = __float_as_uint(x);
@@ -33,21 +34,31 @@ __device__ __forceinline__ uint32_t logit_key(float x) {
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 
+template <int kThreads>
 struct Shared {
-  unsigned long long hist[kBins];
-  unsigned long long group[kMaxGroups];
-  unsigned long long red[kWarps];
+  union {
+    struct {
+      uint32_t lo[kBins], hi[kBins];       // 64-bit sums as two words
+    } hist;
+    unsigned long long group[kBins];
+  };
+  unsigned long long list_w[kList];
+  uint32_t list_k[kList];
   double table[32];                        // 2^(j/32)
-  uint32_t red_lo[kWarps], red_hi[kWarps];
-  unsigned long long above;
-  int bin;
+  unsigned long long warp_sum[kThreads / 32];
+  uint32_t red_lo[kThreads / 32], red_hi[kThreads / 32];
+  unsigned long long before;               // result of find()
+  int at;
+  int n_list;
+  uint32_t list_min, list_max;
+  uint32_t floor_key;
   int token;
 };
 
 struct SampleArgs {
   const void* logits;
   long long row_stride;
-  int V, fixed_bits, group_shift;          // group_shift: log2 of the tokens in a group
+  int V, n_res, fixed_bits, group_shift;   // keys kept in shared memory; log2 of the tokens in a group
   const float* temperature;
   const int32_t* top_k;
   const float *top_p, *min_p, *uniforms;
@@ -85,100 +96,231 @@ __device__ __forceinline__ unsigned long long warp_sum(unsigned long long v) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-__device__ unsigned long long block_sum(unsigned long long v, Shared& sh) {
-  v = warp_sum(v);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) sh.red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  unsigned long long t = 0;
-  for (int i = 0; i < kWarps; ++i) t += sh.red[i];
-  return t;
+
+// Adds w to a 64-bit sum kept as two words (native 32-bit atomics; the carry goes with whoever caused it).
+template <typename S>
+__device__ __forceinline__ void hist_add(S& sh, int bin, unsigned long long w) {
+  const uint32_t lo = (uint32_t)w;
+  const uint32_t old = atomicAdd(&sh.hist.lo[bin], lo);
+  const uint32_t hi = (uint32_t)(w >> 32) + (old + lo < old ? 1u : 0u);
+  if (hi != 0u) atomicAdd(&sh.hist.hi[bin], hi);
 }
 
 template <typename E>
 struct Row {
   const E* g;
-  const uint32_t* s;   // keys of the first n_res tokens
+  uint32_t* s;         // keys of the first n_res tokens
   int V, n_res;
   __device__ __forceinline__ uint32_t key(int i) const { return i < n_res ? s[i] : logit_key(to_float(g[i])); }
 };
 
-// The key x among keys in [lo, hi] with W(> x) < target <= W(>= x), W the weight (1 each, or exp) of keys >= lo; the
-// whole CTA calls it with the same arguments.  Every pass narrows [lo, hi] to one of 2048 steps.
-template <bool kMass, typename E>
-__device__ uint32_t descend(const Row<E>& row, const Weight& weight, uint32_t lo, uint32_t hi, unsigned long long target,
-                            Shared& sh) {
-  unsigned long long above = 0;
+// f(index, key) for every token of the row, in strides of the CTA; four independent reads at a time.
+template <int kThreads, typename E, typename F>
+__device__ __forceinline__ void each(const Row<E>& row, F f) {
+  int i = threadIdx.x;
+  for (; i + 3 * kThreads < row.V; i += 4 * kThreads) {
+    uint32_t k[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) k[q] = row.key(i + q * kThreads);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) f(i + q * kThreads, k[q]);
+  }
+  for (; i < row.V; i += kThreads) f(i, row.key(i));
+}
+
+// The first entry at which the running sum of kBins entries get(i) passes `target` (> target); sh.at and sh.before = the sum
+// in front of it.  target_of(total) is called with the sum of all entries.  sh.at = -1 if the total does not pass it.
+template <int kThreads, typename Get, typename Target>
+__device__ __forceinline__ unsigned long long find(Shared<kThreads>& sh, Get get, Target target_of) {
+  constexpr int kPer = kBins / kThreads;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  unsigned long long v[kPer], sum = 0;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    v[k] = get(threadIdx.x * kPer + k);
+    sum += v[k];
+  }
+  unsigned long long inc = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned long long t = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += t;
+  }
+  if (lane == 31) sh.warp_sum[warp] = inc;
+  if (threadIdx.x == 0) sh.at = -1;
+  __syncthreads();
+  // every warp scans the warps' sums for itself
+  unsigned long long w = lane < kThreads / 32 ? sh.warp_sum[lane] : 0ull, winc = w;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned long long t = __shfl_up_sync(0xffffffffu, winc, o);
+    if (lane >= o) winc += t;
+  }
+  const unsigned long long total = __shfl_sync(0xffffffffu, winc, 31);
+  unsigned long long run = __shfl_sync(0xffffffffu, winc - w, warp) + inc - sum;
+  const unsigned long long target = target_of(total);
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    if (run <= target && target < run + v[k]) {
+      sh.at = threadIdx.x * kPer + k;
+      sh.before = run;
+    }
+    run += v[k];
+  }
+  __syncthreads();
+  return total;
+}
+
+// The key x among keys in [lo, hi] with W(> x) <= target < W(>= x), W the weight (1 each, or exp) of keys >= lo: the
+// general search, 2048 steps of the keys' range at a time.  The whole CTA calls it with the same arguments.
+template <bool kMass, int kThreads, typename E>
+__device__ __noinline__ uint32_t descend(const Row<E>& row, const Weight& weight, uint32_t lo, uint32_t hi, unsigned long long target,
+                                         Shared<kThreads>& sh) {
   while (true) {
     const uint32_t range = hi - lo;
     const int shift = range < (uint32_t)kBins ? 0 : 32 - __clz(range) - 11;  // (range >> shift) < 2048
     __syncthreads();
-    for (int i = threadIdx.x; i < kBins; i += kThreads) sh.hist[i] = 0ull;
+    for (int i = threadIdx.x; i < kBins; i += kThreads) sh.hist.lo[i] = sh.hist.hi[i] = 0u;
     __syncthreads();
-    for (int i = threadIdx.x; i < row.V; i += kThreads) {
-      const uint32_t k = row.key(i);
-      if (k >= lo && k <= hi) atomicAdd(&sh.hist[(k - lo) >> shift], kMass ? weight(k) : 1ull);
-    }
-    __syncthreads();
-    if (threadIdx.x < 32) {
-      const int lane = threadIdx.x;
-      // lane L owns the 64 bins 2047 - 64 L ... , largest first
-      unsigned long long sum = 0;
-      for (int i = 0; i < 64; ++i) sum += sh.hist[kBins - 1 - 64 * lane - i];
-      unsigned long long inc = sum;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const unsigned long long t = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += t;
+    each<kThreads>(row, [&](int, uint32_t k) {
+      if (k >= lo && k <= hi) {
+        const int bin = kBins - 1 - (int)((k - lo) >> shift);   // largest first
+        if (kMass)
+          hist_add(sh, bin, weight(k));
+        else
+          atomicAdd(&sh.hist.lo[bin], 1u);
       }
-      const unsigned long long exc = inc - sum;
-      const bool mine = above + exc < target && target <= above + inc;
-      const uint32_t who = __ballot_sync(0xffffffffu, mine);
-      if (who == 0u) {
-        if (lane == 0) sh.bin = -1;   // the target lies beyond everything: all of it stays
-      } else if (mine) {
-        unsigned long long run = above + exc;
-        for (int i = 0; i < 64; ++i) {
-          const int b = kBins - 1 - 64 * lane - i;
-          if (run + sh.hist[b] >= target) {
-            sh.bin = b;
-            break;
-          }
-          run += sh.hist[b];
-        }
-        sh.above = run;
-      }
-    }
+    });
     __syncthreads();
-    const int bin = sh.bin;
-    if (bin < 0) return lo;
-    above = sh.above;
-    lo += (uint32_t)bin << shift;
+    find<kThreads>(sh, [&](int i) { return ((unsigned long long)sh.hist.hi[i] << 32) | sh.hist.lo[i]; },
+                   [&](unsigned long long) { return target; });
+    if (sh.at < 0) return lo;                                    // all of it stays
+    target -= sh.before;
+    lo += (uint32_t)(kBins - 1 - sh.at) << shift;
     if (shift == 0) return lo;
     const uint32_t step_end = lo + ((1u << shift) - 1u);
-    if (step_end < hi) hi = step_end;   // (the last step may pass the row's largest key)
+    if (step_end < hi) hi = step_end;                            // (the last step may pass the row's largest key)
   }
 }
 
-template <typename E>
-__global__ void __launch_bounds__(kThreads) k_sample(const SampleArgs a) {
-  extern __shared__ uint32_t s_keys[];
-  __shared__ Shared sh;
+// The same threshold by one histogram over the distance to the maximum.  target_of: from the total weight of keys >= floor.
+template <bool kMass, int kThreads, typename E, typename Target>
+__device__ uint32_t threshold(const Row<E>& row, const Weight& weight, float m, float steps_per_unit, uint32_t floor_key,
+                              uint32_t k_max, Target target_of, Shared<kThreads>& sh) {
+  const int tid = threadIdx.x;
+  auto bin_of = [&](uint32_t k) { return min(kBins - 1, (int)((m - key_value(k)) * steps_per_unit)); };
+  __syncthreads();
+  for (int i = tid; i < kBins; i += kThreads) sh.hist.lo[i] = sh.hist.hi[i] = 0u;
+  if (tid == 0) {
+    sh.n_list = 0;
+    sh.list_min = 0xffffffffu;
+    sh.list_max = 0u;
+  }
+  __syncthreads();
+  each<kThreads>(row, [&](int, uint32_t k) {
+    if (k >= floor_key) {
+      if (kMass)
+        hist_add(sh, bin_of(k), weight(k));
+      else
+        atomicAdd(&sh.hist.lo[bin_of(k)], 1u);
+    }
+  });
+  __syncthreads();
+  unsigned long long target = 0;
+  find<kThreads>(sh, [&](int i) { return ((unsigned long long)sh.hist.hi[i] << 32) | sh.hist.lo[i]; },
+                 [&](unsigned long long total) { return target = target_of(total); });
+  const int bin = sh.at;
+  if (bin < 0) return floor_key;                                 // all of it stays
+  const unsigned long long left = target - sh.before;            // of the step's own weight
+  // the tokens of that step
+  uint32_t lo = 0xffffffffu, hi = 0u;
+  each<kThreads>(row, [&](int, uint32_t k) {
+    if (k >= floor_key && bin_of(k) == bin) {
+      const int at = atomicAdd(&sh.n_list, 1);
+      if (at < kList) sh.list_k[at] = k;
+      lo = min(lo, k);
+      hi = max(hi, k);
+    }
+  });
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  if ((tid & 31) == 0 && hi != 0u) {
+    atomicMin(&sh.list_min, lo);
+    atomicMax(&sh.list_max, hi);
+  }
+  __syncthreads();
+  const int n = sh.n_list;
+  lo = sh.list_min;
+  hi = sh.list_max;
+  if (lo == hi) return lo;                                       // ties
+  if (n > kList) return descend<kMass>(row, weight, lo, hi, left, sh);
+  if (kMass) {
+    for (int i = tid; i < n; i += kThreads) sh.list_w[i] = weight(sh.list_k[i]);
+    __syncthreads();
+  }
+  for (int i = tid; i < n; i += kThreads) {
+    const uint32_t k = sh.list_k[i];
+    unsigned long long above = 0, with = 0;
+    for (int j = 0; j < n; ++j) {
+      const unsigned long long w = kMass ? sh.list_w[j] : 1ull;
+      above += sh.list_k[j] > k ? w : 0ull;
+      with += sh.list_k[j] >= k ? w : 0ull;
+    }
+    if (above <= left && left < with) sh.floor_key = k;          // exactly one value; its ties agree
+  }
+  __syncthreads();
+  return sh.floor_key;
+}
+
+template <typename E, int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_sample(const SampleArgs a) {
+  constexpr int kWarps = kThreads / 32;
+  extern __shared__ __align__(16) uint8_t s_raw[];
+  Shared<kThreads>& sh = *reinterpret_cast<Shared<kThreads>*>(s_raw);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = blockIdx.x;
   Row<E> row;
   row.g = static_cast<const E*>(a.logits) + (long long)r * a.row_stride;
-  row.s = s_keys;
+  row.s = reinterpret_cast<uint32_t*>(s_raw + sizeof(Shared<kThreads>));
   row.V = a.V;
-  row.n_res = min(a.V, kResident);
+  row.n_res = min(a.V, a.n_res);
   if (tid < 32) sh.table[tid] = exp2((double)tid / 32.0);
   // the row's keys, largest and smallest of those that can be kept
   uint32_t k_max = kNoKey, k_min = 0xffffffffu;
-  for (int i = tid; i < a.V; i += kThreads) {
-    const uint32_t k = logit_key(to_float(row.g[i]));
-    if (i < row.n_res) s_keys[i] = k;
+  auto take = [&](int i, float x) {
+    const uint32_t k = logit_key(x);
+    if (i < row.n_res) row.s[i] = k;
     k_max = max(k_max, k);
-    if (k != kNoKey) k_min = min(k_min, k);
+    k_min = min(k_min, k - 1u);                                  // kNoKey - 1 wraps to the largest
+  };
+  constexpr int kVec = 16 / sizeof(E);
+  int done = 0;
+  if ((reinterpret_cast<uintptr_t>(row.g) & 15u) == 0) {
+    const uint4* g16 = reinterpret_cast<const uint4*>(row.g);
+    const int n16 = a.V / kVec;
+    auto take16 = [&](int i, const uint4& v) {
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (sizeof(E) == 4) {
+          take(i * kVec + q, __uint_as_float(w[q]));
+        } else {
+          take(i * kVec + 2 * q, __uint_as_float(w[q] << 16));
+          take(i * kVec + 2 * q + 1, __uint_as_float(w[q] & 0xffff0000u));
+        }
+      }
+    };
+    int i = tid;
+    for (; i + 3 * kThreads < n16; i += 4 * kThreads) {
+      uint4 v[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = __ldg(g16 + i + q * kThreads);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) take16(i + q * kThreads, v[q]);
+    }
+    for (; i < n16; i += kThreads) take16(i, __ldg(g16 + i));
+    done = n16 * kVec;
   }
+  for (int i = done + tid; i < a.V; i += kThreads) take(i, to_float(row.g[i]));
   k_max = __reduce_max_sync(0xffffffffu, k_max);
   k_min = __reduce_min_sync(0xffffffffu, k_min);
   if (lane == 0) {
@@ -187,10 +329,8 @@ __global__ void __launch_bounds__(kThreads) k_sample(const SampleArgs a) {
   }
   if (tid == 0) sh.token = INT_MAX;
   __syncthreads();
-  for (int i = 0; i < kWarps; ++i) {
-    k_max = max(k_max, sh.red_hi[i]);
-    k_min = min(k_min, sh.red_lo[i]);
-  }
+  k_max = __reduce_max_sync(0xffffffffu, lane < kWarps ? sh.red_hi[lane] : kNoKey);
+  k_min = __reduce_min_sync(0xffffffffu, lane < kWarps ? sh.red_lo[lane] : 0xffffffffu) + 1u;
   if (k_max == kNoKey) {   // nothing to draw from
     if (tid == 0) {
       a.token[r] = -1;
@@ -202,8 +342,9 @@ __global__ void __launch_bounds__(kThreads) k_sample(const SampleArgs a) {
   const float T = a.temperature == nullptr ? 1.f : a.temperature[r];
   if (!(T > 0.f)) {        // the most likely token, lowest index first
     int best = INT_MAX;
-    for (int i = tid; i < a.V; i += kThreads)
-      if (row.key(i) == k_max) best = min(best, i);
+    each<kThreads>(row, [&](int i, uint32_t k) {
+      if (k == k_max) best = min(best, i);
+    });
     best = __reduce_min_sync(0xffffffffu, best);
     if (lane == 0 && best != INT_MAX) atomicMin(&sh.token, best);
     __syncthreads();
@@ -214,8 +355,9 @@ __global__ void __launch_bounds__(kThreads) k_sample(const SampleArgs a) {
     }
     return;
   }
+  const float m = key_value(k_max);
   Weight weight;
-  weight.m = (double)key_value(k_max);
+  weight.m = (double)m;
   weight.c = 46.166241308446828 / (double)T;   // 32 / ln 2
   weight.m_key = k_max;
   weight.bits = a.fixed_bits;
@@ -224,18 +366,36 @@ __global__ void __launch_bounds__(kThreads) k_sample(const SampleArgs a) {
   const int top_k = a.top_k == nullptr ? 0 : a.top_k[r];
   const float top_p = a.top_p == nullptr ? 1.f : a.top_p[r];
   const float min_p = a.min_p == nullptr ? 0.f : a.min_p[r];
-  if (top_k > 0 && top_k < a.V) floor_key = descend<false>(row, weight, floor_key, k_max, (unsigned long long)top_k, sh);
+  const float reach = fminf(m - key_value(k_min), kReach);
+  const float steps = (float)(kBins - 1) / reach;
+  const bool even = reach > 1e-30f && m < INFINITY;              // the histogram over distances makes sense
+  if (top_k > 0 && top_k < a.V) {
+    const unsigned long long target = (unsigned long long)top_k - 1ull;
+    if (even)
+      floor_key = threshold<false>(row, weight, m, steps, floor_key, k_max, [&](unsigned long long) { return target; }, sh);
+    else
+      floor_key = descend<false>(row, weight, floor_key, k_max, target, sh);
+  }
   if (top_p < 1.f) {
-    unsigned long long z = 0;
-    for (int i = tid; i < a.V; i += kThreads) {
-      const uint32_t k = row.key(i);
-      if (k >= floor_key) z += weight(k);
+    // kept iff W(> x) < top_p z; for whole W: W(> x) <= ceil(top_p z) - 1
+    auto target_of = [&](unsigned long long z) {
+      const double t = ceil((double)top_p * (double)z);
+      return t < 1.0 ? 0ull : (unsigned long long)t - 1ull;
+    };
+    if (even) {
+      floor_key = threshold<true>(row, weight, m, steps, floor_key, k_max, target_of, sh);
+    } else {
+      unsigned long long z = 0;
+      each<kThreads>(row, [&](int, uint32_t k) {
+        if (k >= floor_key) z += weight(k);
+      });
+      z = warp_sum(z);
+      __syncthreads();
+      if (lane == 0) sh.warp_sum[warp] = z;
+      __syncthreads();
+      z = warp_sum(lane < kWarps ? sh.warp_sum[lane] : 0ull);
+      floor_key = descend<true>(row, weight, floor_key, k_max, target_of(z), sh);
     }
-    z = block_sum(z, sh);
-    // W(> x) < top_p z for whole W: target = ceil(top_p z), at least 1
-    const double t = ceil((double)top_p * (double)z);
-    const unsigned long long target = t < 1.0 ? 1ull : (unsigned long long)t;
-    floor_key = descend<true>(row, weight, floor_key, k_max, target, sh);
   }
   if (min_p > 0.f) {
     // w >= min_p  <=>  l >= m + T ln(min_p)
@@ -247,55 +407,45 @@ __global__ void __launch_bounds__(kThreads) k_sample(const SampleArgs a) {
   }
   // weight sums of groups of consecutive tokens, one warp per group
   const int n_groups = ((a.V - 1) >> a.group_shift) + 1;
+  __syncthreads();                                               // the histogram's place becomes the groups'
+  for (int i = n_groups + tid; i < kBins; i += kThreads) sh.group[i] = 0ull;
   unsigned int count = 0;
   for (int g = warp; g < n_groups; g += kWarps) {
     unsigned long long sum = 0;
     const int end = min(a.V, (g + 1) << a.group_shift);
-    for (int i = (g << a.group_shift) + lane; i < end; i += 32) {
-      const uint32_t k = row.key(i);
-      if (k != kNoKey && k >= floor_key) {
-        sum += weight(k);
-        ++count;
-      }
+    for (int i0 = g << a.group_shift; i0 < end; i0 += 128) {
+      uint32_t k[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) k[q] = i0 + 32 * q + lane < end ? row.key(i0 + 32 * q + lane) : kNoKey;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (k[q] >= floor_key) {                                 // (floor_key is above kNoKey)
+          sum += weight(k[q]);
+          ++count;
+        }
     }
     sum = warp_sum(sum);
     if (lane == 0) sh.group[g] = sum;
   }
-  const unsigned long long n_kept = block_sum(count, sh);   // also a barrier behind the group sums
-  if (warp != 0) return;
-  // the group in which the cumulative weight passes u * total, then the token inside it; one warp
-  const int per = (n_groups + 31) / 32, g0 = min(n_groups, lane * per), g1 = min(n_groups, g0 + per);
-  unsigned long long sum = 0;
-  for (int g = g0; g < g1; ++g) sum += sh.group[g];
-  unsigned long long inc = sum;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const unsigned long long t = __shfl_up_sync(0xffffffffu, inc, o);
-    if (lane >= o) inc += t;
-  }
-  const unsigned long long total = __shfl_sync(0xffffffffu, inc, 31);
+  count = __reduce_add_sync(0xffffffffu, count);
+  if (lane == 0) sh.red_lo[warp] = count;
+  __syncthreads();
+  // the group in which the cumulative weight passes u * total (cumulative > u total <=> > floor(u total) for whole sums)
   float u = a.uniforms[r];
-  u = u > 0.f ? fminf(u, 1.f - FLT_EPSILON / 2.f) : 0.f;   // NaN and negative: 0
-  // cumulative > u * total  <=>  cumulative > floor(u * total) for whole sums
-  const unsigned long long target = min((unsigned long long)((double)u * (double)total), total - 1ull);
-  const uint32_t past = __ballot_sync(0xffffffffu, inc > target);
-  const int owner = __ffs(past) - 1;
-  int g_hit = 0;
-  unsigned long long run = 0;
-  if (lane == owner) {
-    run = inc - sum;
-    for (g_hit = g0; g_hit < g1 - 1; ++g_hit) {
-      if (run + sh.group[g_hit] > target) break;
-      run += sh.group[g_hit];
-    }
-  }
-  g_hit = __shfl_sync(0xffffffffu, g_hit, owner);
-  run = __shfl_sync(0xffffffffu, run, owner);
-  const int end = min(a.V, (g_hit + 1) << a.group_shift);
+  u = u > 0.f ? fminf(u, 1.f - FLT_EPSILON / 2.f) : 0.f;         // NaN and negative: 0
+  unsigned long long target = 0;
+  const unsigned long long total = find<kThreads>(sh, [&](int i) { return sh.group[i]; }, [&](unsigned long long z) {
+    return target = min((unsigned long long)((double)u * (double)z), z - 1ull);
+  });
+  if (warp != 0) return;
+  const uint32_t n_kept = __reduce_add_sync(0xffffffffu, lane < kWarps ? sh.red_lo[lane] : 0u);
+  // the token inside it; one warp
+  unsigned long long run = sh.before;
+  const int g_hit = sh.at, end = min(a.V, (g_hit + 1) << a.group_shift);
   for (int i0 = g_hit << a.group_shift; i0 < end; i0 += 32) {
     const int i = i0 + lane;
     const uint32_t k = i < end ? row.key(i) : kNoKey;
-    const unsigned long long w = k != kNoKey && k >= floor_key ? weight(k) : 0ull;
+    const unsigned long long w = k >= floor_key ? weight(k) : 0ull;
     unsigned long long c = w;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -313,6 +463,19 @@ __global__ void __launch_bounds__(kThreads) k_sample(const SampleArgs a) {
     }
     run += __shfl_sync(0xffffffffu, c, 31);
   }
+}
+
+template <typename E, int kThreads>
+int launch(const cascade_ctx* ctx, SampleArgs& a, int n_rows, cudaStream_t s) {
+  // what the row's keys may take: the CTA's share of an SM's 227 KB less its arrays (and 1 KB that the system takes)
+  constexpr int kMost = (kThreads == 1024 ? 226 : 112) * 1024 - (int)sizeof(Shared<kThreads>);
+  a.n_res = kMost / 4 < a.V ? kMost / 4 : a.V;
+  const size_t smem = sizeof(Shared<kThreads>) + (size_t)a.n_res * 4;
+  CASCADE_CUDA_TRY(cudaFuncSetAttribute(k_sample<E, kThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                        (int)sizeof(Shared<kThreads>) + kMost));
+  k_sample<E, kThreads><<<n_rows, kThreads, smem, s>>>(a);
+  CASCADE_CUDA_TRY(cudaGetLastError());
+  return CASCADE_OK;
 }
 
 }  // namespace
@@ -335,7 +498,7 @@ extern "C" int cascade_sample(cascade_ctx* ctx, const void* logits, int32_t logi
   while ((1ll << log_v) < V) ++log_v;
   a.fixed_bits = 62 - log_v < 50 ? 62 - log_v : 50;   // V weights of at most 1 stay below 2^62; one weight below 2^52
   a.group_shift = 7;
-  while (((V - 1) >> a.group_shift) + 1 > kMaxGroups) ++a.group_shift;
+  while (((V - 1) >> a.group_shift) + 1 > kBins) ++a.group_shift;
   a.temperature = temperature;
   a.top_k = top_k;
   a.top_p = top_p;
@@ -344,23 +507,10 @@ extern "C" int cascade_sample(cascade_ctx* ctx, const void* logits, int32_t logi
   a.token = token_out;
   a.prob = prob_out;
   a.kept = kept_out;
-  const size_t smem = (size_t)(V < kResident ? V : kResident) * 4;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (smem > 8 * 1024) {
-    const int most = kResident * 4;
-    if (bf16)
-      CASCADE_CUDA_TRY(cudaFuncSetAttribute(k_sample<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
-    else
-      CASCADE_CUDA_TRY(cudaFuncSetAttribute(k_sample<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
-  }
   ctx->launches = 0;
-  {
-    KernelScope ks(ctx, K_SAMPLE, s);
-    if (bf16)
-      k_sample<__nv_bfloat16><<<n_rows, kThreads, smem, s>>>(a);
-    else
-      k_sample<float><<<n_rows, kThreads, smem, s>>>(a);
-  }
-  CASCADE_CUDA_TRY(cudaGetLastError());
-  return CASCADE_OK;
+  KernelScope ks(ctx, K_SAMPLE, s);
+  const bool many = n_rows > ctx->sm_count;
+  if (bf16) return many ? launch<__nv_bfloat16, 512>(ctx, a, n_rows, s) : launch<__nv_bfloat16, 1024>(ctx, a, n_rows, s);
+  return many ? launch<float, 512>(ctx, a, n_rows, s) : launch<float, 1024>(ctx, a, n_rows, s);
 }
