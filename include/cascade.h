@@ -473,6 +473,7 @@ int cascade_paged_append(cascade_ctx* ctx, const cascade_paged_cache* cache, int
  *   q_begin[n_req] are not read, the same rows of out and lse not written.
  *   max_q, max_kv: no request has more new tokens / keys than this (host bounds that launch sizes come from; a
  *   request beyond them is left out, CASCADE_ERR_BAD_PAGE).  1 <= n_req <= CASCADE_MAX_REQUESTS.
+ *   Hq / Hkv <= 128 (CASCADE_ERR_UNSUPPORTED_SHAPE).
  *   window >= 0 (0: none), sinks >= 0.  Softmax and accumulation are fp32. */
 int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* cache, int32_t n_req, int32_t n_tok, const void* q,
                        int64_t q_stride, const int32_t* q_begin, const int32_t* kv_len, int32_t max_q, int32_t max_kv,

@@ -385,16 +385,18 @@ def _elem(ctx):
     return torch.bfloat16 if ctx.shape.dtype == BF16 else torch.float32
 
 
-def _vectors(dtype, n, **tensors):
-    """Dense tensors of n elements (None: not given)."""
-    for name, t in tensors.items():
-        if t is not None and (t.dtype != dtype or t.shape != (n,) or not t.is_contiguous()):
-            raise ValueError(f"{name}: expected a dense {dtype} tensor of {n} elements, got {t.dtype} {tuple(t.shape)}")
+def _vector(name, t, dtype, n):
+    """A dense tensor of n elements (None: not given); its address."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a dense {dtype} tensor of {n} elements, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
 
 
 def _rows(name, t, n, heads, D, dtype):
     """Row stride of a [n,heads,D] tensor whose rows may lie apart (a part of a stacked projection)."""
-    if t.dtype != dtype or t.shape != (n, heads, D):
+    if t.dtype is not dtype or t.shape != (n, heads, D):
         raise ValueError(f"{name}: expected {dtype} {(n, heads, D)}, got {t.dtype} {tuple(t.shape)}")
     st = t.stride()
     if st[2] != 1 or (heads > 1 and st[1] != D):
@@ -403,11 +405,17 @@ def _rows(name, t, n, heads, D, dtype):
 
 
 def _on_device(*tensors):
-    """Every tensor given lives on the current device."""
-    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+    """Every tensor given lives on the current device; its current stream."""
+    dev = None
     for t in tensors:
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"a tensor lives on {t.device}, not on the current CUDA device")
+        if t is not None:
+            d = t.get_device()
+            if d < 0 or (dev is not None and d != dev):
+                raise ValueError(f"a tensor lives on {t.device}, not on the current CUDA device")
+            dev = d
+    if dev != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors live on cuda:{dev}, not on the current CUDA device")
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
 class PagedCache:
@@ -430,10 +438,11 @@ class PagedCache:
         width = block_table.shape[1] if self.n_req == 1 else block_table.stride(0)
         self.struct = PagedCacheStruct(k_pages.data_ptr(), v_pages.data_ptr(), stride, n_pages, page,
                                        block_table.data_ptr(), width)
+        self.ref = C.byref(self.struct)
 
     def _check(self, ctx):
         sh = ctx.shape
-        if self.dtype != _elem(ctx) or self.heads != (sh.Hkv, sh.D):
+        if self.dtype is not _elem(ctx) or self.heads != (sh.Hkv, sh.D):
             raise ValueError("the pool's element type, key heads or head size are not the context's")
 
 
@@ -441,65 +450,68 @@ def cascade_paged_tables(ctx, page_size, n_pages, new_len, kv_len, block_table, 
                          free_count_out, q_begin, slot, pos):
     """Block tables, slot map and positions of the next pass; int32 device tensors (see include/cascade.h)."""
     n_req, n_tok, i32 = new_len.shape[0], slot.shape[0], torch.int32
-    _vectors(i32, n_req, new_len=new_len, kv_len=kv_len, kv_len_out=kv_len_out)
-    _vectors(i32, n_pages, free_pages=free_pages)
-    _vectors(i32, 1, free_count=free_count, free_count_out=free_count_out)
-    _vectors(i32, n_req + 1, q_begin=q_begin)
-    _vectors(i32, n_tok, slot=slot, pos=pos)
-    if block_table.dtype != i32 or block_table.dim() != 2 or block_table.shape[0] != n_req or not block_table.is_contiguous():
+    if block_table.dtype is not i32 or block_table.dim() != 2 or block_table.shape[0] != n_req or not block_table.is_contiguous():
         raise ValueError(f"block_table: expected a dense int32 tensor of {n_req} rows")
-    _on_device(new_len, kv_len, block_table, free_pages, free_count, kv_len_out, free_count_out, q_begin, slot, pos)
-    _check(lib().cascade_paged_tables(ctx.handle, n_req, n_tok, page_size, n_pages, new_len.data_ptr(), kv_len.data_ptr(),
-                                      block_table.data_ptr(), block_table.shape[1], free_pages.data_ptr(), free_count.data_ptr(),
-                                      kv_len_out.data_ptr(), free_count_out.data_ptr(), q_begin.data_ptr(),
-                                      slot.data_ptr() if n_tok else None, pos.data_ptr() if n_tok else None, _stream()))
+    new_p, kv_p, kv_out_p = (_vector("new_len", new_len, i32, n_req), _vector("kv_len", kv_len, i32, n_req),
+                             _vector("kv_len_out", kv_len_out, i32, n_req))
+    free_p, count_p, count_out_p = (_vector("free_pages", free_pages, i32, n_pages), _vector("free_count", free_count, i32, 1),
+                                    _vector("free_count_out", free_count_out, i32, 1))
+    begin_p, slot_p, pos_p = _vector("q_begin", q_begin, i32, n_req + 1), _vector("slot", slot, i32, n_tok), _vector("pos", pos, i32, n_tok)
+    stream = _on_device(new_len, kv_len, block_table, free_pages, free_count, kv_len_out, free_count_out, q_begin, slot, pos)
+    _check(lib().cascade_paged_tables(ctx.handle, n_req, n_tok, page_size, n_pages, new_p, kv_p, block_table.data_ptr(),
+                                      block_table.shape[1], free_p, count_p, kv_out_p, count_out_p, begin_p, slot_p, pos_p, stream))
 
 
 def cascade_paged_append(ctx, cache, k, v, slot, pos, rope_base=0.0, q=None, q_out=None):
     """Keys and values [n_tok,Hkv,D] (rotated unless rope_base is 0) into their slots; queries [n_tok,Hq,D] rotated."""
     cache._check(ctx)
     sh, e, n = ctx.shape, cache.dtype, slot.shape[0]
-    _vectors(torch.int32, n, slot=slot, pos=pos)
-    ks, vs = _rows("k", k, n, sh.Hkv, sh.D, e), _rows("v", v, n, sh.Hkv, sh.D, e)
-    qs = 0 if q is None else _rows("q", q, n, sh.Hq, sh.D, e)
-    qos = 0 if q_out is None else _rows("q_out", q_out, n, sh.Hq, sh.D, e)
-    _on_device(cache.k_pages, cache.v_pages, k, v, slot, pos, q, q_out)
-    _check(lib().cascade_paged_append(ctx.handle, C.byref(cache.struct), n, None if q is None else q.data_ptr(), qs,
-                                      k.data_ptr(), ks, v.data_ptr(), vs, slot.data_ptr(), pos.data_ptr(), rope_base,
-                                      None if q_out is None else q_out.data_ptr(), qos, _stream()))
+    Hkv, Hq, D = sh.Hkv, sh.Hq, sh.D
+    slot_p, pos_p = _vector("slot", slot, torch.int32, n), _vector("pos", pos, torch.int32, n)
+    ks, vs = _rows("k", k, n, Hkv, D, e), _rows("v", v, n, Hkv, D, e)
+    q_p = q_out_p = None
+    qs = qos = 0
+    if q is not None:
+        qs, q_p = _rows("q", q, n, Hq, D, e), q.data_ptr()
+    if q_out is not None:
+        qos, q_out_p = _rows("q_out", q_out, n, Hq, D, e), q_out.data_ptr()
+    stream = _on_device(cache.k_pages, cache.v_pages, k, v, slot, pos, q, q_out)
+    _check(lib().cascade_paged_append(ctx.handle, cache.ref, n, q_p, qs, k.data_ptr(), ks, v.data_ptr(), vs, slot_p, pos_p, rope_base,
+                                      q_out_p, qos, stream))
 
 
 def cascade_paged_attn(ctx, cache, q, q_begin, kv_len, max_q, max_kv, out, softmax_scale, window=0, sinks=0, lse=None):
     """Causal attention of each request's new tokens over its pages, optionally through a window beside sink tokens."""
     cache._check(ctx)
     sh, e, n_req, n = ctx.shape, cache.dtype, kv_len.shape[0], q.shape[0]
-    _vectors(torch.int32, n_req + 1, q_begin=q_begin)
-    _vectors(torch.int32, n_req, kv_len=kv_len)
+    Hq, D = sh.Hq, sh.D
+    begin_p, kv_p = _vector("q_begin", q_begin, torch.int32, n_req + 1), _vector("kv_len", kv_len, torch.int32, n_req)
     if cache.n_req < n_req:
         raise ValueError(f"block_table has {cache.n_req} rows for {n_req} requests")
-    qs = _rows("q", q, n, sh.Hq, sh.D, e)
-    if out.dtype != e or out.shape != (n, sh.Hq, sh.D) or not out.is_contiguous():
-        raise ValueError(f"out: expected a dense {e} tensor of {(n, sh.Hq, sh.D)}")
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (n, sh.Hq) or not lse.is_contiguous()):
-        raise ValueError(f"lse: expected a dense float32 tensor of {(n, sh.Hq)}")
-    _on_device(cache.k_pages, cache.v_pages, cache.block_table, q, q_begin, kv_len, out, lse)
-    _check(lib().cascade_paged_attn(ctx.handle, C.byref(cache.struct), n_req, n, q.data_ptr(), qs, q_begin.data_ptr(),
-                                    kv_len.data_ptr(), max_q, max_kv, window, sinks, softmax_scale, out.data_ptr(),
-                                    None if lse is None else lse.data_ptr(), _stream()))
+    qs = _rows("q", q, n, Hq, D, e)
+    if out.dtype is not e or out.shape != (n, Hq, D) or not out.is_contiguous():
+        raise ValueError(f"out: expected a dense {e} tensor of {(n, Hq, D)}")
+    lse_p = None
+    if lse is not None:
+        if lse.dtype is not torch.float32 or lse.shape != (n, Hq) or not lse.is_contiguous():
+            raise ValueError(f"lse: expected a dense float32 tensor of {(n, Hq)}")
+        lse_p = lse.data_ptr()
+    stream = _on_device(cache.k_pages, cache.v_pages, cache.block_table, q, q_begin, kv_len, out, lse)
+    _check(lib().cascade_paged_attn(ctx.handle, cache.ref, n_req, n, q.data_ptr(), qs, begin_p, kv_p, max_q, max_kv, window, sinks,
+                                    softmax_scale, out.data_ptr(), lse_p, stream))
 
 
 def cascade_sample(ctx, logits, uniforms, token, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, kept=None):
     """One token per row of [n_rows,V] float or bf16 logits (rows may lie apart); settings are device tensors per row."""
-    if logits.dim() != 2 or logits.shape[1] != ctx.shape.V or logits.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError(f"logits: expected float32 or bfloat16 [n_rows, {ctx.shape.V}], got {logits.dtype} {tuple(logits.shape)}")
+    dt, f32, i32 = logits.dtype, torch.float32, torch.int32
+    if logits.dim() != 2 or logits.shape[1] != ctx.shape.V or (dt is not f32 and dt is not torch.bfloat16):
+        raise ValueError(f"logits: expected float32 or bfloat16 [n_rows, {ctx.shape.V}], got {dt} {tuple(logits.shape)}")
     n, V = logits.shape
     st = logits.stride()
     if st[1] != 1:
         raise ValueError("a row of logits must be dense")
-    _vectors(torch.float32, n, uniforms=uniforms, temperature=temperature, top_p=top_p, min_p=min_p, prob=prob)
-    _vectors(torch.int32, n, token=token, top_k=top_k, kept=kept)
-    _on_device(logits, uniforms, token, temperature, top_k, top_p, min_p, prob, kept)
-    p = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    _check(lib().cascade_sample(ctx.handle, logits.data_ptr(), F32 if logits.dtype == torch.float32 else BF16,
-                                V if n == 1 else st[0], n, p(temperature), p(top_k), p(top_p), p(min_p), p(uniforms),
-                                p(token), p(prob), p(kept), _stream()))
+    args = (_vector("temperature", temperature, f32, n), _vector("top_k", top_k, i32, n), _vector("top_p", top_p, f32, n),
+            _vector("min_p", min_p, f32, n), _vector("uniforms", uniforms, f32, n), _vector("token", token, i32, n),
+            _vector("prob", prob, f32, n), _vector("kept", kept, i32, n))
+    stream = _on_device(logits, uniforms, token, temperature, top_k, top_p, min_p, prob, kept)
+    _check(lib().cascade_sample(ctx.handle, logits.data_ptr(), F32 if dt is f32 else BF16, V if n == 1 else st[0], n, *args, stream))

@@ -64,6 +64,9 @@ struct cascade_ctx {
   // cudaFuncSetAttribute is per device and a context is bound to one device: what has been set is kept here
   int gemm_smem_configured[6] = {0, 0, 0, 0, 0, 0};
   bool attn_configured = false, filter_configured = false;
+  uint32_t paged_configured = 0;         // one bit per kernel of the paged and sampling calls
+  float rope_base = 0.f;                 // base of rope_turns (0: none yet)
+  double rope_turns[64];                 // rope_base^(-2i/D) / 2 pi, turns per position
   std::vector<TimedLaunch> timed;        // event pairs recorded since the last read
   std::vector<cudaEvent_t> event_pool;   // spare events
   void* tmap_cache = nullptr; // TMA tensor maps built so far (tmap.cu)

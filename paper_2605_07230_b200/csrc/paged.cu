@@ -1,6 +1,7 @@
 // The paged KV cache's bookkeeping and its writer: block tables, slot map and free-page stack of the next pass from the
 // requests' lengths, and rotary embedding + cache write of a pass's keys and values (queries rotated beside them).
 #include <cmath>
+#include <cstring>
 
 #include "cascade_internal.h"
 #include "paged.h"
@@ -365,8 +366,7 @@ int cascade_paged_tables(cascade_ctx* ctx, int32_t n_req, int32_t n_tok, int32_t
   a.err = ctx->dev_error;
   const size_t smem = (size_t)(4 * n_req + 1) * sizeof(int);
   if (smem > 48 * 1024)
-    CASCADE_CUDA_TRY(cudaFuncSetAttribute(k_paged_tables, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                          (4 * CASCADE_MAX_REQUESTS + 1) * (int)sizeof(int)));
+    CASCADE_TRY(configure_smem(ctx, PAGED_CFG_TABLES, k_paged_tables, (4 * CASCADE_MAX_REQUESTS + 1) * (int)sizeof(int)));
   // one CTA up to 4096 tokens (no second SM to wait for), then a cluster of eight
   const int n_cta = n_tok <= 4 * kTabThreads && n_req <= 64 ? 1 : 8;
   cudaLaunchConfig_t cfg = {};
@@ -425,8 +425,11 @@ int cascade_paged_append(cascade_ctx* ctx, const cascade_paged_cache* cache, int
   a.slot = slot;
   a.pos = pos;
   a.err = ctx->dev_error;
-  for (int i = 0; i < kMaxHalf; ++i)
-    a.turns[i] = rope && i < sh.D / 2 ? std::pow((double)rope_base, -2.0 * i / sh.D) / 6.283185307179586476925 : 0.0;
+  if (rope && ctx->rope_base != rope_base) {
+    for (int i = 0; i < sh.D / 2; ++i) ctx->rope_turns[i] = std::pow((double)rope_base, -2.0 * i / sh.D) / 6.283185307179586476925;
+    ctx->rope_base = rope_base;
+  }
+  if (rope) std::memcpy(a.turns, ctx->rope_turns, sizeof(double) * (sh.D / 2));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   ctx->launches = 0;
   {

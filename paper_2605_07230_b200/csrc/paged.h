@@ -6,3 +6,14 @@
 int check_paged_cache(const cascade_ctx* ctx, const cascade_paged_cache* cache);
 // CASCADE_ERR_INVALID_ARG unless the context's device is the current one.
 int check_current_device(const cascade_ctx* ctx);
+
+// Bits of cascade_ctx.paged_configured.
+enum : uint32_t { PAGED_CFG_TABLES = 1, PAGED_CFG_ATTN_TC = 2, PAGED_CFG_SAMPLE = 4 /* four bits: type, CTA size */ };
+// Lets kernel `f` use `bytes` of dynamic shared memory, once per context and bit.
+template <typename F>
+int configure_smem(cascade_ctx* ctx, uint32_t bit, F* f, int bytes) {
+  if (ctx->paged_configured & bit) return CASCADE_OK;
+  CASCADE_CUDA_TRY(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  ctx->paged_configured |= bit;
+  return CASCADE_OK;
+}

@@ -1,29 +1,8 @@
-// Causal attention of every request's new tokens over its paged cache: checks, and the kernel of the fp32 type.
+// Causal attention of every request's new tokens over its paged cache: checks and the choice of a kernel.
 #include "paged.h"
 #include "paged_attn.cuh"
 
-namespace {
-
-constexpr int kWarps = 8;
-
-// One warp per (new token, query head).
-template <typename E, int D>
-__global__ void __launch_bounds__(kWarps * 32) k_paged_attn_row(const PagedAttnArgs a) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int i = blockIdx.x * kWarps + warp, head = blockIdx.y, r = blockIdx.z;
-  paged::Request rq;
-  if (!paged::load_request(a, r, &rq) || i >= rq.nq) return;
-  paged::attend_row<E, D>(a, r, rq.q0 + i, rq.kv - rq.nq + i, head, lane);
-}
-
-template <typename E, int D>
-int launch_row(const PagedAttnArgs& a, cudaStream_t s) {
-  k_paged_attn_row<E, D><<<dim3(cascade_detail::ceil_div(a.max_q, kWarps), a.Hq, a.n_req), kWarps * 32, 0, s>>>(a);
-  CASCADE_CUDA_TRY(cudaGetLastError());
-  return CASCADE_OK;
-}
-
-}  // namespace
+constexpr int kMaxGroup = 128;  // query heads a key head: they share a row block
 
 extern "C" int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* cache, int32_t n_req, int32_t n_tok,
                                   const void* q, int64_t q_stride, const int32_t* q_begin, const int32_t* kv_len,
@@ -39,7 +18,7 @@ extern "C" int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* c
   if (q_stride < (int64_t)sh.Hq * sh.D || q_stride * es % 16 != 0) return CASCADE_ERR_INVALID_ARG;
   if (((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15u) != 0 || (reinterpret_cast<uintptr_t>(lse) & 3u) != 0)
     return CASCADE_ERR_INVALID_ARG;
-  if (n_req > CASCADE_MAX_REQUESTS) return CASCADE_ERR_UNSUPPORTED_SHAPE;
+  if (n_req > CASCADE_MAX_REQUESTS || sh.Hq / sh.Hkv > kMaxGroup) return CASCADE_ERR_UNSUPPORTED_SHAPE;
   CASCADE_TRY(check_current_device(ctx));
   PagedAttnArgs a;
   a.n_req = n_req;
@@ -69,8 +48,6 @@ extern "C" int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* c
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   ctx->launches = 0;
   KernelScope ks(ctx, K_PAGED_ATTN, s);
-  if (sh.dtype == CASCADE_BF16 && paged_attn_rows_takes(a)) return launch_paged_attn_rows(ctx, a, s);
-  if (sh.dtype == CASCADE_BF16 && paged_attn_tc_takes(a)) return launch_paged_attn_tc(ctx, a, s);
-  if (sh.dtype == CASCADE_BF16) return sh.D == 128 ? launch_row<__nv_bfloat16, 128>(a, s) : launch_row<__nv_bfloat16, 64>(a, s);
-  return sh.D == 128 ? launch_row<float, 128>(a, s) : launch_row<float, 64>(a, s);
+  if (sh.dtype == CASCADE_BF16) return paged_attn_rows_takes(a) ? launch_paged_attn_rows(ctx, a, s) : launch_paged_attn_tc(ctx, a, s);
+  return launch_paged_attn_f32(ctx, a, s);
 }

@@ -93,11 +93,125 @@ __device__ void attend_row(const PagedAttnArgs& a, int r, int row, int x, int he
   if (a.lse != nullptr && lane == 0) a.lse[(long long)row * a.Hq + head] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
 }
 
+// key / page_size by a multiplication, for keys below 2^31.
+struct PageDiv {
+  uint32_t mul;
+  int shift;
+  __device__ __forceinline__ int page(int key) const { return (int)(((unsigned long long)(uint32_t)key * mul) >> shift); }
+};
+inline PageDiv page_div(int page_size) {
+  int lg = 0;
+  while ((1ll << lg) < page_size) ++lg;
+  return {(uint32_t)(((1ull << (31 + lg)) + (unsigned)page_size - 1) / (unsigned)page_size), 31 + lg};
+}
+
+__device__ __forceinline__ uint4 ld_stream(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.L2::256B.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+
+// Partial results of kernels whose splits are the CTAs of a cluster: [part][row][part_stride] floats in shared memory, a row
+// being D un-normalised outputs, the reference (log2 units) and the sum of weights.
+__host__ __device__ constexpr int part_stride(int D) { return D + 4; }
+
+__device__ __forceinline__ void store4(float* p, const float4& v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const float4& v) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(ptx::pack_bf16x2(v.x, v.y), ptx::pack_bf16x2(v.z, v.w));
+}
+
+// Floats of shared memory for `rows` rows: the parts' results, then what the cluster's CTAs send each other.
+__host__ __device__ constexpr int part_floats(int D, int parts, int rows) { return (parts * rows + rows + 8) * part_stride(D); }
+
+// Ends such a kernel: merges the CTA's `kParts` partial results of rows row0 .. row0 + rows - 1 (row = token * G + query head
+// of the group; x0 = position of the request's first new token) and sends every row to the CTA of the cluster that finishes
+// it (row % splits), which stores outputs and lse and computes a row whose result is not finite again from the keys it sees
+// alone.  max_rows: rows per part in s_part (part_floats(D, kParts, max_rows) floats), at most kMaxRows (<= 32).  splits <= 8.
+// Every thread of every CTA of the cluster calls it, having arrived at the cluster's barrier (splits > 1) without waiting,
+// with the partial results written but no barrier behind them yet.
+template <typename E, int D, int kParts, int kMaxRows>
+__device__ __forceinline__ void merge_and_store(const PagedAttnArgs& a, int r, int q0, int x0, int kh, int row0, int rows, int G, int splits,
+                                                float* s_part, int max_rows) {
+  constexpr int kX = part_stride(D), kMost = 8;
+  static_assert(kMaxRows <= 32 && kParts <= kMost, "row bits, weights");
+  __shared__ uint32_t s_odd;
+  const int threads = (int)blockDim.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  float* s_in = s_part + kParts * max_rows * kX;   // [row / splits][split][kX]
+  if (tid == 0) s_odd = 0u;
+  __syncthreads();
+  // four columns of a row from its parts, `stride` floats apart
+  auto merge = [&](const float* part, int stride, int count, int col, float* ref, float* sum) {
+    float m = -INFINITY, total = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < count; ++s) m = fmaxf(m, part[s * stride + D]);
+#pragma unroll 2
+    for (int s = 0; s < count; ++s) {
+      const float ms = part[s * stride + D], w = ms == -INFINITY ? 0.f : ptx::ex2(ms - m);
+      const float4 v = *reinterpret_cast<const float4*>(part + s * stride + col);
+      total += w * part[s * stride + D + 1];       // (a NaN sum stays one)
+      // a part of weight 0 met nothing of the row: what it holds is 0, or NaN by a value nobody saw
+      acc.x += w == 0.f ? 0.f : w * v.x;
+      acc.y += w == 0.f ? 0.f : w * v.y;
+      acc.z += w == 0.f ? 0.f : w * v.z;
+      acc.w += w == 0.f ? 0.f : w * v.w;
+    }
+    *ref = m;
+    *sum = total;
+    return acc;
+  };
+  auto finish = [&](int row, int col, const float4& acc, float ref, float sum) {
+    const int q_row = row0 + row, x = x0 + q_row / G;
+    const long long at = (long long)(q0 + q_row / G) * a.Hq + kh * G + q_row % G;
+    const float inv = x < 0 ? 0.f : 1.f / sum;
+    const float4 v = x < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    store4(static_cast<E*>(a.out) + at * D + col, v);
+    if (col == 0 && a.lse != nullptr) a.lse[at] = x < 0 ? -INFINITY : (ref + log2f(sum)) * kLn2;
+    const float bad = v.x * 0.f + v.y * 0.f + v.z * 0.f + v.w * 0.f;   // NaN if any is not finite
+    if (x >= 0 && (bad != 0.f || !(sum > 0.f))) atomicOr(&s_odd, 1u << row);
+  };
+  const int rank = splits == 1 ? 0 : (int)ptx::cluster_ctarank();
+  const uint32_t in = ptx::smem_u32(s_in);
+  if (splits > 1) ptx::cluster_wait();             // the others have started: their shared memory may be written
+  for (int i = tid; i < rows * (D / 4); i += threads) {
+    const int row = i / (D / 4), col = i % (D / 4) * 4;
+    float ref, sum;
+    const float4 acc = merge(s_part + row * kX, max_rows * kX, kParts, col, &ref, &sum);
+    if (splits == 1) {
+      finish(row, col, acc, ref, sum);
+    } else {
+      const uint32_t to = ptx::map_to_cta(in + (uint32_t)((row / splits * splits + rank) * kX) * 4u, (uint32_t)(row % splits));
+      ptx::st_cluster_v4(to + col * 4u, acc);
+      if (col == 0) {
+        ptx::st_cluster_f32(to + D * 4u, ref);
+        ptx::st_cluster_f32(to + D * 4u + 4u, sum);
+      }
+    }
+  }
+  if (splits > 1) {
+    __syncwarp();
+    ptx::cluster_arrive();
+    ptx::cluster_wait();                           // all rows of this CTA are here
+    const int mine = rows > rank ? (rows - rank + splits - 1) / splits : 0;
+    for (int i = tid; i < mine * (D / 4); i += threads) {
+      const int row = rank + i / (D / 4) * splits, col = i % (D / 4) * 4;
+      float ref, sum;
+      const float4 acc = merge(s_in + row / splits * splits * kX, kX, splits, col, &ref, &sum);
+      finish(row, col, acc, ref, sum);
+    }
+  }
+  __syncthreads();
+  for (uint32_t left = s_odd; left != 0u; left &= left - 1u) {         // (only where rows were finished)
+    const int row = __ffs(left) - 1, q_row = row0 + row;
+    if (row % (threads / 32) == warp) attend_row<E, D>(a, r, q0 + q_row / G, x0 + q_row / G, kh * G + q_row % G, lane);
+  }
+}
+
 }  // namespace paged
 
-// paged_attn_tc.cu: row blocks on the tensor cores (bf16).  `takes`: the group of query heads fits into a block.
-bool paged_attn_tc_takes(const PagedAttnArgs& a);
+// paged_attn_tc.cu: row blocks on the tensor cores (bf16).
 int launch_paged_attn_tc(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_t s);
 // paged_attn_rows.cu: at most 16 rows a key head, warp-level products straight from memory (bf16).
 bool paged_attn_rows_takes(const PagedAttnArgs& a);
 int launch_paged_attn_rows(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_t s);
+// paged_attn_f32.cu: the fp32 type.
+int launch_paged_attn_f32(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_t s);

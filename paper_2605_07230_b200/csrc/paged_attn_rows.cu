@@ -27,15 +27,9 @@ constexpr int kSortMost = 256;    // requests that are ordered by length
 struct RowArgs {
   PagedAttnArgs a;
   int G, splits, sorted, max_rows;
-  uint32_t page_mul;              // key / page_size = (key * page_mul) >> page_shift for keys below 2^31
-  int page_shift;
+  paged::PageDiv div;
 };
 
-__device__ __forceinline__ uint4 ld_stream(const void* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.L2::256B.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
 // 8 x 8 transpose of 16-bit elements across the warp.
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   uint32_t y;
@@ -55,9 +49,8 @@ __global__ void __launch_bounds__(kThreads, kNb == 1 ? 3 : 2) k_paged_attn_rows(
   constexpr int kQ = D / 32;                     // 16-byte pieces of a key row per lane
   constexpr int kJ = D / 64;                     // 16-byte pieces of a value row per lane
   constexpr int kO = D / 16;                     // output products
-  constexpr int kX = D + 4;                      // floats per row of a partial result: outputs, reference, sum
+  constexpr int kX = paged::part_stride(D);
   extern __shared__ __align__(16) float s_part[];  // [warp][row][kX], as many rows as the call has at most
-  __shared__ int s_odd;
   const PagedAttnArgs& a = p.a;
   const int part = p.max_rows * kX;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -82,7 +75,7 @@ __global__ void __launch_bounds__(kThreads, kNb == 1 ? 3 : 2) k_paged_attn_rows(
   const bool valid = paged::load_request(a, r, &rq);
   const int rows = valid ? rq.nq * p.G : 0;      // at most 8 kNb
   const int x0 = rq.kv - rq.nq;                  // position of the first new token
-  if (threadIdx.x == 0) s_odd = 0;
+  if (p.splits > 1) ptx::cluster_arrive();       // (waited for in merge_and_store)
 
   // 16-key steps that any row sees: [0, n_sink) and [n_sink + skip, ...)
   int n = 0, n_sink = 0, skip = 0;
@@ -129,7 +122,7 @@ __global__ void __launch_bounds__(kThreads, kNb == 1 ? 3 : 2) k_paged_attn_rows(
   // element offset of a group of 8 keys (a group lies in one page); -1: nothing there
   auto page_off = [&](int key) -> long long {
     if (key >= rq.kv) return -1;
-    const int pi = (int)(((unsigned long long)(uint32_t)key * p.page_mul) >> p.page_shift);
+    const int pi = p.div.page(key);
     const int page = table[pi];
     if (page < 0 || page >= a.n_pages) {
       if (lane == 0) atomicOr(a.err, CASCADE_DEV_ERR_BAD_PAGE);
@@ -144,7 +137,7 @@ __global__ void __launch_bounds__(kThreads, kNb == 1 ? 3 : 2) k_paged_attn_rows(
       const bool there = off[h] >= 0 && key0 + 8 * h + g < rq.kv;
       const __nv_bfloat16* src = k_base + (there ? off[h] : 0) + (there ? g : 0) * row_elems + 8 * t;
 #pragma unroll
-      for (int j = 0; j < kQ; ++j) kr[h][j] = there ? ld_stream(src + 32 * j) : make_uint4(0, 0, 0, 0);
+      for (int j = 0; j < kQ; ++j) kr[h][j] = there ? paged::ld_stream(src + 32 * j) : make_uint4(0, 0, 0, 0);
     }
   };
   auto load_v = [&](int key0, const long long* off) {
@@ -154,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, kNb == 1 ? 3 : 2) k_paged_attn_rows(
       const bool there = off[h] >= 0 && key0 + 8 * h + in < rq.kv;
       const __nv_bfloat16* src = v_base + (there ? off[h] : 0) + (there ? in : 0) * row_elems + 8 * g;
 #pragma unroll
-      for (int j = 0; j < kJ; ++j) vr[i][j] = there ? ld_stream(src + 64 * j) : make_uint4(0, 0, 0, 0);
+      for (int j = 0; j < kJ; ++j) vr[i][j] = there ? paged::ld_stream(src + 64 * j) : make_uint4(0, 0, 0, 0);
     }
   };
 
@@ -297,82 +290,7 @@ __global__ void __launch_bounds__(kThreads, kNb == 1 ? 3 : 2) k_paged_attn_rows(
         }
       }
     }
-  __syncthreads();
-  // element i of the CTA's rows, from `count` partial results `get(s, row, column)`
-  auto merge = [&](int row, int col, int count, auto get, float* ref_out, float* sum_out) {
-    float m = -INFINITY;
-    for (int s = 0; s < count; ++s) m = fmaxf(m, get(s, row, D));
-    float acc = 0.f, sum = 0.f;
-    for (int s = 0; s < count; ++s) {
-      const float ms = get(s, row, D);
-      const float w = ms == -INFINITY ? 0.f : ptx::ex2(ms - m);
-      // a split that met nothing has no part in the row: what it holds is 0, or NaN by a value nobody saw
-      acc += ms == -INFINITY ? 0.f : w * get(s, row, col);
-      sum += w * get(s, row, D + 1);
-    }
-    *ref_out = m;
-    *sum_out = sum;
-    return acc;
-  };
-  auto here = [&](int s, int row, int col) { return s_part[s * part + row * kX + col]; };
-  const bool alone = p.splits == 1;
-  auto finish = [&](int row, int col, float acc, float m, float sum) {
-    const int x = x0 + row / p.G, tok = rq.q0 + row / p.G, head = kh * p.G + row % p.G;
-    const long long at = (long long)tok * a.Hq + head;
-    const float v = x < 0 ? 0.f : acc / sum;
-    static_cast<__nv_bfloat16*>(a.out)[at * D + col] = __float2bfloat16(v);
-    if (col == 0 && a.lse != nullptr) a.lse[at] = x < 0 ? -INFINITY : (m + log2f(sum)) * paged::kLn2;
-    if (x >= 0 && !(fabsf(v) < INFINITY && sum > 0.f)) atomicOr(&s_odd, 1 << row);
-  };
-  if (alone) {
-    for (int i = threadIdx.x; i < rows * D; i += kThreads) {
-      float m, sum;
-      const float acc = merge(i / D, i % D, kWarps, here, &m, &sum);
-      finish(i / D, i % D, acc, m, sum);
-    }
-  } else {
-    // merge the CTA's warps into s_part[0] (each thread reads a column of all four before it writes)
-    constexpr int kMine = 8 * kNb * D / kThreads;
-    float mine[kMine], m_mine[kMine], sum_mine[kMine];
-#pragma unroll
-    for (int k = 0; k < kMine; ++k) {
-      const int i = k * kThreads + threadIdx.x;
-      if (i < rows * D) mine[k] = merge(i / D, i % D, kWarps, here, &m_mine[k], &sum_mine[k]);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kMine; ++k) {
-      const int i = k * kThreads + threadIdx.x;
-      if (i < rows * D) {
-        s_part[i / D * kX + i % D] = mine[k];
-        if (i % D == 0) {
-          s_part[i / D * kX + D] = m_mine[k];
-          s_part[i / D * kX + D + 1] = sum_mine[k];
-        }
-      }
-    }
-    __syncwarp();
-    ptx::cluster_arrive();
-    ptx::cluster_wait();
-    if (ptx::cluster_ctarank() == 0) {
-      const uint32_t base = ptx::smem_u32(s_part);
-      auto there = [&](int s, int row, int col) { return ptx::ld_cluster_f32(ptx::map_to_cta(base + (uint32_t)(row * kX + col) * 4u, (uint32_t)s)); };
-      for (int i = threadIdx.x; i < rows * D; i += kThreads) {
-        float m, sum;
-        const float acc = merge(i / D, i % D, p.splits, there, &m, &sum);
-        finish(i / D, i % D, acc, m, sum);
-      }
-    }
-    __syncwarp();
-    ptx::cluster_arrive();   // nobody leaves while its shared memory may still be read
-    ptx::cluster_wait();
-  }
-  __syncthreads();
-  for (uint32_t left = (uint32_t)s_odd; left != 0u; left &= left - 1u) {   // (only where rows were finished)
-    const int row = __ffs(left) - 1;
-    if (row % kWarps == warp)
-      paged::attend_row<__nv_bfloat16, D>(a, r, rq.q0 + row / p.G, x0 + row / p.G, kh * p.G + row % p.G, lane);
-  }
+  paged::merge_and_store<__nv_bfloat16, D, kWarps, 8 * kNb>(a, r, rq.q0, x0, kh, 0, rows, p.G, p.splits, s_part, p.max_rows);
 }
 
 }  // namespace
@@ -383,10 +301,7 @@ int launch_paged_attn_rows(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_
   RowArgs p;
   p.a = a;
   p.G = a.Hq / a.Hkv;
-  int lg = 0;
-  while ((1ll << lg) < a.page_size) ++lg;
-  p.page_shift = 31 + lg;
-  p.page_mul = (uint32_t)(((1ull << p.page_shift) + a.page_size - 1) / a.page_size);
+  p.div = paged::page_div(a.page_size);
   // splits: as many as keep the resident CTAs (three an SM) busy at once, each with at least two steps a warp
   const long long units = (long long)a.n_req * a.Hkv;
   const int span = a.window > 0 && (long long)a.window + a.sinks + a.max_q < a.max_kv ? a.window + a.sinks + a.max_q : a.max_kv;
@@ -400,7 +315,7 @@ int launch_paged_attn_rows(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p.splits, a.Hkv, a.n_req);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = (size_t)kWarps * p.max_rows * (ctx->shape.D + 4) * sizeof(float);
+  cfg.dynamicSmemBytes = (size_t)paged::part_floats(ctx->shape.D, kWarps, p.max_rows) * sizeof(float);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;

@@ -471,7 +471,7 @@ int launch(cascade_ctx* ctx, const TcArgs& p, int n_items, cudaStream_t s) {
   const CUtensorMap* mk = get_tmap_4d_bf16(ctx, a.k, dk, sk, bk);
   const CUtensorMap* mv = get_tmap_4d_bf16(ctx, a.v, dk, sk, bk);
   if (mq == nullptr || mk == nullptr || mv == nullptr) return CASCADE_ERR_CUDA;
-  CASCADE_CUDA_TRY(cudaFuncSetAttribute(k_paged_attn_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::kSmem));
+  CASCADE_TRY(configure_smem(ctx, PAGED_CFG_ATTN_TC, k_paged_attn_tc<D>, Cfg<D>::kSmem));   // (a context has one D)
   const int grid = n_items < ctx->sm_count ? n_items : ctx->sm_count;
   k_paged_attn_tc<D><<<grid, kThreads, Cfg<D>::kSmem, s>>>(*mq, *mk, *mv, p);
   CASCADE_CUDA_TRY(cudaGetLastError());
@@ -479,8 +479,6 @@ int launch(cascade_ctx* ctx, const TcArgs& p, int n_items, cudaStream_t s) {
 }
 
 }  // namespace
-
-bool paged_attn_tc_takes(const PagedAttnArgs& a) { return a.Hq / a.Hkv <= kTile; }
 
 int launch_paged_attn_tc(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_t s) {
   TcArgs p;

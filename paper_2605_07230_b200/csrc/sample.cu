@@ -466,13 +466,13 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_sample(const Samp
 }
 
 template <typename E, int kThreads>
-int launch(const cascade_ctx* ctx, SampleArgs& a, int n_rows, cudaStream_t s) {
+int launch(cascade_ctx* ctx, SampleArgs& a, int n_rows, cudaStream_t s) {
   // what the row's keys may take: the CTA's share of an SM's 227 KB less its arrays (and 1 KB that the system takes)
   constexpr int kMost = (kThreads == 1024 ? 226 : 112) * 1024 - (int)sizeof(Shared<kThreads>);
   a.n_res = kMost / 4 < a.V ? kMost / 4 : a.V;
   const size_t smem = sizeof(Shared<kThreads>) + (size_t)a.n_res * 4;
-  CASCADE_CUDA_TRY(cudaFuncSetAttribute(k_sample<E, kThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                        (int)sizeof(Shared<kThreads>) + kMost));
+  const uint32_t bit = PAGED_CFG_SAMPLE << ((sizeof(E) == 2 ? 2 : 0) + (kThreads == 1024 ? 1 : 0));
+  CASCADE_TRY(configure_smem(ctx, bit, k_sample<E, kThreads>, (int)sizeof(Shared<kThreads>) + kMost));
   k_sample<E, kThreads><<<n_rows, kThreads, smem, s>>>(a);
   CASCADE_CUDA_TRY(cudaGetLastError());
   return CASCADE_OK;
