@@ -26,6 +26,26 @@ constexpr int kTile = 128;        // keys per tile, rows per block
 constexpr int kThreads = 320;
 constexpr int kStages = 5;
 constexpr float kLazy = 8.f;      // log2 units
+constexpr float kFar = 96.f;      // a score this far above the reference: the row is computed again
+constexpr int kPolyPairs = 2;  // of 16 pairs of weights, how many take the polynomial
+
+// 2^x for two x at once without the special-function unit: x = n + f, |f| <= 1/2, 2^f by a cubic (least squares at Chebyshev
+// nodes, weighted to equal relative error 7.5e-5, far below the weights' rounding to bf16), n added to its exponent.  A NaN
+// leaves as the largest float or NaN, which makes the row's result non-finite all the same.
+__device__ __forceinline__ void exp2_poly2(uint64_t x2, float* e0, float* e1) {
+  float x0, x1, t0, t1, p0, p1;
+  ptx::unpack2(x2, &x0, &x1);
+  const uint64_t x = ptx::pack2(ptx::max_nan(x0, -126.f), ptx::max_nan(x1, -126.f));
+  const uint64_t t = ptx::add2(x, ptx::pack2(12582912.f, 12582912.f));   // 1.5 * 2^23: n in the low bits
+  const uint64_t f = ptx::fma2(ptx::add2(t, ptx::pack2(-12582912.f, -12582912.f)), ptx::pack2(-1.f, -1.f), x);
+  uint64_t p = ptx::fma2(f, ptx::pack2(0.05517166493f, 0.05517166493f), ptx::pack2(0.24261112188f, 0.24261112188f));
+  p = ptx::fma2(p, f, ptx::pack2(0.69326098623f, 0.69326098623f));
+  p = ptx::fma2(p, f, ptx::pack2(0.99992807358f, 0.99992807358f));
+  ptx::unpack2(t, &t0, &t1);
+  ptx::unpack2(p, &p0, &p1);
+  *e0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
+  *e1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
+}
 
 template <int D>
 struct Cfg {
@@ -41,32 +61,11 @@ struct TcArgs {
 
 // Items of the requests in order, Hkv x pairs of row blocks each; a whole warp walks forward through them, 32 requests
 // at a time.
+struct Item;
 struct Cursor {
   int chunk = -32, lane_items = 0, lane_first = 0, base = 0, total = 0;
-  __device__ __forceinline__ bool find(const TcArgs& p, int item, int lane, int* r, int* local) {
-    while (chunk < 0 || item >= base + total) {
-      base += total;
-      chunk += 32;
-      if (chunk >= p.a.n_req) return false;
-      paged::Request q;
-      lane_items = 0;
-      if (chunk + lane < p.a.n_req && paged::load_request(p.a, chunk + lane, &q))
-        lane_items = p.a.Hkv * ((q.nq + 2 * p.tpb - 1) / (2 * p.tpb));
-      int inc = lane_items;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int t = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += t;
-      }
-      lane_first = inc - lane_items;
-      total = __shfl_sync(0xffffffffu, inc, 31);
-    }
-    const int x = item - base;
-    const int who = __ffs(__ballot_sync(0xffffffffu, x >= lane_first && x < lane_first + lane_items)) - 1;
-    *r = chunk + who;
-    *local = x - __shfl_sync(0xffffffffu, lane_first, who);
-    return true;
-  }
+  paged::Request lane_rq = {0, 0, 0};
+  __device__ __forceinline__ bool find(const TcArgs& p, int item, int lane, Item* it);
 };
 
 struct Item {
@@ -77,14 +76,33 @@ struct Item {
   __device__ __forceinline__ int tile(int i) const { return i < n_sink ? i : i + skip; }
 };
 
-__device__ __forceinline__ void make_item(const TcArgs& p, int r, int local, Item* it) {
-  it->r = r;
-  it->q0 = p.a.q_begin[r];
-  it->nq = p.a.q_begin[r + 1] - it->q0;
-  it->kv = p.a.kv_len[r];
+__device__ __forceinline__ bool Cursor::find(const TcArgs& p, int item, int lane, Item* it) {
+  while (chunk < 0 || item >= base + total) {
+    base += total;
+    chunk += 32;
+    if (chunk >= p.a.n_req) return false;
+    lane_items = 0;
+    if (chunk + lane < p.a.n_req && paged::load_request(p.a, chunk + lane, &lane_rq))
+      lane_items = p.a.Hkv * ((lane_rq.nq + 2 * p.tpb - 1) / (2 * p.tpb));
+    int inc = lane_items;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int t = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += t;
+    }
+    lane_first = inc - lane_items;
+    total = __shfl_sync(0xffffffffu, inc, 31);
+  }
+  const int x = item - base;
+  const int who = __ffs(__ballot_sync(0xffffffffu, x >= lane_first && x < lane_first + lane_items)) - 1;
+  const int local = x - __shfl_sync(0xffffffffu, lane_first, who);
+  it->r = chunk + who;
+  it->q0 = __shfl_sync(0xffffffffu, lane_rq.q0, who);
+  it->nq = __shfl_sync(0xffffffffu, lane_rq.nq, who);
+  it->kv = __shfl_sync(0xffffffffu, lane_rq.kv, who);
   const int pairs = (it->nq + 2 * p.tpb - 1) / (2 * p.tpb);
   it->head = local / pairs;
-  const int pair = pairs - 1 - local % pairs;   // the longest rows first
+  const int pair = pairs - 1 - (local - it->head * pairs);   // the longest rows first
   const int x0 = it->kv - it->nq;               // position of the request's first new token
   it->tok[0] = pair * 2 * p.tpb;
   it->tok[1] = it->tok[0] + p.tpb;
@@ -102,6 +120,7 @@ __device__ __forceinline__ void make_item(const TcArgs& p, int r, int local, Ite
     }
     it->n_tiles = max(it->n_tiles, it->n[w]);
   }
+  return true;
 }
 
 template <int D>
@@ -131,9 +150,9 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       ptx::mbar_init(&q_full[w], 1);
       ptx::mbar_init(&q_empty[w], 1);
       ptx::mbar_init(&s_full[w], 1);
-      ptx::mbar_init(&p_full[w], 128);
+      ptx::mbar_init(&p_full[w], 4);
       ptx::mbar_init(&o_full[w], 1);
-      ptx::mbar_init(&o_empty[w], 128);
+      ptx::mbar_init(&o_empty[w], 4);
     }
     s_abort = 0;
     ptx::fence_mbar_init();
@@ -153,7 +172,6 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   const uint32_t tmem = s_tmem_base;   // S0, S1 at 0, 128; O0, O1 at 256, 384
 
   Cursor cur;
-  int r, local;
   Item it;
   if (warp == 8) {
     // ---------------- loads ----------------
@@ -164,11 +182,10 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     int stage = 0, items[2] = {0, 0};
     uint32_t ph = 0;
     bool ok = true;
-    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &r, &local); item += gridDim.x) {
-      make_item(p, r, local, &it);
+    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &it); item += gridDim.x) {
       for (int w = 0; w < 2; ++w) {
         if (it.n[w] == 0) continue;
-        if (items[w] > 0) ok = ok && ptx::mbar_wait(&q_empty[w], (items[w] - 1) & 1u, abort_flag, err, wait_ns);
+        if (items[w] > 0) ok = ok && ptx::mbar_wait_short(&q_empty[w], (items[w] - 1) & 1u, abort_flag, err, wait_ns);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         ++items[w];
@@ -198,7 +215,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         if (wanted && !load) atomicOr(err, CASCADE_DEV_ERR_BAD_PAGE);
         const uint32_t bytes = box_bytes * (uint32_t)__popc(__ballot_sync(0xffffffffu, load));
         for (int kv = 0; kv < 2; ++kv) {
-          ok = ptx::mbar_wait(&kv_empty[stage], ph ^ 1u, abort_flag, err, wait_ns);
+          ok = ptx::mbar_wait_short(&kv_empty[stage], ph ^ 1u, abort_flag, err, wait_ns);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           if (lane == 0) ptx::mbar_arrive_expect_tx(&kv_full[stage], bytes);
@@ -218,93 +235,105 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     }
     // every stage and query tile has been given back before the CTA may end (the arrivals are asynchronous)
     for (int i = 0; ok && i < kStages; ++i) {
-      ok = ptx::mbar_wait(&kv_empty[stage], ph ^ 1u, abort_flag, err, wait_ns);
+      ok = ptx::mbar_wait_short(&kv_empty[stage], ph ^ 1u, abort_flag, err, wait_ns);
       if (++stage == kStages) {
         stage = 0;
         ph ^= 1u;
       }
     }
     for (int w = 0; ok && w < 2; ++w)
-      if (items[w] > 0) ok = ptx::mbar_wait(&q_empty[w], (items[w] - 1) & 1u, abort_flag, err, wait_ns);
+      if (items[w] > 0) ok = ptx::mbar_wait_short(&q_empty[w], (items[w] - 1) & 1u, abort_flag, err, wait_ns);
   } else if (warp == 9) {
     // ---------------- products ----------------
+    // The whole warp runs this code and lane 0 issues, so that the descriptors stay in uniform registers: with one running
+    // lane every product cost a dozen instructions beside the softmax warps', 2200 cycles a tile instead of 1030.
+    const uint32_t live = lane == 0;
+    const uint32_t t0 = __shfl_sync(0xffffffffu, tmem, 0);
     const uint32_t idesc_s = ptx::umma_idesc_bf16(128, kTile);
     const uint32_t idesc_o = ptx::umma_idesc_bf16_b_mn(128, D);
+    const uint64_t q_desc = ptx::umma_desc_sw128(q_addr), k_desc = ptx::umma_desc_sw128(ring),
+                   v_desc = ptx::umma_desc_sw128_strides(ring, kTile * 128, 1024);
     int used[2] = {0, 0}, tiles[2] = {0, 0};   // items / tiles of each block so far
     int stage = 0;                             // the next stage to be consumed; K(i) and V(i) alternate
     uint32_t ph = 0;
     bool ok = true;
-    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &r, &local); item += gridDim.x) {
-      make_item(p, r, local, &it);
-      if (lane == 0 && it.n_tiles > 0) {
-        auto wait = [&](uint64_t* bar, uint32_t parity) { ok = ok && ptx::mbar_wait(bar, parity, abort_flag, err, wait_ns); };
-        auto scores = [&](int w, int st) {
-          ptx::tc_fence_after();
-          const uint32_t k_addr = ring + st * C::kTileBytes;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      if (ok) ok = ptx::mbar_wait_short(bar, parity, abort_flag, err, wait_ns);
+      ok = __all_sync(0xffffffffu, ok);
+    };
+    auto stage_off = [&](int st) { return __shfl_sync(0xffffffffu, st * (C::kTileBytes >> 4), 0); };   // in descriptor units
+    auto scores = [&](int w, int st) {
+      ptx::tc_fence_after();
+      const uint64_t kd = k_desc + (uint32_t)stage_off(st);
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) {
-            const uint32_t off = (ks >> 2) * (kTile * 128) + (ks & 3) * 32;
-            ptx::umma_bf16(tmem + w * 128, ptx::umma_desc_sw128(q_addr + w * C::kTileBytes + off), ptx::umma_desc_sw128(k_addr + off),
-                           idesc_s, ks != 0);
-          }
-          ptx::umma_commit(&s_full[w]);
-        };
-        auto advance = [&]() {
-          if (++stage == kStages) {
-            stage = 0;
-            ph ^= 1u;
-          }
-        };
-        wait(&kv_full[stage], ph);
-        for (int w = 0; w < 2 && ok; ++w) {
-          if (it.n[w] == 0) continue;
-          wait(&q_full[w], used[w] & 1u);
-          if (!ok) break;
-          scores(w, stage);
-          if (it.n[w] == 1) ptx::umma_commit(&q_empty[w]);
-        }
-        if (ok) ptx::umma_commit(&kv_empty[stage]);
-        advance();
-        for (int i = 0; ok && i < it.n_tiles; ++i) {
-          const int v_stage = stage;
-          wait(&kv_full[stage], ph);
-          advance();
-          const int k_stage = stage;
-          const bool more = i + 1 < it.n_tiles;
-          bool k_here = false;
-          for (int w = 0; w < 2 && ok; ++w) {
-            if (i >= it.n[w]) continue;
-            if (i == 0 && used[w] > 0) wait(&o_empty[w], (used[w] - 1) & 1u);
-            wait(&p_full[w], tiles[w] & 1u);
-            if (!ok) break;
-            ++tiles[w];
-            ptx::tc_fence_after();
-            const uint32_t v_addr = ring + v_stage * C::kTileBytes;
-#pragma unroll
-            for (int ks = 0; ks < kTile / 16; ++ks)
-              ptx::umma_bf16_ts(tmem + 256 + w * 128, tmem + w * 128 + ks * 8,
-                                ptx::umma_desc_sw128_strides(v_addr + ks * 2048, kTile * 128, 1024), idesc_o, (i | ks) != 0);
-            if (i + 1 == it.n[w]) ptx::umma_commit(&o_full[w]);
-            if (i + 1 < it.n[w]) {
-              if (!k_here) {
-                wait(&kv_full[k_stage], ph);
-                k_here = true;
-                if (!ok) break;
-              }
-              scores(w, k_stage);
-              if (i + 2 == it.n[w]) ptx::umma_commit(&q_empty[w]);
-            }
-          }
-          if (!ok) break;
-          ptx::umma_commit(&kv_empty[v_stage]);
-          if (more) {
-            ptx::umma_commit(&kv_empty[k_stage]);
-            advance();
-          }
-        }
-        for (int w = 0; w < 2; ++w) used[w] += it.n[w] > 0;
+      for (int ks = 0; ks < D / 16; ++ks) {
+        const uint32_t off = ((ks >> 2) * (kTile * 128) + (ks & 3) * 32) >> 4;
+        ptx::umma_bf16_warp(live, t0 + w * 128, q_desc + (w * (C::kTileBytes >> 4) + off), kd + off, idesc_s, ks != 0);
       }
-      ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+      ptx::umma_commit_if(live, &s_full[w]);
+    };
+    auto outputs = [&](int w, int st, bool first) {
+      ptx::tc_fence_after();
+      const uint64_t vd = v_desc + (uint32_t)stage_off(st);
+      ptx::umma_bf16_ts_warp(live, t0 + 256 + w * 128, t0 + w * 128, vd, idesc_o, !first);
+#pragma unroll
+      for (int ks = 1; ks < kTile / 16; ++ks)
+        ptx::umma_bf16_ts_warp(live, t0 + 256 + w * 128, t0 + w * 128 + ks * 8, vd + ks * (2048 >> 4), idesc_o, true);
+    };
+    auto advance = [&]() {
+      if (++stage == kStages) {
+        stage = 0;
+        ph ^= 1u;
+      }
+    };
+    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &it); item += gridDim.x) {
+      if (it.n_tiles == 0) continue;
+      wait(&kv_full[stage], ph);
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        if (it.n[w] == 0) continue;
+        wait(&q_full[w], used[w] & 1u);
+        if (!ok) break;
+        scores(w, stage);
+        if (it.n[w] == 1) ptx::umma_commit_if(live, &q_empty[w]);
+      }
+      if (!ok) break;
+      ptx::umma_commit_if(live, &kv_empty[stage]);
+      advance();
+      for (int i = 0; ok && i < it.n_tiles; ++i) {
+        const int v_stage = stage;
+        wait(&kv_full[stage], ph);
+        advance();
+        const int k_stage = stage;
+        const bool more = i + 1 < it.n_tiles;
+        bool k_here = false;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          if (!ok || i >= it.n[w]) continue;
+          if (i == 0 && used[w] > 0) wait(&o_empty[w], (used[w] - 1) & 1u);
+          wait(&p_full[w], tiles[w] & 1u);
+          if (!ok) break;
+          ++tiles[w];
+          outputs(w, v_stage, i == 0);
+          if (i + 1 == it.n[w]) ptx::umma_commit_if(live, &o_full[w]);
+          if (i + 1 < it.n[w]) {
+            if (!k_here) {
+              wait(&kv_full[k_stage], ph);
+              k_here = true;
+              if (!ok) break;
+            }
+            scores(w, k_stage);
+            if (i + 2 == it.n[w]) ptx::umma_commit_if(live, &q_empty[w]);
+          }
+        }
+        if (!ok) break;
+        ptx::umma_commit_if(live, &kv_empty[v_stage]);
+        if (more) {
+          ptx::umma_commit_if(live, &kv_empty[k_stage]);
+          advance();
+        }
+      }
+      for (int w = 0; w < 2; ++w) used[w] += it.n[w] > 0;
     }
   } else {
     // ---------------- softmax, one row per thread ----------------
@@ -316,42 +345,25 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     const float c = p.a.scale * paged::kLog2e;
     int tiles = 0, used = 0, kv_count = 0;                     // tiles / items of this block, ring stages of all items
     bool ok = true;
-    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &r, &local); item += gridDim.x) {
-      make_item(p, r, local, &it);
+    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &it); item += gridDim.x) {
       const int tok = it.tok[w] + my_tok;
       const bool live = in_block && tok < it.nq;
-      const int x = live ? it.kv - it.nq + tok : -1;           // position; -1: sees nothing
-      const int lo = paged::window_begin(x, p.a.window), n_sink = p.a.sinks;
+      // position (below 0: sees nothing); a place without a row sees everything, which spares its warp the masks
+      const int x = live ? it.kv - it.nq + tok : INT_MAX / 2;
+      const int lo = live ? paged::window_begin(x, p.a.window) : 0, n_sink = p.a.sinks;
       const int n = it.n[w];
-      float ref = -INFINITY, l = 0.f;
+      float ref = -INFINITY, next_ref = -INFINITY, l = 0.f;
+      bool odd = false;                                        // to be computed again from the keys the row sees alone
       for (int i = 0; i < n; ++i, ++tiles) {
         const int k0 = it.tile(i) * kTile;
-        ok = ptx::mbar_wait(&s_full[w], tiles & 1u, abort_flag, err, wait_ns);
+        ok = ptx::mbar_wait_short(&s_full[w], tiles & 1u, abort_flag, err, wait_ns);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         ptx::tc_fence_after();
-        uint32_t s[kTile];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) ptx::tmem_ld32_async(t_s + 32 * q, s + 32 * q);
-        ptx::tmem_wait_ld();
-        const bool whole = k0 + kTile - 1 <= x && (k0 >= lo || k0 + kTile <= n_sink);
-        if (!__all_sync(0xffffffffu, whole)) {
-          const int hi_j = x - k0, lo_j = lo - k0, sink_j = n_sink - k0;
-#pragma unroll
-          for (int j = 0; j < kTile; ++j)
-            if (!(j <= hi_j && (j >= lo_j || j < sink_j))) s[j] = 0xff800000u;   // -inf
-        }
-        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int j = 0; j < kTile; ++j) m4[j & 3] = fmaxf(m4[j & 3], __uint_as_float(s[j]));
-        const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * c;
-        float alpha = 1.f;
-        if (m > ref + kLazy || (ref == -INFINITY && m > -INFINITY)) {
-          alpha = ref == -INFINITY ? 0.f : ptx::ex2(ref - m);
-          ref = m;
-        }
-        if (i > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
+        if (__any_sync(0xffffffffu, next_ref > ref)) {
           // the scores of tile i come after the output product of tile i - 1, so the accumulator is at rest
+          const float alpha = next_ref > ref ? ptx::ex2(ref - next_ref) : 1.f;
+          ref = fmaxf(ref, next_ref);
           l *= alpha;
 #pragma unroll 1
           for (int q = 0; q < D / 16; ++q) {
@@ -362,26 +374,95 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             ptx::tmem_st16(t_o + 16 * q, t);
           }
         }
-        const float minus = ref == -INFINITY ? 0.f : -ref;
-        float sum4[4] = {0.f, 0.f, 0.f, 0.f};
+        const bool whole = __all_sync(0xffffffffu, k0 + kTile - 1 <= x && (k0 >= lo || k0 + kTile <= n_sink));
+        // bit k: this row sees key k0 + 32 q + k
+        auto visible = [&](int q) {
+          const int j0 = k0 + 32 * q;
+          auto below = [](int n) { return n >= 32 ? 0xffffffffu : (1u << max(n, 0)) - 1u; };
+          return below(x - j0 + 1) & (~below(lo - j0) | below(n_sink - j0));
+        };
+        if (__any_sync(0xffffffffu, ref == -INFINITY && k0 <= x && live)) {
+          // rows that have met no key yet take their reference from this tile
+          float m = -INFINITY;
+#pragma unroll 1
+          for (int q = 0; q < 4; ++q) {
+            uint32_t v[32];
+            ptx::tmem_ld32_async(t_s + 32 * q, v);
+            const uint32_t vis = visible(q);
+            ptx::tmem_wait_ld();
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          uint32_t pk[16];
-#pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            const float a = ptx::ex2(fmaf(__uint_as_float(s[32 * q + 2 * k]), c, minus));
-            const float b = ptx::ex2(fmaf(__uint_as_float(s[32 * q + 2 * k + 1]), c, minus));
-            sum4[k & 3] += a + b;
-            pk[k] = ptx::pack_bf16x2(a, b);
+            for (int k = 0; k < 32; ++k) m = fmaxf(m, (vis >> k) & 1u ? __uint_as_float(v[k]) : -INFINITY);
           }
-          ptx::tmem_st16_async(t_s + 16 * q, pk);
+          if (ref == -INFINITY) ref = m * c;
+          next_ref = ref;
         }
-        l += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
+        const float minus = ref == -INFINITY ? 0.f : -ref;
+        float m = -INFINITY;
+        if (whole) {
+          const uint64_t c2 = ptx::pack2(c, c), minus2 = ptx::pack2(minus, minus);
+          uint64_t sum2 = 0;
+          float mb = -INFINITY;
+          uint32_t v[2][32];
+          ptx::tmem_ld32_async(t_s, v[0]);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            ptx::tmem_wait_ld();
+            if (q < 3) ptx::tmem_ld32_async(t_s + 32 * (q + 1), v[(q + 1) & 1]);
+            uint32_t pk[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const float s0 = __uint_as_float(v[q & 1][2 * k]), s1 = __uint_as_float(v[q & 1][2 * k + 1]);
+              if (k & 1)
+                mb = ptx::max3(mb, s0, s1);
+              else
+                m = ptx::max3(m, s0, s1);
+              const uint64_t x2 = ptx::fma2(ptx::pack2(s0, s1), c2, minus2);
+              float e0, e1;
+              if (k % 16 < kPolyPairs)
+                exp2_poly2(x2, &e0, &e1);
+              else {
+                ptx::unpack2(x2, &e0, &e1);
+                e0 = ptx::ex2(e0);
+                e1 = ptx::ex2(e1);
+              }
+              sum2 = ptx::add2(sum2, ptx::pack2(e0, e1));
+              pk[k] = ptx::pack_bf16x2(e0, e1);
+            }
+            ptx::tmem_st16_async(t_s + 16 * q, pk);
+          }
+          m = fmaxf(m, mb);
+          float sa, sb;
+          ptx::unpack2(sum2, &sa, &sb);
+          l += sa + sb;
+        } else {
+          float sum = 0.f;
+#pragma unroll 1
+          for (int q = 0; q < 4; ++q) {
+            uint32_t v[32], pk[16];
+            ptx::tmem_ld32_async(t_s + 32 * q, v);
+            const uint32_t vis = visible(q);
+            ptx::tmem_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const float s0 = (vis >> (2 * k)) & 1u ? __uint_as_float(v[2 * k]) : -INFINITY;
+              const float s1 = (vis >> (2 * k + 1)) & 1u ? __uint_as_float(v[2 * k + 1]) : -INFINITY;
+              m = fmaxf(m, fmaxf(s0, s1));
+              const float e0 = ptx::ex2(fmaf(s0, c, minus)), e1 = ptx::ex2(fmaf(s1, c, minus));
+              sum += e0 + e1;
+              pk[k] = ptx::pack_bf16x2(e0, e1);
+            }
+            ptx::tmem_st16_async(t_s + 16 * q, pk);
+          }
+          l += sum;
+        }
+        m *= c;
+        if (m > ref + kLazy) next_ref = m;
+        odd = odd || m > ref + kFar;
         // values behind the last key: zeros (block 0 does it while it takes part, its product comes first)
         if (k0 + kTile > it.kv && (w == 0 || i >= it.n[0])) {
           const int st = (kv_count + 2 * i + 1) % kStages;
           const uint32_t st_ph = ((uint32_t)(kv_count + 2 * i + 1) / kStages) & 1u;
-          ok = ptx::mbar_wait(&kv_full[st], st_ph, abort_flag, err, wait_ns);
+          ok = ptx::mbar_wait_short(&kv_full[st], st_ph, abort_flag, err, wait_ns);
           if (ok && k0 + rr >= it.kv) {
             for (int h = 0; h < C::kHalves; ++h)
               for (int k = 0; k < 8; ++k) ptx::st_shared_v4(ring + st * C::kTileBytes + h * (kTile * 128) + rr * 128 + k * 16, 0, 0, 0, 0);
@@ -392,22 +473,22 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         }
         ptx::tmem_wait_st();
         ptx::tc_fence_before();
-        ptx::mbar_arrive(&p_full[w]);
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&p_full[w]);
       }
       kv_count += 2 * it.n_tiles;
       if (!ok) break;
       // ---- the rows' results ----
       const int row = it.q0 + tok, head = it.head * p.G + my_g;
-      bool odd = false;                                        // something is not finite, or every visible score was -inf
       if (n > 0) {
-        ok = ptx::mbar_wait(&o_full[w], used & 1u, abort_flag, err, wait_ns);
+        ok = ptx::mbar_wait_short(&o_full[w], used & 1u, abort_flag, err, wait_ns);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         ptx::tc_fence_after();
         ++used;
       }
       const float inv = l > 0.f ? 1.f / l : 0.f;
-      odd = x >= 0 && !(l > 0.f && l < INFINITY);
+      odd = live && x >= 0 && (odd || !(l > 0.f && l < INFINITY));   // (or a sum that is no number)
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.a.out) + ((long long)row * p.a.Hq + head) * D;
 #pragma unroll 1
       for (int q = 0; q < D / 32; ++q) {
@@ -422,7 +503,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         float bad = 0.f;
 #pragma unroll
         for (int k = 0; k < 32; ++k) bad = fmaf(__uint_as_float(o[k]), 0.f, bad);   // NaN if any is not finite
-        odd = odd || (x >= 0 && bad != 0.f);
+        odd = odd || (live && x >= 0 && bad != 0.f);
         if (live) {
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
@@ -438,10 +519,11 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       }
       if (n > 0) {
         ptx::tc_fence_before();
-        ptx::mbar_arrive(&o_empty[w]);
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&o_empty[w]);
       }
       if (live && p.a.lse != nullptr)
-        p.a.lse[(long long)row * p.a.Hq + head] = l > 0.f ? (ref + log2f(l)) * paged::kLn2 : -INFINITY;
+        p.a.lse[(long long)row * p.a.Hq + head] = x >= 0 ? (ref + log2f(l)) * paged::kLn2 : -INFINITY;
       __syncwarp();
       for (uint32_t left = __ballot_sync(0xffffffffu, odd); left != 0u; left &= left - 1u) {
         const int who = __ffs(left) - 1;
