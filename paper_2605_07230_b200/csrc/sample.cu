@@ -2,14 +2,15 @@
 //
 //   w[v] = exp((l[v] - m) / T),  token = first v whose cumulative kept weight exceeds u * (total kept weight)
 //
-// One CTA per row.  The row's order-preserving 32-bit keys stay in shared memory as far as they fit (the rest is read again
-// through the L2), so HBM sees each logit once.  Weights are formed in 64 bits (relative error 1e-12) and summed as 64-bit
-// fixed point: sums do not depend on the order of additions, and a draw differs from exact arithmetic only where u falls
-// within about 1e-11 of a boundary.
+// One CTA per row.  The row stays in shared memory as far as it fits (the rest is read again through the L2), so HBM sees
+// each logit once.  Weights are formed in 64 bits (relative error 1e-10) and summed as 64-bit fixed point: sums do not
+// depend on the order of additions, and a draw differs from exact arithmetic only where u falls within about 1e-10 of a
+// boundary.
 // Thresholds are exact.  A histogram over 2048 equal steps of the distance to the row's maximum (counts for top-k, weights
 // for the nucleus) finds the step in which the threshold lies; the few tokens of that step are then ranked among each
 // other.  Where a step holds too many different values (logits spread over more than 48 and the threshold far down, or
-// infinities), the search goes over the keys' own range instead, 2048 steps at a time.
+// infinities), the search goes over the range of the values' ordered bit patterns instead, 2048 steps at a time.
+// Once a truncation has left at most 4096 tokens, they are gathered and the later passes go over them alone.
 #include <cfloat>
 
 #include "cascade_internal.h"
@@ -19,7 +20,8 @@
 namespace {
 
 constexpr int kBins = 2048;                // steps of a histogram; groups of consecutive tokens with a weight sum each
-constexpr int kList = 1024;                // tokens of one step that are ranked directly
+constexpr int kList = 4096;                // kept tokens that are gathered
+constexpr int kRank = 1024;                // tokens of one step that are ranked directly
 constexpr float kReach = 48.f;             // how far below the maximum the histogram reaches (its last step takes the rest)
 
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -27,38 +29,36 @@ __device__ __forceinline__ uint32_t order_key(float x) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);  // larger float <=> larger key
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
-constexpr uint32_t kNoKey = 0u;            // -inf and NaN: never kept (the key of -inf would be 0x007fffff)
-__device__ __forceinline__ uint32_t logit_key(float x) {
-  return x > -INFINITY ? order_key(x + 0.f) : kNoKey;   // + 0: the two zeros are one value
-}
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 
 template <int kThreads>
-struct Shared {
+struct alignas(16) Shared {                // (the row's logits follow it and are read 16 bytes at a time)
   union {
     struct {
       uint32_t lo[kBins], hi[kBins];       // 64-bit sums as two words
     } hist;
     unsigned long long group[kBins];
   };
-  unsigned long long list_w[kList];
-  uint32_t list_k[kList];
-  double table[32];                        // 2^(j/32)
+  float list_l[kList];                     // gathered tokens: logit, index
+  int list_i[kList];
+  unsigned long long rank_w[kRank];        // tokens of one step: weight, logit, index
+  float rank_l[kRank];
+  int rank_i[kRank];
+  double table[64];                        // 2^(j/64)
   unsigned long long warp_sum[kThreads / 32];
-  uint32_t red_lo[kThreads / 32], red_hi[kThreads / 32];
+  float red_lo[kThreads / 32], red_hi[kThreads / 32];
+  uint32_t red_n[kThreads / 32];
   unsigned long long before;               // result of find()
   int at;
-  int n_list;
-  uint32_t list_min, list_max;
-  uint32_t floor_key;
+  int n_list, n_rank;
+  uint32_t key_min, key_max;               // of one step
+  float floor;
   int token;
 };
 
 struct SampleArgs {
   const void* logits;
   long long row_stride;
-  int V, n_res, fixed_bits, group_shift;   // keys kept in shared memory; log2 of the tokens in a group
+  int V, n_res, fixed_bits, group_shift;   // logits kept in shared memory; log2 of the tokens in a group
   const float* temperature;
   const int32_t* top_k;
   const float *top_p, *min_p, *uniforms;
@@ -67,28 +67,27 @@ struct SampleArgs {
   int32_t* kept;
 };
 
-// exp((l - m) / T) * 2^bits, rounded to an integer.  x = (l - m) * 32 / (T ln 2) is split into whole octaves, one of 32
-// table steps and a remainder |g| <= ln 2 / 64, whose exponential is its Taylor sum to g^4 (error g^5/120 < 2e-12).
+// exp((l - m) / T) * 2^bits, rounded to an integer, for l >= zero.  x = (l - m) * 64 / (T ln 2) is split into whole octaves,
+// one of 64 table steps and a remainder |g| <= 1/2 of a step, whose exponential is its Taylor sum to the third power (error
+// (ln 2 / 128)^4 / 24 < 4e-11).  The last product adds 2^52, which leaves the rounded integer in the mantissa.
 struct Weight {
-  double m, c;      // row maximum, 32 / (T ln 2)
-  uint32_t m_key;
+  float m, zero;    // row maximum; logits below weigh nothing
+  double md, c;     // the maximum, 64 / (T ln 2)
   int bits;
   const double* table;
-  __device__ __forceinline__ unsigned long long operator()(uint32_t key) const {
-    if (key == m_key) return 1ull << bits;
-    const double x = ((double)key_value(key) - m) * c;
-    if (!(x > -2048.0)) return 0ull;                         // below 2^-64 (and -inf, NaN of infinite maxima)
-    const double magic = 6755399441055744.0;                 // 1.5 * 2^52: rounds to an integer
-    const double k = x + magic;
+  __device__ __forceinline__ unsigned long long of(float l) const {
+    constexpr double a1 = 0.010830424696249146, a2 = a1 * a1 / 2, a3 = a1 * a1 * a1 / 6;   // ln 2 / 64
+    const double magic = 6755399441055744.0;                     // 1.5 * 2^52: rounds to an integer
+    const double x = ((double)l - md) * c, k = x + magic;
     const int n = __double2loint(k);
-    const double g = (x - (k - magic)) * 0.021660849392498290;  // ln 2 / 32
-    const double e = 1.0 + g * (1.0 + g * (0.5 + g * (1.0 / 6.0 + g * (1.0 / 24.0))));
-    const double w = e * table[n & 31];
-    const int exponent = (n >> 5) + bits;                    // w * 2^exponent
-    if (exponent < -1) return 0ull;
-    const double scaled = __hiloint2double(__double2hiint(w) + (exponent << 20), __double2loint(w));
-    return (unsigned long long)__double_as_longlong(scaled + 4503599627370496.0) & 0xfffffffffffffull;  // + 2^52: the integer is in the mantissa
+    const double g = x - (k - magic);
+    const double e = fma(g, fma(g, fma(g, a3, a2), a1), 1.0);
+    const double t = table[n & 63];
+    const double scaled = __hiloint2double(__double2hiint(t) + (((n >> 6) + bits) << 20), __double2loint(t));
+    const unsigned long long w = (unsigned long long)__double_as_longlong(fma(e, scaled, 4503599627370496.0)) & 0xfffffffffffffull;
+    return l == m ? 1ull << bits : w;                            // (the maximum may be infinite)
   }
+  __device__ __forceinline__ unsigned long long operator()(float l) const { return l >= zero ? of(l) : 0ull; }
 };
 
 __device__ __forceinline__ unsigned long long warp_sum(unsigned long long v) {
@@ -96,36 +95,82 @@ __device__ __forceinline__ unsigned long long warp_sum(unsigned long long v) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
 
 // Adds w to a 64-bit sum kept as two words (native 32-bit atomics; the carry goes with whoever caused it).
-template <typename S>
-__device__ __forceinline__ void hist_add(S& sh, int bin, unsigned long long w) {
+__device__ __forceinline__ void add_pair(uint32_t* lo_word, uint32_t* hi_word, unsigned long long w) {
   const uint32_t lo = (uint32_t)w;
-  const uint32_t old = atomicAdd(&sh.hist.lo[bin], lo);
+  const uint32_t old = atomicAdd(lo_word, lo);
   const uint32_t hi = (uint32_t)(w >> 32) + (old + lo < old ? 1u : 0u);
-  if (hi != 0u) atomicAdd(&sh.hist.hi[bin], hi);
+  if (hi != 0u) atomicAdd(hi_word, hi);
 }
 
 template <typename E>
 struct Row {
   const E* g;
-  uint32_t* s;         // keys of the first n_res tokens
+  float* s;            // the first n_res logits (a multiple of 4)
   int V, n_res;
-  __device__ __forceinline__ uint32_t key(int i) const { return i < n_res ? s[i] : logit_key(to_float(g[i])); }
+  bool wide;           // four logits can be read at once
+  __device__ __forceinline__ float at(int i) const {
+    if (i < n_res) return s[i];
+    if constexpr (sizeof(E) == 4)
+      return g[i];
+    else
+      return __bfloat162float(g[i]);
+  }
+  __device__ __forceinline__ float4 from_memory(int i4) const {
+    if constexpr (sizeof(E) == 4) {
+      if (wide) return __ldg(reinterpret_cast<const float4*>(g) + i4);
+      return make_float4(g[4 * i4], g[4 * i4 + 1], g[4 * i4 + 2], g[4 * i4 + 3]);
+    } else {
+      uint2 u;
+      if (wide) {
+        u = __ldg(reinterpret_cast<const uint2*>(g) + i4);
+      } else {
+        const unsigned short* h = reinterpret_cast<const unsigned short*>(g) + 4 * i4;
+        u = make_uint2(h[0] | ((uint32_t)h[1] << 16), h[2] | ((uint32_t)h[3] << 16));
+      }
+      return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                         __uint_as_float(u.y & 0xffff0000u));
+    }
+  }
+  __device__ __forceinline__ float4 four(int i4) const { return 4 * i4 < n_res ? reinterpret_cast<const float4*>(s)[i4] : from_memory(i4); }
 };
 
-// f(index, key) for every token of the row, in strides of the CTA; four independent reads at a time.
+// f(index, logit) for every token of the row, four at a time (V is a multiple of 8).
 template <int kThreads, typename E, typename F>
 __device__ __forceinline__ void each(const Row<E>& row, F f) {
+  const int n4 = row.V / 4;
+  auto take = [&](int i, const float4& v) {
+    f(4 * i, v.x);
+    f(4 * i + 1, v.y);
+    f(4 * i + 2, v.z);
+    f(4 * i + 3, v.w);
+  };
   int i = threadIdx.x;
-  for (; i + 3 * kThreads < row.V; i += 4 * kThreads) {
-    uint32_t k[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) k[q] = row.key(i + q * kThreads);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) f(i + q * kThreads, k[q]);
+  for (; i + kThreads < n4; i += 2 * kThreads) {
+    const float4 a = row.four(i), b = row.four(i + kThreads);
+    take(i, a);
+    take(i + kThreads, b);
   }
-  for (; i < row.V; i += kThreads) f(i, row.key(i));
+  if (i < n4) take(i, row.four(i));
+}
+
+// The tokens still in play: the gathered ones, or those of the row from `floor` up.
+template <int kThreads, typename E, typename F>
+__device__ __forceinline__ void each_kept(const Row<E>& row, const Shared<kThreads>& sh, bool gathered, float floor, F f) {
+  if (gathered) {
+    for (int i = threadIdx.x; i < sh.n_list; i += kThreads)
+      if (sh.list_l[i] >= floor) f(sh.list_i[i], sh.list_l[i]);
+  } else {
+    each<kThreads>(row, [&](int i, float l) {
+      if (l >= floor) f(i, l);
+    });
+  }
 }
 
 // The first entry at which the running sum of kBins entries get(i) passes `target` (> target); sh.at and sh.before = the sum
@@ -171,22 +216,28 @@ __device__ __forceinline__ unsigned long long find(Shared<kThreads>& sh, Get get
   return total;
 }
 
-// The key x among keys in [lo, hi] with W(> x) <= target < W(>= x), W the weight (1 each, or exp) of keys >= lo: the
-// general search, 2048 steps of the keys' range at a time.  The whole CTA calls it with the same arguments.
+template <int kThreads>
+__device__ __forceinline__ void clear_hist(Shared<kThreads>& sh) {
+  __syncthreads();
+  for (int i = threadIdx.x; i < kBins; i += kThreads) sh.hist.lo[i] = sh.hist.hi[i] = 0u;
+  __syncthreads();
+}
+
+// The value x among keys in [lo, hi] with W(> x) <= target < W(>= x), W the weight (1 each, or exp) of the tokens in play
+// with a key >= lo: the general search, 2048 steps of the keys' range at a time.  The whole CTA calls it.
 template <bool kMass, int kThreads, typename E>
-__device__ __noinline__ uint32_t descend(const Row<E>& row, const Weight& weight, uint32_t lo, uint32_t hi, unsigned long long target,
-                                         Shared<kThreads>& sh) {
+__device__ __noinline__ float descend(const Row<E>& row, const Weight& weight, bool gathered, uint32_t lo, uint32_t hi,
+                                      unsigned long long target, Shared<kThreads>& sh) {
   while (true) {
     const uint32_t range = hi - lo;
     const int shift = range < (uint32_t)kBins ? 0 : 32 - __clz(range) - 11;  // (range >> shift) < 2048
-    __syncthreads();
-    for (int i = threadIdx.x; i < kBins; i += kThreads) sh.hist.lo[i] = sh.hist.hi[i] = 0u;
-    __syncthreads();
-    each<kThreads>(row, [&](int, uint32_t k) {
+    clear_hist(sh);
+    each_kept<kThreads>(row, sh, gathered, key_value(lo), [&](int, float l) {
+      const uint32_t k = order_key(l + 0.f);                     // + 0: the two zeros are one value
       if (k >= lo && k <= hi) {
         const int bin = kBins - 1 - (int)((k - lo) >> shift);   // largest first
         if (kMass)
-          hist_add(sh, bin, weight(k));
+          add_pair(&sh.hist.lo[bin], &sh.hist.hi[bin], weight(l));
         else
           atomicAdd(&sh.hist.lo[bin], 1u);
       }
@@ -194,50 +245,78 @@ __device__ __noinline__ uint32_t descend(const Row<E>& row, const Weight& weight
     __syncthreads();
     find<kThreads>(sh, [&](int i) { return ((unsigned long long)sh.hist.hi[i] << 32) | sh.hist.lo[i]; },
                    [&](unsigned long long) { return target; });
-    if (sh.at < 0) return lo;                                    // all of it stays
+    if (sh.at < 0) return key_value(lo);                         // all of it stays
     target -= sh.before;
     lo += (uint32_t)(kBins - 1 - sh.at) << shift;
-    if (shift == 0) return lo;
+    if (shift == 0) return key_value(lo);
     const uint32_t step_end = lo + ((1u << shift) - 1u);
     if (step_end < hi) hi = step_end;                            // (the last step may pass the row's largest key)
   }
 }
 
-// The same threshold by one histogram over the distance to the maximum.  target_of: from the total weight of keys >= floor.
+// The same threshold, over the tokens in play from `floor` up, by one histogram over the distance to the maximum; `even`:
+// that makes sense.  target_of: from the total weight.  Leaves what stays gathered (*gathered) if it is few enough.
 template <bool kMass, int kThreads, typename E, typename Target>
-__device__ uint32_t threshold(const Row<E>& row, const Weight& weight, float m, float steps_per_unit, uint32_t floor_key,
-                              uint32_t k_max, Target target_of, Shared<kThreads>& sh) {
+__device__ __forceinline__ float threshold(const Row<E>& row, const Weight& weight, bool* gathered, float floor, bool even,
+                                           float steps, Target target_of, Shared<kThreads>& sh) {
   const int tid = threadIdx.x;
-  auto bin_of = [&](uint32_t k) { return min(kBins - 1, (int)((m - key_value(k)) * steps_per_unit)); };
-  __syncthreads();
-  for (int i = tid; i < kBins; i += kThreads) sh.hist.lo[i] = sh.hist.hi[i] = 0u;
-  if (tid == 0) {
-    sh.n_list = 0;
-    sh.list_min = 0xffffffffu;
-    sh.list_max = 0u;
+  auto bin_of = [&](float l) { return min(kBins - 1, (int)((weight.m - l) * steps)); };
+  auto bins = [&](int i) { return ((unsigned long long)sh.hist.hi[i] << 32) | sh.hist.lo[i]; };
+  unsigned long long target = 0;
+  if (!even) {
+    unsigned long long z = 0;
+    if (kMass) {
+      each_kept<kThreads>(row, sh, *gathered, floor, [&](int, float l) { z += weight(l); });
+      z = warp_sum(z);
+      __syncthreads();
+      if ((tid & 31) == 0) sh.warp_sum[tid >> 5] = z;
+      __syncthreads();
+      z = warp_sum((tid & 31) < kThreads / 32 ? sh.warp_sum[tid & 31] : 0ull);
+    }
+    return descend<kMass>(row, weight, *gathered, order_key(floor + 0.f), order_key(weight.m + 0.f), target_of(z), sh);
   }
-  __syncthreads();
-  each<kThreads>(row, [&](int, uint32_t k) {
-    if (k >= floor_key) {
-      if (kMass)
-        hist_add(sh, bin_of(k), weight(k));
-      else
-        atomicAdd(&sh.hist.lo[bin_of(k)], 1u);
+  if (tid == 0) {
+    sh.n_rank = 0;
+    sh.key_min = 0xffffffffu;
+    sh.key_max = 0u;
+    if (!*gathered) sh.n_list = 0;
+  }
+  clear_hist(sh);
+  each_kept<kThreads>(row, sh, *gathered, floor, [&](int, float l) {
+    if (kMass) {
+      if (l >= weight.zero) {
+        const int bin = bin_of(l);
+        add_pair(&sh.hist.lo[bin], &sh.hist.hi[bin], weight.of(l));
+      }
+    } else {
+      atomicAdd(&sh.hist.lo[bin_of(l)], 1u);
     }
   });
   __syncthreads();
-  unsigned long long target = 0;
-  find<kThreads>(sh, [&](int i) { return ((unsigned long long)sh.hist.hi[i] << 32) | sh.hist.lo[i]; },
-                 [&](unsigned long long total) { return target = target_of(total); });
+  find<kThreads>(sh, bins, [&](unsigned long long total) { return target = target_of(total); });
   const int bin = sh.at;
-  if (bin < 0) return floor_key;                                 // all of it stays
+  if (bin < 0) return floor;                                     // all of it stays
   const unsigned long long left = target - sh.before;            // of the step's own weight
-  // the tokens of that step
+  // the tokens of that step; those above it are gathered unless everything in play is already
   uint32_t lo = 0xffffffffu, hi = 0u;
-  each<kThreads>(row, [&](int, uint32_t k) {
-    if (k >= floor_key && bin_of(k) == bin) {
-      const int at = atomicAdd(&sh.n_list, 1);
-      if (at < kList) sh.list_k[at] = k;
+  const bool gather = !*gathered;
+  each_kept<kThreads>(row, sh, *gathered, floor, [&](int i, float l) {
+    const int b = bin_of(l);
+    if (b < bin) {
+      if (gather) {
+        const int at = atomicAdd(&sh.n_list, 1);
+        if (at < kList) {
+          sh.list_l[at] = l;
+          sh.list_i[at] = i;
+        }
+      }
+    } else if (b == bin) {
+      const int at = atomicAdd(&sh.n_rank, 1);
+      if (at < kRank) {
+        sh.rank_l[at] = l;
+        sh.rank_i[at] = i;
+      }
+      const uint32_t k = order_key(l + 0.f);
       lo = min(lo, k);
       hi = max(hi, k);
     }
@@ -245,31 +324,49 @@ __device__ uint32_t threshold(const Row<E>& row, const Weight& weight, float m, 
   lo = __reduce_min_sync(0xffffffffu, lo);
   hi = __reduce_max_sync(0xffffffffu, hi);
   if ((tid & 31) == 0 && hi != 0u) {
-    atomicMin(&sh.list_min, lo);
-    atomicMax(&sh.list_max, hi);
+    atomicMin(&sh.key_min, lo);
+    atomicMax(&sh.key_max, hi);
   }
   __syncthreads();
-  const int n = sh.n_list;
-  lo = sh.list_min;
-  hi = sh.list_max;
-  if (lo == hi) return lo;                                       // ties
-  if (n > kList) return descend<kMass>(row, weight, lo, hi, left, sh);
-  if (kMass) {
-    for (int i = tid; i < n; i += kThreads) sh.list_w[i] = weight(sh.list_k[i]);
+  const int n = sh.n_rank, above = sh.n_list;
+  lo = sh.key_min;
+  hi = sh.key_max;
+  if (n > kRank) {
+    if (lo == hi) return key_value(lo);                          // ties
+    return descend<kMass>(row, weight, *gathered, lo, hi, left, sh);
+  }
+  if (lo == hi) {
+    floor = key_value(lo);
+    __syncthreads();                                             // (n_list has been read by everybody)
+  } else {
+    if (kMass) {
+      for (int i = tid; i < n; i += kThreads) sh.rank_w[i] = weight(sh.rank_l[i]);
+      __syncthreads();
+    }
+    for (int i = tid; i < n; i += kThreads) {
+      const float l = sh.rank_l[i];
+      unsigned long long over = 0, with = 0;
+      for (int j = 0; j < n; ++j) {
+        const unsigned long long w = kMass ? sh.rank_w[j] : 1ull;
+        over += sh.rank_l[j] > l ? w : 0ull;
+        with += sh.rank_l[j] >= l ? w : 0ull;
+      }
+      if (over <= left && left < with) sh.floor = l;             // exactly one value; its ties agree
+    }
+    __syncthreads();
+    floor = sh.floor;
+  }
+  if (gather && above + n <= kList) {
+    for (int i = tid; i < n; i += kThreads)
+      if (sh.rank_l[i] >= floor) {
+        const int at = atomicAdd(&sh.n_list, 1);
+        sh.list_l[at] = sh.rank_l[i];
+        sh.list_i[at] = sh.rank_i[i];
+      }
+    *gathered = true;
     __syncthreads();
   }
-  for (int i = tid; i < n; i += kThreads) {
-    const uint32_t k = sh.list_k[i];
-    unsigned long long above = 0, with = 0;
-    for (int j = 0; j < n; ++j) {
-      const unsigned long long w = kMass ? sh.list_w[j] : 1ull;
-      above += sh.list_k[j] > k ? w : 0ull;
-      with += sh.list_k[j] >= k ? w : 0ull;
-    }
-    if (above <= left && left < with) sh.floor_key = k;          // exactly one value; its ties agree
-  }
-  __syncthreads();
-  return sh.floor_key;
+  return floor;
 }
 
 template <typename E, int kThreads>
@@ -278,157 +375,140 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_sample(const Samp
   extern __shared__ __align__(16) uint8_t s_raw[];
   Shared<kThreads>& sh = *reinterpret_cast<Shared<kThreads>*>(s_raw);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = blockIdx.x;
+  const float T = a.temperature == nullptr ? 1.f : a.temperature[r];
+  const bool greedy = !(T > 0.f);
   Row<E> row;
   row.g = static_cast<const E*>(a.logits) + (long long)r * a.row_stride;
-  row.s = reinterpret_cast<uint32_t*>(s_raw + sizeof(Shared<kThreads>));
+  row.s = reinterpret_cast<float*>(s_raw + sizeof(Shared<kThreads>));
   row.V = a.V;
-  row.n_res = min(a.V, a.n_res);
-  if (tid < 32) sh.table[tid] = exp2((double)tid / 32.0);
-  // the row's keys, largest and smallest of those that can be kept
-  uint32_t k_max = kNoKey, k_min = 0xffffffffu;
-  auto take = [&](int i, float x) {
-    const uint32_t k = logit_key(x);
-    if (i < row.n_res) row.s[i] = k;
-    k_max = max(k_max, k);
-    k_min = min(k_min, k - 1u);                                  // kNoKey - 1 wraps to the largest
-  };
-  constexpr int kVec = 16 / sizeof(E);
-  int done = 0;
-  if ((reinterpret_cast<uintptr_t>(row.g) & 15u) == 0) {
-    const uint4* g16 = reinterpret_cast<const uint4*>(row.g);
-    const int n16 = a.V / kVec;
-    auto take16 = [&](int i, const uint4& v) {
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  row.n_res = a.n_res;
+  row.wide = (reinterpret_cast<uintptr_t>(row.g) & (4 * sizeof(E) - 1)) == 0;
+  if (tid < 64) sh.table[tid] = exp2((double)tid / 64.0);
+  // the row: largest logit and its first place, smallest that can be kept
+  float m = -INFINITY, low = INFINITY;
+  int best = INT_MAX;
+  auto take = [&](int i4, const float4& v) {
+    if (greedy) {
+      const float l[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if (sizeof(E) == 4) {
-          take(i * kVec + q, __uint_as_float(w[q]));
-        } else {
-          take(i * kVec + 2 * q, __uint_as_float(w[q] << 16));
-          take(i * kVec + 2 * q + 1, __uint_as_float(w[q] & 0xffff0000u));
+      for (int q = 0; q < 4; ++q)
+        if (l[q] > m) {
+          m = l[q];
+          best = 4 * i4 + q;
         }
-      }
-    };
-    int i = tid;
-    for (; i + 3 * kThreads < n16; i += 4 * kThreads) {
-      uint4 v[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = __ldg(g16 + i + q * kThreads);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) take16(i + q * kThreads, v[q]);
+    } else {
+      if (4 * i4 < row.n_res) reinterpret_cast<float4*>(row.s)[i4] = v;
+      m = fmaxf(fmaxf(m, fmaxf(v.x, v.y)), fmaxf(v.z, v.w));     // (NaN is passed over)
+      low = fminf(low, v.x > -INFINITY ? v.x : INFINITY);
+      low = fminf(low, v.y > -INFINITY ? v.y : INFINITY);
+      low = fminf(low, v.z > -INFINITY ? v.z : INFINITY);
+      low = fminf(low, v.w > -INFINITY ? v.w : INFINITY);
     }
-    for (; i < n16; i += kThreads) take16(i, __ldg(g16 + i));
-    done = n16 * kVec;
+  };
+  {
+    const int n4 = a.V / 4;
+    int i = tid;
+    for (; i + 3 * kThreads < n4; i += 4 * kThreads) {
+      float4 v[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = row.from_memory(i + q * kThreads);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) take(i + q * kThreads, v[q]);
+    }
+    for (; i < n4; i += kThreads) take(i, row.from_memory(i));
   }
-  for (int i = done + tid; i < a.V; i += kThreads) take(i, to_float(row.g[i]));
-  k_max = __reduce_max_sync(0xffffffffu, k_max);
-  k_min = __reduce_min_sync(0xffffffffu, k_min);
+  const float thread_m = m;
+  m = warp_max(m);
+  low = -warp_max(-low);
   if (lane == 0) {
-    sh.red_hi[warp] = k_max;
-    sh.red_lo[warp] = k_min;
+    sh.red_hi[warp] = m;
+    sh.red_lo[warp] = low;
   }
   if (tid == 0) sh.token = INT_MAX;
   __syncthreads();
-  k_max = __reduce_max_sync(0xffffffffu, lane < kWarps ? sh.red_hi[lane] : kNoKey);
-  k_min = __reduce_min_sync(0xffffffffu, lane < kWarps ? sh.red_lo[lane] : 0xffffffffu) + 1u;
-  if (k_max == kNoKey) {   // nothing to draw from
-    if (tid == 0) {
-      a.token[r] = -1;
-      if (a.prob != nullptr) a.prob[r] = 0.f;
-      if (a.kept != nullptr) a.kept[r] = 0;
-    }
-    return;
-  }
-  const float T = a.temperature == nullptr ? 1.f : a.temperature[r];
-  if (!(T > 0.f)) {        // the most likely token, lowest index first
-    int best = INT_MAX;
-    each<kThreads>(row, [&](int i, uint32_t k) {
-      if (k == k_max) best = min(best, i);
-    });
-    best = __reduce_min_sync(0xffffffffu, best);
+  m = warp_max(lane < kWarps ? sh.red_hi[lane] : -INFINITY);
+  low = -warp_max(lane < kWarps ? -sh.red_lo[lane] : -INFINITY);
+  if (greedy || m == -INFINITY) {
+    // the most likely token, lowest index first; or nothing to draw from
+    best = __reduce_min_sync(0xffffffffu, thread_m == m ? best : INT_MAX);
     if (lane == 0 && best != INT_MAX) atomicMin(&sh.token, best);
     __syncthreads();
     if (tid == 0) {
-      a.token[r] = sh.token;
-      if (a.prob != nullptr) a.prob[r] = 1.f;
-      if (a.kept != nullptr) a.kept[r] = 1;
+      const bool any = m != -INFINITY;
+      a.token[r] = any ? sh.token : -1;
+      if (a.prob != nullptr) a.prob[r] = any ? 1.f : 0.f;
+      if (a.kept != nullptr) a.kept[r] = any ? 1 : 0;
     }
     return;
   }
-  const float m = key_value(k_max);
   Weight weight;
-  weight.m = (double)m;
-  weight.c = 46.166241308446828 / (double)T;   // 32 / ln 2
-  weight.m_key = k_max;
+  weight.m = m;
+  weight.md = (double)m;
+  weight.c = 92.332482616893656 / (double)T;   // 64 / ln 2
   weight.bits = a.fixed_bits;
   weight.table = sh.table;
-  uint32_t floor_key = k_min;
+  const float zero = m - T * (0.6931472f * (float)(a.fixed_bits + 2));
+  weight.zero = zero == zero ? zero : m;       // (infinite maximum and temperature)
+  float floor = low;
+  bool gathered = false;
   const int top_k = a.top_k == nullptr ? 0 : a.top_k[r];
   const float top_p = a.top_p == nullptr ? 1.f : a.top_p[r];
   const float min_p = a.min_p == nullptr ? 0.f : a.min_p[r];
-  const float reach = fminf(m - key_value(k_min), kReach);
+  const float reach = fminf(m - low, kReach);
   const float steps = (float)(kBins - 1) / reach;
   const bool even = reach > 1e-30f && m < INFINITY;              // the histogram over distances makes sense
-  if (top_k > 0 && top_k < a.V) {
-    const unsigned long long target = (unsigned long long)top_k - 1ull;
-    if (even)
-      floor_key = threshold<false>(row, weight, m, steps, floor_key, k_max, [&](unsigned long long) { return target; }, sh);
-    else
-      floor_key = descend<false>(row, weight, floor_key, k_max, target, sh);
-  }
+  if (top_k > 0 && top_k < a.V)
+    floor = threshold<false>(row, weight, &gathered, floor, even, steps,
+                             [&](unsigned long long) { return (unsigned long long)top_k - 1ull; }, sh);
   if (top_p < 1.f) {
     // kept iff W(> x) < top_p z; for whole W: W(> x) <= ceil(top_p z) - 1
-    auto target_of = [&](unsigned long long z) {
-      const double t = ceil((double)top_p * (double)z);
-      return t < 1.0 ? 0ull : (unsigned long long)t - 1ull;
-    };
-    if (even) {
-      floor_key = threshold<true>(row, weight, m, steps, floor_key, k_max, target_of, sh);
-    } else {
-      unsigned long long z = 0;
-      each<kThreads>(row, [&](int, uint32_t k) {
-        if (k >= floor_key) z += weight(k);
-      });
-      z = warp_sum(z);
-      __syncthreads();
-      if (lane == 0) sh.warp_sum[warp] = z;
-      __syncthreads();
-      z = warp_sum(lane < kWarps ? sh.warp_sum[lane] : 0ull);
-      floor_key = descend<true>(row, weight, floor_key, k_max, target_of(z), sh);
-    }
+    floor = threshold<true>(row, weight, &gathered, floor, even, steps,
+                            [&](unsigned long long z) {
+                              const double t = ceil((double)top_p * (double)z);
+                              return t < 1.0 ? 0ull : (unsigned long long)t - 1ull;
+                            },
+                            sh);
   }
   if (min_p > 0.f) {
     // w >= min_p  <=>  l >= m + T ln(min_p)
-    const double bound = weight.m + (double)T * log(min((double)min_p, 1.0));
+    const double bound = weight.md + (double)T * log(min((double)min_p, 1.0));
     const float f = (float)bound;
-    uint32_t k = logit_key((double)f >= bound ? f : nextafterf(f, INFINITY));
-    if (!(f > -INFINITY)) k = floor_key;
-    floor_key = max(floor_key, min(k, k_max));
+    const float up = (double)f >= bound ? f : nextafterf(f, INFINITY);
+    if (f > -INFINITY) floor = fmaxf(floor, fminf(up, m));
   }
-  // weight sums of groups of consecutive tokens, one warp per group
+  // weight sums of groups of consecutive tokens: by the gathered tokens, or one warp per group
   const int n_groups = ((a.V - 1) >> a.group_shift) + 1;
+  uint32_t count = 0;
   __syncthreads();                                               // the histogram's place becomes the groups'
-  for (int i = n_groups + tid; i < kBins; i += kThreads) sh.group[i] = 0ull;
-  unsigned int count = 0;
-  for (int g = warp; g < n_groups; g += kWarps) {
-    unsigned long long sum = 0;
-    const int end = min(a.V, (g + 1) << a.group_shift);
-    for (int i0 = g << a.group_shift; i0 < end; i0 += 128) {
-      uint32_t k[4];
+  if (gathered) {
+    for (int i = tid; i < kBins; i += kThreads) sh.group[i] = 0ull;
+    __syncthreads();
+    each_kept<kThreads>(row, sh, true, floor, [&](int i, float l) {
+      uint32_t* word = reinterpret_cast<uint32_t*>(&sh.group[i >> a.group_shift]);
+      add_pair(word, word + 1, weight(l));
+      ++count;
+    });
+  } else {
+    for (int i = n_groups + tid; i < kBins; i += kThreads) sh.group[i] = 0ull;
+    for (int g = warp; g < n_groups; g += kWarps) {
+      unsigned long long sum = 0;
+      const int end = min(a.V, (g + 1) << a.group_shift) / 4;
+      for (int i = ((g << a.group_shift) >> 2) + lane; i < end; i += 32) {
+        const float4 v = row.four(i);
+        const float l[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int q = 0; q < 4; ++q) k[q] = i0 + 32 * q + lane < end ? row.key(i0 + 32 * q + lane) : kNoKey;
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (k[q] >= floor_key) {                                 // (floor_key is above kNoKey)
-          sum += weight(k[q]);
-          ++count;
-        }
+        for (int q = 0; q < 4; ++q)
+          if (l[q] >= floor) {
+            sum += weight(l[q]);
+            ++count;
+          }
+      }
+      sum = warp_sum(sum);
+      if (lane == 0) sh.group[g] = sum;
     }
-    sum = warp_sum(sum);
-    if (lane == 0) sh.group[g] = sum;
   }
   count = __reduce_add_sync(0xffffffffu, count);
-  if (lane == 0) sh.red_lo[warp] = count;
+  if (lane == 0) sh.red_n[warp] = count;
   __syncthreads();
   // the group in which the cumulative weight passes u * total (cumulative > u total <=> > floor(u total) for whole sums)
   float u = a.uniforms[r];
@@ -438,14 +518,14 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_sample(const Samp
     return target = min((unsigned long long)((double)u * (double)z), z - 1ull);
   });
   if (warp != 0) return;
-  const uint32_t n_kept = __reduce_add_sync(0xffffffffu, lane < kWarps ? sh.red_lo[lane] : 0u);
+  const uint32_t n_kept = __reduce_add_sync(0xffffffffu, lane < kWarps ? sh.red_n[lane] : 0u);
   // the token inside it; one warp
   unsigned long long run = sh.before;
   const int g_hit = sh.at, end = min(a.V, (g_hit + 1) << a.group_shift);
   for (int i0 = g_hit << a.group_shift; i0 < end; i0 += 32) {
     const int i = i0 + lane;
-    const uint32_t k = i < end ? row.key(i) : kNoKey;
-    const unsigned long long w = k >= floor_key ? weight(k) : 0ull;
+    const float l = i < end ? row.at(i) : -INFINITY;
+    const unsigned long long w = l >= floor ? weight(l) : 0ull;
     unsigned long long c = w;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -467,8 +547,9 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_sample(const Samp
 
 template <typename E, int kThreads>
 int launch(cascade_ctx* ctx, SampleArgs& a, int n_rows, cudaStream_t s) {
-  // what the row's keys may take: the CTA's share of an SM's 227 KB less its arrays (and 1 KB that the system takes)
-  constexpr int kMost = (kThreads == 1024 ? 226 : 112) * 1024 - (int)sizeof(Shared<kThreads>);
+  // what the row's logits may take: the CTA's share of an SM's 227 KB less its arrays (and 1 KB that the system takes)
+  constexpr int kMost = ((kThreads == 1024 ? 226 : 112) * 1024 - (int)sizeof(Shared<kThreads>)) / 16 * 16;
+  static_assert(sizeof(Shared<kThreads>) % 16 == 0 && kMost % 16 == 0, "alignment of the row in shared memory");
   a.n_res = kMost / 4 < a.V ? kMost / 4 : a.V;
   const size_t smem = sizeof(Shared<kThreads>) + (size_t)a.n_res * 4;
   const uint32_t bit = PAGED_CFG_SAMPLE << ((sizeof(E) == 2 ? 2 : 0) + (kThreads == 1024 ? 1 : 0));
