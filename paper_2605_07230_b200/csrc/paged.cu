@@ -1,16 +1,19 @@
 // The paged KV cache's bookkeeping and its writer: block tables, slot map and free-page stack of the next pass from the
 // requests' lengths, and rotary embedding + cache write of a pass's keys and values (queries rotated beside them).
+#include <climits>
 #include <cmath>
 #include <cstring>
 
 #include "cascade_internal.h"
 #include "paged.h"
+#include "paged_attn.cuh"
 #include "ptx.cuh"
 
 namespace {
 
 constexpr int kTabThreads = 1024;
 constexpr int kTabWarps = kTabThreads / 32;
+static_assert(kTabWarps == 32, "one lane per warp in the scan of the warps' sums");
 constexpr int kPerThread = CASCADE_MAX_REQUESTS / kTabThreads;  // requests per thread of the scan
 
 struct TablesArgs {
@@ -18,6 +21,9 @@ struct TablesArgs {
   const int32_t *new_len, *kv_len, *free_count;
   int32_t *block_table, *free_pages, *kv_len_out, *free_count_out, *q_begin, *slot, *pos;
   int* err;
+  paged::PageDiv div;
+  // pages that n tokens fill (n >= 0)
+  __device__ __forceinline__ int pages(int n) const { return n == 0 ? 0 : div.page(n - 1) + 1; }
 };
 
 // One cluster does the whole job.  Every CTA scans all requests (three exclusive sums: new tokens, pages needed, pages
@@ -35,7 +41,7 @@ __global__ void __launch_bounds__(kTabThreads) k_paged_tables(const TablesArgs a
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = (int)ptx::cluster_ctarank(), n_cta = (int)ptx::cluster_nctarank();
   const int P = a.page_size;
-  const long long cap = (long long)a.table_stride * P;
+  const long long cap = min((long long)a.table_stride * P, (long long)INT_MAX);   // (a pool holds fewer tokens than 2^31)
   const int count = *a.free_count;
   if (tid == 0) s_bad = 0;
   __syncthreads();
@@ -55,12 +61,12 @@ __global__ void __launch_bounds__(kTabThreads) k_paged_tables(const TablesArgs a
       if (kv < 0 || (long long)kv + (n > 0 ? n : 0) > cap) {
         bad = true;
       } else {
-        const int had = (int)(((long long)kv + P - 1) / P);
+        const int had = a.pages(kv);
         if (n < 0) {
           back[k] = had;
         } else {
           add[k] = n;
-          need[k] = (int)(((long long)kv + n + P - 1) / P) - had;
+          need[k] = a.pages(kv + n) - had;
         }
       }
       sum[0] += add[k];
@@ -81,14 +87,18 @@ __global__ void __launch_bounds__(kTabThreads) k_paged_tables(const TablesArgs a
     for (int i = 0; i < 3; ++i) s_warp[i][warp] = inc[i];
   if (bad) s_bad = 1;
   __syncthreads();
-  long long total[3] = {0, 0, 0}, run[3];
-  for (int i = 0; i < 3; ++i) {
-    long long before = 0;
-    for (int w = 0; w < kTabWarps; ++w) {
-      if (w == warp) before = total[i];
-      total[i] += s_warp[i][w];
+  long long total[3], run[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {   // every warp scans the warps' sums for itself
+    const long long v = s_warp[i][lane];
+    long long c = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long t = __shfl_up_sync(0xffffffffu, c, o);
+      if (lane >= o) c += t;
     }
-    run[i] = before + inc[i] - sum[i];
+    total[i] = __shfl_sync(0xffffffffu, c, 31);
+    run[i] = __shfl_sync(0xffffffffu, c - v, warp) + inc[i] - sum[i];
   }
   const long long count1 = (long long)count + total[2];
   const bool ok = s_bad == 0 && total[0] <= a.n_tok && count1 <= a.n_pages && total[1] <= count1;  // the same in every CTA
@@ -110,7 +120,7 @@ __global__ void __launch_bounds__(kTabThreads) k_paged_tables(const TablesArgs a
   if (ok)
     for (int r = rank * kTabWarps + warp; r < a.n_req; r += n_cta * kTabWarps) {
       if (s_kv[r] >= 0) continue;
-      const int held = (int)(((long long)(-1 - s_kv[r]) + P - 1) / P);
+      const int held = a.pages(-1 - s_kv[r]);
       for (int j = lane; j < held; j += 32) a.free_pages[count + s_back[r] + j] = a.block_table[(size_t)r * a.table_stride + j];
     }
   __syncwarp();
@@ -122,7 +132,7 @@ __global__ void __launch_bounds__(kTabThreads) k_paged_tables(const TablesArgs a
     const bool done = s_kv[r] < 0;
     const int kv = done ? -1 - s_kv[r] : s_kv[r], n = s_q[r + 1] - s_q[r];
     if (ok && !done) {
-      const int had = (int)(((long long)kv + P - 1) / P), has = (int)(((long long)kv + n + P - 1) / P);
+      const int had = a.pages(kv), has = a.pages(kv + n);
       for (int j = had + lane; j < has; j += 32)
         a.block_table[(size_t)r * a.table_stride + j] = a.free_pages[count1 - 1 - s_need[r] - (j - had)];
     }
@@ -158,10 +168,10 @@ __global__ void __launch_bounds__(kTabThreads) k_paged_tables(const TablesArgs a
           ++r;
           page_at = -1;
         }
-        const int x = s_kv[r] + t - s_q[r], pi = x / P;
+        const int x = s_kv[r] + t - s_q[r], pi = a.div.page(x);
         if (pi != page_at) {
           page_at = pi;
-          const int had = (int)(((long long)s_kv[r] + P - 1) / P);
+          const int had = a.pages(s_kv[r]);
           page = pi < had ? a.block_table[(size_t)r * a.table_stride + pi] : a.free_pages[count1 - 1 - s_need[r] - (pi - had)];
           if (page < 0 || page >= a.n_pages) {
             page = -1;
@@ -364,6 +374,7 @@ int cascade_paged_tables(cascade_ctx* ctx, int32_t n_req, int32_t n_tok, int32_t
   a.slot = slot;
   a.pos = pos;
   a.err = ctx->dev_error;
+  a.div = paged::page_div(page_size);
   const size_t smem = (size_t)(4 * n_req + 1) * sizeof(int);
   if (smem > 48 * 1024)
     CASCADE_TRY(configure_smem(ctx, PAGED_CFG_TABLES, k_paged_tables, (4 * CASCADE_MAX_REQUESTS + 1) * (int)sizeof(int)));

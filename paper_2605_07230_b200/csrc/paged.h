@@ -8,7 +8,7 @@ int check_paged_cache(const cascade_ctx* ctx, const cascade_paged_cache* cache);
 int check_current_device(const cascade_ctx* ctx);
 
 // Bits of cascade_ctx.paged_configured.
-enum : uint32_t { PAGED_CFG_TABLES = 1, PAGED_CFG_ATTN_TC = 2, PAGED_CFG_SAMPLE = 4 /* four bits: type, CTA size */ };
+enum : uint32_t { PAGED_CFG_TABLES = 1, PAGED_CFG_ATTN_TC = 2, PAGED_CFG_SAMPLE = 4, PAGED_CFG_SAMPLE_BF16 = 8 };
 // Lets kernel `f` use `bytes` of dynamic shared memory, once per context and bit.
 template <typename F>
 int configure_smem(cascade_ctx* ctx, uint32_t bit, F* f, int bytes) {

@@ -19,6 +19,7 @@
 
 namespace {
 
+constexpr int kThreads = 1024;             // one CTA an SM: two of 512 took 186 us where this takes 164 (488 rows of 65536)
 constexpr int kBins = 2048;                // steps of a histogram; groups of consecutive tokens with a weight sum each
 constexpr int kList = 4096;                // kept tokens that are gathered
 constexpr int kRank = 1024;                // tokens of one step that are ranked directly
@@ -30,7 +31,6 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 
-template <int kThreads>
 struct alignas(16) Shared {                // (the row's logits follow it and are read 16 bytes at a time)
   union {
     struct {
@@ -142,7 +142,7 @@ struct Row {
 };
 
 // f(index, logit) for every token of the row, four at a time (V is a multiple of 8).
-template <int kThreads, typename E, typename F>
+template <typename E, typename F>
 __device__ __forceinline__ void each(const Row<E>& row, F f) {
   const int n4 = row.V / 4;
   auto take = [&](int i, const float4& v) {
@@ -161,13 +161,13 @@ __device__ __forceinline__ void each(const Row<E>& row, F f) {
 }
 
 // The tokens still in play: the gathered ones, or those of the row from `floor` up.
-template <int kThreads, typename E, typename F>
-__device__ __forceinline__ void each_kept(const Row<E>& row, const Shared<kThreads>& sh, bool gathered, float floor, F f) {
+template <typename E, typename F>
+__device__ __forceinline__ void each_kept(const Row<E>& row, const Shared& sh, bool gathered, float floor, F f) {
   if (gathered) {
     for (int i = threadIdx.x; i < sh.n_list; i += kThreads)
       if (sh.list_l[i] >= floor) f(sh.list_i[i], sh.list_l[i]);
   } else {
-    each<kThreads>(row, [&](int i, float l) {
+    each(row, [&](int i, float l) {
       if (l >= floor) f(i, l);
     });
   }
@@ -175,8 +175,8 @@ __device__ __forceinline__ void each_kept(const Row<E>& row, const Shared<kThrea
 
 // The first entry at which the running sum of kBins entries get(i) passes `target` (> target); sh.at and sh.before = the sum
 // in front of it.  target_of(total) is called with the sum of all entries.  sh.at = -1 if the total does not pass it.
-template <int kThreads, typename Get, typename Target>
-__device__ __forceinline__ unsigned long long find(Shared<kThreads>& sh, Get get, Target target_of) {
+template <typename Get, typename Target>
+__device__ __forceinline__ unsigned long long find(Shared& sh, Get get, Target target_of) {
   constexpr int kPer = kBins / kThreads;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   unsigned long long v[kPer], sum = 0;
@@ -216,8 +216,7 @@ __device__ __forceinline__ unsigned long long find(Shared<kThreads>& sh, Get get
   return total;
 }
 
-template <int kThreads>
-__device__ __forceinline__ void clear_hist(Shared<kThreads>& sh) {
+__device__ __forceinline__ void clear_hist(Shared& sh) {
   __syncthreads();
   for (int i = threadIdx.x; i < kBins; i += kThreads) sh.hist.lo[i] = sh.hist.hi[i] = 0u;
   __syncthreads();
@@ -225,14 +224,14 @@ __device__ __forceinline__ void clear_hist(Shared<kThreads>& sh) {
 
 // The value x among keys in [lo, hi] with W(> x) <= target < W(>= x), W the weight (1 each, or exp) of the tokens in play
 // with a key >= lo: the general search, 2048 steps of the keys' range at a time.  The whole CTA calls it.
-template <bool kMass, int kThreads, typename E>
+template <bool kMass, typename E>
 __device__ __noinline__ float descend(const Row<E>& row, const Weight& weight, bool gathered, uint32_t lo, uint32_t hi,
-                                      unsigned long long target, Shared<kThreads>& sh) {
+                                      unsigned long long target, Shared& sh) {
   while (true) {
     const uint32_t range = hi - lo;
     const int shift = range < (uint32_t)kBins ? 0 : 32 - __clz(range) - 11;  // (range >> shift) < 2048
     clear_hist(sh);
-    each_kept<kThreads>(row, sh, gathered, key_value(lo), [&](int, float l) {
+    each_kept(row, sh, gathered, key_value(lo), [&](int, float l) {
       const uint32_t k = order_key(l + 0.f);                     // + 0: the two zeros are one value
       if (k >= lo && k <= hi) {
         const int bin = kBins - 1 - (int)((k - lo) >> shift);   // largest first
@@ -243,7 +242,7 @@ __device__ __noinline__ float descend(const Row<E>& row, const Weight& weight, b
       }
     });
     __syncthreads();
-    find<kThreads>(sh, [&](int i) { return ((unsigned long long)sh.hist.hi[i] << 32) | sh.hist.lo[i]; },
+    find(sh, [&](int i) { return ((unsigned long long)sh.hist.hi[i] << 32) | sh.hist.lo[i]; },
                    [&](unsigned long long) { return target; });
     if (sh.at < 0) return key_value(lo);                         // all of it stays
     target -= sh.before;
@@ -256,9 +255,9 @@ __device__ __noinline__ float descend(const Row<E>& row, const Weight& weight, b
 
 // The same threshold, over the tokens in play from `floor` up, by one histogram over the distance to the maximum; `even`:
 // that makes sense.  target_of: from the total weight.  Leaves what stays gathered (*gathered) if it is few enough.
-template <bool kMass, int kThreads, typename E, typename Target>
+template <bool kMass, typename E, typename Target>
 __device__ __forceinline__ float threshold(const Row<E>& row, const Weight& weight, bool* gathered, float floor, bool even,
-                                           float steps, Target target_of, Shared<kThreads>& sh) {
+                                           float steps, Target target_of, Shared& sh) {
   const int tid = threadIdx.x;
   auto bin_of = [&](float l) { return min(kBins - 1, (int)((weight.m - l) * steps)); };
   auto bins = [&](int i) { return ((unsigned long long)sh.hist.hi[i] << 32) | sh.hist.lo[i]; };
@@ -266,7 +265,7 @@ __device__ __forceinline__ float threshold(const Row<E>& row, const Weight& weig
   if (!even) {
     unsigned long long z = 0;
     if (kMass) {
-      each_kept<kThreads>(row, sh, *gathered, floor, [&](int, float l) { z += weight(l); });
+      each_kept(row, sh, *gathered, floor, [&](int, float l) { z += weight(l); });
       z = warp_sum(z);
       __syncthreads();
       if ((tid & 31) == 0) sh.warp_sum[tid >> 5] = z;
@@ -282,7 +281,7 @@ __device__ __forceinline__ float threshold(const Row<E>& row, const Weight& weig
     if (!*gathered) sh.n_list = 0;
   }
   clear_hist(sh);
-  each_kept<kThreads>(row, sh, *gathered, floor, [&](int, float l) {
+  each_kept(row, sh, *gathered, floor, [&](int, float l) {
     if (kMass) {
       if (l >= weight.zero) {
         const int bin = bin_of(l);
@@ -293,14 +292,14 @@ __device__ __forceinline__ float threshold(const Row<E>& row, const Weight& weig
     }
   });
   __syncthreads();
-  find<kThreads>(sh, bins, [&](unsigned long long total) { return target = target_of(total); });
+  find(sh, bins, [&](unsigned long long total) { return target = target_of(total); });
   const int bin = sh.at;
   if (bin < 0) return floor;                                     // all of it stays
   const unsigned long long left = target - sh.before;            // of the step's own weight
   // the tokens of that step; those above it are gathered unless everything in play is already
   uint32_t lo = 0xffffffffu, hi = 0u;
   const bool gather = !*gathered;
-  each_kept<kThreads>(row, sh, *gathered, floor, [&](int i, float l) {
+  each_kept(row, sh, *gathered, floor, [&](int i, float l) {
     const int b = bin_of(l);
     if (b < bin) {
       if (gather) {
@@ -369,17 +368,22 @@ __device__ __forceinline__ float threshold(const Row<E>& row, const Weight& weig
   return floor;
 }
 
-template <typename E, int kThreads>
-__global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_sample(const SampleArgs a) {
+template <typename E>
+__global__ void __launch_bounds__(kThreads, 1) k_sample(const SampleArgs a) {
   constexpr int kWarps = kThreads / 32;
   extern __shared__ __align__(16) uint8_t s_raw[];
-  Shared<kThreads>& sh = *reinterpret_cast<Shared<kThreads>*>(s_raw);
+  Shared& sh = *reinterpret_cast<Shared*>(s_raw);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = blockIdx.x;
   const float T = a.temperature == nullptr ? 1.f : a.temperature[r];
   const bool greedy = !(T > 0.f);
+  const int top_k = a.top_k == nullptr ? 0 : a.top_k[r];
+  const float top_p = a.top_p == nullptr ? 1.f : a.top_p[r];
+  const float min_p = a.min_p == nullptr ? 0.f : a.min_p[r];
+  float u = a.uniforms[r];
+  u = u > 0.f ? fminf(u, 1.f - FLT_EPSILON / 2.f) : 0.f;         // NaN and negative: 0
   Row<E> row;
   row.g = static_cast<const E*>(a.logits) + (long long)r * a.row_stride;
-  row.s = reinterpret_cast<float*>(s_raw + sizeof(Shared<kThreads>));
+  row.s = reinterpret_cast<float*>(s_raw + sizeof(Shared));
   row.V = a.V;
   row.n_res = a.n_res;
   row.wide = (reinterpret_cast<uintptr_t>(row.g) & (4 * sizeof(E) - 1)) == 0;
@@ -451,9 +455,6 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_sample(const Samp
   weight.zero = zero == zero ? zero : m;       // (infinite maximum and temperature)
   float floor = low;
   bool gathered = false;
-  const int top_k = a.top_k == nullptr ? 0 : a.top_k[r];
-  const float top_p = a.top_p == nullptr ? 1.f : a.top_p[r];
-  const float min_p = a.min_p == nullptr ? 0.f : a.min_p[r];
   const float reach = fminf(m - low, kReach);
   const float steps = (float)(kBins - 1) / reach;
   const bool even = reach > 1e-30f && m < INFINITY;              // the histogram over distances makes sense
@@ -483,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_sample(const Samp
   if (gathered) {
     for (int i = tid; i < kBins; i += kThreads) sh.group[i] = 0ull;
     __syncthreads();
-    each_kept<kThreads>(row, sh, true, floor, [&](int i, float l) {
+    each_kept(row, sh, true, floor, [&](int i, float l) {
       uint32_t* word = reinterpret_cast<uint32_t*>(&sh.group[i >> a.group_shift]);
       add_pair(word, word + 1, weight(l));
       ++count;
@@ -511,10 +512,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_sample(const Samp
   if (lane == 0) sh.red_n[warp] = count;
   __syncthreads();
   // the group in which the cumulative weight passes u * total (cumulative > u total <=> > floor(u total) for whole sums)
-  float u = a.uniforms[r];
-  u = u > 0.f ? fminf(u, 1.f - FLT_EPSILON / 2.f) : 0.f;         // NaN and negative: 0
   unsigned long long target = 0;
-  const unsigned long long total = find<kThreads>(sh, [&](int i) { return sh.group[i]; }, [&](unsigned long long z) {
+  const unsigned long long total = find(sh, [&](int i) { return sh.group[i]; }, [&](unsigned long long z) {
     return target = min((unsigned long long)((double)u * (double)z), z - 1ull);
   });
   if (warp != 0) return;
@@ -545,16 +544,16 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_sample(const Samp
   }
 }
 
-template <typename E, int kThreads>
+template <typename E>
 int launch(cascade_ctx* ctx, SampleArgs& a, int n_rows, cudaStream_t s) {
-  // what the row's logits may take: the CTA's share of an SM's 227 KB less its arrays (and 1 KB that the system takes)
-  constexpr int kMost = ((kThreads == 1024 ? 226 : 112) * 1024 - (int)sizeof(Shared<kThreads>)) / 16 * 16;
-  static_assert(sizeof(Shared<kThreads>) % 16 == 0 && kMost % 16 == 0, "alignment of the row in shared memory");
+  // what the row's logits may take: a CTA's 227 KB less its arrays, and 1 KB to spare
+  constexpr int kMost = (226 * 1024 - (int)sizeof(Shared)) / 16 * 16;
+  static_assert(sizeof(Shared) % 16 == 0 && kMost % 16 == 0, "alignment of the row in shared memory");
   a.n_res = kMost / 4 < a.V ? kMost / 4 : a.V;
-  const size_t smem = sizeof(Shared<kThreads>) + (size_t)a.n_res * 4;
-  const uint32_t bit = PAGED_CFG_SAMPLE << ((sizeof(E) == 2 ? 2 : 0) + (kThreads == 1024 ? 1 : 0));
-  CASCADE_TRY(configure_smem(ctx, bit, k_sample<E, kThreads>, (int)sizeof(Shared<kThreads>) + kMost));
-  k_sample<E, kThreads><<<n_rows, kThreads, smem, s>>>(a);
+  const size_t smem = sizeof(Shared) + (size_t)a.n_res * 4;
+  const uint32_t bit = sizeof(E) == 2 ? PAGED_CFG_SAMPLE_BF16 : PAGED_CFG_SAMPLE;
+  CASCADE_TRY(configure_smem(ctx, bit, k_sample<E>, (int)sizeof(Shared) + kMost));
+  k_sample<E><<<n_rows, kThreads, smem, s>>>(a);
   CASCADE_CUDA_TRY(cudaGetLastError());
   return CASCADE_OK;
 }
@@ -591,7 +590,5 @@ extern "C" int cascade_sample(cascade_ctx* ctx, const void* logits, int32_t logi
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   ctx->launches = 0;
   KernelScope ks(ctx, K_SAMPLE, s);
-  const bool many = n_rows > ctx->sm_count;
-  if (bf16) return many ? launch<__nv_bfloat16, 512>(ctx, a, n_rows, s) : launch<__nv_bfloat16, 1024>(ctx, a, n_rows, s);
-  return many ? launch<float, 512>(ctx, a, n_rows, s) : launch<float, 1024>(ctx, a, n_rows, s);
+  return bf16 ? launch<__nv_bfloat16>(ctx, a, n_rows, s) : launch<float>(ctx, a, n_rows, s);
 }

@@ -103,6 +103,21 @@ def test_tables_take_nothing_when_something_does_not_fit(what):
     ctx.close()
 
 
+def test_tables_of_lengths_at_the_end_of_32_bits():
+    P, top = 1 << 28, 2**31 - 1                     # ten entries of a row reach past 2^31 tokens, the pool does not
+    ctx = make_ctx()
+    for new, kv in (([10], [top]), ([top], [top]), ([1], [top])):
+        got = run_tables(ctx, new, kv, [[0, 1, 2, 3, 4, 5, 6, 7, -1, -1]], [0] * 7, 0, P, 16)
+        with pytest.raises(cb.CascadeError) as e:
+            ctx.check()
+        assert e.value.status == cb.ERR_OVERFLOW
+        assert got["kv"].tolist() == kv and set(got["slot"].tolist()) == {-1}
+    got = run_tables(ctx, [1], [6 * P + P - 2], [[3, 1, 2, 0, 4, 5, 6, -1]], [0] * 7, 0, P, 2)
+    ctx.check()
+    assert got["slot"].tolist() == [6 * P + P - 2, -1] and got["pos"].tolist() == [7 * P - 2, -1]
+    ctx.close()
+
+
 def test_tables_without_rows_and_with_a_bad_page():
     ctx = make_ctx()
     got = run_tables(ctx, [0, -1], [9, 8], [[1, 0], [2, -1]], [-1, -1, -1, -1], 0, 8, 0)
