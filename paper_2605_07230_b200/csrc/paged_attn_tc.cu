@@ -16,37 +16,20 @@
 // the same (a non-finite value at a key that another row of the block sees) is computed again by one warp from the keys
 // it sees alone.
 // Tensor bound for prompts; every wait is bounded (error word, normal teardown).
+#include <type_traits>
+
 #include "paged.h"
 #include "paged_attn.cuh"
 #include "tmap.h"
 
 namespace {
 
-constexpr int kTile = 128;        // keys per tile, rows per block
-constexpr int kThreads = 320;
-constexpr int kStages = 5;
+constexpr int kTile = 128;        // keys per tile (a stage of the ring), rows per block
+constexpr int kHalf = 64;         // keys per step of the softmax: half a tile
+constexpr int kThreads = 352;
+constexpr int kStages = 4;         // keys and values of two tiles
 constexpr float kLazy = 8.f;      // log2 units
 constexpr float kFar = 96.f;      // a score this far above the reference: the row is computed again
-constexpr int kPolyPairs = 2;  // of 16 pairs of weights, how many take the polynomial
-
-// 2^x for two x at once without the special-function unit: x = n + f, |f| <= 1/2, 2^f by a cubic (least squares at Chebyshev
-// nodes, weighted to equal relative error 7.5e-5, far below the weights' rounding to bf16), n added to its exponent.  A NaN
-// leaves as the largest float or NaN, which makes the row's result non-finite all the same.
-__device__ __forceinline__ void exp2_poly2(uint64_t x2, float* e0, float* e1) {
-  float x0, x1, t0, t1, p0, p1;
-  ptx::unpack2(x2, &x0, &x1);
-  const uint64_t x = ptx::pack2(ptx::max_nan(x0, -126.f), ptx::max_nan(x1, -126.f));
-  const uint64_t t = ptx::add2(x, ptx::pack2(12582912.f, 12582912.f));   // 1.5 * 2^23: n in the low bits
-  const uint64_t f = ptx::fma2(ptx::add2(t, ptx::pack2(-12582912.f, -12582912.f)), ptx::pack2(-1.f, -1.f), x);
-  uint64_t p = ptx::fma2(f, ptx::pack2(0.05517166493f, 0.05517166493f), ptx::pack2(0.24261112188f, 0.24261112188f));
-  p = ptx::fma2(p, f, ptx::pack2(0.69326098623f, 0.69326098623f));
-  p = ptx::fma2(p, f, ptx::pack2(0.99992807358f, 0.99992807358f));
-  ptx::unpack2(t, &t0, &t1);
-  ptx::unpack2(p, &p0, &p1);
-  *e0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
-  *e1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
-}
-
 template <int D>
 struct Cfg {
   static constexpr int kHalves = D / 64;                 // 64-element column blocks of a tile
@@ -68,15 +51,28 @@ struct Cursor {
   __device__ __forceinline__ bool find(const TcArgs& p, int item, int lane, Item* it);
 };
 
+// The items that a CTA takes: its own index first, then those of blocks that have not started yet, one at a time
+// (the launch has a block per item).  The loading warp asks one item ahead; every warp reads the answers in turn.
+struct Queue {
+  uint4 answer[2];
+  uint64_t full[2], empty[2];
+};
+constexpr int kWarps = kThreads / 32;
+
 struct Item {
   int r, head, q0, nq, kv;    // request, key head, the request's first row, rows, keys
   int tok[2];                 // first token of each block
-  int n[2], n_tiles;          // key tiles each block needs, tiles loaded
+  int n[2], n_tiles;          // half tiles of keys each block needs, tiles loaded
   int n_sink, skip;           // tile i is i (i < n_sink) or i + skip
   __device__ __forceinline__ int tile(int i) const { return i < n_sink ? i : i + skip; }
+  // (a block chosen at run time: an index would put the struct into local memory)
+  __device__ __forceinline__ int first(int w) const { return w == 0 ? tok[0] : tok[1]; }
+  __device__ __forceinline__ int count(int w) const { return w == 0 ? n[0] : n[1]; }
 };
 
 __device__ __forceinline__ bool Cursor::find(const TcArgs& p, int item, int lane, Item* it) {
+  if (item < 0) return false;
+  if (item < base) chunk = -32, base = total = 0;              // (the indexes grow as a rule)
   while (chunk < 0 || item >= base + total) {
     base += total;
     chunk += 32;
@@ -116,9 +112,9 @@ __device__ __forceinline__ bool Cursor::find(const TcArgs& p, int item, int lane
     it->n[w] = 0;
     if (it->tok[w] < it->nq) {
       const int last = x0 + min(it->nq, it->tok[w] + p.tpb) - 1;   // position of the block's last token
-      if (last >= 0) it->n[w] = last / kTile + 1 - it->skip;
+      if (last >= 0) it->n[w] = last / kHalf + 1 - 2 * it->skip;
     }
-    it->n_tiles = max(it->n_tiles, it->n[w]);
+    it->n_tiles = max(it->n_tiles, (it->n[w] + 2 - 1) / 2);
   }
   return true;
 }
@@ -129,8 +125,9 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 const __grid_constant__ CUtensorMap tm_v, const TcArgs p) {
   using C = Cfg<D>;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t q_full[2], q_empty[2], kv_full[kStages], kv_empty[kStages], s_full[2], p_full[2], o_full[2],
-      o_empty[2];
+  __shared__ __align__(8) uint64_t q_full[2], q_empty[2], kv_full[kStages], kv_empty[kStages], s_full[2][2], p_full[2][2],
+      o_full[2], o_empty[2];
+  __shared__ Queue queue;
   __shared__ uint32_t s_tmem_base;
   __shared__ int s_abort;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -144,15 +141,21 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
       ptx::mbar_init(&kv_full[i], 1);
-      ptx::mbar_init(&kv_empty[i], 1);
+      ptx::mbar_init(&kv_empty[i], 2);
     }
     for (int w = 0; w < 2; ++w) {
       ptx::mbar_init(&q_full[w], 1);
       ptx::mbar_init(&q_empty[w], 1);
-      ptx::mbar_init(&s_full[w], 1);
-      ptx::mbar_init(&p_full[w], 4);
+      for (int b = 0; b < 2; ++b) {
+        ptx::mbar_init(&s_full[w][b], 1);
+        ptx::mbar_init(&p_full[w][b], 4);
+      }
       ptx::mbar_init(&o_full[w], 1);
       ptx::mbar_init(&o_empty[w], 4);
+    }
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(&queue.full[i], 1);
+      ptx::mbar_init(&queue.empty[i], kWarps);
     }
     s_abort = 0;
     ptx::fence_mbar_init();
@@ -169,20 +172,42 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
-  const uint32_t tmem = s_tmem_base;   // S0, S1 at 0, 128; O0, O1 at 256, 384
+  const uint32_t tmem = s_tmem_base;   // S of block w and half b at 128 w + 64 b; O0, O1 at 256, 384
 
   Cursor cur;
   Item it;
+  uint32_t turn = 0;                                            // items that this warp has taken
+  auto ask = [&]() {                                            // for the item after this one
+    const uint32_t slot = turn & 1u, use = turn >> 1;
+    if (use > 0 && !ptx::mbar_wait_short(&queue.empty[slot], (use - 1) & 1u, abort_flag, err, wait_ns)) return false;
+    ptx::mbar_arrive_expect_tx(&queue.full[slot], 16);
+    ptx::take_block(&queue.answer[slot], &queue.full[slot]);
+    return true;
+  };
+  auto next = [&]() {                                           // the next item, -1 when there is none
+    const uint32_t slot = turn & 1u, use = turn >> 1;
+    ++turn;
+    const bool here = ptx::mbar_wait_short(&queue.full[slot], use & 1u, abort_flag, err, wait_ns);
+    int item = here ? ptx::taken_block(&queue.answer[slot]) : -1;
+    ptx::fence_proxy_async_smem();                              // (the next answer comes through the async proxy)
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(&queue.empty[slot]);
+    return __shfl_sync(0xffffffffu, item, 0);
+  };
   if (warp == 8) {
     // ---------------- loads ----------------
     const int n_box = kTile / p.box_rows;                       // boxes of a tile along the keys
     const int box_i = lane % n_box, half = lane / n_box;        // this lane's box
     const bool has_box = half < C::kHalves;
     const uint32_t box_bytes = (uint32_t)p.box_rows * 128u;
-    int stage = 0, items[2] = {0, 0};
-    uint32_t ph = 0;
+    int items[2] = {0, 0};
+    uint32_t ph = 0;                                            // bit j: parity of the next use of stages 2 j, 2 j + 1
     bool ok = true;
-    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &it); item += gridDim.x) {
+    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &it); item = next()) {
+      if (lane == 0) ok = ask();
+      ok = __shfl_sync(0xffffffffu, ok, 0);
+      if (!ok) break;
+#pragma unroll
       for (int w = 0; w < 2; ++w) {
         if (it.n[w] == 0) continue;
         if (items[w] > 0) ok = ok && ptx::mbar_wait_short(&q_empty[w], (items[w] - 1) & 1u, abort_flag, err, wait_ns);
@@ -215,7 +240,8 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         if (wanted && !load) atomicOr(err, CASCADE_DEV_ERR_BAD_PAGE);
         const uint32_t bytes = box_bytes * (uint32_t)__popc(__ballot_sync(0xffffffffu, load));
         for (int kv = 0; kv < 2; ++kv) {
-          ok = ptx::mbar_wait_short(&kv_empty[stage], ph ^ 1u, abort_flag, err, wait_ns);
+          const int stage = 2 * (i & 1) + kv;
+          ok = ptx::mbar_wait_short(&kv_empty[stage], ((ph >> (i & 1)) & 1u) ^ 1u, abort_flag, err, wait_ns);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           if (lane == 0) ptx::mbar_arrive_expect_tx(&kv_full[stage], bytes);
@@ -223,117 +249,92 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
           if (load)
             ptx::tma_load_4d(smem + (2 + stage) * C::kTileBytes + half * (kTile * 128) + box_i * box_bytes, kv == 0 ? &tm_k : &tm_v,
                              half * 64, it.head, row, page, &kv_full[stage]);
-          if (++stage == kStages) {
-            stage = 0;
-            ph ^= 1u;
-          }
         }
+        ph ^= 1u << (i & 1);
         page = next;
         row = next_row;
         wanted = next_wanted;
       }
     }
     // every stage and query tile has been given back before the CTA may end (the arrivals are asynchronous)
-    for (int i = 0; ok && i < kStages; ++i) {
-      ok = ptx::mbar_wait_short(&kv_empty[stage], ph ^ 1u, abort_flag, err, wait_ns);
-      if (++stage == kStages) {
-        stage = 0;
-        ph ^= 1u;
-      }
-    }
-    for (int w = 0; ok && w < 2; ++w)
-      if (items[w] > 0) ok = ptx::mbar_wait_short(&q_empty[w], (items[w] - 1) & 1u, abort_flag, err, wait_ns);
-  } else if (warp == 9) {
+    for (int i = 0; ok && i < kStages; ++i)
+      ok = ptx::mbar_wait_short(&kv_empty[i], ((ph >> (i >> 1)) & 1u) ^ 1u, abort_flag, err, wait_ns);
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+      if (ok && items[w] > 0) ok = ptx::mbar_wait_short(&q_empty[w], (items[w] - 1) & 1u, abort_flag, err, wait_ns);
+  } else if (warp >= 9) {
     // ---------------- products ----------------
-    // The whole warp runs this code and lane 0 issues, so that the descriptors stay in uniform registers: with one running
-    // lane every product cost a dozen instructions beside the softmax warps', 2200 cycles a tile instead of 1030.
-    const uint32_t live = lane == 0;
-    const uint32_t t0 = __shfl_sync(0xffffffffu, tmem, 0);
-    const uint32_t idesc_s = ptx::umma_idesc_bf16(128, kTile);
+    // One lane issues.  Stages and halves are known at compile time (two tiles a turn), so that every descriptor is the base
+    // plus a constant: beside the softmax warps each instruction of this warp costs some ten cycles.
+    const uint32_t idesc_s = ptx::umma_idesc_bf16(128, kHalf);
     const uint32_t idesc_o = ptx::umma_idesc_bf16_b_mn(128, D);
     const uint64_t q_desc = ptx::umma_desc_sw128(q_addr), k_desc = ptx::umma_desc_sw128(ring),
                    v_desc = ptx::umma_desc_sw128_strides(ring, kTile * 128, 1024);
-    int used[2] = {0, 0}, tiles[2] = {0, 0};   // items / tiles of each block so far
-    int stage = 0;                             // the next stage to be consumed; K(i) and V(i) alternate
-    uint32_t ph = 0;
+    int used = 0;                              // items of the block so far
+    uint32_t p_ph = 0, kv_ph = 0;              // bit b: parity of the next weights; bit j: of the next use of stages 2 j, 2 j + 1
     bool ok = true;
-    auto wait = [&](uint64_t* bar, uint32_t parity) {
-      if (ok) ok = ptx::mbar_wait_short(bar, parity, abort_flag, err, wait_ns);
-      ok = __all_sync(0xffffffffu, ok);
-    };
-    auto stage_off = [&](int st) { return __shfl_sync(0xffffffffu, st * (C::kTileBytes >> 4), 0); };   // in descriptor units
-    auto scores = [&](int w, int st) {
-      ptx::tc_fence_after();
-      const uint64_t kd = k_desc + (uint32_t)stage_off(st);
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return ok = ptx::mbar_wait_short(bar, parity & 1u, abort_flag, err, wait_ns); };
+    const int w = warp - 9;
+    auto scores = [&](int b, int st) {
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
         const uint32_t off = ((ks >> 2) * (kTile * 128) + (ks & 3) * 32) >> 4;
-        ptx::umma_bf16_warp(live, t0 + w * 128, q_desc + (w * (C::kTileBytes >> 4) + off), kd + off, idesc_s, ks != 0);
+        ptx::umma_bf16(tmem + w * 128 + b * kHalf, q_desc + (w * (C::kTileBytes >> 4) + off),
+                       k_desc + (st * (C::kTileBytes >> 4) + b * (kHalf * 128 >> 4) + off), idesc_s, ks != 0);
       }
-      ptx::umma_commit_if(live, &s_full[w]);
     };
-    auto outputs = [&](int w, int st, bool first) {
-      ptx::tc_fence_after();
-      const uint64_t vd = v_desc + (uint32_t)stage_off(st);
-      ptx::umma_bf16_ts_warp(live, t0 + 256 + w * 128, t0 + w * 128, vd, idesc_o, !first);
+    auto outputs = [&](int b, int st, bool first) {
 #pragma unroll
-      for (int ks = 1; ks < kTile / 16; ++ks)
-        ptx::umma_bf16_ts_warp(live, t0 + 256 + w * 128, t0 + w * 128 + ks * 8, vd + ks * (2048 >> 4), idesc_o, true);
+      for (int ks = 0; ks < kHalf / 16; ++ks)
+        ptx::umma_bf16_ts(tmem + 256 + w * 128, tmem + w * 128 + b * kHalf + ks * 8,
+                          v_desc + (st * (C::kTileBytes >> 4) + (b * (kHalf / 16) + ks) * (2048 >> 4)), idesc_o, ks != 0 || !first);
     };
-    auto advance = [&]() {
-      if (++stage == kStages) {
-        stage = 0;
-        ph ^= 1u;
+    // the products that follow the weights of tile i (j = i & 1)
+    auto tile = [&](int i, int n, int n_tiles) {
+      const int j = i & 1, kV = 2 * j + 1, kK = 2 * (j ^ 1);
+      if (!wait(&kv_full[kV], kv_ph >> j)) return;
+      kv_ph ^= 1u << j;
+      if (i + 1 < n_tiles && !wait(&kv_full[kK], kv_ph >> (j ^ 1))) return;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int h = 2 * i + b;
+        if (h >= n) break;
+        if (b == 0 && h == 0 && used > 0 && !wait(&o_empty[w], used - 1)) return;
+        if (!wait(&p_full[w][b], p_ph >> b)) return;
+        p_ph ^= 1u << b;
+        ptx::tc_fence_after();
+        outputs(b, kV, h == 0);
+        if (h + 1 == n) {
+          ptx::umma_commit(&o_full[w]);
+          break;
+        }
+        if (h + 2 < n) scores(b, kK);
+        ptx::umma_commit(&s_full[w][b]);     // (behind the last scores: tells that the product is done)
+        if (h + 2 + 1 == n) ptx::umma_commit(&q_empty[w]);
       }
+      ptx::umma_commit(&kv_empty[kV]);
+      if (i + 1 < n_tiles) ptx::umma_commit(&kv_empty[kK]);
     };
-    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &it); item += gridDim.x) {
+    auto block = [&](int n, int n_tiles) {
+      if (!wait(&kv_full[0], kv_ph)) return;
+      if (n > 0) {
+        if (!wait(&q_full[w], used)) return;
+#pragma unroll 1
+        for (int b = 0; b < 2 && b < n; ++b) {
+          scores(b, 0);
+          ptx::umma_commit(&s_full[w][b]);
+        }
+        if (n <= 2) ptx::umma_commit(&q_empty[w]);
+      }
+      ptx::umma_commit(&kv_empty[0]);
+#pragma unroll 1
+      for (int i = 0; ok && i < n_tiles; ++i) tile(i, n, n_tiles);
+      used += n > 0;
+    };
+    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &it); item = next()) {
       if (it.n_tiles == 0) continue;
-      wait(&kv_full[stage], ph);
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        if (it.n[w] == 0) continue;
-        wait(&q_full[w], used[w] & 1u);
-        if (!ok) break;
-        scores(w, stage);
-        if (it.n[w] == 1) ptx::umma_commit_if(live, &q_empty[w]);
-      }
-      if (!ok) break;
-      ptx::umma_commit_if(live, &kv_empty[stage]);
-      advance();
-      for (int i = 0; ok && i < it.n_tiles; ++i) {
-        const int v_stage = stage;
-        wait(&kv_full[stage], ph);
-        advance();
-        const int k_stage = stage;
-        const bool more = i + 1 < it.n_tiles;
-        bool k_here = false;
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          if (!ok || i >= it.n[w]) continue;
-          if (i == 0 && used[w] > 0) wait(&o_empty[w], (used[w] - 1) & 1u);
-          wait(&p_full[w], tiles[w] & 1u);
-          if (!ok) break;
-          ++tiles[w];
-          outputs(w, v_stage, i == 0);
-          if (i + 1 == it.n[w]) ptx::umma_commit_if(live, &o_full[w]);
-          if (i + 1 < it.n[w]) {
-            if (!k_here) {
-              wait(&kv_full[k_stage], ph);
-              k_here = true;
-              if (!ok) break;
-            }
-            scores(w, k_stage);
-            if (i + 2 == it.n[w]) ptx::umma_commit_if(live, &q_empty[w]);
-          }
-        }
-        if (!ok) break;
-        ptx::umma_commit_if(live, &kv_empty[v_stage]);
-        if (more) {
-          ptx::umma_commit_if(live, &kv_empty[k_stage]);
-          advance();
-        }
-      }
-      for (int w = 0; w < 2; ++w) used[w] += it.n[w] > 0;
+      if (lane == 0) block(it.count(w), it.n_tiles);
+      ok = __shfl_sync(0xffffffffu, ok, 0);
     }
   } else {
     // ---------------- softmax, one row per thread ----------------
@@ -343,129 +344,129 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     const int my_tok = rr / p.G, my_g = rr % p.G;
     const bool in_block = rr < p.tpb * p.G;
     const float c = p.a.scale * paged::kLog2e;
-    int tiles = 0, used = 0, kv_count = 0;                     // tiles / items of this block, ring stages of all items
+    int used = 0, kv_used[2] = {0, 0};                         // items of this block; tiles of all items by the stages they used
+    uint32_t s_ph = 0;                                         // bit b: parity of the next scores of half b
     bool ok = true;
-    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &it); item += gridDim.x) {
-      const int tok = it.tok[w] + my_tok;
+    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &it); item = next()) {
+      const int tok = it.first(w) + my_tok;
       const bool live = in_block && tok < it.nq;
       // position (below 0: sees nothing); a place without a row sees everything, which spares its warp the masks
       const int x = live ? it.kv - it.nq + tok : INT_MAX / 2;
       const int lo = live ? paged::window_begin(x, p.a.window) : 0, n_sink = p.a.sinks;
-      const int n = it.n[w];
+      const int n = it.count(w);
       float ref = -INFINITY, next_ref = -INFINITY, l = 0.f;
       bool odd = false;                                        // to be computed again from the keys the row sees alone
-      for (int i = 0; i < n; ++i, ++tiles) {
-        const int k0 = it.tile(i) * kTile;
-        ok = ptx::mbar_wait_short(&s_full[w], tiles & 1u, abort_flag, err, wait_ns);
+      const int x_min = __reduce_min_sync(0xffffffffu, x), lo_max = __reduce_max_sync(0xffffffffu, lo);
+      const bool waits_first = live && x >= 0;
+      for (int h = 0; h < n; ++h) {
+        const int b = h % 2, k0 = it.tile(h / 2) * kTile + b * kHalf;
+        const uint32_t t_h = t_s + b * kHalf;
+        const bool special = !(k0 + kHalf - 1 <= x_min && (k0 >= lo_max || k0 + kHalf <= n_sink));   // the warp needs masks
+        const bool raise = next_ref > ref, none = ref == -INFINITY && waits_first;
+        const bool act = __any_sync(0xffffffffu, raise || none);
+        ok = ptx::mbar_wait_short(&s_full[w][b], (s_ph >> b) & 1u, abort_flag, err, wait_ns);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
+        s_ph ^= 1u << b;
         ptx::tc_fence_after();
-        if (__any_sync(0xffffffffu, next_ref > ref)) {
-          // the scores of tile i come after the output product of tile i - 1, so the accumulator is at rest
-          const float alpha = next_ref > ref ? ptx::ex2(ref - next_ref) : 1.f;
-          ref = fmaxf(ref, next_ref);
-          l *= alpha;
-#pragma unroll 1
-          for (int q = 0; q < D / 16; ++q) {
-            float t[16];
-            ptx::tmem_ld16(t_o + 16 * q, t);
-#pragma unroll
-            for (int k = 0; k < 16; ++k) t[k] *= alpha;
-            ptx::tmem_st16(t_o + 16 * q, t);
-          }
-        }
-        const bool whole = __all_sync(0xffffffffu, k0 + kTile - 1 <= x && (k0 >= lo || k0 + kTile <= n_sink));
         // bit k: this row sees key k0 + 32 q + k
         auto visible = [&](int q) {
           const int j0 = k0 + 32 * q;
           auto below = [](int n) { return n >= 32 ? 0xffffffffu : (1u << max(n, 0)) - 1u; };
           return below(x - j0 + 1) & (~below(lo - j0) | below(n_sink - j0));
         };
-        if (__any_sync(0xffffffffu, ref == -INFINITY && k0 <= x && live)) {
-          // rows that have met no key yet take their reference from this tile
-          float m = -INFINITY;
+        if (act) {
+          if (__any_sync(0xffffffffu, raise)) {
+            // once the product of the half before is done (the next commit on the other half's scores), the accumulator is
+            // at rest
+            ok = ptx::mbar_wait_short(&s_full[w][b ^ 1], (s_ph >> (b ^ 1)) & 1u, abort_flag, err, wait_ns);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            ptx::tc_fence_after();
+            const float alpha = raise ? ptx::ex2(ref - next_ref) : 1.f;
+            ref = fmaxf(ref, next_ref);
+            l *= alpha;
 #pragma unroll 1
-          for (int q = 0; q < 4; ++q) {
-            uint32_t v[32];
-            ptx::tmem_ld32_async(t_s + 32 * q, v);
-            const uint32_t vis = visible(q);
-            ptx::tmem_wait_ld();
+            for (int q = 0; q < D / 16; ++q) {
+              float t[16];
+              ptx::tmem_ld16(t_o + 16 * q, t);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) m = fmaxf(m, (vis >> k) & 1u ? __uint_as_float(v[k]) : -INFINITY);
+              for (int k = 0; k < 16; ++k) t[k] *= alpha;
+              ptx::tmem_st16(t_o + 16 * q, t);
+            }
           }
-          if (ref == -INFINITY) ref = m * c;
-          next_ref = ref;
+          if (__any_sync(0xffffffffu, none)) {
+            // rows that have met no key yet take their reference from this half
+            float m = -INFINITY;
+#pragma unroll 1
+            for (int q = 0; q < kHalf / 32; ++q) {
+              uint32_t v[32];
+              ptx::tmem_ld32_async(t_h + 32 * q, v);
+              const uint32_t vis = visible(q);
+              ptx::tmem_wait_ld();
+#pragma unroll
+              for (int k = 0; k < 32; ++k) asm volatile("" : "+r"(v[k]));
+#pragma unroll
+              for (int k = 0; k < 32; ++k) m = fmaxf(m, (vis >> k) & 1u ? __uint_as_float(v[k]) : -INFINITY);
+            }
+            if (none) next_ref = ref = m * c;
+          }
         }
         const float minus = ref == -INFINITY ? 0.f : -ref;
-        float m = -INFINITY;
-        if (whole) {
-          const uint64_t c2 = ptx::pack2(c, c), minus2 = ptx::pack2(minus, minus);
-          uint64_t sum2 = 0;
-          float mb = -INFINITY;
-          uint32_t v[2][32];
-          ptx::tmem_ld32_async(t_s, v[0]);
+        float m = -INFINITY, mb = -INFINITY;
+        const uint64_t c2 = ptx::pack2(c, c), minus2 = ptx::pack2(minus, minus);
+        uint64_t sum2 = 0;
+        uint32_t v[2][32];
+        ptx::tmem_ld32_async(t_h, v[0]);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            ptx::tmem_wait_ld();
-            if (q < 3) ptx::tmem_ld32_async(t_s + 32 * (q + 1), v[(q + 1) & 1]);
-            uint32_t pk[16];
+        for (int q = 0; q < kHalf / 32; ++q) {
+          uint32_t pk[16];
+          ptx::tmem_wait_ld();
+          uint32_t* vq = v[q & 1];
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const float s0 = __uint_as_float(v[q & 1][2 * k]), s1 = __uint_as_float(v[q & 1][2 * k + 1]);
-              if (k & 1)
-                mb = ptx::max3(mb, s0, s1);
-              else
-                m = ptx::max3(m, s0, s1);
-              const uint64_t x2 = ptx::fma2(ptx::pack2(s0, s1), c2, minus2);
-              float e0, e1;
-              if (k % 16 < kPolyPairs)
-                exp2_poly2(x2, &e0, &e1);
-              else {
-                ptx::unpack2(x2, &e0, &e1);
-                e0 = ptx::ex2(e0);
-                e1 = ptx::ex2(e1);
-              }
-              sum2 = ptx::add2(sum2, ptx::pack2(e0, e1));
-              pk[k] = ptx::pack_bf16x2(e0, e1);
-            }
-            ptx::tmem_st16_async(t_s + 16 * q, pk);
-          }
-          m = fmaxf(m, mb);
-          float sa, sb;
-          ptx::unpack2(sum2, &sa, &sb);
-          l += sa + sb;
-        } else {
-          float sum = 0.f;
-#pragma unroll 1
-          for (int q = 0; q < 4; ++q) {
-            uint32_t v[32], pk[16];
-            ptx::tmem_ld32_async(t_s + 32 * q, v);
+          for (int k = 0; k < 32; ++k) asm volatile("" : "+r"(vq[k]));   // no use of the scores before the wait
+          if (q + 1 < kHalf / 32) ptx::tmem_ld32_async(t_h + 32 * (q + 1), v[(q + 1) & 1]);
+          if (special) {
             const uint32_t vis = visible(q);
-            ptx::tmem_wait_ld();
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const float s0 = (vis >> (2 * k)) & 1u ? __uint_as_float(v[2 * k]) : -INFINITY;
-              const float s1 = (vis >> (2 * k + 1)) & 1u ? __uint_as_float(v[2 * k + 1]) : -INFINITY;
-              m = fmaxf(m, fmaxf(s0, s1));
-              const float e0 = ptx::ex2(fmaf(s0, c, minus)), e1 = ptx::ex2(fmaf(s1, c, minus));
-              sum += e0 + e1;
-              pk[k] = ptx::pack_bf16x2(e0, e1);
-            }
-            ptx::tmem_st16_async(t_s + 16 * q, pk);
+            for (int k = 0; k < 32; ++k) vq[k] = (vis >> k) & 1u ? vq[k] : 0xff800000u;
           }
-          l += sum;
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const float s0 = __uint_as_float(vq[2 * k]), s1 = __uint_as_float(vq[2 * k + 1]);
+            if (k & 1)
+              mb = ptx::max3(mb, s0, s1);
+            else
+              m = ptx::max3(m, s0, s1);
+            float e0, e1;
+            const uint64_t x2 = ptx::fma2(ptx::pack2(s0, s1), c2, minus2);
+            ptx::unpack2(x2, &e0, &e1);
+            e0 = ptx::ex2(e0);
+            e1 = ptx::ex2(e1);
+            sum2 = ptx::add2(sum2, ptx::pack2(e0, e1));
+            pk[k] = ptx::pack_bf16x2(e0, e1);
+          }
+          ptx::tmem_st16_async(t_h + 16 * q, pk);
         }
+        m = fmaxf(m, mb);
+        float sa, sb;
+        ptx::unpack2(sum2, &sa, &sb);
+        l += sa + sb;
         m *= c;
-        if (m > ref + kLazy) next_ref = m;
+        if (live && m > ref + kLazy) next_ref = m;
         odd = odd || m > ref + kFar;
-        // values behind the last key: zeros (block 0 does it while it takes part, its product comes first)
-        if (k0 + kTile > it.kv && (w == 0 || i >= it.n[0])) {
-          const int st = (kv_count + 2 * i + 1) % kStages;
-          const uint32_t st_ph = ((uint32_t)(kv_count + 2 * i + 1) / kStages) & 1u;
+        // values behind the last key: zeros (both blocks write them, each ahead of its own product)
+        if (k0 + kHalf > it.kv) {
+          const int j = (h / 2) & 1, st = 2 * j + 1;
+          const uint32_t st_ph = (uint32_t)((j == 0 ? kv_used[0] : kv_used[1]) + h / 4) & 1u;
           ok = ptx::mbar_wait_short(&kv_full[st], st_ph, abort_flag, err, wait_ns);
-          if (ok && k0 + rr >= it.kv) {
-            for (int h = 0; h < C::kHalves; ++h)
-              for (int k = 0; k < 8; ++k) ptx::st_shared_v4(ring + st * C::kTileBytes + h * (kTile * 128) + rr * 128 + k * 16, 0, 0, 0, 0);
+          const int key = rr & (kHalf - 1);                    // two threads a key, each half of its values
+          if (ok && k0 + key >= it.kv) {
+            constexpr int kChunks = D / 16;
+            for (int k = 0; k < kChunks; ++k) {
+              const int at = (rr / kHalf) * kChunks + k;
+              ptx::st_shared_v4(ring + st * C::kTileBytes + (at >> 3) * (kTile * 128) + (b * kHalf + key) * 128 + (at & 7) * 16, 0, 0, 0, 0);
+            }
             ptx::fence_proxy_async_smem();
           }
           ok = __all_sync(0xffffffffu, ok);
@@ -474,10 +475,17 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         ptx::tmem_wait_st();
         ptx::tc_fence_before();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&p_full[w]);
+        if (lane == 0) ptx::mbar_arrive(&p_full[w][b]);
       }
-      kv_count += 2 * it.n_tiles;
+      kv_used[0] += (it.n_tiles + 1) / 2;
+      kv_used[1] += it.n_tiles / 2;
       if (!ok) break;
+      if (n > 1) {                               // the commit without scores, behind the last product but one
+        ok = ptx::mbar_wait_short(&s_full[w][n & 1], (s_ph >> (n & 1)) & 1u, abort_flag, err, wait_ns);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        s_ph ^= 1u << (n & 1);
+      }
       // ---- the rows' results ----
       const int row = it.q0 + tok, head = it.head * p.G + my_g;
       if (n > 0) {
@@ -554,8 +562,7 @@ int launch(cascade_ctx* ctx, const TcArgs& p, int n_items, cudaStream_t s) {
   const CUtensorMap* mv = get_tmap_4d_bf16(ctx, a.v, dk, sk, bk);
   if (mq == nullptr || mk == nullptr || mv == nullptr) return CASCADE_ERR_CUDA;
   CASCADE_TRY(configure_smem(ctx, PAGED_CFG_ATTN_TC, k_paged_attn_tc<D>, Cfg<D>::kSmem));   // (a context has one D)
-  const int grid = n_items < ctx->sm_count ? n_items : ctx->sm_count;
-  k_paged_attn_tc<D><<<grid, kThreads, Cfg<D>::kSmem, s>>>(*mq, *mk, *mv, p);
+  k_paged_attn_tc<D><<<n_items, kThreads, Cfg<D>::kSmem, s>>>(*mq, *mk, *mv, p);
   CASCADE_CUDA_TRY(cudaGetLastError());
   return CASCADE_OK;
 }
@@ -571,7 +578,9 @@ int launch_paged_attn_tc(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_t 
   while (p.box_rows < kTile && a.page_size % (2 * p.box_rows) == 0) p.box_rows *= 2;
   // no more items than this: a request's pairs of row blocks are at most ceil(tokens / (2 tpb))
   const long long pairs = (long long)a.n_tok / (2 * p.tpb) + a.n_req;
-  const long long items = pairs * a.Hkv;
-  const int n_items = items > (1 << 20) ? (1 << 20) : (int)items;
+  const long long by_length = (long long)a.n_req * ((a.max_q + 2 * p.tpb - 1) / (2 * p.tpb));
+  const long long items = (pairs < by_length ? pairs : by_length) * a.Hkv;
+  if (items > INT_MAX) return CASCADE_ERR_UNSUPPORTED_SHAPE;
+  const int n_items = (int)items;
   return ctx->shape.D == 128 ? launch<128>(ctx, p, n_items, s) : launch<64>(ctx, p, n_items, s);
 }
