@@ -253,6 +253,25 @@ __device__ __noinline__ float descend(const Row<E>& row, const Weight& weight, b
   }
 }
 
+// kept iff W(> x) < top_p z; for whole W: W(> x) <= ceil(top_p z) - 1
+__device__ __forceinline__ unsigned long long nucleus_target(float top_p, unsigned long long z) {
+  const double t = ceil((double)top_p * (double)z);
+  return t < 1.0 ? 0ull : (unsigned long long)t - 1ull;
+}
+
+// *floor = l if the threshold is l: W(> l) <= left < W(>= l) among n values (w: their weights, null: 1 each).  That holds for
+// exactly one value, or for none; its ties agree.
+__device__ __forceinline__ void rank(const float* values, const unsigned long long* w, int n, float l, unsigned long long left,
+                                     float* floor) {
+  unsigned long long over = 0, with = 0;
+  for (int j = 0; j < n; ++j) {
+    const unsigned long long x = w == nullptr ? 1ull : w[j];
+    over += values[j] > l ? x : 0ull;
+    with += values[j] >= l ? x : 0ull;
+  }
+  if (over <= left && left < with) *floor = l;
+}
+
 // The same threshold, over the tokens in play from `floor` up, by one histogram over the distance to the maximum; `even`:
 // that makes sense.  target_of: from the total weight.  Leaves what stays gathered (*gathered) if it is few enough.
 template <bool kMass, typename E, typename Target>
@@ -342,16 +361,7 @@ __device__ __forceinline__ float threshold(const Row<E>& row, const Weight& weig
       for (int i = tid; i < n; i += kThreads) sh.rank_w[i] = weight(sh.rank_l[i]);
       __syncthreads();
     }
-    for (int i = tid; i < n; i += kThreads) {
-      const float l = sh.rank_l[i];
-      unsigned long long over = 0, with = 0;
-      for (int j = 0; j < n; ++j) {
-        const unsigned long long w = kMass ? sh.rank_w[j] : 1ull;
-        over += sh.rank_l[j] > l ? w : 0ull;
-        with += sh.rank_l[j] >= l ? w : 0ull;
-      }
-      if (over <= left && left < with) sh.floor = l;             // exactly one value; its ties agree
-    }
+    for (int i = tid; i < n; i += kThreads) rank(sh.rank_l, kMass ? sh.rank_w : nullptr, n, sh.rank_l[i], left, &sh.floor);
     __syncthreads();
     floor = sh.floor;
   }
@@ -366,6 +376,105 @@ __device__ __forceinline__ float threshold(const Row<E>& row, const Weight& weig
     __syncthreads();
   }
   return floor;
+}
+
+// The nucleus without a gathered list, in one pass over the weights: a histogram of counts and of the places inside the steps
+// estimates each step's weight to about 1e-4 of itself, which leaves a band of few steps around the threshold.  The pass over
+// the exact weights then sums all tokens, those above the band and their groups, and gathers the band, whose tokens are
+// ranked among each other.  That the exact threshold lies in the band is checked with the exact sums: false where it does
+// not, or where the band is too full, and then the groups' sums and *count mean nothing.  least: tokens below it are not
+// drawn (min-p), though they count for the nucleus.
+template <typename E>
+__device__ __forceinline__ bool nucleus(const Row<E>& row, const Weight& weight, const SampleArgs& a, float* floor, float least,
+                                        float top_p, float T, float steps, int n_groups, uint32_t* count, Shared& sh) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const float from = *floor;
+  if (tid == 0) sh.n_list = 0;
+  clear_hist(sh);
+  each_kept(row, sh, false, from, [&](int, float l) {
+    const float d = (weight.m - l) * steps;
+    const int bin = min(kBins - 1, (int)d);
+    atomicAdd(&sh.hist.lo[bin], 1u);
+    atomicAdd(&sh.hist.hi[bin], (uint32_t)fminf((d - (float)bin) * 256.f, 255.f));
+  });
+  __syncthreads();
+  const float step = 1.f / (steps * T), per_step = 1.4426950f * step;   // nats, octaves
+  auto mass = [&](int i) {
+    const float n = (float)sh.hist.lo[i];
+    if (n == 0.f) return 0ull;
+    const float place = ((float)sh.hist.hi[i] / n + 0.5f) * (1.f / 256.f);
+    return (unsigned long long)(n * exp2f(32.f - ((float)i + place) * per_step));
+  };
+  // a step's estimate is off by step^2 / 24 (its weights are not all the mean place's), by step / 512 (the places' steps) and
+  // by what float rounds; taken a few times over
+  const float slack = 0.1f * step * step + 0.01f * step + 1e-5f;
+  find(sh, mass, [&](unsigned long long z) { return (unsigned long long)(fmaxf(top_p - slack, 0.f) * (double)z); });
+  const int first = sh.at;
+  __syncthreads();
+  find(sh, mass, [&](unsigned long long z) { return (unsigned long long)((double)(top_p + slack) * (double)z); });
+  const int last = sh.at < 0 ? kBins - 1 : sh.at;
+  __syncthreads();                                               // the histogram's place becomes the groups'
+  for (int i = n_groups + tid; i < kBins; i += kThreads) sh.group[i] = 0ull;
+  unsigned long long all = 0, above = 0;
+  for (int g = warp; g < n_groups; g += kThreads / 32) {
+    unsigned long long sum = 0;
+    const int end = min(a.V, (g + 1) << a.group_shift) / 4;
+    for (int i = ((g << a.group_shift) >> 2) + lane; i < end; i += 32) {
+      const float4 v = row.four(i);
+      const float l[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (l[q] >= from) {
+          const unsigned long long w = weight(l[q]);
+          const int bin = min(kBins - 1, (int)((weight.m - l[q]) * steps));
+          all += w;
+          if (bin < first) {
+            above += w;
+            if (l[q] >= least) {
+              sum += w;
+              ++*count;
+            }
+          } else if (bin <= last) {
+            const int at = atomicAdd(&sh.n_list, 1);
+            if (at < kRank) {
+              sh.list_l[at] = l[q];
+              sh.list_i[at] = 4 * i + q;
+            }
+          }
+        }
+    }
+    sum = warp_sum(sum);
+    if (lane == 0) sh.group[g] = sum;
+  }
+  all = warp_sum(all);
+  above = warp_sum(above);
+  if (lane == 0) {
+    sh.warp_sum[warp] = all;
+    sh.rank_w[warp] = above;
+  }
+  if (tid == 0) sh.floor = NAN;
+  __syncthreads();
+  all = warp_sum(sh.warp_sum[lane]);
+  above = warp_sum(sh.rank_w[lane]);
+  const int n = sh.n_list;
+  __syncthreads();
+  const unsigned long long target = nucleus_target(top_p, all);
+  if (first < 0 || n > kRank || above > target) return false;
+  const unsigned long long left = target - above;
+  for (int i = tid; i < n; i += kThreads) sh.rank_w[i] = weight(sh.list_l[i]);
+  __syncthreads();
+  for (int i = tid; i < n; i += kThreads) rank(sh.list_l, sh.rank_w, n, sh.list_l[i], left, &sh.floor);
+  __syncthreads();
+  const float x = sh.floor;
+  if (!(x == x)) return false;
+  *floor = fmaxf(x, least);
+  for (int i = tid; i < n; i += kThreads)
+    if (sh.list_l[i] >= *floor) {
+      uint32_t* word = reinterpret_cast<uint32_t*>(&sh.group[sh.list_i[i] >> a.group_shift]);
+      add_pair(word, word + 1, sh.rank_w[i]);
+      ++*count;
+    }
+  return true;
 }
 
 template <typename E>
@@ -461,27 +570,31 @@ __global__ void __launch_bounds__(kThreads, 1) k_sample(const SampleArgs a) {
   if (top_k > 0 && top_k < a.V)
     floor = threshold<false>(row, weight, &gathered, floor, even, steps,
                              [&](unsigned long long) { return (unsigned long long)top_k - 1ull; }, sh);
-  if (top_p < 1.f) {
-    // kept iff W(> x) < top_p z; for whole W: W(> x) <= ceil(top_p z) - 1
-    floor = threshold<true>(row, weight, &gathered, floor, even, steps,
-                            [&](unsigned long long z) {
-                              const double t = ceil((double)top_p * (double)z);
-                              return t < 1.0 ? 0ull : (unsigned long long)t - 1ull;
-                            },
-                            sh);
-  }
+  float least = floor;
   if (min_p > 0.f) {
     // w >= min_p  <=>  l >= m + T ln(min_p)
     const double bound = weight.md + (double)T * log(min((double)min_p, 1.0));
     const float f = (float)bound;
     const float up = (double)f >= bound ? f : nextafterf(f, INFINITY);
-    if (f > -INFINITY) floor = fmaxf(floor, fminf(up, m));
+    if (f > -INFINITY) least = fmaxf(least, fminf(up, m));
   }
-  // weight sums of groups of consecutive tokens: by the gathered tokens, or one warp per group
+  // weight sums of groups of consecutive tokens: with the nucleus, by the gathered tokens, or one warp per group
   const int n_groups = ((a.V - 1) >> a.group_shift) + 1;
   uint32_t count = 0;
+  bool summed = false;
+  if (top_p < 1.f) {
+    if (even && !gathered) {
+      summed = nucleus(row, weight, a, &floor, least, top_p, T, steps, n_groups, &count, sh);
+      if (!summed) count = 0;
+    }
+    if (!summed)
+      floor = threshold<true>(row, weight, &gathered, floor, even, steps,
+                              [&](unsigned long long z) { return nucleus_target(top_p, z); }, sh);
+  }
+  floor = fmaxf(floor, least);
   __syncthreads();                                               // the histogram's place becomes the groups'
-  if (gathered) {
+  if (summed) {
+  } else if (gathered) {
     for (int i = tid; i < kBins; i += kThreads) sh.group[i] = 0ull;
     __syncthreads();
     each_kept(row, sh, true, floor, [&](int i, float l) {
