@@ -79,6 +79,21 @@ def test_settings_per_row_and_rows_apart():
     ctx.close()
 
 
+@pytest.mark.parametrize("n", [149, 600, 4096, 4100])
+def test_many_rows_with_settings_of_their_own(n):
+    V = 96
+    rng = np.random.default_rng(n)
+    ctx = make_ctx(V)
+    logits = torch.from_numpy(cluster_logits(rng, n, V)).to(G.DEV)
+    u = rng.random(n).astype(np.float32)
+    kw = dict(T=rng.choice([0.0, 0.7, 1.0, 1.4], n).astype(np.float32), k=rng.choice([0, 1, 7, V], n).astype(np.int32),
+              p=rng.choice([0.5, 0.9, 1.0], n).astype(np.float32), mp=rng.choice([0.0, 0.05], n).astype(np.float32))
+    compare(logits, run(ctx, logits, u, **kw), u, **kw)
+    compare(logits, run(ctx, logits, u, p=kw["p"]), u, p=kw["p"])
+    compare(logits, run(ctx, logits, u, T=np.zeros(n, np.float32)), u, T=np.zeros(n, np.float32))
+    ctx.close()
+
+
 def test_every_token_gets_its_share():
     """Uniforms on a fine grid over one row: the counts are the kept probabilities."""
     V, n = 64, 4096
