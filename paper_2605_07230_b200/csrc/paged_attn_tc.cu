@@ -1,21 +1,26 @@
 // Causal attention of new tokens over a paged cache on the tensor cores (bf16): prompts and chunks.
 //
-// One persistent CTA per SM walks over work items: two blocks of up to 128 query rows of one (request, key head), a row
-// being (token, query head of the group), with all the key tiles (128 keys) that any of the rows sees.
-//   * warp 8 loads: every lane owns one box of a tile (32 / 64 / ... rows of one page and 64 elements), looks its page up one
-//     tile ahead and issues its own TMA copy; keys and values share one ring of five 32 KB stages;
-//   * warp 9 issues the products: S_w = Q_w K^T (128 x 128) and O_w += P_w V with P_w taken from tensor memory, block 0
-//     and block 1 in turn, so that one block's softmax runs beside the other's products;
-//   * warps 0-3 and 4-7: softmax of block 0 and block 1, one row per thread.  A row's scores come from tensor memory in
-//     one go, the weights 2^(s c - ref) go back as bf16 over the scores' own columns.  ref is the running maximum, raised
-//     only when a score passes it by more than 2^8: then the row's accumulator is rescaled in place (rare).
+// A work item is two blocks of up to 128 query rows of one (request, key head), a row being (token, query head of the group),
+// with all the key tiles (128 keys) that any of the rows sees.  One CTA an SM works through items that the hardware's block
+// scheduler hands out.
+//   * warp 8 loads: every lane owns one box of a tile (8 to 128 rows of one page and 64 elements), looks its page up one
+//     tile ahead and issues its own TMA copy; keys and values share a ring of four 32 KB stages;
+//   * warps 9 and 10 issue the products of block 0 and block 1, in halves of a tile: S_w = Q_w K^T (128 x 64) and
+//     O_w += P_w V with P_w taken from tensor memory.  A block has two halves of scores in tensor memory, so that the next
+//     scores are formed while the softmax works: 450 us for 8 prompts of 2480 tokens and 32 heads where whole tiles took
+//     591, although a product with 64 keys takes 53 cycles where one with 128 takes 64 (both operands in shared memory);
+//   * warps 0-3 and 4-7: softmax of block 0 and block 1, one row per thread.  The weights 2^(s c - ref) go back as bf16 over
+//     the scores' own columns.  ref starts as the first half's maximum and is raised one half late, when the sum of a half's
+//     weights passes 2^8: then the row's accumulator is rescaled in place (rare), and no maximum has to be taken.
+// What bounds it: the products take 0.5 million of 0.77 million cycles an SM there; the rest is the softmax's latency beside
+// them (exponentials: half of the special-function unit's time) and the start and end of 17 items.  896 TFLOP/s of 1709.
 // Weights are rounded to bf16 for the product (the tensor cores take both operands in one type, and the values are bf16);
 // the sums and accumulators stay fp32.
 // Rows of the last tile behind the request's last key hold whatever the page held before: their scores are masked, and
 // their values are set to zero in shared memory, since 0 x NaN would reach the sum.  A row whose result is not finite all
 // the same (a non-finite value at a key that another row of the block sees) is computed again by one warp from the keys
 // it sees alone.
-// Tensor bound for prompts; every wait is bounded (error word, normal teardown).
+// Every wait is bounded (error word, normal teardown).
 #include <type_traits>
 
 #include "paged.h"
@@ -30,6 +35,7 @@ constexpr int kThreads = 352;
 constexpr int kStages = 4;         // keys and values of two tiles
 constexpr float kLazy = 256.f;    // a sum of a half's weights from which the reference is raised
 constexpr float kFar = 0x1p96f;   // and from which the row is computed again
+
 template <int D>
 struct Cfg {
   static constexpr int kHalves = D / 64;                 // 64-element column blocks of a tile
@@ -267,8 +273,9 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       if (ok && items[w] > 0) ok = ptx::mbar_wait_short(&q_empty[w], (items[w] - 1) & 1u, abort_flag, err, wait_ns);
   } else if (warp >= 9) {
     // ---------------- products ----------------
-    // One lane issues.  Stages and halves are known at compile time (two tiles a turn), so that every descriptor is the base
-    // plus a constant: beside the softmax warps each instruction of this warp costs some ten cycles.
+    // One lane issues, a warp for each block: one warp for both took 800 us where two take 526.  Only the halves are known at
+    // compile time; with stages and blocks as constants too the code leaves the instruction cache (720 us), with rolled
+    // loops the issue is too slow (667 us).  Offsets go to the descriptors' low words alone (2 %).
     const uint32_t idesc_s = ptx::umma_idesc_bf16(128, kHalf);
     const uint32_t idesc_o = ptx::umma_idesc_bf16_b_mn(128, D);
     const uint64_t q_desc = ptx::umma_desc_sw128(q_addr), k_desc = ptx::umma_desc_sw128(ring),
@@ -278,9 +285,10 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) { return ok = ptx::mbar_wait_short(bar, parity & 1u, abort_flag, err, wait_ns); };
     const int w = warp - 9;
+    auto full = [](uint32_t lo, uint64_t d) { return (uint64_t)lo | (d & 0xffffffff00000000ull); };
     auto scores = [&](int b, int st) {
-      const uint32_t kl = (uint32_t)k_desc + st * (C::kTileBytes >> 4) + b * (kHalf * 128 >> 4), ql = (uint32_t)q_desc + w * (C::kTileBytes >> 4);
-      auto full = [](uint32_t lo, uint64_t d) { return (uint64_t)lo | (d & 0xffffffff00000000ull); };
+      const uint32_t kl = (uint32_t)k_desc + st * (C::kTileBytes >> 4) + b * (kHalf * 128 >> 4);
+      const uint32_t ql = (uint32_t)q_desc + w * (C::kTileBytes >> 4);
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
         const uint32_t off = ((ks >> 2) * (kTile * 128) + (ks & 3) * 32) >> 4;
@@ -289,7 +297,6 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     };
     auto outputs = [&](int b, int st, bool first) {
       const uint32_t vl = (uint32_t)v_desc + st * (C::kTileBytes >> 4) + b * (kHalf / 16) * (2048 >> 4);
-      auto full = [](uint32_t lo, uint64_t d) { return (uint64_t)lo | (d & 0xffffffff00000000ull); };
 #pragma unroll
       for (int ks = 0; ks < kHalf / 16; ++ks)
         ptx::umma_bf16_ts(tmem + 256 + w * 128, tmem + w * 128 + b * kHalf + ks * 8,
