@@ -468,12 +468,13 @@ int cascade_paged_append(cascade_ctx* ctx, const cascade_paged_cache* cache, int
  *     out[row,head,:] = sum_j softmax_j(softmax_scale * <q[row,head,:], k_j>) v_j ;   lse[row,head] = log sum_j exp(...)
  * Query head `head` reads kv head head / (Hq / Hkv).  A row that sees no key (kv_len smaller than its new tokens) gets
  * zeros and lse -inf.  What lies at keys a row does not see, NaN and infinities included, does not reach it.
- *   q [n_tok,Hq,D] elem, rows q_stride apart; out [n_tok,Hq,D] elem, dense; lse [n_tok,Hq] float or NULL
+ *   q [n_tok,Hq,D] elem, rows q_stride apart; out [n_tok,Hq,D] elem, dense, no part of q (CASCADE_ERR_INVALID_ARG);
+ *   lse [n_tok,Hq] float or NULL
  *   q_begin [n_req+1], kv_len [n_req] int32, DEVICE: as cascade_paged_tables leaves them.  Rows of q behind
  *   q_begin[n_req] are not read, the same rows of out and lse not written.
  *   max_q, max_kv: no request has more new tokens / keys than this (host bounds that launch sizes come from; a
  *   request beyond them is left out, CASCADE_ERR_BAD_PAGE).  1 <= n_req <= CASCADE_MAX_REQUESTS.
- *   Hq / Hkv <= 128 (CASCADE_ERR_UNSUPPORTED_SHAPE).
+ *   Hq / Hkv <= 128, max_kv <= 2^31 - 65536 (CASCADE_ERR_UNSUPPORTED_SHAPE).
  *   window >= 0 (0: none), sinks >= 0.  Softmax and accumulation are fp32. */
 int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* cache, int32_t n_req, int32_t n_tok, const void* q,
                        int64_t q_stride, const int32_t* q_begin, const int32_t* kv_len, int32_t max_q, int32_t max_kv,
@@ -497,7 +498,8 @@ int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* cache, int32
  *   temperature, top_p, min_p [n_rows] float, top_k [n_rows] int32, DEVICE, or NULL: 1 / off / off / off for all rows.
  *     Per row, off is top_k <= 0 or >= V, top_p >= 1 or NaN, min_p <= 0 or NaN; a NaN temperature counts as 0, +inf
  *     weighs all finite logits alike; min_p above 1 counts as 1.
- *   token_out [n_rows] int32; prob_out [n_rows] float or NULL; kept_out [n_rows] int32 or NULL.
+ *   token_out [n_rows] int32; prob_out [n_rows] float or NULL; kept_out [n_rows] int32 or NULL.  They overlap neither each
+ *   other nor an input (CASCADE_ERR_INVALID_ARG where two arrays are the same).
  * Weights are formed in 64 bits and summed in fixed point, so the draw does not depend on the order of additions. */
 int cascade_sample(cascade_ctx* ctx, const void* logits, int32_t logits_dtype, int64_t row_stride, int32_t n_rows,
                    const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,

@@ -3,6 +3,14 @@
 #include "paged_attn.cuh"
 
 constexpr int kMaxGroup = 128;  // query heads a key head: they share a row block
+constexpr int kMaxKeys = INT32_MAX - 65535;  // so that a key's index rounded up to a tile stays in 32 bits
+
+// Whether [out, out + out_bytes) meets one of `rows` rows of `width` bytes that start `stride` bytes apart.
+static bool meets_rows(const void* rows_at, int64_t rows, int64_t stride, int64_t width, const void* out, int64_t out_bytes) {
+  const int64_t d = (int64_t)(reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(rows_at));
+  const int64_t first = d < width ? 0 : (d - width) / stride + 1;   // the first row that ends behind where `out` starts
+  return first < rows && first * stride < d + out_bytes;
+}
 
 extern "C" int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* cache, int32_t n_req, int32_t n_tok,
                                   const void* q, int64_t q_stride, const int32_t* q_begin, const int32_t* kv_len,
@@ -18,7 +26,10 @@ extern "C" int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* c
   if (q_stride < (int64_t)sh.Hq * sh.D || q_stride * es % 16 != 0) return CASCADE_ERR_INVALID_ARG;
   if (((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15u) != 0 || (reinterpret_cast<uintptr_t>(lse) & 3u) != 0)
     return CASCADE_ERR_INVALID_ARG;
+  if (max_kv > kMaxKeys) return CASCADE_ERR_UNSUPPORTED_SHAPE;
   if (n_req > CASCADE_MAX_REQUESTS || sh.Hq / sh.Hkv > kMaxGroup) return CASCADE_ERR_UNSUPPORTED_SHAPE;
+  if (meets_rows(q, n_tok, q_stride * es, (int64_t)sh.Hq * sh.D * es, out, (int64_t)n_tok * sh.Hq * sh.D * es))
+    return CASCADE_ERR_INVALID_ARG;
   CASCADE_TRY(check_current_device(ctx));
   PagedAttnArgs a;
   a.n_req = n_req;

@@ -36,7 +36,7 @@ __device__ __forceinline__ bool load_request(const PagedAttnArgs& a, int r, Requ
 }
 
 // First key of the window of position x; a row sees [0, min(sinks, lo)) and [lo, x].
-__device__ __forceinline__ int window_begin(int x, int window) { return window == 0 ? 0 : max(0, x - window + 1); }
+__device__ __forceinline__ int window_begin(int x, int window) { return window == 0 || x < window ? 0 : x - window + 1; }
 
 __device__ __forceinline__ float load_elem(const float* p) { return *p; }
 __device__ __forceinline__ float load_elem(const __nv_bfloat16* p) { return __bfloat162float(*p); }

@@ -511,6 +511,42 @@ def test_prompt_into_the_dense_cache_then_tree():
     ctx.close()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q,kv", [([9, 4], [5, 0]), ([300], [290])])
+def test_rows_before_the_first_key_and_the_widest_window(dtype, q, kv):
+    """x - window + 1 of a row in front of the first key does not fit 32 bits."""
+    ctx = make_ctx(dtype, 2, 2, 64)
+    for window, sinks in ((2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31 - 2, 3), (4, 2 ** 31 - 1)):
+        c = Case(dtype, 2, 2, 64, 16, q, kv, seed=len(q))
+        c.run(ctx, window, sinks)
+        ctx.check()
+        c.check(window, sinks)
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_outputs_that_meet_the_queries_and_lengths_past_the_end_are_refused(dtype):
+    L = cb.lib()
+    ctx = make_ctx(dtype, 2, 2, 64)
+    es = 2 if dtype == "bf16" else 4
+    row, n = 128, 3                                       # rows of 128 elements, 400 elements apart
+    buf = torch.zeros(8192, dtype=DT[dtype], device=G.DEV)
+    idx = torch.zeros(64, dtype=torch.int32, device=G.DEV)
+    p, i = buf.data_ptr(), idx.data_ptr()
+    cache = cb.PagedCacheStruct(p + 6000 * es, p + 6000 * es, 8 * 128, 1, 8, i, 1)
+    def call(at, mk=0, stride=400, q=1000):
+        return L.cascade_paged_attn(ctx.handle, C.byref(cache), 1, n, p + q * es, stride, i, i, 1, mk, 0, 0, 1.0, p + at * es, None, None)
+    for at in (1000, 1000 - n * row + 8, 1000 + 400 * 2 + row - 8, 1000 + row, 1000 + 400, 1000 + 400 + row):
+        assert call(at) == cb.ERR_INVALID_ARG, at
+    for at in (1000 - n * row, 1000 + 400 * 2 + row, 4000):
+        assert call(at) == cb.OK, at
+    assert call(1000 + row, stride=row + n * row) == cb.OK      # between two rows
+    assert call(4000, mk=2 ** 31 - 65535) == cb.ERR_UNSUPPORTED_SHAPE
+    assert call(4000, mk=2 ** 31 - 65536) == cb.OK
+    ctx.check()
+    ctx.close()
+
+
 def test_refusals():
     L = cb.lib()
     ctx = make_ctx("bf16", 4, 2, 64)

@@ -208,3 +208,19 @@ def test_refusals():
     assert call(logits=p + 2, dt=cb.BF16) == cb.OK
     ctx.check()
     ctx.close()
+
+
+def test_arrays_that_are_the_same_are_refused():
+    L = cb.lib()
+    ctx = make_ctx(64)
+    b = torch.zeros(4096, device=G.DEV)
+    p = [b.data_ptr() + 1024 * i for i in range(9)]           # logits T k p mp u token prob kept
+    def call(a):
+        return L.cascade_sample(ctx.handle, a[0], cb.F32, 64, 2, *a[1:], None)
+    assert call(p) == cb.OK
+    for out in (6, 7, 8):
+        for other in range(9):
+            if other != out:
+                assert call([p[out] if i == other else x for i, x in enumerate(p)]) == cb.ERR_INVALID_ARG, (out, other)
+    ctx.check()
+    ctx.close()
