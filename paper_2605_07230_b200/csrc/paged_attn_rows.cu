@@ -8,6 +8,7 @@
 // give pairs of keys after one byte permute per register, and the weights turn with one 8 x 8 transpose per eight keys.
 // No shared memory and no barrier in the loop: the keys of the next 16 are requested as soon as the scores have used the
 // registers, the values as soon as the output has; with up to eight rows three CTAs fit an SM, 96 KB in flight.
+// 48 single tokens over 256 to 2880 keys, 32 heads of 128: 195 us, 6.66 TB/s; two over 385 keys: 8.2 us.
 // (The 5th-generation tensor cores want 128 rows and operands in shared memory; here they would multiply padding.)
 // Weights are 2^(s c - ref); ref is the running maximum, raised only when a score passes it by more than 2^8.  Weights are
 // rounded to bf16 for the product with the bf16 values, sums and accumulators stay fp32.
@@ -295,6 +296,8 @@ __global__ void __launch_bounds__(kThreads, kNb == 1 ? 3 : 2) k_paged_attn_rows(
 
 }  // namespace
 
+// 16 tokens, 32 key heads, 16 requests over 1000 to 2000 keys: 94 us here, 112 us in 128-row blocks on the 5th-generation
+// tensor cores; 4 tokens of 4 query heads a key head: 34 / 36 us, two such requests over 300 to 400 keys 9.4 / 12.7 us.
 bool paged_attn_rows_takes(const PagedAttnArgs& a) { return (long long)a.max_q * (a.Hq / a.Hkv) <= kRows && a.Hkv <= 65535; }
 
 int launch_paged_attn_rows(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_t s) {

