@@ -280,9 +280,10 @@ __device__ __forceinline__ void rank(const float* values, const unsigned long lo
 
 // The same threshold, over the tokens in play from `floor` up, by one histogram over the distance to the maximum; `even`:
 // that makes sense.  target_of: from the total weight.  Leaves what stays gathered (*gathered) if it is few enough.
+// clean: the histogram, its counters and (unless gathered) the list are empty.
 template <bool kMass, typename E, typename Target>
 __device__ __forceinline__ float threshold(const Row<E>& row, const Weight& weight, bool* gathered, float floor, bool even,
-                                           float steps, Target target_of, Shared& sh) {
+                                           float steps, Target target_of, bool clean, Shared& sh) {
   const int tid = threadIdx.x;
   auto bin_of = [&](float l) { return min(kBins - 1, (int)((weight.m - l) * steps)); };
   auto bins = [&](int i) { return ((unsigned long long)sh.hist.hi[i] << 32) | sh.hist.lo[i]; };
@@ -299,13 +300,15 @@ __device__ __forceinline__ float threshold(const Row<E>& row, const Weight& weig
     }
     return descend<kMass>(row, weight, *gathered, order_key(floor + 0.f), order_key(weight.m + 0.f), target_of(z), sh);
   }
-  if (tid == 0) {
-    sh.n_rank = 0;
-    sh.key_min = 0xffffffffu;
-    sh.key_max = 0u;
-    if (!*gathered) sh.n_list = 0;
+  if (!clean) {
+    if (tid == 0) {
+      sh.n_rank = 0;
+      sh.key_min = 0xffffffffu;
+      sh.key_max = 0u;
+      if (!*gathered) sh.n_list = 0;
+    }
+    clear_hist(sh);
   }
-  clear_hist(sh);
   each_kept(row, sh, *gathered, floor, [&](int, float l) {
     if (kMass) {
       if (l >= weight.zero) {
@@ -392,11 +395,13 @@ __device__ __forceinline__ float threshold(const Row<E>& row, const Weight& weig
 // drawn (min-p), though they count for the nucleus.
 template <typename E>
 __device__ __forceinline__ bool nucleus(const Row<E>& row, const Weight& weight, const SampleArgs& a, float* floor, float least,
-                                        float top_p, float T, float steps, int n_groups, uint32_t* count, Shared& sh) {
+                                        float top_p, float T, float steps, int n_groups, uint32_t* count, bool clean, Shared& sh) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const float from = *floor;
-  if (tid == 0) sh.n_list = 0;
-  clear_hist(sh);
+  if (!clean) {
+    if (tid == 0) sh.n_list = 0;
+    clear_hist(sh);
+  }
   each_kept(row, sh, false, from, [&](int, float l) {
     const float d = (weight.m - l) * steps;
     const int bin = min(kBins - 1, (int)d);
@@ -552,6 +557,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_sample(const SampleArgs a) {
   row.n_res = a.n_res;
   row.wide = (reinterpret_cast<uintptr_t>(row.g) & (4 * sizeof(E) - 1)) == 0;
   if (tid < 64) sh.table[tid] = exp2((double)tid / 64.0);
+  // for the first histogram, so that it need not wait
+  for (int i = tid; i < kBins; i += kThreads) sh.hist.lo[i] = sh.hist.hi[i] = 0u;
+  bool clean = true;
   // the row: largest logit and its first place, smallest that can be kept
   float m = -INFINITY, low = INFINITY;
   int best = INT_MAX;
@@ -592,7 +600,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_sample(const SampleArgs a) {
     sh.red_hi[warp] = m;
     sh.red_lo[warp] = low;
   }
-  if (tid == 0) sh.token = INT_MAX;
+  if (tid == 0) {
+    sh.token = INT_MAX;
+    sh.n_list = sh.n_rank = 0;
+    sh.key_min = 0xffffffffu;
+    sh.key_max = 0u;
+  }
   __syncthreads();
   m = warp_max(lane < kWarps ? sh.red_hi[lane] : -INFINITY);
   low = -warp_max(lane < kWarps ? -sh.red_lo[lane] : -INFINITY);
@@ -622,9 +635,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_sample(const SampleArgs a) {
   const float reach = fminf(m - low, kReach);
   const float steps = (float)(kBins - 1) / reach;
   const bool even = reach > 1e-30f && m < INFINITY;              // the histogram over distances makes sense
-  if (top_k > 0 && top_k < a.V)
+  if (top_k > 0 && top_k < a.V) {
     floor = threshold<false>(row, weight, &gathered, floor, even, steps,
-                             [&](unsigned long long) { return (unsigned long long)top_k - 1ull; }, sh);
+                             [&](unsigned long long) { return (unsigned long long)top_k - 1ull; }, clean, sh);
+    clean = false;
+  }
   float least = floor;
   if (min_p > 0.f) {
     // w >= min_p  <=>  l >= m + T ln(min_p)
@@ -639,12 +654,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_sample(const SampleArgs a) {
   bool summed = false;
   if (top_p < 1.f) {
     if (even && !gathered) {
-      summed = nucleus(row, weight, a, &floor, least, top_p, T, steps, n_groups, &count, sh);
+      summed = nucleus(row, weight, a, &floor, least, top_p, T, steps, n_groups, &count, clean, sh);
       if (!summed) count = 0;
+      clean = false;
     }
     if (!summed)
       floor = threshold<true>(row, weight, &gathered, floor, even, steps,
-                              [&](unsigned long long z) { return nucleus_target(top_p, z); }, sh);
+                              [&](unsigned long long z) { return nucleus_target(top_p, z); }, clean, sh);
   }
   floor = fmaxf(floor, least);
   __syncthreads();                                               // the histogram's place becomes the groups'
@@ -686,14 +702,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_sample(const SampleArgs a) {
   });
   if (warp != 0) return;
   const uint32_t n_kept = __reduce_add_sync(0xffffffffu, lane < kWarps ? sh.red_n[lane] : 0u);
-  // the token inside it; one warp
+  // the token inside it: one warp, four consecutive tokens a lane
   unsigned long long run = sh.before;
   const int g_hit = sh.at, end = min(a.V, (g_hit + 1) << a.group_shift);
-  for (int i0 = g_hit << a.group_shift; i0 < end; i0 += 32) {
-    const int i = i0 + lane;
-    const float l = i < end ? row.at(i) : -INFINITY;
-    const unsigned long long w = l >= floor ? weight(l) : 0ull;
-    unsigned long long c = w;
+  for (int i0 = g_hit << a.group_shift; i0 < end; i0 += 128) {
+    const int i = i0 + 4 * lane;
+    const float4 v = i < end ? row.four(i / 4) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    const float l[4] = {v.x, v.y, v.z, v.w};
+    unsigned long long w[4], mine = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      w[q] = l[q] >= floor ? weight(l[q]) : 0ull;
+      mine += w[q];
+    }
+    unsigned long long c = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const unsigned long long t = __shfl_up_sync(0xffffffffu, c, o);
@@ -702,8 +724,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_sample(const SampleArgs a) {
     const uint32_t hit = __ballot_sync(0xffffffffu, run + c > target);
     if (hit != 0u) {
       if (lane == __ffs(hit) - 1) {
-        a.token[r] = i;
-        if (a.prob != nullptr) a.prob[r] = (float)((double)w / (double)total);
+        unsigned long long at = run + c - mine;
+        bool found = false;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          at += w[q];
+          if (!found && at > target) {
+            found = true;
+            a.token[r] = i + q;
+            if (a.prob != nullptr) a.prob[r] = (float)((double)w[q] / (double)total);
+          }
+        }
         if (a.kept != nullptr) a.kept[r] = (int32_t)n_kept;
       }
       break;
