@@ -511,6 +511,40 @@ def test_prompt_into_the_dense_cache_then_tree():
     ctx.close()
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (70, 3)])
+def test_more_blocks_than_multiprocessors(window, sinks):
+    """32 key heads and requests of very different lengths: several hundred items, handed out one by one."""
+    ctx = make_ctx("bf16", 32, 32, 64)
+    c = Case("bf16", 32, 32, 64, 32, [17, 300, 1, 40, 0, 90, 33, 18, 20, 25], [400, 300, 700, 40, 9, 91, 64, 18, 500, 33], seed=5, pad=2)
+    for _ in range(2):
+        c.run(ctx, window, sinks)
+        ctx.check()
+        c.check(window, sinks)
+        c.out.fill_(3.0)
+        c.lse.fill_(3.0)
+    ctx.close()
+
+
+def test_two_contexts_at_once():
+    """Chunks and single tokens of two contexts on two streams, the calls of each in order, results as when alone."""
+    ctxs = [make_ctx("bf16", 16, 4, 128) for _ in range(2)]
+    cases = [[Case("bf16", 16, 4, 128, 16, [33, 60, 17], [200, 333, 17], seed=1), Case("bf16", 16, 4, 128, 16, [1, 1], [300, 41], seed=2)],
+             [Case("bf16", 16, 4, 128, 32, [130, 5], [130, 900], seed=3), Case("bf16", 16, 4, 128, 64, [2, 4], [77, 65], seed=4)]]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for ctx, mine, st in zip(ctxs, cases, streams):
+            with torch.cuda.stream(st):
+                for c in mine:
+                    cb.cascade_paged_attn(ctx, c.cache, c.q, c.q_begin, c.kv, max(c.q_len), max(c.kv_len), c.out, c.scale, lse=c.lse)
+    torch.cuda.synchronize()
+    for ctx, mine in zip(ctxs, cases):
+        ctx.check()
+        for c in mine:
+            c.check()
+        ctx.close()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("q,kv", [([9, 4], [5, 0]), ([300], [290])])
 def test_rows_before_the_first_key_and_the_widest_window(dtype, q, kv):

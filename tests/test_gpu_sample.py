@@ -79,6 +79,25 @@ def test_settings_per_row_and_rows_apart():
     ctx.close()
 
 
+@pytest.mark.parametrize("V", [4096, 16384, 65536])
+@pytest.mark.parametrize("T", [0.02, 1.0, 30.0])
+def test_nucleus_in_a_crowd(V, T):
+    """One logit far above thousands that nearly agree: the threshold's step, and the estimate's band, hold too many tokens."""
+    rng = np.random.default_rng(V)
+    ctx = make_ctx(V)
+    x = (1e-3 * rng.normal(size=(4, V))).astype(np.float32)
+    x[np.arange(4), rng.integers(0, V, 4)] = 30.0
+    x[2] = np.round(x[2] * 256) / 256                        # and ties
+    logits = torch.from_numpy(x).to(G.DEV)
+    u = rng.random(4).astype(np.float32)
+    for p in (0.3, 0.7):
+        kw = dict(T=np.full(4, T, np.float32), p=np.full(4, p, np.float32))
+        compare(logits, run(ctx, logits, u, **kw), u, **kw)
+        kw["k"] = np.full(4, 5000, np.int32)
+        compare(logits, run(ctx, logits, u, **kw), u, **kw)
+    ctx.close()
+
+
 @pytest.mark.parametrize("n", [149, 600, 4096, 4100])
 def test_many_rows_with_settings_of_their_own(n):
     V = 96
