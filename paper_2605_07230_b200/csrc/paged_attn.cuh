@@ -44,9 +44,11 @@ __device__ __forceinline__ void store_elem(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_elem(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }
 
 // One warp, one row and head, from the definition: only keys that the row sees are read, so that nothing else can reach
-// the result.  Lane l holds elements l, l + 32, ...; fp32 throughout.
+// the result.  Lane l holds elements l, l + 32, ...; fp32 throughout.  *alive takes the global timer
+// every 256 keys.
 template <typename E, int D>
-__device__ void attend_row(const PagedAttnArgs& a, int r, int row, int x, int head, int lane) {
+__device__ void attend_row(const PagedAttnArgs& a, int r, int row, int x, int head, int lane,
+                           volatile uint64_t* alive = nullptr) {
   constexpr int kE = D / 32;
   const int kh = head / (a.Hq / a.Hkv);
   const E* q = static_cast<const E*>(a.q) + (long long)row * a.q_stride + head * D;
@@ -61,6 +63,7 @@ __device__ void attend_row(const PagedAttnArgs& a, int r, int row, int x, int he
   float m = -INFINITY, l = 0.f;
   const float c = a.scale * kLog2e;
   for (int i = 0; i < n; ++i) {
+    if (alive != nullptr && i % 256 == 0) *alive = ptx::global_timer_ns();
     const int j = i < n_sink ? i : lo + (i - n_sink);
     const int page = a.block_table[(size_t)r * a.table_stride + j / a.page_size];
     if (page < 0 || page >= a.n_pages) {

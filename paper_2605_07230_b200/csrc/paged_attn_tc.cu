@@ -139,11 +139,13 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   __shared__ Queue queue;
   __shared__ uint32_t s_tmem_base;
   __shared__ int s_abort;
+  __shared__ uint64_t s_alive;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
   const uint32_t q_addr = smem_base, ring = smem_base + 2 * C::kTileBytes;
   volatile int* abort_flag = &s_abort;
+  volatile uint64_t* alive = &s_alive;   // (when a row was last computed again, see below)
   int* err = p.a.err;
   const uint64_t wait_ns = p.a.wait_ns;
 
@@ -167,6 +169,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       ptx::mbar_init(&queue.empty[i], kWarps);
     }
     s_abort = 0;
+    s_alive = 0;
     ptx::fence_mbar_init();
   }
   if (warp == 8 && lane == 0) {
@@ -188,7 +191,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   uint32_t turn = 0;                                            // items that this warp has taken
   auto ask = [&]() {                                            // for the item after this one
     const uint32_t slot = turn & 1u, use = turn >> 1;
-    if (use > 0 && !ptx::mbar_wait_short(&queue.empty[slot], (use - 1) & 1u, abort_flag, err, wait_ns)) return false;
+    if (use > 0 && !ptx::mbar_wait_short(&queue.empty[slot], (use - 1) & 1u, abort_flag, err, wait_ns, alive)) return false;
     ptx::mbar_arrive_expect_tx(&queue.full[slot], 16);
     ptx::take_block(&queue.answer[slot], &queue.full[slot]);
     return true;
@@ -196,7 +199,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   auto next = [&]() {                                           // the next item, -1 when there is none
     const uint32_t slot = turn & 1u, use = turn >> 1;
     ++turn;
-    const bool here = ptx::mbar_wait_short(&queue.full[slot], use & 1u, abort_flag, err, wait_ns);
+    const bool here = ptx::mbar_wait_short(&queue.full[slot], use & 1u, abort_flag, err, wait_ns, alive);
     int item = here ? ptx::taken_block(&queue.answer[slot]) : -1;
     ptx::fence_proxy_async_smem();                              // (the next answer comes through the async proxy)
     __syncwarp();
@@ -219,7 +222,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         if (it.n[w] == 0) continue;
-        if (items[w] > 0) ok = ok && ptx::mbar_wait_short(&q_empty[w], (items[w] - 1) & 1u, abort_flag, err, wait_ns);
+        if (items[w] > 0) ok = ok && ptx::mbar_wait_short(&q_empty[w], (items[w] - 1) & 1u, abort_flag, err, wait_ns, alive);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         ++items[w];
@@ -250,7 +253,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         const uint32_t bytes = box_bytes * (uint32_t)__popc(__ballot_sync(0xffffffffu, load));
         for (int kv = 0; kv < 2; ++kv) {
           const int stage = 2 * (i & 1) + kv;
-          ok = ptx::mbar_wait_short(&kv_empty[stage], ((ph >> (i & 1)) & 1u) ^ 1u, abort_flag, err, wait_ns);
+          ok = ptx::mbar_wait_short(&kv_empty[stage], ((ph >> (i & 1)) & 1u) ^ 1u, abort_flag, err, wait_ns, alive);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           if (lane == 0) ptx::mbar_arrive_expect_tx(&kv_full[stage], bytes);
@@ -267,10 +270,10 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     }
     // every stage and query tile has been given back before the CTA may end (the arrivals are asynchronous)
     for (int i = 0; ok && i < kStages; ++i)
-      ok = ptx::mbar_wait_short(&kv_empty[i], ((ph >> (i >> 1)) & 1u) ^ 1u, abort_flag, err, wait_ns);
+      ok = ptx::mbar_wait_short(&kv_empty[i], ((ph >> (i >> 1)) & 1u) ^ 1u, abort_flag, err, wait_ns, alive);
 #pragma unroll
     for (int w = 0; w < 2; ++w)
-      if (ok && items[w] > 0) ok = ptx::mbar_wait_short(&q_empty[w], (items[w] - 1) & 1u, abort_flag, err, wait_ns);
+      if (ok && items[w] > 0) ok = ptx::mbar_wait_short(&q_empty[w], (items[w] - 1) & 1u, abort_flag, err, wait_ns, alive);
   } else if (warp >= 9) {
     // ---------------- products ----------------
     // One lane issues, a warp for each block: one warp for both took 800 us where two take 526.  Only the halves are known at
@@ -283,7 +286,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     int used = 0;                              // items of the block so far
     uint32_t p_ph = 0, kv_ph = 0;              // bit b: parity of the next weights; bit j: of the next use of stages 2 j, 2 j + 1
     bool ok = true;
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return ok = ptx::mbar_wait_short(bar, parity & 1u, abort_flag, err, wait_ns); };
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return ok = ptx::mbar_wait_short(bar, parity & 1u, abort_flag, err, wait_ns, alive); };
     const int w = warp - 9;
     auto full = [](uint32_t lo, uint64_t d) { return (uint64_t)lo | (d & 0xffffffff00000000ull); };
     auto scores = [&](int b, int st) {
@@ -384,7 +387,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       for (int h = 0; h < n; ++h) {
         const int b = h & 1;
         const uint32_t t_h = t_s + b * kHalf;
-        ok = ptx::mbar_wait_short(&s_full[w][b], (s_ph >> b) & 1u, abort_flag, err, wait_ns);
+        ok = ptx::mbar_wait_short(&s_full[w][b], (s_ph >> b) & 1u, abort_flag, err, wait_ns, alive);
         const bool raise = next_ref > ref, none = ref == -INFINITY && waits_first;
         const bool special = !(h < h_end && (h >= h_begin || h < h_sink));
         s_ph ^= 1u << b;
@@ -402,7 +405,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
           if (__any_sync(0xffffffffu, raise)) {
             // once the product of the half before is done (the next commit on the other half's scores), the accumulator is
             // at rest
-            ok = ptx::mbar_wait_short(&s_full[w][b ^ 1], (s_ph >> (b ^ 1)) & 1u, abort_flag, err, wait_ns);
+            ok = ptx::mbar_wait_short(&s_full[w][b ^ 1], (s_ph >> (b ^ 1)) & 1u, abort_flag, err, wait_ns, alive);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             ptx::tc_fence_after();
@@ -477,7 +480,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         if (h >= h_kv) {
           const int j = (h / 2) & 1, st = 2 * j + 1;
           const uint32_t st_ph = (uint32_t)((j == 0 ? kv_used[0] : kv_used[1]) + h / 4) & 1u;
-          ok = ptx::mbar_wait_short(&kv_full[st], st_ph, abort_flag, err, wait_ns);
+          ok = ptx::mbar_wait_short(&kv_full[st], st_ph, abort_flag, err, wait_ns, alive);
           const int key = rr & (kHalf - 1);                    // two threads a key, each half of its values
           if (ok && k0 + key >= it.kv) {
             constexpr int kChunks = D / 16;
@@ -499,7 +502,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       kv_used[1] += it.n_tiles / 2;
       if (!ok) break;
       if (n > 1) {                               // the commit without scores, behind the last product but one
-        ok = ptx::mbar_wait_short(&s_full[w][n & 1], (s_ph >> (n & 1)) & 1u, abort_flag, err, wait_ns);
+        ok = ptx::mbar_wait_short(&s_full[w][n & 1], (s_ph >> (n & 1)) & 1u, abort_flag, err, wait_ns, alive);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         s_ph ^= 1u << (n & 1);
@@ -507,7 +510,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       // ---- the rows' results ----
       const int row = it.q0 + tok, head = it.head * p.G + my_g;
       if (n > 0) {
-        ok = ptx::mbar_wait_short(&o_full[w], used & 1u, abort_flag, err, wait_ns);
+        ok = ptx::mbar_wait_short(&o_full[w], used & 1u, abort_flag, err, wait_ns, alive);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         ptx::tc_fence_after();
@@ -563,10 +566,11 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       if (live && p.a.lse != nullptr)
         p.a.lse[(long long)row * p.a.Hq + head] = x >= 0 ? (ref + log2f(l)) * paged::kLn2 : -INFINITY;
       __syncwarp();
+      // (0.6 us a key and row: whoever waits for this warp meanwhile starts its limit anew with every 256 keys)
       for (uint32_t left = __ballot_sync(0xffffffffu, odd); left != 0u; left &= left - 1u) {
         const int who = __ffs(left) - 1;
         paged::attend_row<__nv_bfloat16, D>(p.a, it.r, __shfl_sync(0xffffffffu, row, who), __shfl_sync(0xffffffffu, x, who),
-                                            __shfl_sync(0xffffffffu, head, who), lane);
+                                            __shfl_sync(0xffffffffu, head, who), lane, alive);
       }
     }
   }

@@ -84,17 +84,19 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
   }
 }
 
-// The same, for waits that are short as a rule: the clock is first read after 256 failed polls.
+// The same, for waits that are short as a rule: the clock is first read after 256 failed polls.  *alive: when somebody who may
+// be waited for last went on with finite work of any length (global timer); the limit counts from there.
 __device__ __forceinline__ bool mbar_wait_short(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* err_word,
-                                                uint64_t limit_ns) {
+                                                uint64_t limit_ns, volatile uint64_t* alive) {
   uint64_t t0 = 0;
   for (uint32_t polls = 1;; ++polls) {
     if (mbar_try_wait(bar, parity)) return true;
     if ((polls & 255u) == 0) {
       if (*abort_flag) return false;
-      const uint64_t now = global_timer_ns();
+      const uint64_t now = global_timer_ns(), last = *alive;
       if (t0 == 0) t0 = now;
-      if (now - t0 > limit_ns) {
+      if (last > t0) t0 = last;
+      if ((int64_t)(now - t0) > (int64_t)limit_ns) {
         *abort_flag = 1;
         atomicOr(err_word, 1);
         return false;

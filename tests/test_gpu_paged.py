@@ -525,6 +525,32 @@ def test_more_blocks_than_multiprocessors(window, sinks):
     ctx.close()
 
 
+def test_rows_summed_again_hold_nobody_past_the_wait_limit():
+    """Every row meets a NaN and is computed again key by key, for much longer than the limit of the waits beside it."""
+    H, D, page, n_req, q, kv = 40, 64, 16, 4, 20, 3000
+    ctx = make_ctx("bf16", H, H, D)
+    ctx.set_wait_limit(2_000_000)
+    gen = torch.Generator(device=G.DEV)
+    gen.manual_seed(1)
+    pages = -(-kv // page)
+    pool = torch.randn((2, n_req * pages, page, H, D), device=G.DEV, generator=gen).to(torch.bfloat16)
+    pool[1, ::pages, 0] = float("nan")                       # the value of every request's first key
+    cache = cb.PagedCache(pool[0], pool[1], torch.arange(n_req * pages, dtype=torch.int32, device=G.DEV).view(n_req, pages))
+    x = torch.randn((n_req * q, H, D), device=G.DEV, generator=gen).to(torch.bfloat16)
+    out, lse = torch.zeros_like(x), torch.zeros((n_req * q, H), device=G.DEV)
+    begin, lens = i32(np.arange(n_req + 1) * q), i32([kv] * n_req)
+    cb.cascade_paged_attn(ctx, cache, x, begin, lens, q, kv, out, 0.125, lse=lse)
+    torch.cuda.synchronize()
+    ctx.check()
+    assert torch.isnan(out).all() and torch.isfinite(lse).all()
+    pool[1, ::pages, 0] = 1.0
+    cb.cascade_paged_attn(ctx, cache, x, begin, lens, q, kv, out, 0.125)
+    torch.cuda.synchronize()
+    ctx.check()
+    assert torch.isfinite(out).all()
+    ctx.close()
+
+
 def test_two_contexts_at_once():
     """Chunks and single tokens of two contexts on two streams, the calls of each in order, results as when alone."""
     ctxs = [make_ctx("bf16", 16, 4, 128) for _ in range(2)]
