@@ -1,8 +1,7 @@
 // Causal attention of new tokens over a paged cache on the tensor cores (bf16): prompts and chunks.
 //
 // A work item is two blocks of up to 128 query rows of one (request, key head), a row being (token, query head of the group),
-// with all the key tiles (128 keys) that any of the rows sees.  One CTA an SM works through items that the hardware's block
-// scheduler hands out.
+// with all the key tiles (128 keys) that any of the rows sees.  One CTA an SM works through items that a counter hands out.
 //   * warp 8 loads: every lane owns one box of a tile (8 to 128 rows of one page and 64 elements), looks its page up one
 //     tile ahead and issues its own TMA copy; keys and values share a ring of four 32 KB stages;
 //   * warps 9 and 10 issue the products of block 0 and block 1, in halves of a tile: S_w = Q_w K^T (128 x 64) and
@@ -47,6 +46,7 @@ struct Cfg {
 struct TcArgs {
   PagedAttnArgs a;
   int G, tpb, box_rows;           // query heads a key head; tokens per row block; rows of a page box
+  int* taken;                     // [0] items handed out beyond the blocks' own, [1] blocks that are done; zero between launches
 };
 
 // Items of the requests in order, Hkv x pairs of row blocks each; a whole warp walks forward through them, 32 requests
@@ -58,10 +58,12 @@ struct Cursor {
   __device__ __forceinline__ bool find(const TcArgs& p, int item, int lane, Item* it);
 };
 
-// The items that a CTA takes: its own index first, then those of blocks that have not started yet, one at a time
-// (the launch has a block per item).  The loading warp asks one item ahead; every warp reads the answers in turn.
+// The items that a CTA takes: its own index first, then what the launch's counter gives.  The loading warp asks one item
+// ahead; every warp reads the answers in turn.  (8 prompts of 2480 tokens: 507 us with a fixed share of items, 486 with the
+// counter.  A block per item and the hardware's own scheduler was as fast there, but took 0.8 ms for one chunk beside 511
+// requests without tokens.)
 struct Queue {
-  uint4 answer[2];
+  int answer[2];
   uint64_t full[2], empty[2];
 };
 constexpr int kWarps = kThreads / 32;
@@ -78,15 +80,15 @@ struct Item {
 };
 
 __device__ __forceinline__ bool Cursor::find(const TcArgs& p, int item, int lane, Item* it) {
-  if (item < 0) return false;
-  if (item < base) chunk = -32, base = total = 0;              // (the indexes grow as a rule)
   while (chunk < 0 || item >= base + total) {
     base += total;
     chunk += 32;
     if (chunk >= p.a.n_req) return false;
+    const int n_rows = p.a.q_begin[p.a.n_req];
     lane_items = 0;
     if (chunk + lane < p.a.n_req && paged::load_request(p.a, chunk + lane, &lane_rq))
       lane_items = p.a.Hkv * ((lane_rq.nq + 2 * p.tpb - 1) / (2 * p.tpb));
+    if (__shfl_sync(0xffffffffu, lane_rq.q0, 0) == n_rows) return false;   // no tokens from here on
     int inc = lane_items;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -186,22 +188,19 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   ptx::tc_fence_after();
   const uint32_t tmem = s_tmem_base;   // S of block w and half b at 128 w + 64 b; O0, O1 at 256, 384
 
+  if (blockIdx.x == gridDim.x - 1)                              // requests without tokens are checked here alone
+    for (int r = threadIdx.x; r < p.a.n_req; r += kThreads) {
+      paged::Request rq;
+      paged::load_request(p.a, r, &rq);
+    }
   Cursor cur;
   Item it;
   uint32_t turn = 0;                                            // items that this warp has taken
-  auto ask = [&]() {                                            // for the item after this one
-    const uint32_t slot = turn & 1u, use = turn >> 1;
-    if (use > 0 && !ptx::mbar_wait_short(&queue.empty[slot], (use - 1) & 1u, abort_flag, err, wait_ns, alive)) return false;
-    ptx::mbar_arrive_expect_tx(&queue.full[slot], 16);
-    ptx::take_block(&queue.answer[slot], &queue.full[slot]);
-    return true;
-  };
-  auto next = [&]() {                                           // the next item, -1 when there is none
+  auto next = [&]() {                                           // the next item
     const uint32_t slot = turn & 1u, use = turn >> 1;
     ++turn;
     const bool here = ptx::mbar_wait_short(&queue.full[slot], use & 1u, abort_flag, err, wait_ns, alive);
-    int item = here ? ptx::taken_block(&queue.answer[slot]) : -1;
-    ptx::fence_proxy_async_smem();                              // (the next answer comes through the async proxy)
+    const int item = here ? *static_cast<volatile int*>(&queue.answer[slot]) : INT_MAX;
     __syncwarp();
     if (lane == 0) ptx::mbar_arrive(&queue.empty[slot]);
     return __shfl_sync(0xffffffffu, item, 0);
@@ -216,9 +215,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     uint32_t ph = 0;                                            // bit j: parity of the next use of stages 2 j, 2 j + 1
     bool ok = true;
     for (int item = blockIdx.x; ok && cur.find(p, item, lane, &it); item = next()) {
-      if (lane == 0) ok = ask();
-      ok = __shfl_sync(0xffffffffu, ok, 0);
-      if (!ok) break;
+      const int granted = lane == 0 ? (int)gridDim.x + atomicAdd(p.taken, 1) : 0;   // (told at the end: the answer takes its time)
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         if (it.n[w] == 0) continue;
@@ -266,6 +263,14 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         page = next;
         row = next_row;
         wanted = next_wanted;
+      }
+      const uint32_t slot = turn & 1u, use = turn >> 1;
+      if (use > 0) ok = ok && ptx::mbar_wait_short(&queue.empty[slot], (use - 1) & 1u, abort_flag, err, wait_ns, alive);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      if (lane == 0) {
+        *static_cast<volatile int*>(&queue.answer[slot]) = granted;
+        ptx::mbar_arrive(&queue.full[slot]);
       }
     }
     // every stage and query tile has been given back before the CTA may end (the arrivals are asynchronous)
@@ -579,6 +584,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
+  if (threadIdx.x == 0 && atomicAdd(p.taken + 1, 1) == (int)gridDim.x - 1) p.taken[0] = p.taken[1] = 0;
   if (warp == 9) ptx::tmem_dealloc(tmem, 512);
 }
 
@@ -596,7 +602,8 @@ int launch(cascade_ctx* ctx, const TcArgs& p, int n_items, cudaStream_t s) {
   const CUtensorMap* mv = get_tmap_4d_bf16(ctx, a.v, dk, sk, bk);
   if (mq == nullptr || mk == nullptr || mv == nullptr) return CASCADE_ERR_CUDA;
   CASCADE_TRY(configure_smem(ctx, PAGED_CFG_ATTN_TC, k_paged_attn_tc<D>, Cfg<D>::kSmem));   // (a context has one D)
-  k_paged_attn_tc<D><<<n_items, kThreads, Cfg<D>::kSmem, s>>>(*mq, *mk, *mv, p);
+  const int grid = n_items < ctx->sm_count ? n_items : ctx->sm_count;
+  k_paged_attn_tc<D><<<grid, kThreads, Cfg<D>::kSmem, s>>>(*mq, *mk, *mv, p);
   CASCADE_CUDA_TRY(cudaGetLastError());
   return CASCADE_OK;
 }
@@ -614,7 +621,8 @@ int launch_paged_attn_tc(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_t 
   const long long pairs = (long long)a.n_tok / (2 * p.tpb) + a.n_req;
   const long long by_length = (long long)a.n_req * ((a.max_q + 2 * p.tpb - 1) / (2 * p.tpb));
   const long long items = (pairs < by_length ? pairs : by_length) * a.Hkv;
-  if (items > INT_MAX) return CASCADE_ERR_UNSUPPORTED_SHAPE;
+  if (items > INT_MAX / 2) return CASCADE_ERR_UNSUPPORTED_SHAPE;
   const int n_items = (int)items;
+  p.taken = ctx->dev_error + 32;   // (cleared with the error word when the context is made; a line of its own)
   return ctx->shape.D == 128 ? launch<128>(ctx, p, n_items, s) : launch<64>(ctx, p, n_items, s);
 }

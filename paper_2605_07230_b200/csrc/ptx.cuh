@@ -451,28 +451,6 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-// Takes over a block of this launch that has not started: the answer (16 bytes) arrives at `answer`, counted by `bar`.  Not to
-// be asked again after an answer without a block.
-__device__ __forceinline__ void take_block(void* answer, uint64_t* bar) {
-  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
-                   smem_u32(answer)),
-               "r"(smem_u32(bar))
-               : "memory");
-}
-// The block's index along x, or -1.
-__device__ __forceinline__ int taken_block(const void* answer) {
-  int x;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 lo, hi;\n\t.reg .b128 a;\n\t"
-      "ld.shared.v2.b64 {lo, hi}, [%1];\n\tmov.b128 a, {lo, hi};\n\t"
-      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n\tmov.s32 %0, -1;\n\t"
-      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, a;\n\t}"
-      : "=r"(x)
-      : "r"(smem_u32(answer))
-      : "memory");
-  return x;
-}
-
 __device__ __forceinline__ void named_bar_sync(int id, int nthreads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
 }

@@ -525,6 +525,27 @@ def test_more_blocks_than_multiprocessors(window, sinks):
     ctx.close()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("live", [{0: (20, 25)}, {40: (33, 70), 41: (1, 9), 95: (150, 150)}, {299: (40, 41)}, {}])
+def test_padded_batch(dtype, live):
+    """300 places, most of them without new tokens; one of those with a length out of bounds is reported all the same."""
+    ctx = make_ctx(dtype, 4, 2, 64)
+    q = [live.get(r, (0, 0))[0] for r in range(300)]
+    kv = [live.get(r, (0, 3 * (r % 2)))[1] for r in range(300)]
+    c = Case(dtype, 4, 2, 64, 8, q, kv, seed=3, pad=2)
+    for _ in range(2):
+        c.run(ctx, max_q=150, max_kv=200)
+        ctx.check()
+        c.check()
+    c.kv[7 if 7 not in live else 8] = 10 ** 6
+    c.run(ctx, max_q=150, max_kv=200)
+    with pytest.raises(cb.CascadeError) as e:
+        ctx.check()
+    assert e.value.status == cb.ERR_BAD_PAGE
+    c.check(requests=list(live))
+    ctx.close()
+
+
 def test_rows_summed_again_hold_nobody_past_the_wait_limit():
     """Every row meets a NaN and is computed again key by key, for much longer than the limit of the waits beside it."""
     H, D, page, n_req, q, kv = 40, 64, 16, 4, 20, 3000
