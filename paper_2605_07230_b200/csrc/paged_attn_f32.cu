@@ -57,11 +57,12 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) k_paged_attn_f32(co
   const PagedAttnArgs& a = p.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int split_i = blockIdx.x, kh = blockIdx.y / p.n_rb, rb = blockIdx.y % p.n_rb, r = blockIdx.z;
-  if (p.splits > 1) ptx::cluster_arrive();       // (waited for in merge_and_store)
   paged::Request rq;
   const bool valid = paged::load_request(a, r, &rq);
   const int row0 = rb * kBlock;
   const int rows = valid ? max(0, min(kBlock, rq.nq * p.G - row0)) : 0;
+  if (rows == 0) return;                         // (the same in all CTAs of a cluster)
+  if (p.splits > 1) ptx::cluster_arrive();       // (waited for in merge_and_store)
   const int w_row = kByRow ? warp * kRows : 0;                       // this warp's first row of the block
   const int w_rows = max(0, min(kRows, rows - w_row));
   const int x0 = rq.kv - rq.nq;                                      // position of the request's first new token

@@ -76,6 +76,7 @@ __global__ void __launch_bounds__(kThreads, kNb == 1 ? 3 : 2) k_paged_attn_rows(
   const bool valid = paged::load_request(a, r, &rq);
   const int rows = valid ? rq.nq * p.G : 0;      // at most 8 kNb
   const int x0 = rq.kv - rq.nq;                  // position of the first new token
+  if (rows == 0) return;                         // (the same in all CTAs of a cluster)
   if (p.splits > 1) ptx::cluster_arrive();       // (waited for in merge_and_store)
 
   // 16-key steps that any row sees: [0, n_sink) and [n_sink + skip, ...)
