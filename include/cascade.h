@@ -468,6 +468,8 @@ int cascade_paged_append(cascade_ctx* ctx, const cascade_paged_cache* cache, int
  *     out[row,head,:] = sum_j softmax_j(softmax_scale * <q[row,head,:], k_j>) v_j ;   lse[row,head] = log sum_j exp(...)
  * Query head `head` reads kv head head / (Hq / Hkv).  A row that sees no key (kv_len smaller than its new tokens) gets
  * zeros and lse -inf.  What lies at keys a row does not see, NaN and infinities included, does not reach it.
+ * Keys of a page outside the pool count as not seen (CASCADE_ERR_BAD_PAGE): rows that would have seen one, and rows beside
+ * them, are summed again key by key, which takes long.
  *   q [n_tok,Hq,D] elem, rows q_stride apart; out [n_tok,Hq,D] elem, dense, no part of q (CASCADE_ERR_INVALID_ARG);
  *   lse [n_tok,Hq] float or NULL
  *   q_begin [n_req+1], kv_len [n_req] int32, DEVICE: as cascade_paged_tables leaves them.  Rows of q behind

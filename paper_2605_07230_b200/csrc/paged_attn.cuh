@@ -128,8 +128,8 @@ __host__ __device__ constexpr int part_floats(int D, int parts, int rows) { retu
 
 // Ends such a kernel: merges the CTA's `kParts` partial results of rows row0 .. row0 + rows - 1 (row = token * G + query head
 // of the group; x0 = position of the request's first new token) and sends every row to the CTA of the cluster that finishes
-// it (row % splits), which stores outputs and lse and computes a row whose result is not finite again from the keys it sees
-// alone.  max_rows: rows per part in s_part (part_floats(D, kParts, max_rows) floats), at most kMaxRows (<= 32).  splits <= 8.
+// it (row % splits), which stores outputs and lse and computes a row whose result is not finite, or whose sum is no number
+// because a page was not there, again from the keys it sees alone.  max_rows: rows per part in s_part (part_floats(D, kParts, max_rows) floats), at most kMaxRows (<= 32).  splits <= 8.
 // Every thread of every CTA of the cluster calls it, having arrived at the cluster's barrier (splits > 1) without waiting,
 // with the partial results written but no barrier behind them yet.
 template <typename E, int D, int kParts, int kMaxRows>

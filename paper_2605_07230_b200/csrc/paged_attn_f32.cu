@@ -54,6 +54,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) k_paged_attn_f32(co
   constexpr int kStep = kByRow ? 1 : kWarps;
   constexpr int kBlock = kByRow ? kWarps * kRows : kRows;
   __shared__ __align__(16) float s_part[paged::part_floats(D, 1, kWarps * kRows)];   // (no fewer than kWarps parts of kRows need)
+  __shared__ bool s_lost[kWarps];                // the warp met a page outside the pool
   const PagedAttnArgs& a = p.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int split_i = blockIdx.x, kh = blockIdx.y / p.n_rb, rb = blockIdx.y % p.n_rb, r = blockIdx.z;
@@ -63,6 +64,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) k_paged_attn_f32(co
   const int rows = valid ? max(0, min(kBlock, rq.nq * p.G - row0)) : 0;
   if (rows == 0) return;                         // (the same in all CTAs of a cluster)
   if (p.splits > 1) ptx::cluster_arrive();       // (waited for in merge_and_store)
+  if (lane == 0) s_lost[warp] = false;
   const int w_row = kByRow ? warp * kRows : 0;                       // this warp's first row of the block
   const int w_rows = max(0, min(kRows, rows - w_row));
   const int x0 = rq.kv - rq.nq;                                      // position of the request's first new token
@@ -112,7 +114,10 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) k_paged_attn_f32(co
     const int pi = p.div.page(key);
     const int page = table[pi];
     if (page < 0 || page >= a.n_pages) {
-      if (lane == 0) atomicOr(a.err, CASCADE_DEV_ERR_BAD_PAGE);
+      if (lane == 0) {
+        atomicOr(a.err, CASCADE_DEV_ERR_BAD_PAGE);
+        s_lost[warp] = true;
+      }
       return -1;
     }
     return (long long)page * a.page_stride + (long long)(key - pi * a.page_size) * row_elems;
@@ -270,6 +275,9 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) k_paged_attn_f32(co
   }
 
   // ---- partial results: [warp][row] with keys shared out, [row of the block] with rows shared out ----
+  // (keys of a lost page went in as zeros: a sum that is no number has the rows computed again without them)
+  __syncwarp();
+  const bool lost = s_lost[warp];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
 #pragma unroll
@@ -284,7 +292,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) k_paged_attn_f32(co
               make_float4(o[4 * jj][2 * half + i], o[4 * jj + 1][2 * half + i], o[4 * jj + 2][2 * half + i], o[4 * jj + 3][2 * half + i]);
       if (g == 0) {
         x[D] = ref[i];
-        x[D + 1] = l[i];
+        x[D + 1] = lost ? NAN : l[i];
       }
     }
   }

@@ -52,6 +52,7 @@ __global__ void __launch_bounds__(kThreads, kNb == 1 ? 3 : 2) k_paged_attn_rows(
   constexpr int kO = D / 16;                     // output products
   constexpr int kX = paged::part_stride(D);
   extern __shared__ __align__(16) float s_part[];  // [warp][row][kX], as many rows as the call has at most
+  __shared__ bool s_lost[kWarps];                // the warp met a page outside the pool
   const PagedAttnArgs& a = p.a;
   const int part = p.max_rows * kX;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -78,6 +79,7 @@ __global__ void __launch_bounds__(kThreads, kNb == 1 ? 3 : 2) k_paged_attn_rows(
   const int x0 = rq.kv - rq.nq;                  // position of the first new token
   if (rows == 0) return;                         // (the same in all CTAs of a cluster)
   if (p.splits > 1) ptx::cluster_arrive();       // (waited for in merge_and_store)
+  if (lane == 0) s_lost[warp] = false;
 
   // 16-key steps that any row sees: [0, n_sink) and [n_sink + skip, ...)
   int n = 0, n_sink = 0, skip = 0;
@@ -127,7 +129,10 @@ __global__ void __launch_bounds__(kThreads, kNb == 1 ? 3 : 2) k_paged_attn_rows(
     const int pi = p.div.page(key);
     const int page = table[pi];
     if (page < 0 || page >= a.n_pages) {
-      if (lane == 0) atomicOr(a.err, CASCADE_DEV_ERR_BAD_PAGE);
+      if (lane == 0) {
+        atomicOr(a.err, CASCADE_DEV_ERR_BAD_PAGE);
+        s_lost[warp] = true;
+      }
       return -1;
     }
     return (long long)page * a.page_stride + (long long)(key - pi * a.page_size) * row_elems;
@@ -266,6 +271,9 @@ __global__ void __launch_bounds__(kThreads, kNb == 1 ? 3 : 2) k_paged_attn_rows(
   }
 
   // ---- the warps' partial results -> one per CTA (in place of the first) -> one per cluster ----
+  // (keys of a lost page went in as zeros: a sum that is no number has the rows computed again without them)
+  __syncwarp();
+  const bool lost = s_lost[warp];
 #pragma unroll
   for (int b = 0; b < kNb; ++b)
 #pragma unroll
@@ -288,7 +296,7 @@ __global__ void __launch_bounds__(kThreads, kNb == 1 ? 3 : 2) k_paged_attn_rows(
         }
         if (g == 0) {
           x[D] = ref[b][i];
-          x[D + 1] = l[b][i];
+          x[D + 1] = lost ? NAN : l[b][i];
         }
       }
     }

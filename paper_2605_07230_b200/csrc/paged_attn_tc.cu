@@ -17,8 +17,8 @@
 // the sums and accumulators stay fp32.
 // Rows of the last tile behind the request's last key hold whatever the page held before: their scores are masked, and
 // their values are set to zero in shared memory, since 0 x NaN would reach the sum.  A row whose result is not finite all
-// the same (a non-finite value at a key that another row of the block sees) is computed again by one warp from the keys
-// it sees alone.
+// the same (a non-finite value at a key that another row of the block sees), and every row of an item that met a page
+// outside the pool, is computed again by one warp from the keys it sees alone.
 // Every wait is bounded (error word, normal teardown).
 #include <type_traits>
 
@@ -64,6 +64,7 @@ struct Cursor {
 // chunk beside 511 requests without tokens, the counter 18 us.)
 struct Queue {
   int answer[2];
+  bool lost[2];               // the item before met a page outside the pool
   uint64_t full[2], empty[2];
 };
 constexpr int kWarps = kThreads / 32;
@@ -196,11 +197,13 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   Cursor cur;
   Item it;
   uint32_t turn = 0;                                            // items that this warp has taken
+  bool lost = false;                                            // the item that was left for this one met a bad page
   auto next = [&]() {                                           // the next item
     const uint32_t slot = turn & 1u, use = turn >> 1;
     ++turn;
     const bool here = ptx::mbar_wait_short(&queue.full[slot], use & 1u, abort_flag, err, wait_ns, alive);
     const int item = here ? *static_cast<volatile int*>(&queue.answer[slot]) : INT_MAX;
+    lost = here && *static_cast<volatile bool*>(&queue.lost[slot]);
     __syncwarp();
     if (lane == 0) ptx::mbar_arrive(&queue.empty[slot]);
     return __shfl_sync(0xffffffffu, item, 0);
@@ -215,6 +218,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     uint32_t ph = 0;                                            // bit j: parity of the next use of stages 2 j, 2 j + 1
     bool ok = true;
     for (int item = blockIdx.x; ok && cur.find(p, item, lane, &it); item = next()) {
+      bool met_bad = false;
       const int granted = lane == 0 ? (int)gridDim.x + atomicAdd(p.taken, 1) : 0;   // (told at the end: the answer takes its time)
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
@@ -246,7 +250,10 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
           next_wanted = has_box && it.tile(i + 1) * kTile + box_i * p.box_rows < it.kv;
         }
         const bool load = wanted && page >= 0 && page < p.a.n_pages;
-        if (wanted && !load) atomicOr(err, CASCADE_DEV_ERR_BAD_PAGE);
+        if (wanted && !load) {
+          atomicOr(err, CASCADE_DEV_ERR_BAD_PAGE);
+          met_bad = true;                                       // (its place keeps what it held: the rows are computed again)
+        }
         const uint32_t bytes = box_bytes * (uint32_t)__popc(__ballot_sync(0xffffffffu, load));
         for (int kv = 0; kv < 2; ++kv) {
           const int stage = 2 * (i & 1) + kv;
@@ -268,8 +275,10 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       if (use > 0) ok = ok && ptx::mbar_wait_short(&queue.empty[slot], (use - 1) & 1u, abort_flag, err, wait_ns, alive);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
+      met_bad = __any_sync(0xffffffffu, met_bad);
       if (lane == 0) {
         *static_cast<volatile int*>(&queue.answer[slot]) = granted;
+        *static_cast<volatile bool*>(&queue.lost[slot]) = met_bad;
         ptx::mbar_arrive(&queue.full[slot]);
       }
     }
@@ -372,7 +381,7 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     int used = 0, kv_used[2] = {0, 0};                         // items of this block; tiles of all items by the stages they used
     uint32_t s_ph = 0;                                         // bit b: parity of the next scores of half b
     bool ok = true;
-    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &it); item = next()) {
+    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &it);) {
       const int tok = it.first(w) + my_tok;
       const bool live = in_block && tok < it.nq;
       // position (below 0: sees nothing); a place without a row sees everything, which spares its warp the masks
@@ -571,6 +580,9 @@ k_paged_attn_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       if (live && p.a.lse != nullptr)
         p.a.lse[(long long)row * p.a.Hq + head] = x >= 0 ? (ref + log2f(l)) * paged::kLn2 : -INFINITY;
       __syncwarp();
+      // the answer for the next item tells whether this one's keys were all there: the loads ended long ago
+      item = next();
+      odd = odd || (lost && live && x >= 0);
       // (0.6 us a key and row: whoever waits for this warp meanwhile starts its limit anew with every 256 keys)
       for (uint32_t left = __ballot_sync(0xffffffffu, odd); left != 0u; left &= left - 1u) {
         const int who = __ffs(left) - 1;
