@@ -412,7 +412,9 @@ int cascade_filter_logits(cascade_ctx* ctx, float* logits, int32_t n_rows, int32
  *              (page_stride >= page_size*Hkv*D; larger where keys and values of a page lie side by side in one pool);
  *              16-byte aligned, page_stride a multiple of 16 bytes
  *   page_size  a multiple of 8; n_pages * page_size < 2^31
- *   block_table [n_req,table_stride] int32, DEVICE.  Entries behind a request's last page are never used.
+ *   block_table [n_req,table_width] int32, DEVICE, rows table_stride entries apart.  Entries behind a request's last page
+ *              are never used, nor is anything between two rows
+ *   table_width at most table_stride; 0: table_stride
  * Device-resident lengths, pages and slots cannot be checked on the host.  A kernel that meets one outside its range
  * leaves it out, touches nothing outside the buffers it was given, and cascade_check returns CASCADE_ERR_BAD_PAGE.
  * All four calls allocate nothing, take their sizes from host arguments alone and can be recorded into a CUDA graph.
@@ -423,7 +425,7 @@ typedef struct {
   int64_t page_stride;
   int32_t n_pages, page_size;
   const int32_t* block_table;
-  int32_t table_stride;
+  int32_t table_stride, table_width;
 } cascade_paged_cache;
 
 /* Block tables and slot map of the next pass, from the requests' lengths, in one kernel.

@@ -69,7 +69,7 @@ class Step(C.Structure):
 
 class PagedCacheStruct(C.Structure):
     _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_stride", C.c_int64), ("n_pages", C.c_int32),
-                ("page_size", C.c_int32), ("block_table", C.c_void_p), ("table_stride", C.c_int32)]
+                ("page_size", C.c_int32), ("block_table", C.c_void_p), ("table_stride", C.c_int32), ("table_width", C.c_int32)]
 
 
 _lib = None
@@ -435,9 +435,10 @@ class PagedCache:
         self.k_pages, self.v_pages, self.block_table = k_pages, v_pages, block_table
         self.dtype, self.heads, self.n_req = k_pages.dtype, (Hkv, D), block_table.shape[0]
         stride = k_pages.stride(0) if n_pages > 1 else page * Hkv * D
-        width = block_table.shape[1] if self.n_req == 1 else block_table.stride(0)
+        width = block_table.shape[1]                  # rows may lie further apart (columns of a wider table)
+        row = width if self.n_req == 1 or width == 0 else block_table.stride(0)
         self.struct = PagedCacheStruct(k_pages.data_ptr(), v_pages.data_ptr(), stride, n_pages, page,
-                                       block_table.data_ptr(), width)
+                                       block_table.data_ptr(), row, min(width, row))
         self.ref = C.byref(self.struct)
 
     def _check(self, ctx):

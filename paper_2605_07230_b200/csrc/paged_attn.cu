@@ -21,6 +21,7 @@ extern "C" int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* c
   const cascade_shape& sh = ctx->shape;
   const int es = sh.dtype == CASCADE_BF16 ? 2 : 4;
   if (cache->block_table == nullptr || cache->table_stride < 1) return CASCADE_ERR_INVALID_ARG;
+  if (cache->table_width < 0 || cache->table_width > cache->table_stride) return CASCADE_ERR_INVALID_ARG;
   if (n_req < 1 || n_tok < 1 || max_q < 1 || max_kv < 0 || window < 0 || sinks < 0) return CASCADE_ERR_INVALID_ARG;
   if (!(softmax_scale > 0.f) || softmax_scale > 3e38f) return CASCADE_ERR_INVALID_ARG;
   if (q_stride < (int64_t)sh.Hq * sh.D || q_stride * es % 16 != 0) return CASCADE_ERR_INVALID_ARG;
@@ -39,6 +40,7 @@ extern "C" int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* c
   a.page_size = cache->page_size;
   a.n_pages = cache->n_pages;
   a.table_stride = cache->table_stride;
+  a.table_width = cache->table_width == 0 ? cache->table_stride : cache->table_width;
   a.max_q = max_q < n_tok ? max_q : n_tok;
   a.max_kv = max_kv;
   a.window = window;

@@ -4,7 +4,7 @@
 #include "ptx.cuh"
 
 struct PagedAttnArgs {
-  int n_req, n_tok, Hq, Hkv, page_size, n_pages, table_stride, max_q, max_kv, window, sinks;
+  int n_req, n_tok, Hq, Hkv, page_size, n_pages, table_stride, table_width, max_q, max_kv, window, sinks;
   long long page_stride, q_stride;
   const void *q, *k, *v;
   void* out;
@@ -30,7 +30,7 @@ __device__ __forceinline__ bool load_request(const PagedAttnArgs& a, int r, Requ
   q->nq = e - b;
   q->kv = kv;
   const bool ok = b >= 0 && e >= b && e <= a.n_tok && e - b <= a.max_q && kv >= 0 && kv <= a.max_kv &&
-                  kv <= (long long)a.table_stride * a.page_size;
+                  kv <= (long long)a.table_width * a.page_size;
   if (!ok) atomicOr(a.err, CASCADE_DEV_ERR_BAD_PAGE);
   return ok;
 }
