@@ -378,8 +378,8 @@ int cascade_paged_tables(cascade_ctx* ctx, int32_t n_req, int32_t n_tok, int32_t
   a.err = ctx->dev_error;
   a.div = paged::page_div(page_size);
   const size_t smem = (size_t)(4 * n_req + 1) * sizeof(int);
-  if (smem > 48 * 1024)
-    CASCADE_TRY(configure_smem(ctx, PAGED_CFG_TABLES, k_paged_tables, (4 * CASCADE_MAX_REQUESTS + 1) * (int)sizeof(int)));
+  // (for every count: what a kernel gets unasked, 48 KB, has to hold its static arrays too)
+  CASCADE_TRY(configure_smem(ctx, PAGED_CFG_TABLES, k_paged_tables, (4 * CASCADE_MAX_REQUESTS + 1) * (int)sizeof(int)));
   // one CTA for few (2048 tokens of 32 requests: 6.0 us, 6.1 with a cluster of eight), then a cluster of eight (4096 of 64:
   // 6.6 us, 7.1 with one CTA; 256 requests of a token: 6.7 us, 9.2)
   const int n_cta = n_tok <= 2 * kTabThreads && n_req <= 32 ? 1 : 8;
