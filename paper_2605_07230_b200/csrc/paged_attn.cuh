@@ -61,6 +61,7 @@ __device__ void attend_row(const PagedAttnArgs& a, int r, int row, int x, int he
   const int lo = window_begin(x, a.window), n_sink = min(a.sinks, lo);
   const int n = x < 0 ? 0 : n_sink + (x - lo + 1);
   float m = -INFINITY, l = 0.f;
+  bool met = false;                              // a key, whatever its score
   const float c = a.scale * kLog2e;
   for (int i = 0; i < n; ++i) {
     if (alive != nullptr && i % 256 == 0) *alive = ptx::global_timer_ns();
@@ -82,13 +83,16 @@ __device__ void attend_row(const PagedAttnArgs& a, int r, int row, int x, int he
 #pragma unroll
     for (int w = 16; w > 0; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
     s *= c;
+    met = true;
     const float m_new = fmaxf(m, s);
-    const float corr = m == m_new ? 1.f : exp2f(m - m_new), p = exp2f(s - m_new);
+    // (a score of -inf weighs nothing, the first ones too, whose reference is not finite yet)
+    const float corr = m == m_new ? 1.f : exp2f(m - m_new), p = s == -INFINITY ? 0.f : exp2f(s - m_new);
     l = l * corr + p;
 #pragma unroll
     for (int e = 0; e < kE; ++e) o[e] = o[e] * corr + p * vv[e];
     m = m_new;
   }
+  if (met && m == -INFINITY) l = NAN;            // all scores -inf, or no numbers: 0 / 0
   const float inv = l == 0.f ? 0.f : 1.f / l;
   E* out = static_cast<E*>(a.out) + ((long long)row * a.Hq + head) * D;
 #pragma unroll
