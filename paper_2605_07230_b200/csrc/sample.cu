@@ -642,8 +642,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_sample(const SampleArgs a) {
   }
   float least = floor;
   if (min_p > 0.f) {
-    // w >= min_p  <=>  l >= m + T ln(min_p)
-    const double bound = weight.md + (double)T * log(min((double)min_p, 1.0));
+    // w >= min_p  <=>  l >= m + T ln(min_p); beside an infinite maximum nothing else weighs anything, at any temperature
+    const double bound = m == INFINITY ? (double)m : weight.md + (double)T * log(min((double)min_p, 1.0));
     const float f = (float)bound;
     const float up = (double)f >= bound ? f : nextafterf(f, INFINITY);
     if (f > -INFINITY) least = fmaxf(least, fminf(up, m));
