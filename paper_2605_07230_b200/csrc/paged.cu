@@ -270,8 +270,8 @@ __global__ void __launch_bounds__(kAppThreads) k_paged_append(const __grid_const
     const int t = t_base + tt;
     if (t >= a.n_tok) break;
     const int slot = a.slot[t];
-    if (slot < 0) continue;
-    if (slot >= a.n_slots) {
+    if (slot == -1) continue;
+    if (slot < 0 || slot >= a.n_slots) {
       if (threadIdx.x == 0) atomicOr(a.err, CASCADE_DEV_ERR_BAD_PAGE);
       continue;
     }
