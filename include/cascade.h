@@ -444,7 +444,8 @@ typedef struct {
  * A negative kv_len, lengths that pass the table's width or n_tok, a pool that runs out or over: nothing is taken or
  * given back -- kv_len_out and free_count_out repeat the inputs, q_begin is all 0, slot and pos all -1, so that what is
  * enqueued behind does nothing -- and cascade_check returns CASCADE_ERR_OVERFLOW.  A token whose page id is outside
- * the pool gets slot -1 (CASCADE_ERR_BAD_PAGE).
+ * the pool gets slot -1 (CASCADE_ERR_BAD_PAGE); one that a finished request gives back is pushed as it is, so that the
+ * stack's count holds, and reported the same way.
  * 1 <= n_req <= CASCADE_MAX_REQUESTS; n_tok >= 0.  All arrays int32, DEVICE. */
 #define CASCADE_MAX_REQUESTS 4096
 int cascade_paged_tables(cascade_ctx* ctx, int32_t n_req, int32_t n_tok, int32_t page_size, int32_t n_pages,

@@ -122,7 +122,11 @@ __global__ void __launch_bounds__(kTabThreads) k_paged_tables(const TablesArgs a
     for (int r = rank * kTabWarps + warp; r < a.n_req; r += n_cta * kTabWarps) {
       if (s_kv[r] >= 0) continue;
       const int held = a.pages(-1 - s_kv[r]);
-      for (int j = lane; j < held; j += 32) a.free_pages[count + s_back[r] + j] = a.block_table[(size_t)r * a.table_stride + j];
+      for (int j = lane; j < held; j += 32) {
+        const int page = a.block_table[(size_t)r * a.table_stride + j];
+        if (page < 0 || page >= a.n_pages) atomicOr(a.err, CASCADE_DEV_ERR_BAD_PAGE);
+        a.free_pages[count + s_back[r] + j] = page;
+      }
     }
   __syncwarp();
   ptx::cluster_arrive();

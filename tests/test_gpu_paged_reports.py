@@ -3,8 +3,9 @@ import pytest
 import torch
 
 from paper_2605_07230_b200 import binding as cb
+from oracle import paged_oracle as PO
 from tests import gpu_util as G
-from tests.test_gpu_paged import i32, make_ctx
+from tests.test_gpu_paged import i32, make_ctx, run_tables
 
 pytestmark = pytest.mark.gpu
 
@@ -29,4 +30,17 @@ def test_append_reports_every_slot_that_is_neither_in_the_pool_nor_minus_one(dty
     cb.cascade_paged_append(ctx, cache, k, k, i32([3, slot, 5]), i32([0, 0, 1]))
     assert reports_bad_page(ctx)
     assert float(pool.float().sum()) == 4 * 128
+    ctx.close()
+
+
+@pytest.mark.parametrize("page", [-1, 6, 10 ** 9])
+def test_tables_report_a_bad_page_that_is_given_back(page):
+    ctx = make_ctx()
+    args = ([-1, 0], [17, 8], [[4, page, 1], [2, -1, -1]], [3, -5, -5, -5, -5, -5], 1)
+    got = run_tables(ctx, *args, 8, 2)
+    assert reports_bad_page(ctx)
+    ref = PO.tables(*args, 8, 2)                     # the stack's count and order hold; the entry is the caller's own
+    assert got["free"].tolist() == ref["free"].tolist() and int(got["count"]) == ref["count"] == 4
+    got = run_tables(ctx, [-1, 0], [17, 8], [[4, 0, 1], [2, -1, -1]], [3, -5, -5, -5, -5, -5], 1, 8, 2)
+    ctx.check()
     ctx.close()
