@@ -9,6 +9,8 @@
 // The tensor cores add with truncation, so long sums stay out of them: the outputs of 16 keys are summed apart and added to
 // the running fp32 outputs by ordinary additions, and scores are summed over at most 64 elements at a time.
 // Splits of the keys are the CTAs of a cluster and meet through distributed shared memory.
+#include <climits>
+
 #include "paged.h"
 #include "paged_attn.cuh"
 
@@ -57,7 +59,9 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2) k_paged_attn_f32(co
   __shared__ bool s_lost[kWarps];                // the warp met a page outside the pool
   const PagedAttnArgs& a = p.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int split_i = blockIdx.x, kh = blockIdx.y / p.n_rb, rb = blockIdx.y % p.n_rb, r = blockIdx.z;
+  // (the splits of one cluster lie side by side; x is the one dimension of a grid with room for long passes)
+  const int unit = blockIdx.x / p.splits, split_i = blockIdx.x - unit * p.splits;
+  const int kh = unit / p.n_rb, rb = unit % p.n_rb, r = blockIdx.y;
   paged::Request rq;
   const bool valid = paged::load_request(a, r, &rq);
   const int row0 = rb * kBlock;
@@ -307,7 +311,7 @@ int launch(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_t s) {
   p.div = paged::page_div(a.page_size);
   constexpr int kBlock = kByRow ? kWarps * kRows : kRows;
   const long long row_blocks = ((long long)a.max_q * p.G + kBlock - 1) / kBlock;
-  if (row_blocks * a.Hkv > 65535) return CASCADE_ERR_UNSUPPORTED_SHAPE;
+  if (row_blocks * a.Hkv > INT_MAX / 8) return CASCADE_ERR_UNSUPPORTED_SHAPE;   // (the queries would not fit a GPU)
   p.n_rb = (int)row_blocks;
   // splits: as many as keep the resident CTAs busy at once, each with at least four steps a warp
   const long long units = (long long)a.n_req * a.Hkv * p.n_rb;
@@ -317,7 +321,7 @@ int launch(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_t s) {
   p.splits = 1;
   while (p.splits < 8 && units * p.splits * 2 <= 4ll * ctx->sm_count && steps >= 4ll * p.splits) p.splits *= 2;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.splits, a.Hkv * p.n_rb, a.n_req);
+  cfg.gridDim = dim3(p.splits * a.Hkv * p.n_rb, a.n_req);
   cfg.blockDim = dim3(kThreads);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
