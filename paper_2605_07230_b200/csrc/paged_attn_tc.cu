@@ -609,13 +609,15 @@ int launch(cascade_ctx* ctx, const TcArgs& p, int n_items, cudaStream_t s) {
   const uint64_t dk[4] = {(uint64_t)D, (uint64_t)a.Hkv, (uint64_t)a.page_size, (uint64_t)a.n_pages};
   const uint64_t sk[3] = {(uint64_t)D, (uint64_t)a.Hkv * D, (uint64_t)a.page_stride};
   const uint32_t bk[4] = {64, 1, (uint32_t)p.box_rows, 1};
-  const CUtensorMap* mq = get_tmap_4d_bf16(ctx, a.q, dq, sq, bq);
+  // the queries' map goes by the pass's token count, so none is kept: the list would grow by one a pass and every call on the
+  // context walk through it (38 us of host time a call after 3500 lengths, 11 us with an empty list)
+  CUtensorMap mq;
   const CUtensorMap* mk = get_tmap_4d_bf16(ctx, a.k, dk, sk, bk);
   const CUtensorMap* mv = get_tmap_4d_bf16(ctx, a.v, dk, sk, bk);
-  if (mq == nullptr || mk == nullptr || mv == nullptr) return CASCADE_ERR_CUDA;
+  if (mk == nullptr || mv == nullptr || !make_tmap_4d_bf16(&mq, a.q, dq, sq, bq)) return CASCADE_ERR_CUDA;
   CASCADE_TRY(configure_smem(ctx, PAGED_CFG_ATTN_TC, k_paged_attn_tc<D>, Cfg<D>::kSmem));   // (a context has one D)
   const int grid = n_items < ctx->sm_count ? n_items : ctx->sm_count;
-  k_paged_attn_tc<D><<<grid, kThreads, Cfg<D>::kSmem, s>>>(*mq, *mk, *mv, p);
+  k_paged_attn_tc<D><<<grid, kThreads, Cfg<D>::kSmem, s>>>(mq, *mk, *mv, p);
   CASCADE_CUDA_TRY(cudaGetLastError());
   return CASCADE_OK;
 }

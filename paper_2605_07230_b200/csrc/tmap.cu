@@ -45,6 +45,21 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
+bool encode(const Key& key, CUtensorMap* map) {
+  auto fn = encode_fn();
+  if (fn == nullptr) return false;
+  cuuint64_t dims[4], strides[3];
+  cuuint32_t box[4], estr[4] = {1, 1, 1, 1};
+  for (int i = 0; i < key.rank; ++i) {
+    dims[i] = key.dims[i];
+    box[i] = key.box[i];
+  }
+  for (int i = 0; i + 1 < key.rank; ++i) strides[i] = key.strides[i] * 2;  // bytes
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)key.rank, const_cast<void*>(key.base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 const CUtensorMap* lookup_or_make(cascade_ctx* ctx, const Key& key) {
   if (ctx->tmap_cache == nullptr) ctx->tmap_cache = new Cache();
   Cache* c = static_cast<Cache*>(ctx->tmap_cache);
@@ -53,24 +68,12 @@ const CUtensorMap* lookup_or_make(cascade_ctx* ctx, const Key& key) {
       c->entries.splice(c->entries.end(), c->entries, it);  // most recently used last; the element stays where it is in memory
       return &it->map;
     }
-  auto fn = encode_fn();
-  if (fn == nullptr) return nullptr;
   if (c->entries.size() >= kMaxEntries) c->entries.pop_front();  // callers that churn through buffers
   c->entries.emplace_back();
   Entry& e = c->entries.back();
   std::memset(&e.key, 0, sizeof(Key));
   e.key = key;
-  cuuint64_t dims[4], strides[3];
-  cuuint32_t box[4], estr[4] = {1, 1, 1, 1};
-  for (int i = 0; i < key.rank; ++i) {
-    dims[i] = key.dims[i];
-    box[i] = key.box[i];
-  }
-  for (int i = 0; i + 1 < key.rank; ++i) strides[i] = key.strides[i] * 2;  // bytes
-  CUresult r = fn(&e.map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)key.rank, const_cast<void*>(key.base), dims,
-                  strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) {
+  if (!encode(key, &e.map)) {
     c->entries.pop_back();
     return nullptr;
   }
@@ -93,8 +96,7 @@ const CUtensorMap* get_tmap_2d_bf16(cascade_ctx* ctx, const void* base, uint64_t
   return lookup_or_make(ctx, k);
 }
 
-const CUtensorMap* get_tmap_4d_bf16(cascade_ctx* ctx, const void* base, const uint64_t dims[4],
-                                    const uint64_t strides_elems[3], const uint32_t box[4]) {
+static Key key_4d(const void* base, const uint64_t dims[4], const uint64_t strides_elems[3], const uint32_t box[4]) {
   Key k;
   std::memset(&k, 0, sizeof(k));
   k.base = base;
@@ -104,7 +106,17 @@ const CUtensorMap* get_tmap_4d_bf16(cascade_ctx* ctx, const void* base, const ui
     k.box[i] = box[i];
   }
   for (int i = 0; i < 3; ++i) k.strides[i] = strides_elems[i];
-  return lookup_or_make(ctx, k);
+  return k;
+}
+
+const CUtensorMap* get_tmap_4d_bf16(cascade_ctx* ctx, const void* base, const uint64_t dims[4],
+                                    const uint64_t strides_elems[3], const uint32_t box[4]) {
+  return lookup_or_make(ctx, key_4d(base, dims, strides_elems, box));
+}
+
+bool make_tmap_4d_bf16(CUtensorMap* map, const void* base, const uint64_t dims[4], const uint64_t strides_elems[3],
+                       const uint32_t box[4]) {
+  return encode(key_4d(base, dims, strides_elems, box), map);
 }
 
 const CUtensorMap* get_tmap_bf16(cascade_ctx* ctx, const void* base, int rank, const uint64_t* dims,
