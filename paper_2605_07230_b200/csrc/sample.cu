@@ -3,10 +3,12 @@
 //   w[v] = exp((l[v] - m) / T),  token = first v whose cumulative kept weight exceeds u * (total kept weight)
 //
 // One CTA per row.  The row stays in shared memory as far as it fits (the rest is read again through the L2), so HBM sees
-// each logit once.  Weights are formed in 64 bits (relative error 1e-10) and summed as 64-bit fixed point: sums do not
-// depend on the order of additions, and a draw differs from exact arithmetic only where u falls within about 1e-10 of a
-// boundary.
-// Thresholds are exact.  A histogram over 2048 equal steps of the distance to the row's maximum (counts for top-k, weights
+// each logit once.  Weights are formed in 64 bits (relative error 1e-10), rounded to multiples of 2^-b of the largest one,
+// b = min(50, 62 - log2 V), log2 rounded up, and summed in 64-bit fixed point: sums do not depend on the order of additions.
+// V roundings of at most half a unit each leave a sum within V 2^-(b+1) + 1e-10 of it (largest weight 1): 1.3e-10 for V = 16384,
+// 5.7e-10 for 65536, 3.8e-9 for 131080, 1.2e-7 for 2^20, all of it only where most tokens weigh about half a unit.  A draw, and
+// where the nucleus ends, differ from exact arithmetic only where u or top_p falls that close to a boundary.
+// For the rounded weights thresholds are exact.  A histogram over 2048 equal steps of the distance to the row's maximum (counts for top-k, weights
 // for the nucleus) finds the step in which the threshold lies; the few tokens of that step are then ranked among each
 // other.  Where a step holds too many different values (logits spread over more than 48 and the threshold far down, or
 // infinities), the search goes over the range of the values' ordered bit patterns instead, 2048 steps at a time.
