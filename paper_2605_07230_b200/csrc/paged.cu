@@ -30,7 +30,7 @@ struct TablesArgs {
 // given back; a few kilobytes of lengths, cheaper to scan eight times than to exchange), all CTAs share the writes.  The
 // cluster barrier parts the reads of what is updated in place (lengths, count, free list) and the pushes onto the free
 // list from everything that is written or popped afterwards.  Latency-bound: 14.4 us for 512
-// requests with about 110 thousand new tokens (1 MB), 5.0 us for two with one each.
+// requests with about 110 thousand new tokens (1 MB), 5 us for two with one each (graph replays).
 __global__ void __launch_bounds__(kTabThreads) k_paged_tables(const TablesArgs a) {
   extern __shared__ int smem[];
   int* s_q = smem;                     // [n_req + 1] exclusive sums of the new tokens
@@ -384,17 +384,17 @@ int cascade_paged_tables(cascade_ctx* ctx, int32_t n_req, int32_t n_tok, int32_t
   const size_t smem = (size_t)(4 * n_req + 1) * sizeof(int);
   // (for every count: what a kernel gets unasked, 48 KB, has to hold its static arrays too)
   CASCADE_TRY(configure_smem(ctx, PAGED_CFG_TABLES, k_paged_tables, (4 * CASCADE_MAX_REQUESTS + 1) * (int)sizeof(int)));
-  // one CTA for few (2048 tokens of 32 requests: 6.0 us, 6.1 with a cluster of eight), then a cluster of eight (4096 of 64:
-  // 6.6 us, 7.1 with one CTA; 256 requests of a token: 6.7 us, 9.2)
-  const int n_cta = n_tok <= 2 * kTabThreads && n_req <= 32 ? 1 : 8;
+  // a cluster of eight for few tokens too (against one CTA: two tokens 5.1 us either way, 2000 tokens of 32 requests 6.8 either
+  // way, 4000 of 64 7.1 and 7.8, 256 requests of one token 6.7 and 9.4)
+  constexpr int kCtas = 8;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(n_cta);
+  cfg.gridDim = dim3(kCtas);
   cfg.blockDim = dim3(kTabThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = static_cast<cudaStream_t>(stream);
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = n_cta;
+  attr[0].val.clusterDim.x = kCtas;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
