@@ -6,6 +6,10 @@
 // the 16-bit kernel for few rows, a warp takes 16 keys at a time straight from memory into operand registers, keys and
 // values on M, eight rows on N.  Single tokens and short chunks (up to eight rows) share the keys out between the warps;
 // beyond that every warp has eight rows of its own and walks over all keys, which the four then share in the L1.
+// 8 chunks of 47 to 122 tokens over 109 to 397 keys, 4 heads of 64: 20 us.  The case has four splits of at most 7 steps a warp,
+// 1170 instructions a step with start and merge (operands are split by every warp for itself); 2.4 warps a scheduler use 31 % of
+// the issue slots of active SMs, and an SM is active for 69 % of the time (512 uneven CTAs).
+// D = 128 needs more than the 255 registers there are and spills some 60 words a thread; long chunks run at 13 to 16 TFLOP/s.
 // The tensor cores add with truncation, so long sums stay out of them: the outputs of 16 keys are summed apart and added to
 // the running fp32 outputs by ordinary additions, and scores are summed over at most 64 elements at a time.
 // Splits of the keys are the CTAs of a cluster and meet through distributed shared memory.
@@ -313,7 +317,10 @@ int launch(cascade_ctx* ctx, const PagedAttnArgs& a, cudaStream_t s) {
   const long long row_blocks = ((long long)a.max_q * p.G + kBlock - 1) / kBlock;
   if (row_blocks * a.Hkv > INT_MAX / 8) return CASCADE_ERR_UNSUPPORTED_SHAPE;   // (the queries would not fit a GPU)
   p.n_rb = (int)row_blocks;
-  // splits: as many as keep the resident CTAs busy at once, each with at least four steps a warp
+  // splits: up to four CTAs an SM, each with at least four steps a warp.  Three (D = 128: two) fit at once; the row blocks' work
+  // is uneven, and a queue behind them fills the gaps: 8 chunks of up to 130 tokens, 4 heads of 64, take 20 us with up to four,
+  // 29 with up to three or two, 26 with up to eight; 4 chunks of 30 to 60 tokens, 8 heads of 128, 47, 43, 42 and 47; 16 single
+  // tokens over 1000 to 2000 keys, 8 heads of 128, 77, 76, 76 and 89.
   const long long units = (long long)a.n_req * a.Hkv * p.n_rb;
   const long long window = (long long)a.window + a.sinks + kBlock;
   const long long span = a.window > 0 && window < a.max_kv ? window : a.max_kv;

@@ -8,7 +8,8 @@
 // give pairs of keys after one byte permute per register, and the weights turn with one 8 x 8 transpose per eight keys.
 // No shared memory and no barrier in the loop: the keys of the next 16 are requested as soon as the scores have used the
 // registers, the values as soon as the output has; with up to eight rows three CTAs fit an SM, 96 KB in flight.
-// 48 single tokens over 256 to 2880 keys, 32 heads of 128: 195 us, 6.66 TB/s; two over 385 keys: 8.2 us.
+// 48 single tokens over 256 to 2880 keys, 32 heads of 128: 196 us in graph replays, 6.6 TB/s of reads (a copy, half of it
+// writes, runs at 6.45), 207 us called one by one; two over 385 keys: 8.2 and 10.2 us.
 // (The 5th-generation tensor cores want 128 rows and operands in shared memory; here they would multiply padding.)
 // Weights are 2^(s c - ref); ref is the running maximum, raised only when a score passes it by more than 2^8.  Weights are
 // rounded to bf16 for the product with the bf16 values, sums and accumulators stay fp32.
@@ -83,7 +84,7 @@ __global__ void __launch_bounds__(kThreads, kNb == 1 ? 3 : 2) k_paged_attn_rows(
 
   // 16-key steps that any row sees: [0, n_sink) and [n_sink + skip, ...)
   int n = 0, n_sink = 0, skip = 0;
-  if (rows > 0 && rq.kv > 0) {
+  if (rq.kv > 0) {
     const int lo = paged::window_begin(x0, a.window), lo_c = lo / kChunk;
     n_sink = min((min(a.sinks, lo) + kChunk - 1) / kChunk, lo_c);
     skip = lo_c - n_sink;

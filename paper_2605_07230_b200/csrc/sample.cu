@@ -15,7 +15,7 @@
 // Once a truncation has left at most 4096 tokens, they are gathered and the later passes go over them alone.
 // Bound by the instructions of two to four passes over the row: 148 rows of 65536 take 6 us for the most likely token (HBM),
 // 24 to 31 us with top-k, 30 us without truncation, 51 us for a nucleus of 0.9; 488 rows with mixed settings 123 us; two rows
-// of 16384, where the passes' latencies add up, 13.5 us.
+// of 16384, where the passes' latencies add up, 13.5 us (graph replays; 15.2 called one by one).
 #include <cfloat>
 
 #include "cascade_internal.h"
