@@ -417,6 +417,7 @@ int cascade_filter_logits(cascade_ctx* ctx, float* logits, int32_t n_rows, int32
  *   table_width at most table_stride; 0: table_stride
  * Device-resident lengths, pages and slots cannot be checked on the host.  A kernel that meets one outside its range
  * leaves it out, touches nothing outside the buffers it was given, and cascade_check returns CASCADE_ERR_BAD_PAGE.
+ * Arrays of 32-bit numbers start on 4-byte boundaries (CASCADE_ERR_INVALID_ARG).
  * All four calls allocate nothing, take their sizes from host arguments alone and can be recorded into a CUDA graph.
  * The context must have been created on the current device (CASCADE_ERR_INVALID_ARG otherwise). */
 typedef struct {

@@ -359,6 +359,8 @@ int cascade_paged_tables(cascade_ctx* ctx, int32_t n_req, int32_t n_tok, int32_t
     return CASCADE_ERR_INVALID_ARG;
   if (n_req < 1 || n_tok < 0 || page_size < 1 || n_pages < 1 || table_stride < 1) return CASCADE_ERR_INVALID_ARG;
   if (n_tok > 0 && (slot == nullptr || pos == nullptr)) return CASCADE_ERR_INVALID_ARG;
+  if (!aligned4(new_len, kv_len, block_table, free_pages, free_count, kv_len_out, free_count_out, q_begin, slot, pos))
+    return CASCADE_ERR_INVALID_ARG;
   if (n_req > CASCADE_MAX_REQUESTS || page_size % 8 != 0 || (int64_t)n_pages * page_size > INT32_MAX)
     return CASCADE_ERR_UNSUPPORTED_SHAPE;
   if (n_tok > INT32_MAX - 65536) return CASCADE_ERR_UNSUPPORTED_SHAPE;  // the token loop's stride must not pass 32 bits
@@ -418,7 +420,7 @@ int cascade_paged_append(cascade_ctx* ctx, const cascade_paged_cache* cache, int
   if (rope && !(rope_base > 1.f && std::isfinite(rope_base))) return CASCADE_ERR_INVALID_ARG;
   if ((q == nullptr) != (q_out == nullptr) || (q != nullptr && !rope)) return CASCADE_ERR_INVALID_ARG;
   if (k_stride < kv_row || v_stride < kv_row || k_stride * es % 16 != 0 || v_stride * es % 16 != 0) return CASCADE_ERR_INVALID_ARG;
-  if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out)) return CASCADE_ERR_INVALID_ARG;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out) || !aligned4(slot, pos)) return CASCADE_ERR_INVALID_ARG;
   if (q != nullptr && (q_stride < q_row || q_out_stride < q_row || q_stride * es % 16 != 0 || q_out_stride * es % 16 != 0 ||
                        (q == q_out && q_stride != q_out_stride)))
     return CASCADE_ERR_INVALID_ARG;

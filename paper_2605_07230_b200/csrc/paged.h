@@ -4,6 +4,11 @@
 
 // Status of a paged cache's host-side fields (pointers, alignment, strides, sizes) for this context.
 int check_paged_cache(const cascade_ctx* ctx, const cascade_paged_cache* cache);
+// Whether 32-bit arrays (null: not given) all start on 4-byte boundaries.
+template <typename... P>
+bool aligned4(const P*... p) {
+  return ((... | reinterpret_cast<uintptr_t>(p)) & 3u) == 0;
+}
 // CASCADE_ERR_INVALID_ARG unless the context's device is the current one.
 int check_current_device(const cascade_ctx* ctx);
 

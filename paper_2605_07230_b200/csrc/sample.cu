@@ -770,6 +770,7 @@ extern "C" int cascade_sample(cascade_ctx* ctx, const void* logits, int32_t logi
   if (n_rows < 1 || row_stride < V) return CASCADE_ERR_INVALID_ARG;
   const bool bf16 = logits_dtype == CASCADE_BF16;
   if ((reinterpret_cast<uintptr_t>(logits) & (bf16 ? 1u : 3u)) != 0) return CASCADE_ERR_INVALID_ARG;
+  if (!aligned4(temperature, top_k, top_p, min_p, uniforms, token_out, prob_out, kept_out)) return CASCADE_ERR_INVALID_ARG;
   const void* arrays[] = {token_out, prob_out, kept_out, temperature, top_k, top_p, min_p, uniforms, logits};
   for (int i = 0; i < 3; ++i)
     for (int k = i + 1; k < 9; ++k)
