@@ -407,7 +407,8 @@ int cascade_filter_logits(cascade_ctx* ctx, float* logits, int32_t n_rows, int32
  * is a pool of pages; a request's token at position x lives in page block_table[r][x / page_size] at row
  * x % page_size.  The dense prefix cache of cascade_verify_step ([R,prefix_cap,Hkv,D]) is the special case
  * n_pages = R * prefix_cap / page_size, block_table[r][i] = r * (prefix_cap / page_size) + i: prompts written through
- * these calls into such a pool can be verified against without a copy.
+ * these calls into such a pool can be verified against without a copy.  The verification step itself reads that layout only:
+ * behind any other block table a prefix has to be copied into a dense cache first.
  *   k_pages, v_pages [n_pages,page_size,Hkv,D] elem, page p starting page_stride elements after page p - 1
  *              (page_stride >= page_size*Hkv*D; larger where keys and values of a page lie side by side in one pool);
  *              16-byte aligned, page_stride a multiple of 16 bytes
@@ -460,7 +461,7 @@ int cascade_paged_tables(cascade_ctx* ctx, int32_t n_req, int32_t n_tok, int32_t
  *   q [n_tok,Hq,D] rows q_stride apart -> q_out rows q_out_stride apart, rotated; q_out may be q (same stride).
  *   q = q_out = NULL: keys and values only.  rope_base = 0: no rotation (then q has to be NULL).
  *   slot, pos [n_tok] int32 from cascade_paged_tables; a row with slot -1 is left out (its q_out row too).  No two rows
- *   may name the same slot.  pos >= 0 for the others.
+ *   may name the same slot.  pos >= 0 for the others.  n_tok >= 1.  But for q_out = q no output overlaps an input.
  * block_table is not used.  All bases 16-byte aligned, strides multiples of 16 bytes. */
 int cascade_paged_append(cascade_ctx* ctx, const cascade_paged_cache* cache, int32_t n_tok, const void* q, int64_t q_stride,
                          const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* slot,
@@ -471,17 +472,22 @@ int cascade_paged_append(cascade_ctx* ctx, const cascade_paged_cache* cache, int
  * j iff j <= x and (window == 0 or j > x - window or j < sinks):
  *     out[row,head,:] = sum_j softmax_j(softmax_scale * <q[row,head,:], k_j>) v_j ;   lse[row,head] = log sum_j exp(...)
  * Query head `head` reads kv head head / (Hq / Hkv).  A row that sees no key (kv_len smaller than its new tokens) gets
- * zeros and lse -inf.  What lies at keys a row does not see, NaN and infinities included, does not reach it.
+ * zeros and lse -inf, one all of whose scores are -inf NaN.  What lies at keys a row does not see, NaN and infinities
+ * included, does not reach it.
  * Keys of a page outside the pool count as not seen (CASCADE_ERR_BAD_PAGE): rows that would have seen one, and rows beside
  * them, are summed again key by key, which takes long.
  *   q [n_tok,Hq,D] elem, rows q_stride apart; out [n_tok,Hq,D] elem, dense, no part of q (CASCADE_ERR_INVALID_ARG);
  *   lse [n_tok,Hq] float or NULL
  *   q_begin [n_req+1], kv_len [n_req] int32, DEVICE: as cascade_paged_tables leaves them.  Rows of q behind
- *   q_begin[n_req] are not read, the same rows of out and lse not written.
+ *   q_begin[n_req] (all n_tok rows are memory) reach no result, the same rows of out and lse are not written.  n_tok >= 1.
  *   max_q, max_kv: no request has more new tokens / keys than this (host bounds that launch sizes come from; a
  *   request beyond them is left out, CASCADE_ERR_BAD_PAGE).  1 <= n_req <= CASCADE_MAX_REQUESTS.
  *   Hq / Hkv <= 128, max_kv <= 2^31 - 65536 (CASCADE_ERR_UNSUPPORTED_SHAPE).
- *   window >= 0 (0: none), sinks >= 0.  Softmax and accumulation are fp32. */
+ *   window >= 0 (0: none), sinks >= 0.
+ * Scores, statistics, sums and accumulators are fp32.  bf16: the weights are rounded to bf16 for their product with the values.
+ * fp32: every operand of a product counts with about 22 bits (two 19-bit parts).  A row whose result is not finite, or (bf16,
+ * more than 16 rows a key head) whose scores climb by more than 66 from one 64 keys to the next, is summed again key by key,
+ * 0.6 us a key. */
 int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* cache, int32_t n_req, int32_t n_tok, const void* q,
                        int64_t q_stride, const int32_t* q_begin, const int32_t* kv_len, int32_t max_q, int32_t max_kv,
                        int32_t window, int32_t sinks, float softmax_scale, void* out, float* lse, void* stream);

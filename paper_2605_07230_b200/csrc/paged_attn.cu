@@ -25,7 +25,8 @@ extern "C" int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* c
   if (n_req < 1 || n_tok < 1 || max_q < 1 || max_kv < 0 || window < 0 || sinks < 0) return CASCADE_ERR_INVALID_ARG;
   if (!(softmax_scale > 0.f) || softmax_scale > 3e38f) return CASCADE_ERR_INVALID_ARG;
   if (q_stride < (int64_t)sh.Hq * sh.D || q_stride * es % 16 != 0) return CASCADE_ERR_INVALID_ARG;
-  if (((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15u) != 0 || !aligned4(q_begin, kv_len, cache->block_table, lse))
+  if (((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15u) != 0 ||
+      !aligned4(q_begin, kv_len, cache->block_table, lse))
     return CASCADE_ERR_INVALID_ARG;
   if (max_kv > kMaxKeys) return CASCADE_ERR_UNSUPPORTED_SHAPE;
   if (n_req > CASCADE_MAX_REQUESTS || sh.Hq / sh.Hkv > kMaxGroup) return CASCADE_ERR_UNSUPPORTED_SHAPE;

@@ -8,9 +8,9 @@
 // V roundings of at most half a unit each leave a sum within V 2^-(b+1) + 1e-10 of it (largest weight 1): 1.3e-10 for V = 16384,
 // 5.7e-10 for 65536, 3.8e-9 for 131080, 1.2e-7 for 2^20, all of it only where most tokens weigh about half a unit.  A draw, and
 // where the nucleus ends, differ from exact arithmetic only where u or top_p falls that close to a boundary.
-// For the rounded weights thresholds are exact.  A histogram over 2048 equal steps of the distance to the row's maximum (counts for top-k, weights
-// for the nucleus) finds the step in which the threshold lies; the few tokens of that step are then ranked among each
-// other.  Where a step holds too many different values (logits spread over more than 48 and the threshold far down, or
+// For the rounded weights thresholds are exact.  A histogram over 2048 equal steps of the distance to the row's maximum (counts
+// for top-k, weights for the nucleus) finds the step in which the threshold lies; the few tokens of that step are then ranked
+// among each other.  Where a step holds too many different values (logits spread over more than 48 and the threshold far down, or
 // infinities), the search goes over the range of the values' ordered bit patterns instead, 2048 steps at a time.
 // Once a truncation has left at most 4096 tokens, they are gathered and the later passes go over them alone.
 // Bound by the instructions of two to four passes over the row: 148 rows of 65536 take 6 us for the most likely token (HBM),
