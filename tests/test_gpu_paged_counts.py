@@ -20,7 +20,7 @@ def tables_in_ascending_order():
     """Request counts around the shared memory that a kernel gets unasked, small ones first, in a process of their own (what a
     larger call asked for holds for the smaller ones behind it)."""
     ctx = make_ctx()
-    for n_req in (3000, 3022, 3023, 3050, 3071, 3072, 4096):
+    for n_req in (3000, 3022, 3023, 3050, 3071, 3075, 4096):
         rng = np.random.default_rng(n_req)
         new, kv, table, free, count = random_requests(rng, n_req, 8, 3, 20, 0.2)
         n_tok = int(np.maximum(new, 0).sum()) + 1
