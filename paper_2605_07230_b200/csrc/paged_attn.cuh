@@ -1,7 +1,7 @@
 // What the paged-attention kernels share: arguments, the visibility rule, and the attention of one row by one warp.
 #pragma once
 #include "cascade_internal.h"
-#include "ptx.cuh"
+#include "ptx_paged.cuh"
 
 struct PagedAttnArgs {
   int n_req, n_tok, Hq, Hkv, page_size, n_pages, table_stride, table_width, max_q, max_kv, window, sinks;
