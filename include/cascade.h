@@ -535,6 +535,40 @@ int cascade_drafter_loss(const float* target_logits, const float* draft_logits, 
                          int32_t h, float tau_seq, float c, float* loss_out, float* weight_out, float* total_out,
                          void* stream);
 
+/* The same loss from what is stored of the target: its n_top largest logits of every position (2000 in the paper's sampling
+ * settings, Appendix D.1) instead of whole rows, and the gradient with respect to the drafter's logits.  With T = temperature,
+ * d = draft_logits[k], p = softmax(d / T), (t_i, id_i) the stored logits and tokens of position k:
+ *     q_i = exp(t_i / T) / sum_j exp(t_j / T)       target_lse == NULL: renormalised over what is stored
+ *     q_i = exp(t_i / T - target_lse[k])            target_lse [K]: the log-sum-exp of the whole target row over T; the mass that
+ *                                                   is not stored is left out
+ *     loss_out[k] = - w_k sum_i q_i log p[id_i]
+ *     grad_out[k] = scale * grad_loss[k] * w_k / T * (Q_k p - sum_i q_i e_(id_i)),   Q_k = sum_i q_i
+ * w_k = c where feat[k] and feat[k+1] converge (cosine >= tau_seq) and belong to one sequence, else 1; feat NULL: 1 everywhere.
+ * seq [K] int32 or NULL (one sequence): the sequence a position belongs to; negative: padding, whose loss, gradient and saved
+ * row are zeros whatever its logits hold.
+ *   draft_logits [K,V] float (logits_dtype CASCADE_F32) or bf16 (CASCADE_BF16), rows row_stride elements apart (>= V, at most
+ *     2^40), aligned to the element; V, n_top <= 2^31 - 65536 (CASCADE_ERR_UNSUPPORTED_SHAPE)
+ *   top_logits [K,n_top] float, top_ids [K,n_top] int32: in any order; an id outside [0,V) marks a place without an entry, a
+ *     token given more than once adds up.  A position none of whose entries weighs anything has loss and gradient 0.
+ *   saved_out [K,4] float, 16-byte aligned: log-sum-exp of d / T, that of the target, Q_k, w_k: what the gradient needs
+ *   total_out [1] float or NULL: sum of loss_out, in a fixed order
+ *   grad_loss [K] float or NULL (1); scale: finite
+ *   grad_out [K,V] of the logits' type, rows grad_stride apart; may be draft_logits itself (same stride): the gradient then
+ *     replaces the logits.  Where scale * grad_loss[k] * w_k is 0 the row is zeros.  But for that no output overlaps another or
+ *     an input (CASCADE_ERR_INVALID_ARG).
+ * A logit that is no number, or +inf, makes its position's loss and gradient NaN; one of -inf has p = 0.
+ * Sums and statistics are 32 bits (the sums over stored entries and of the cosine 64); a bf16 gradient is rounded once.
+ * Results do not depend on the order of additions.  No context is needed and nothing is allocated; one kernel each, and one for
+ * total_out.  Errors: CASCADE_ERR_INVALID_ARG (null pointers, sizes < 1, 1e-30 <= temperature <= 1e30 not met, c <= 0, NaN
+ * threshold). */
+int cascade_distill_loss(const void* draft_logits, int32_t logits_dtype, int64_t row_stride, const float* top_logits,
+                         const int32_t* top_ids, int32_t n_top, const float* target_lse, const float* feat, const int32_t* seq,
+                         int32_t K, int32_t V, int32_t h, float temperature, float tau_seq, float c, float* loss_out,
+                         float* saved_out, float* total_out, void* stream);
+int cascade_distill_grad(const void* draft_logits, int32_t logits_dtype, int64_t row_stride, const float* top_logits,
+                         const int32_t* top_ids, int32_t n_top, const float* saved, const float* grad_loss, float scale, int32_t K,
+                         int32_t V, float temperature, void* grad_out, int64_t grad_stride, void* stream);
+
 /* ---- acceptance without any device allocation --------------------------------------------------- */
 /* The paper has no counterpart to this entry point; it exists for deployment.  Some callers of this
  * library may not allocate device memory at all: a plug-in running inside a serving process that

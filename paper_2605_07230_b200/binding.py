@@ -33,6 +33,7 @@ EXPORTS = [
     "cascade_filter_logits", "cascade_set_wait_limit", "cascade_wait_probe",
     "cascade_tree_update_device", "cascade_tree_download", "cascade_drafter_loss",
     "cascade_paged_tables", "cascade_paged_append", "cascade_paged_attn", "cascade_sample",
+    "cascade_distill_loss", "cascade_distill_grad",
 ]
 
 
@@ -123,6 +124,8 @@ def lib() -> C.CDLL:
         L.cascade_paged_append.argtypes = [vp, cache, i32, vp, i64, vp, i64, vp, i64, vp, vp, f32, vp, i64, vp]
         L.cascade_paged_attn.argtypes = [vp, cache, i32, i32, vp, i64, vp, vp, i32, i32, i32, i32, f32, vp, vp, vp]
         L.cascade_sample.argtypes = [vp, vp, i32, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.cascade_distill_loss.argtypes = [vp, i32, i64, vp, vp, i32, vp, vp, vp, i32, i32, i32, f32, f32, f32, vp, vp, vp, vp]
+        L.cascade_distill_grad.argtypes = [vp, i32, i64, vp, vp, i32, vp, vp, f32, i32, i32, f32, vp, i64, vp]
         L.cascade_set_wait_limit.argtypes = [vp, C.c_int64]
         L.cascade_wait_probe.argtypes = [vp, vp, vp]
         _lib = L
@@ -516,3 +519,52 @@ def cascade_sample(ctx, logits, uniforms, token, temperature=None, top_k=None, t
             _vector("prob", prob, f32, n), _vector("kept", kept, i32, n))
     stream = _on_device(logits, uniforms, token, temperature, top_k, top_p, min_p, prob, kept)
     _check(lib().cascade_sample(ctx.handle, logits.data_ptr(), F32 if dt is f32 else BF16, V if n == 1 else st[0], n, *args, stream))
+
+
+# ---- a drafter's training step -----------------------------------------------------------------------------------------
+
+
+def _logit_rows(name, t, shape=None, dtype=None):
+    """[K,V] float32 or bfloat16 logits whose rows may lie apart: their type and row stride."""
+    if t.dim() != 2 or (t.dtype is not torch.float32 and t.dtype is not torch.bfloat16) or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: expected float32 or bfloat16 rows of dense logits, got {t.dtype} {tuple(t.shape)}")
+    if (shape is not None and t.shape != shape) or (dtype is not None and t.dtype is not dtype):
+        raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return (F32 if t.dtype is torch.float32 else BF16), t.shape[1] if t.shape[0] == 1 else t.stride(0)
+
+
+def _dense(name, t, dtype, shape):
+    """The address of a dense tensor (None: not given)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a dense {dtype} tensor {shape}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def cascade_distill_loss(draft_logits, top_logits, top_ids, loss, saved, total=None, target_lse=None, feat=None, seq=None,
+                         temperature=1.0, tau_seq=0.5, c=2.0):
+    """Eq. 4 against the target's stored logits top_logits, top_ids [K,n] (see include/cascade.h); `saved` is for the gradient."""
+    kind, stride = _logit_rows("draft_logits", draft_logits)
+    (K, V), f32, i32 = draft_logits.shape, torch.float32, torch.int32
+    n = top_ids.shape[-1]
+    h = 0 if feat is None else feat.shape[-1]
+    top_p, ids_p = _dense("top_logits", top_logits, f32, (K, n)), _dense("top_ids", top_ids, i32, (K, n))
+    lse_p, feat_p, seq_p = _vector("target_lse", target_lse, f32, K), _dense("feat", feat, f32, (K, h)), _vector("seq", seq, i32, K)
+    loss_p, saved_p, total_p = _vector("loss", loss, f32, K), _dense("saved", saved, f32, (K, 4)), _vector("total", total, f32, 1)
+    stream = _on_device(draft_logits, top_logits, top_ids, target_lse, feat, seq, loss, saved, total)
+    _check(lib().cascade_distill_loss(draft_logits.data_ptr(), kind, stride, top_p, ids_p, n, lse_p, feat_p, seq_p, K, V, h,
+                                      temperature, tau_seq, c, loss_p, saved_p, total_p, stream))
+
+
+def cascade_distill_grad(draft_logits, top_logits, top_ids, saved, grad, temperature=1.0, grad_loss=None, scale=1.0):
+    """The gradient of that loss with respect to draft_logits; `grad` may be draft_logits itself."""
+    kind, stride = _logit_rows("draft_logits", draft_logits)
+    (K, V), f32, i32 = draft_logits.shape, torch.float32, torch.int32
+    n = top_ids.shape[-1]
+    grad_stride = _logit_rows("grad", grad, draft_logits.shape, draft_logits.dtype)[1]
+    top_p, ids_p = _dense("top_logits", top_logits, f32, (K, n)), _dense("top_ids", top_ids, i32, (K, n))
+    saved_p, up_p = _dense("saved", saved, f32, (K, 4)), _vector("grad_loss", grad_loss, f32, K)
+    stream = _on_device(draft_logits, top_logits, top_ids, saved, grad, grad_loss)
+    _check(lib().cascade_distill_grad(draft_logits.data_ptr(), kind, stride, top_p, ids_p, n, saved_p, up_p, scale, K, V, temperature,
+                                      grad.data_ptr(), grad_stride, stream))
