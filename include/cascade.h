@@ -419,7 +419,7 @@ int cascade_filter_logits(cascade_ctx* ctx, float* logits, int32_t n_rows, int32
  * Device-resident lengths, pages and slots cannot be checked on the host.  A kernel that meets one outside its range
  * leaves it out, touches nothing outside the buffers it was given, and cascade_check returns CASCADE_ERR_BAD_PAGE.
  * Arrays of 32-bit numbers start on 4-byte boundaries (CASCADE_ERR_INVALID_ARG).
- * All four calls allocate nothing, take their sizes from host arguments alone and can be recorded into a CUDA graph.
+ * All five calls allocate nothing, take their sizes from host arguments alone and can be recorded into a CUDA graph.
  * The context must have been created on the current device (CASCADE_ERR_INVALID_ARG otherwise). */
 typedef struct {
   void* k_pages;
@@ -491,6 +491,33 @@ int cascade_paged_append(cascade_ctx* ctx, const cascade_paged_cache* cache, int
 int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* cache, int32_t n_req, int32_t n_tok, const void* q,
                        int64_t q_stride, const int32_t* q_begin, const int32_t* kv_len, int32_t max_q, int32_t max_kv,
                        int32_t window, int32_t sinks, float softmax_scale, void* out, float* lse, void* stream);
+
+/* The gradient of cascade_paged_attn, from what it was given and what it left: with P_ij = exp(softmax_scale <q_i, k_j> - lse_i)
+ * where row i sees key j and 0 elsewhere, delta_i = <d_out_i, out_i> and dS_ij = P_ij (<d_out_i, v_j> - delta_i):
+ *     dq_i = softmax_scale sum_j dS_ij k_j      dk_j = softmax_scale sum_i dS_ij q_i      dv_j = sum_i P_ij d_out_i
+ * the sums of dk, dv running over all query heads that read the key head.  (The gradients of rotated queries and keys: a rotation
+ * is undone by turning them back.)
+ *   cache, n_req, n_tok, q, q_stride, q_begin, kv_len, max_q, max_kv, window, sinks, softmax_scale: as in the call before
+ *   out [n_tok,Hq,D] elem, lse [n_tok,Hq] float: what it left;  d_out [n_tok,Hq,D] elem: the gradient of its output; all dense
+ *   scratch [n_tok,Hq,2] float, DEVICE: work space, written
+ *   dq [n_tok,Hq,D] elem, rows dq_stride elements apart (>= Hq*D); rows behind q_begin[n_req] are not written
+ *   dk, dv [n_kv,Hkv,D] elem, rows dk_stride / dv_stride apart (>= Hkv*D): key j of request r is row k_begin[r] + j, and the rows of
+ *     all its kv_len[r] keys are written, with zeros where no row sees the key; other rows are not.  Requests that share a page
+ *     have gradients of their own for its keys.
+ *   k_begin [n_req] int32, DEVICE, or NULL: rows go by q_begin, which needs kv_len[r] = q_begin[r+1] - q_begin[r] (all of a
+ *     request's keys are of this pass).  Ranges of requests may not overlap.  A range outside [0, n_kv), or keys that are not all
+ *     of this pass without k_begin, leave the request out (CASCADE_ERR_BAD_PAGE).
+ *   q, out, d_out, scratch, dq, dk, dv 16-byte aligned, strides multiples of 16 bytes, at most 2^40.  No output overlaps another
+ *   (rows may lie between each other: parts of one stacked gradient) or an input (CASCADE_ERR_INVALID_ARG).
+ * A row that sees no key has dq = 0.  What lies at keys that a row does not see reaches neither its gradient nor, from rows that
+ * do not see it, a key's.  Keys of a page outside the pool count as not seen, by rows that are summed again key by key
+ * (CASCADE_ERR_BAD_PAGE); their dk and dv are zeros.  A row or key whose result is not finite is summed again the same way.
+ * Statistics, sums and accumulators are fp32.  Results do not depend on the order of additions. */
+int cascade_paged_attn_grad(cascade_ctx* ctx, const cascade_paged_cache* cache, int32_t n_req, int32_t n_tok, const void* q,
+                            int64_t q_stride, const int32_t* q_begin, const int32_t* kv_len, int32_t max_q, int32_t max_kv,
+                            int32_t window, int32_t sinks, float softmax_scale, const void* out, const float* lse,
+                            const void* d_out, float* scratch, void* dq, int64_t dq_stride, void* dk, int64_t dk_stride, void* dv,
+                            int64_t dv_stride, int32_t n_kv, const int32_t* k_begin, void* stream);
 
 /* ---- one token a row ------------------------------------------------------------------------------- */
 /* Draws a token from every row of logits (a drafter's proposals, or plain decoding), with the truncations of

@@ -33,7 +33,7 @@ EXPORTS = [
     "cascade_filter_logits", "cascade_set_wait_limit", "cascade_wait_probe",
     "cascade_tree_update_device", "cascade_tree_download", "cascade_drafter_loss",
     "cascade_paged_tables", "cascade_paged_append", "cascade_paged_attn", "cascade_sample",
-    "cascade_distill_loss", "cascade_distill_grad",
+    "cascade_paged_attn_grad", "cascade_distill_loss", "cascade_distill_grad",
 ]
 
 
@@ -124,6 +124,8 @@ def lib() -> C.CDLL:
         L.cascade_paged_append.argtypes = [vp, cache, i32, vp, i64, vp, i64, vp, i64, vp, vp, f32, vp, i64, vp]
         L.cascade_paged_attn.argtypes = [vp, cache, i32, i32, vp, i64, vp, vp, i32, i32, i32, i32, f32, vp, vp, vp]
         L.cascade_sample.argtypes = [vp, vp, i32, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.cascade_paged_attn_grad.argtypes = [vp, cache, i32, i32, vp, i64, vp, vp, i32, i32, i32, i32, f32, vp, vp, vp, vp, vp, i64, vp,
+                                              i64, vp, i64, i32, vp, vp]
         L.cascade_distill_loss.argtypes = [vp, i32, i64, vp, vp, i32, vp, vp, vp, i32, i32, i32, f32, f32, f32, vp, vp, vp, vp]
         L.cascade_distill_grad.argtypes = [vp, i32, i64, vp, vp, i32, vp, vp, f32, i32, i32, f32, vp, i64, vp]
         L.cascade_set_wait_limit.argtypes = [vp, C.c_int64]
@@ -540,6 +542,26 @@ def _dense(name, t, dtype, shape):
     if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: expected a dense {dtype} tensor {shape}, got {t.dtype} {tuple(t.shape)}")
     return t.data_ptr()
+
+
+def cascade_paged_attn_grad(ctx, cache, q, q_begin, kv_len, max_q, max_kv, out, lse, d_out, scratch, dq, dk, dv, softmax_scale, window=0,
+                            sinks=0, k_begin=None):
+    """The gradient of cascade_paged_attn; rows of dq, dk and dv may lie apart.  scratch: float32 [n_tok,Hq,2]."""
+    cache._check(ctx)
+    sh, e, n_req, n, n_kv = ctx.shape, cache.dtype, kv_len.shape[0], q.shape[0], dk.shape[0]
+    Hq, Hkv, D = sh.Hq, sh.Hkv, sh.D
+    begin_p, kv_p = _vector("q_begin", q_begin, torch.int32, n_req + 1), _vector("kv_len", kv_len, torch.int32, n_req)
+    at_p = _vector("k_begin", k_begin, torch.int32, n_req)
+    if cache.n_req < n_req:
+        raise ValueError(f"block_table has {cache.n_req} rows for {n_req} requests")
+    qs, dqs = _rows("q", q, n, Hq, D, e), _rows("dq", dq, n, Hq, D, e)
+    dks, dvs = _rows("dk", dk, n_kv, Hkv, D, e), _rows("dv", dv, n_kv, Hkv, D, e)
+    out_p, d_out_p = _dense("out", out, e, (n, Hq, D)), _dense("d_out", d_out, e, (n, Hq, D))
+    lse_p, scratch_p = _dense("lse", lse, torch.float32, (n, Hq)), _dense("scratch", scratch, torch.float32, (n, Hq, 2))
+    stream = _on_device(cache.k_pages, cache.v_pages, cache.block_table, q, q_begin, kv_len, out, lse, d_out, scratch, dq, dk, dv, k_begin)
+    _check(lib().cascade_paged_attn_grad(ctx.handle, cache.ref, n_req, n, q.data_ptr(), qs, begin_p, kv_p, max_q, max_kv, window, sinks,
+                                         softmax_scale, out_p, lse_p, d_out_p, scratch_p, dq.data_ptr(), dqs, dk.data_ptr(), dks,
+                                         dv.data_ptr(), dvs, n_kv, at_p, stream))
 
 
 def cascade_distill_loss(draft_logits, top_logits, top_ids, loss, saved, total=None, target_lse=None, feat=None, seq=None,

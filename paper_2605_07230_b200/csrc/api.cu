@@ -155,7 +155,7 @@ const char* cascade_kernel_name(int32_t id) {
                                 "head_f32", "row_stats", "row_lse", "similarity", "accept", "tail", "select_path",
                                 "embed_norm", "gemm_qkv", "rope_split", "gemm_o", "resid_norm", "gemm_gate_up",
                                 "swiglu", "gemm_down", "gemm_f32", "resid_add", "kv_append", "bonus_token", "filter_logits", "wait_probe", "build_tree",
-                                "paged_tables", "paged_append", "paged_attn", "sample"};
+                                "paged_tables", "paged_append", "paged_attn", "sample", "paged_grad_stats", "paged_grad"};
   static_assert(sizeof(names) / sizeof(names[0]) == K_KERNEL_ID_END, "one name per kernel id");
   if (id < 0 || id >= K_KERNEL_ID_END) return nullptr;
   return names[id];
