@@ -66,9 +66,11 @@ __device__ __forceinline__ long long key_offset(const PagedAttnArgs& a, int r, i
   return (long long)page * a.page_stride + ((long long)(j % a.page_size) * a.Hkv + kh) * D;
 }
 
-// One warp, one row and head, from the definition: only keys that the row sees are read.  Lane l holds elements l, l + 32, ...
+// One warp, one row and head, from the definition: only keys that the row sees are read.  Lane l holds elements l, l + 32, ..., of
+// which those of groups e0 .. e1 - 1 are written.
 template <typename E, int D>
-__device__ void grad_row(const PagedGradArgs& p, int r, int row, int x, int head, int lane, volatile uint64_t* alive = nullptr) {
+__device__ void grad_row(const PagedGradArgs& p, int r, int row, int x, int head, int lane, int e0 = 0, int e1 = D / 32,
+                         volatile uint64_t* alive = nullptr) {
   constexpr int kE = D / 32;
   const PagedAttnArgs& a = p.a;
   const int kh = head / (a.Hq / a.Hkv);
@@ -101,11 +103,12 @@ __device__ void grad_row(const PagedGradArgs& p, int r, int row, int x, int head
   }
   E* to = static_cast<E*>(p.dq) + (long long)row * p.dq_stride + head * D;
 #pragma unroll
-  for (int e = 0; e < kE; ++e) store_elem(to + e * 32 + lane, a.scale * dq[e]);
+  for (int e = 0; e < kE; ++e)
+    if (e >= e0 && e < e1) store_elem(to + e * 32 + lane, a.scale * dq[e]);
 }
 
-// One warp, one key and key head, from the definition: only rows that see the key are read.
-template <typename E, int D>
+// One warp, one key and key head, from the definition: only rows that see the key are read.  kDk, kDv: which gradients to write.
+template <typename E, int D, bool kDk = true, bool kDv = true>
 __device__ void grad_key(const PagedGradArgs& p, int r, const GradRequest& rq, int j, int kh, int lane, volatile uint64_t* alive = nullptr) {
   constexpr int kE = D / 32;
   const PagedAttnArgs& a = p.a;
@@ -146,12 +149,12 @@ __device__ void grad_key(const PagedGradArgs& p, int r, const GradRequest& rq, i
   const long long to = (long long)rq.k0 + j;
 #pragma unroll
   for (int e = 0; e < kE; ++e) {
-    store_elem(static_cast<E*>(p.dk) + to * p.dk_stride + kh * D + e * 32 + lane, a.scale * dk[e]);
-    store_elem(static_cast<E*>(p.dv) + to * p.dv_stride + kh * D + e * 32 + lane, dv[e]);
+    if (kDk) store_elem(static_cast<E*>(p.dk) + to * p.dk_stride + kh * D + e * 32 + lane, a.scale * dk[e]);
+    if (kDv) store_elem(static_cast<E*>(p.dv) + to * p.dv_stride + kh * D + e * 32 + lane, dv[e]);
   }
 }
 
 }  // namespace paged
 
-// paged_grad_f32.cu: tiles in shared memory, packed fp32 multiply-adds (queries' gradients, then keys' and values').
+// paged_grad_f32.cu: tiles in shared memory, packed fp32 multiply-adds (the fp32 type).
 int launch_paged_grad_f32(cascade_ctx* ctx, const PagedGradArgs& p, cudaStream_t s);

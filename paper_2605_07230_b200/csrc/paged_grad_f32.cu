@@ -20,11 +20,6 @@ struct Cfg {
 };
 
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
-  const uint2 v = *reinterpret_cast<const uint2*>(p);
-  return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
-}
-
 // s[i][j] = sum_d x[ty + 16 i][d] y[tx + 16 j][d]
 template <int D>
 __device__ __forceinline__ void scores(const float* x, const float* y, int tx, int ty, float (&s)[4][4]) {
@@ -77,7 +72,7 @@ __device__ __forceinline__ void outputs(const float* w, const float* x, int mx, 
   }
 }
 
-template <typename E, int D>
+template <int D>
 struct Tile {
   float *a, *b, *c, *d;       // [kT][D + 4] each
   float *w, *e;               // [kT][kSp]: weights and their gradients
@@ -96,8 +91,8 @@ struct Tile {
 };
 
 // Rows first .. first + 63 of (token, head of the group) of a key head: queries and output gradients, zeros behind the last.
-template <typename E, int D>
-__device__ __forceinline__ void load_rows(const PagedGradArgs& p, int q0, int kh, int G, int first, int n_rows, const Tile<E, D>& t) {
+template <int D>
+__device__ __forceinline__ void load_rows(const PagedGradArgs& p, int q0, int kh, int G, int first, int n_rows, const Tile<D>& t) {
   const PagedAttnArgs& a = p.a;
   for (int i = threadIdx.x; i < kT * (D / 4); i += kThreads) {
     const int row = i / (D / 4), col = i % (D / 4) * 4, rr = first + row;
@@ -105,8 +100,8 @@ __device__ __forceinline__ void load_rows(const PagedGradArgs& p, int q0, int kh
     if (rr < n_rows) {
       const long long token = q0 + rr / G;
       const int head = kh * G + rr % G;
-      q = load4(static_cast<const E*>(a.q) + token * a.q_stride + head * D + col);
-      g = load4(static_cast<const E*>(p.d_out) + (token * a.Hq + head) * D + col);
+      q = load4(static_cast<const float*>(a.q) + token * a.q_stride + head * D + col);
+      g = load4(static_cast<const float*>(p.d_out) + (token * a.Hq + head) * D + col);
     }
     paged::store4(t.a + row * Cfg<D>::kRow + col, q);
     paged::store4(t.b + row * Cfg<D>::kRow + col, g);
@@ -120,15 +115,15 @@ __device__ __forceinline__ void load_rows(const PagedGradArgs& p, int q0, int kh
   }
 }
 // Keys first .. first + 63 of a request and their values, zeros where there is none; there[] tells which.
-template <typename E, int D>
-__device__ __forceinline__ void load_keys(const PagedAttnArgs& a, int r, int kh, int first, int kv, const Tile<E, D>& t, uint8_t* there) {
+template <int D>
+__device__ __forceinline__ void load_keys(const PagedAttnArgs& a, int r, int kh, int first, int kv, const Tile<D>& t, uint8_t* there) {
   for (int i = threadIdx.x; i < kT * (D / 4); i += kThreads) {
     const int row = i / (D / 4), col = i % (D / 4) * 4, j = first + row;
     const long long off = j < kv ? paged::key_offset(a, r, j, kh, D) : -1;
     float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
     if (off >= 0) {
-      k = load4(static_cast<const E*>(a.k) + off + col);
-      v = load4(static_cast<const E*>(a.v) + off + col);
+      k = load4(static_cast<const float*>(a.k) + off + col);
+      v = load4(static_cast<const float*>(a.v) + off + col);
     }
     paged::store4(t.c + row * Cfg<D>::kRow + col, k);
     paged::store4(t.d + row * Cfg<D>::kRow + col, v);
@@ -137,8 +132,8 @@ __device__ __forceinline__ void load_keys(const PagedAttnArgs& a, int r, int kh,
 }
 
 // Results of four rows a thread; a row that is not finite is noted in odd[].
-template <typename E, int D>
-__device__ __forceinline__ void store_out(E* to, long long stride, const uint64_t (&o)[4][D / 32], float by, int mx, int my, int n, uint32_t* odd) {
+template <int D>
+__device__ __forceinline__ void store_out(float* to, long long stride, const uint64_t (&o)[4][D / 32], float by, int mx, int my, int n, uint32_t* odd) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = 4 * my + i;
@@ -154,12 +149,12 @@ __device__ __forceinline__ void store_out(E* to, long long stride, const uint64_
   }
 }
 
-template <typename E, int D>
+template <int D>
 __global__ void __launch_bounds__(kThreads) k_paged_grad_kv_f32(const PagedGradArgs p) {
   extern __shared__ __align__(16) float smem[];
   __shared__ uint8_t there[kT];
   __shared__ uint32_t odd[2];
-  const Tile<E, D> t(smem);
+  const Tile<D> t(smem);
   const PagedAttnArgs& a = p.a;
   const int G = a.Hq / a.Hkv, kh = blockIdx.x % a.Hkv, k_first = blockIdx.x / a.Hkv * kT, r = blockIdx.y;
   paged::GradRequest rq;
@@ -167,7 +162,7 @@ __global__ void __launch_bounds__(kThreads) k_paged_grad_kv_f32(const PagedGradA
   const int n_keys = min(kT, rq.kv - k_first), x0 = rq.kv - rq.nq;
   const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
   if (threadIdx.x < 2) odd[threadIdx.x] = 0u;
-  load_keys<E, D>(a, r, kh, k_first, rq.kv, t, there);
+  load_keys<D>(a, r, kh, k_first, rq.kv, t, there);
   uint64_t dk[4][D / 32], dv[4][D / 32];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -177,7 +172,7 @@ __global__ void __launch_bounds__(kThreads) k_paged_grad_kv_f32(const PagedGradA
   paged::tokens_that_see(a, x0, rq.nq, k_first, k_first + n_keys - 1, &lo, &hi);
   for (int first = lo * G; first < hi * G; first += kT) {
     __syncthreads();
-    load_rows<E, D>(p, rq.q0, kh, G, first, hi * G, t);
+    load_rows<D>(p, rq.q0, kh, G, first, hi * G, t);
     __syncthreads();
     float s[4][4], g[4][4];
     scores<D>(t.a, t.c, tx, ty, s);
@@ -190,7 +185,7 @@ __global__ void __launch_bounds__(kThreads) k_paged_grad_kv_f32(const PagedGradA
       for (int j = 0; j < 4; ++j) {
         const int key = tx + 16 * j;
         const bool see = first + row < hi * G && there[key] && paged::sees(a, x, k_first + key);
-        const float w = see ? paged::grad_weight<E>(s[i][j], a.scale, lse) : 0.f;
+        const float w = see ? paged::grad_weight<float>(s[i][j], a.scale, lse) : 0.f;
         t.w[row * kSp + key] = w;
         t.e[row * kSp + key] = see ? w * (g[i][j] - delta) : 0.f;
       }
@@ -201,20 +196,20 @@ __global__ void __launch_bounds__(kThreads) k_paged_grad_kv_f32(const PagedGradA
   }
   __syncthreads();
   const long long to = (long long)rq.k0 + k_first;
-  store_out<E, D>(static_cast<E*>(p.dk) + to * p.dk_stride + kh * D, p.dk_stride, dk, a.scale, tx, ty, n_keys, odd);
-  store_out<E, D>(static_cast<E*>(p.dv) + to * p.dv_stride + kh * D, p.dv_stride, dv, 1.f, tx, ty, n_keys, odd);
+  store_out<D>(static_cast<float*>(p.dk) + to * p.dk_stride + kh * D, p.dk_stride, dk, a.scale, tx, ty, n_keys, odd);
+  store_out<D>(static_cast<float*>(p.dv) + to * p.dv_stride + kh * D, p.dv_stride, dv, 1.f, tx, ty, n_keys, odd);
   __syncthreads();
   // (a value that is no number, or too large, at a row that another key of the tile sees)
   for (int key = threadIdx.x / 32; key < n_keys; key += kThreads / 32)
-    if (odd[key >> 5] >> (key & 31) & 1u) paged::grad_key<E, D>(p, r, rq, k_first + key, kh, threadIdx.x % 32);
+    if (odd[key >> 5] >> (key & 31) & 1u) paged::grad_key<float, D>(p, r, rq, k_first + key, kh, threadIdx.x % 32);
 }
 
-template <typename E, int D>
+template <int D>
 __global__ void __launch_bounds__(kThreads) k_paged_grad_q_f32(const PagedGradArgs p) {
   extern __shared__ __align__(16) float smem[];
   __shared__ uint8_t there[kT];
   __shared__ uint32_t odd[2];
-  const Tile<E, D> t(smem);
+  const Tile<D> t(smem);
   const PagedAttnArgs& a = p.a;
   const int G = a.Hq / a.Hkv, kh = blockIdx.x % a.Hkv, first = blockIdx.x / a.Hkv * kT, r = blockIdx.y;
   paged::GradRequest rq;
@@ -222,7 +217,7 @@ __global__ void __launch_bounds__(kThreads) k_paged_grad_q_f32(const PagedGradAr
   const int n_rows = min(kT, rq.nq * G - first), x0 = rq.kv - rq.nq;
   const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
   if (threadIdx.x < 2) odd[threadIdx.x] = 0u;
-  load_rows<E, D>(p, rq.q0, kh, G, first, rq.nq * G, t);
+  load_rows<D>(p, rq.q0, kh, G, first, rq.nq * G, t);
   uint64_t dq[4][D / 32];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -232,7 +227,7 @@ __global__ void __launch_bounds__(kThreads) k_paged_grad_q_f32(const PagedGradAr
   const int begin = paged::window_begin(max(x_first, 0), a.window), sink_end = min(a.sinks, begin);
   for (int k_first = sink_end > 0 ? 0 : begin / kT * kT; k_first <= x_last;) {
     __syncthreads();
-    load_keys<E, D>(a, r, kh, k_first, rq.kv, t, there);
+    load_keys<D>(a, r, kh, k_first, rq.kv, t, there);
     __syncthreads();
     float s[4][4], g[4][4];
     scores<D>(t.a, t.c, tx, ty, s);
@@ -245,7 +240,7 @@ __global__ void __launch_bounds__(kThreads) k_paged_grad_q_f32(const PagedGradAr
       for (int j = 0; j < 4; ++j) {
         const int key = tx + 16 * j;
         const bool see = row < n_rows && there[key] && paged::sees(a, x, k_first + key);
-        t.e[key * kSp + row] = see ? paged::grad_weight<E>(s[i][j], a.scale, lse) * (g[i][j] - delta) : 0.f;
+        t.e[key * kSp + row] = see ? paged::grad_weight<float>(s[i][j], a.scale, lse) * (g[i][j] - delta) : 0.f;
       }
     }
     __syncthreads();
@@ -258,7 +253,7 @@ __global__ void __launch_bounds__(kThreads) k_paged_grad_q_f32(const PagedGradAr
   for (int i = 0; i < 4; ++i) {
     const int row = 4 * ty + i;
     if (row >= n_rows) continue;
-    E* to = static_cast<E*>(p.dq) + (long long)(rq.q0 + (first + row) / G) * p.dq_stride + (kh * G + (first + row) % G) * D;
+    float* to = static_cast<float*>(p.dq) + (long long)(rq.q0 + (first + row) / G) * p.dq_stride + (kh * G + (first + row) % G) * D;
 #pragma unroll
     for (int m = 0; m < D / 64; ++m) {
       float4 v;
@@ -271,24 +266,24 @@ __global__ void __launch_bounds__(kThreads) k_paged_grad_q_f32(const PagedGradAr
   __syncthreads();
   for (int row = threadIdx.x / 32; row < n_rows; row += kThreads / 32)
     if (odd[row >> 5] >> (row & 31) & 1u)
-      paged::grad_row<E, D>(p, r, rq.q0 + (first + row) / G, x0 + (first + row) / G, kh * G + (first + row) % G, threadIdx.x % 32);
+      paged::grad_row<float, D>(p, r, rq.q0 + (first + row) / G, x0 + (first + row) / G, kh * G + (first + row) % G, threadIdx.x % 32);
 }
 
-template <typename E, int D>
+template <int D>
 int launch(cascade_ctx* ctx, const PagedGradArgs& p, cudaStream_t s) {
   const PagedAttnArgs& a = p.a;
   const int G = a.Hq / a.Hkv;
   const long long kv_blocks = ((long long)a.max_kv + kT - 1) / kT * a.Hkv, q_blocks = ((long long)a.max_q * G + kT - 1) / kT * a.Hkv;
   if (kv_blocks > INT_MAX || q_blocks > INT_MAX) return CASCADE_ERR_UNSUPPORTED_SHAPE;
-  CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_KV, k_paged_grad_kv_f32<E, D>, Cfg<D>::kSmem));
-  CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_Q, k_paged_grad_q_f32<E, D>, Cfg<D>::kSmem));
+  CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_KV, k_paged_grad_kv_f32<D>, Cfg<D>::kSmem));
+  CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_Q, k_paged_grad_q_f32<D>, Cfg<D>::kSmem));
   if (kv_blocks > 0) {
     KernelScope ks(ctx, K_PAGED_GRAD, s);
-    k_paged_grad_kv_f32<E, D><<<dim3((unsigned)kv_blocks, a.n_req), kThreads, Cfg<D>::kSmem, s>>>(p);
+    k_paged_grad_kv_f32<D><<<dim3((unsigned)kv_blocks, a.n_req), kThreads, Cfg<D>::kSmem, s>>>(p);
     CASCADE_CUDA_TRY(cudaGetLastError());
   }
   KernelScope ks(ctx, K_PAGED_GRAD, s);
-  k_paged_grad_q_f32<E, D><<<dim3((unsigned)q_blocks, a.n_req), kThreads, Cfg<D>::kSmem, s>>>(p);
+  k_paged_grad_q_f32<D><<<dim3((unsigned)q_blocks, a.n_req), kThreads, Cfg<D>::kSmem, s>>>(p);
   CASCADE_CUDA_TRY(cudaGetLastError());
   return CASCADE_OK;
 }
@@ -296,6 +291,5 @@ int launch(cascade_ctx* ctx, const PagedGradArgs& p, cudaStream_t s) {
 }  // namespace
 
 int launch_paged_grad_f32(cascade_ctx* ctx, const PagedGradArgs& p, cudaStream_t s) {
-  if (ctx->shape.dtype == CASCADE_BF16) return ctx->shape.D == 128 ? launch<__nv_bfloat16, 128>(ctx, p, s) : launch<__nv_bfloat16, 64>(ctx, p, s);
-  return ctx->shape.D == 128 ? launch<float, 128>(ctx, p, s) : launch<float, 64>(ctx, p, s);
+  return ctx->shape.D == 128 ? launch<128>(ctx, p, s) : launch<64>(ctx, p, s);
 }

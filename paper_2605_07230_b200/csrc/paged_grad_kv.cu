@@ -1,0 +1,429 @@
+// Keys' and values' gradients of the paged attention on the tensor cores (bf16).
+//
+// A work item is a tile of 128 keys of one (request, key head) and all row blocks (128 rows: token, query head of the group) that
+// see any of them.  One CTA an SM works through items that a counter hands out.  With rows on the columns, per block:
+//     S^T = K Q^T      P^T = 2^(c S^T - lse)      dP^T = V dO^T      dS^T = P^T (dP^T - delta)      dV += P^T dO      dK += dS^T Q
+// S^T, dP^T, dV and dK fill the tensor memory (4 x 128 columns at D = 128); P^T and dS^T go back as bf16 over their own scores
+// and are the products' operand from there.  The products of one block alternate with the next block's scores:
+//     dV, S^T of the next block  beside the computation of dS^T;   dK, dP^T of the next block  beside that of P^T
+//   * warp 8 loads keys and values once an item, queries through three stages (the next block's are wanted right behind the
+//     product that frees a stage) and output gradients through two;
+//   * warp 9 issues the products;  warp 10 brings the rows' statistics;
+//   * warps 0-7: a key per lane, half of a block's rows each; P stays in registers between the two halves of the work.
+#include <climits>
+
+#include "paged_grad_tc.cuh"
+
+namespace {
+
+using namespace grad_tc;
+
+struct Shared {
+  uint64_t kv_full, kv_empty, q_full[3], q_empty[3], do_full[2], do_empty[2], s_full, p_full, dp_full, ds_full, acc_full, acc_empty, stat_full[2],
+      stat_empty[2];
+  Queue queue;
+  uint64_t alive;
+  int abort_flag;
+  uint32_t tmem;
+  __align__(16) float lse[2][kTile], delta[2][kTile];                  // negated
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do, const __grid_constant__ CUtensorMap tm_k,
+                const __grid_constant__ CUtensorMap tm_v, const Args p) {
+  using C = Cfg<D>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  Shared& sh = *reinterpret_cast<Shared*>(smem + C::kTiles * C::kTileBytes);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t base = ptx::smem_u32(smem);
+  // tiles: keys, values, queries of three stages, output gradients of two
+  constexpr int kQ = 2, kDo = 5;
+  auto tile = [&](int i) { return base + i * C::kTileBytes; };
+  const PagedAttnArgs& a = p.g.a;
+  if ((base & 1023u) != 0) {                                           // (the same in all threads of all CTAs)
+    if (threadIdx.x == 0) atomicOr(a.err, CASCADE_DEV_ERR_WAIT);
+    return;
+  }
+  const Waits wait = {&sh.abort_flag, &sh.alive, a.err, a.wait_ns};
+
+  if (threadIdx.x == 0) {
+    for (uint64_t* b : {&sh.kv_full, &sh.kv_empty, &sh.s_full, &sh.dp_full, &sh.acc_full}) ptx::mbar_init(b, 1);
+    for (uint64_t* b : {&sh.p_full, &sh.ds_full, &sh.acc_empty}) ptx::mbar_init(b, kComputeWarps);
+    for (int i = 0; i < 3; ++i) {
+      ptx::mbar_init(&sh.q_full[i], 1);
+      ptx::mbar_init(&sh.q_empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      for (uint64_t* b : {&sh.do_full[i], &sh.do_empty[i], &sh.stat_full[i], &sh.queue.full[i]}) ptx::mbar_init(b, 1);
+      ptx::mbar_init(&sh.stat_empty[i], kComputeWarps);
+      ptx::mbar_init(&sh.queue.empty[i], kWarps);
+    }
+    sh.abort_flag = 0;
+    sh.alive = 0;
+    ptx::fence_mbar_init();
+  }
+  const int block_rows = p.tpb * p.G;
+  if (block_rows < kTile && warp < kComputeWarps) {                    // rows that no load ever fills
+    for (int i = kQ; i < C::kTiles; ++i) clear_rows<D>(tile(i), block_rows, kTile, threadIdx.x);
+    ptx::fence_proxy_async_smem();
+  }
+  if (warp == kLoads && lane == 0) {
+    ptx::prefetch_tmap(&tm_q);
+    ptx::prefetch_tmap(&tm_do);
+    ptx::prefetch_tmap(&tm_k);
+    ptx::prefetch_tmap(&tm_v);
+  }
+  if (warp == kProducts) {
+    ptx::tmem_alloc(&sh.tmem, 512);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t t_s = sh.tmem, t_dp = t_s + 128, t_dv = t_s + 256, t_dk = t_dv + D;
+
+  Cursor<true> cur;
+  paged::GradRequest rq = {};
+  int r = 0, head = 0, line = 0;
+  uint32_t turn = 0;                                                   // items that this warp has taken
+  auto next = [&]() {
+    const uint32_t slot = turn & 1u, use = turn >> 1;
+    ++turn;
+    const bool here = wait(&sh.queue.full[slot], use);
+    const int item = here ? *static_cast<volatile int*>(&sh.queue.answer[slot]) : INT_MAX;
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(&sh.queue.empty[slot]);
+    return __shfl_sync(0xffffffffu, item, 0);
+  };
+  // row blocks of the item: the first and how many
+  auto blocks = [&](int* first) {
+    int lo, hi;
+    paged::tokens_that_see(a, rq.kv - rq.nq, rq.nq, line * kTile, min(rq.kv, (line + 1) * kTile) - 1, &lo, &hi);
+    *first = lo / p.tpb;
+    return hi > lo ? (hi - 1) / p.tpb - *first + 1 : 0;
+  };
+  uint32_t used = 0, blk = 0;                                          // items with blocks, and blocks, so far
+  Ring<3> ring;                                                        // the queries' stages
+  bool ok = true;
+  int first;
+
+  if (warp == kLoads) {
+    const Box box(p, lane);
+    const uint32_t box_bytes = (uint32_t)p.box_rows * 128u, row_bytes = (uint32_t)block_rows * 128u * C::kHalves;
+    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &rq, &r, &head, &line); item = next()) {
+      const int granted = lane == 0 ? (int)gridDim.x + atomicAdd(p.taken, 1) : 0;
+      const int n = blocks(&first);
+      auto load_rows = [&](int i, const CUtensorMap* m, uint64_t* full, uint64_t* empty, uint32_t ph, int to) {
+        ok = ok && wait(empty, ph ^ 1u);
+        ok = __all_sync(0xffffffffu, ok);
+        if (ok && lane == 0) {
+          ptx::mbar_arrive_expect_tx(full, row_bytes);
+          for (int h = 0; h < C::kHalves; ++h)
+            ptx::tma_load_4d(smem + to * C::kTileBytes + h * (kTile * 128), m, h * 64, 0, head, rq.q0 + (first + i) * p.tpb, full);
+        }
+      };
+      auto load_q = [&](int i) {
+        load_rows(i, &tm_q, &sh.q_full[ring.stage], &sh.q_empty[ring.stage], ring.ph, kQ + ring.stage);
+        ring.step();
+      };
+      if (n > 0) {
+        int row;
+        bool bad = false;
+        const int page = box.page(p, a.block_table + (size_t)r * a.table_stride, line * kTile, rq.kv, C::kHalves, &row, &bad);
+        load_q(0);
+        ok = ok && wait(&sh.kv_empty, used ^ 1u);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        const uint32_t bytes = 2u * box_bytes * (uint32_t)__popc(__ballot_sync(0xffffffffu, page >= 0));
+        if (lane == 0) ptx::mbar_arrive_expect_tx(&sh.kv_full, bytes);
+        __syncwarp();
+        if (page >= 0)
+          for (int kv = 0; kv < 2; ++kv)
+            ptx::tma_load_4d(smem + kv * C::kTileBytes + box.half * (kTile * 128) + box.i * box_bytes, kv == 0 ? &tm_k : &tm_v, box.half * 64, head,
+                             row, page, &sh.kv_full);
+        ++used;
+        for (int i = 0; ok && i < n; ++i) {
+          if (i > 0) load_q(i);
+          const uint32_t stage = (blk + i) & 1u;
+          load_rows(i, &tm_do, &sh.do_full[stage], &sh.do_empty[stage], (blk + i) >> 1, kDo + stage);
+        }
+        blk += n;
+      }
+      const uint32_t slot = turn & 1u, use = turn >> 1;
+      ok = ok && wait(&sh.queue.empty[slot], use ^ 1u);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      if (lane == 0) {
+        *static_cast<volatile int*>(&sh.queue.answer[slot]) = granted;
+        ptx::mbar_arrive(&sh.queue.full[slot]);
+      }
+    }
+    // everything has been given back before the CTA may end (the arrivals are asynchronous)
+    if (used > 0) ok = ok && wait(&sh.kv_empty, used ^ 1u);
+    for (uint32_t i = 0; i < 2; ++i) ok = ok && wait(&sh.do_empty[(blk + i) & 1u], ((blk + i) >> 1) ^ 1u);
+    for (uint32_t i = 0; i < 3; ++i, ring.step()) ok = ok && wait(&sh.q_empty[ring.stage], ring.ph ^ 1u);
+  } else if (warp == kProducts) {
+    const uint32_t idesc_s = ptx::umma_idesc_bf16(128, 128), idesc_o = ptx::umma_idesc_bf16_b_mn(128, D);
+    const uint64_t desc = ptx::umma_desc_sw128(base), desc_mn = ptx::umma_desc_sw128_strides(base, kTile * 128, 1024);
+    auto lo = [&](int i) { return (uint32_t)desc + i * (C::kTileBytes >> 4); };
+    auto lo_mn = [&](int i) { return (uint32_t)desc_mn + i * (C::kTileBytes >> 4); };
+    Ring<3> behind;                                                    // the stage of the block whose last product comes next
+    auto scores = [&]() {
+      if (!(ok = wait(&sh.q_full[ring.stage], ring.ph))) return;
+      product_ss<D>(t_s, lo(0), lo(kQ + ring.stage), desc, idesc_s);
+      ptx::umma_commit(&sh.s_full);
+      ring.step();
+    };
+    auto d_weights = [&](uint32_t b) {
+      if (!(ok = wait(&sh.do_full[b & 1u], b >> 1))) return;
+      product_ss<D>(t_dp, lo(1), lo(kDo + (b & 1u)), desc, idesc_s);
+      ptx::umma_commit(&sh.dp_full);
+    };
+    auto work = [&](int n) {
+      if (!(ok = wait(&sh.kv_full, used))) return;
+      ptx::tc_fence_after();
+      scores();
+      if (!ok) return;
+      d_weights(blk);
+      if (!ok) return;
+      if (n == 1) ptx::umma_commit(&sh.kv_empty);
+#pragma unroll 1
+      for (int i = 0; i < n; ++i) {
+        const uint32_t b = blk + i;
+        if (i == 0 && !(ok = wait(&sh.acc_empty, used ^ 1u))) return;
+        if (!(ok = wait(&sh.p_full, b))) return;
+        ptx::tc_fence_after();
+        product_ts(t_dv, t_s, lo_mn(kDo + (b & 1u)), desc_mn, idesc_o, i == 0);
+        ptx::umma_commit(&sh.do_empty[b & 1u]);
+        if (i + 1 < n) scores();
+        if (!ok || !(ok = wait(&sh.ds_full, b))) return;
+        ptx::tc_fence_after();
+        product_ts(t_dk, t_dp, lo_mn(kQ + behind.stage), desc_mn, idesc_o, i == 0);
+        ptx::umma_commit(&sh.q_empty[behind.stage]);
+        behind.step();
+        if (i + 1 < n) {
+          d_weights(b + 1);
+          if (!ok) return;
+          if (i + 2 == n) ptx::umma_commit(&sh.kv_empty);
+        }
+      }
+      ptx::umma_commit(&sh.acc_full);
+    };
+    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &rq, &r, &head, &line); item = next()) {
+      const int n = blocks(&first);
+      if (n == 0) continue;
+      if (lane == 0) work(n);
+      ok = __shfl_sync(0xffffffffu, ok, 0);
+      ++used;
+      blk += n;
+    }
+  } else if (warp == kStats) {
+    int tok[kTile / 32], g[kTile / 32];                                // token and head of rows lane, lane + 32, ...
+#pragma unroll
+    for (int m = 0; m < kTile / 32; ++m) {
+      tok[m] = (lane + 32 * m) / p.G;
+      g[m] = (lane + 32 * m) % p.G;
+    }
+    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &rq, &r, &head, &line); item = next()) {
+      const int n = blocks(&first);
+      for (int i = 0; ok && i < n; ++i, ++blk) {
+        float2 st[kTile / 32];
+#pragma unroll
+        for (int m = 0; m < kTile / 32; ++m) {
+          const int t = (first + i) * p.tpb + tok[m];
+          st[m] = make_float2(0.f, 0.f);
+          if (tok[m] < p.tpb && t < rq.nq) st[m] = p.g.stats[(long long)(rq.q0 + t) * a.Hq + head * p.G + g[m]];
+        }
+        ok = wait(&sh.stat_empty[blk & 1u], (blk >> 1) ^ 1u);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+#pragma unroll
+        for (int m = 0; m < kTile / 32; ++m) {
+          sh.lse[blk & 1u][lane + 32 * m] = -st[m].x;
+          sh.delta[blk & 1u][lane + 32 * m] = -st[m].y;
+        }
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&sh.stat_full[blk & 1u]);
+      }
+    }
+  } else {
+    const int part = warp >> 2, key = threadIdx.x & (kTile - 1);       // which half of the rows; this lane's key
+    const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16, half_col = part * 64;
+    const uint32_t my_s = t_s + lane_addr + half_col, my_dp = t_dp + lane_addr + half_col;
+    const float c = a.scale * paged::kLog2e;
+    const uint64_t c2 = ptx::pack2(c, c);
+    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &rq, &r, &head, &line); item = next()) {
+      const int n = blocks(&first), j = line * kTile + key, x0 = rq.kv - rq.nq;
+      const int page = j < rq.kv ? a.block_table[(size_t)r * a.table_stride + j / a.page_size] : 0;
+      for (int i = 0; i < n; ++i) {
+        const uint32_t b = blk + i;
+        const int t0 = (first + i) * p.tpb, rows = min(p.tpb, rq.nq - t0) * p.G;
+        // rows of the block that see this lane's key: lo .. hi - 1
+        const int lo = min(max(j - x0 - t0, 0), p.tpb) * p.G;
+        int hi = rows;
+        if (a.window > 0 && j >= a.sinks) hi = min(rows, (int)min(max((long long)j + a.window - x0 - t0, 0ll), (long long)p.tpb) * p.G);
+        const bool masked = __any_sync(0xffffffffu, lo > (int)half_col || hi < (int)half_col + 64);
+        const uint32_t see[2] = {bits(lo - half_col, hi - half_col), bits(lo - half_col - 32, hi - half_col - 32)};
+        ok = wait(&sh.s_full, b) && wait(&sh.stat_full[b & 1u], b >> 1);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        ptx::tc_fence_after();
+        uint64_t w[32];                                                // weights of this lane's key, a pair of rows each
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          uint32_t v[32], pk[16];
+          load32(my_s + 32 * q, v);
+          const ulonglong2* lse = reinterpret_cast<const ulonglong2*>(&sh.lse[b & 1u][half_col + 32 * q]);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const ulonglong2 l = lse[k / 2];
+            float e0, e1;
+            ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), c2, k & 1 ? l.y : l.x), &e0, &e1);
+            e0 = ptx::ex2(e0);
+            e1 = ptx::ex2(e1);
+            if (masked) {
+              e0 = (see[q] >> (2 * k)) & 1u ? e0 : 0.f;
+              e1 = (see[q] >> (2 * k + 1)) & 1u ? e1 : 0.f;
+            }
+            w[16 * q + k] = ptx::pack2(e0, e1);
+            pk[k] = ptx::pack_bf16x2(e0, e1);
+          }
+          ptx::tmem_st16_async(my_s + 16 * q, pk);
+        }
+        if (rows < block_rows) {                                       // what the load has brought behind the request's rows
+          ok = wait(&sh.do_full[b & 1u], b >> 1);
+          if (ok) {
+            clear_rows<D>(tile(kDo + (b & 1u)), rows, block_rows, threadIdx.x);
+            clear_rows<D>(tile(kQ + ring.stage), rows, block_rows, threadIdx.x);
+            ptx::fence_proxy_async_smem();
+          }
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+        }
+        ptx::tmem_wait_st();
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&sh.p_full);
+        ok = wait(&sh.dp_full, b);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        ptx::tc_fence_after();
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          uint32_t v[32], pk[16];
+          load32(my_dp + 32 * q, v);
+          const ulonglong2* delta = reinterpret_cast<const ulonglong2*>(&sh.delta[b & 1u][half_col + 32 * q]);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const ulonglong2 d = delta[k / 2];
+            const uint64_t ds = mul2(w[16 * q + k], ptx::add2(ptx::pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), k & 1 ? d.y : d.x));
+            float e0, e1;
+            ptx::unpack2(ds, &e0, &e1);
+            if (masked) {                                              // (beside rows that do not exist anything may stand)
+              e0 = (see[q] >> (2 * k)) & 1u ? e0 : 0.f;
+              e1 = (see[q] >> (2 * k + 1)) & 1u ? e1 : 0.f;
+            }
+            pk[k] = ptx::pack_bf16x2(e0, e1);
+          }
+          ptx::tmem_st16_async(my_dp + 16 * q, pk);
+        }
+        ptx::tmem_wait_st();
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          ptx::mbar_arrive(&sh.ds_full);
+          ptx::mbar_arrive(&sh.stat_empty[b & 1u]);
+        }
+        ring.step();
+      }
+      if (!ok) break;
+      // ---- results: values' gradients by one half of the warps, keys' by the other ----
+      __nv_bfloat16* to = static_cast<__nv_bfloat16*>(part == 0 ? p.g.dv : p.g.dk) +
+                          ((long long)rq.k0 + j) * (part == 0 ? p.g.dv_stride : p.g.dk_stride) + head * D;
+      const float by = part == 0 ? 1.f : a.scale;
+      bool odd = page < 0 || page >= a.n_pages;
+      if (n > 0) {
+        ok = wait(&sh.acc_full, used);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        ptx::tc_fence_after();
+        ++used;
+        blk += n;
+      }
+      float bad = 0.f;
+#pragma unroll 1
+      for (int q = 0; q < D / 32; ++q) {
+        uint32_t v[32];
+        if (n > 0) {
+          load32((part == 0 ? t_dv : t_dk) + lane_addr + 32 * q, v);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) v[k] = 0u;
+        }
+#pragma unroll
+        for (int k = 0; k < 32; ++k) bad = fmaf(__uint_as_float(v[k]), 0.f, bad);   // NaN if any is not finite
+        if (j < rq.kv) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            uint32_t x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = ptx::pack_bf16x2(__uint_as_float(v[8 * k + 2 * e]) * by, __uint_as_float(v[8 * k + 2 * e + 1]) * by);
+            *reinterpret_cast<uint4*>(to + 32 * q + 8 * k) = make_uint4(x[0], x[1], x[2], x[3]);
+          }
+        }
+      }
+      if (n > 0) {
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&sh.acc_empty);
+      }
+      // a value that is no number, or too large, at a row that another key of the tile sees; a page outside the pool
+      odd = j < rq.kv && (odd || bad != 0.f);
+      __syncwarp();
+      for (uint32_t left = __ballot_sync(0xffffffffu, odd); left != 0u; left &= left - 1u) {
+        // (0.6 us a row: whoever waits meanwhile starts its limit anew)
+        const int k = line * kTile + (warp & 3) * 32 + __ffs(left) - 1;
+        if (part == 0)
+          paged::grad_key<__nv_bfloat16, D, false, true>(p.g, r, rq, k, head, lane, &sh.alive);
+        else
+          paged::grad_key<__nv_bfloat16, D, true, false>(p.g, r, rq, k, head, lane, &sh.alive);
+      }
+    }
+  }
+  __syncwarp();
+  if (*wait.abort_flag) __nanosleep(1000000);                          // copies still in flight
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  if (threadIdx.x == 0 && atomicAdd(p.taken + 1, 1) == (int)gridDim.x - 1) p.taken[0] = p.taken[1] = 0;
+  if (warp == kProducts) ptx::tmem_dealloc(t_s, 512);
+}
+
+template <int D>
+int launch(cascade_ctx* ctx, const Args& p, int grid, cudaStream_t s) {
+  const PagedAttnArgs& a = p.g.a;
+  CUtensorMap mq, mo;
+  const CUtensorMap *mk = page_map(ctx, p, D, a.k), *mv = page_map(ctx, p, D, a.v);
+  if (mk == nullptr || mv == nullptr || !row_map(&mq, p, D, a.q, a.q_stride) || !row_map(&mo, p, D, p.g.d_out, (long long)a.Hq * D))
+    return CASCADE_ERR_CUDA;
+  constexpr int kSmem = smem_bytes<D, Shared>();
+  CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_KV, k_paged_grad_kv<D>, kSmem));   // (a context has one D)
+  KernelScope ks(ctx, K_PAGED_GRAD, s);
+  k_paged_grad_kv<D><<<grid, kThreads, kSmem, s>>>(mq, mo, *mk, *mv, p);
+  CASCADE_CUDA_TRY(cudaGetLastError());
+  return CASCADE_OK;
+}
+
+}  // namespace
+
+int launch_paged_grad_kv(cascade_ctx* ctx, const grad_tc::Args& p, cudaStream_t s) {
+  const PagedAttnArgs& a = p.g.a;
+  // no more items than this: a request's tiles are at most ceil(keys / 128)
+  const long long tiles = (long long)p.g.n_kv / kTile + a.n_req, by_length = (long long)a.n_req * ((a.max_kv + kTile - 1) / kTile);
+  const long long items = (tiles < by_length ? tiles : by_length) * a.Hkv;
+  if (items > INT_MAX / 2) return CASCADE_ERR_UNSUPPORTED_SHAPE;
+  if (items == 0) return CASCADE_OK;
+  const int grid = (int)(items < ctx->sm_count ? items : ctx->sm_count);
+  return ctx->shape.D == 128 ? launch<128>(ctx, p, grid, s) : launch<64>(ctx, p, grid, s);
+}
