@@ -55,9 +55,12 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       ptx::mbar_init(&sh.q_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      for (uint64_t* b : {&sh.do_full[i], &sh.do_empty[i], &sh.stat_full[i], &sh.queue.full[i]}) ptx::mbar_init(b, 1);
+      for (uint64_t* b : {&sh.do_full[i], &sh.do_empty[i], &sh.stat_full[i]}) ptx::mbar_init(b, 1);
       ptx::mbar_init(&sh.stat_empty[i], kComputeWarps);
-      ptx::mbar_init(&sh.queue.empty[i], kWarps);
+    }
+    for (int i = 0; i < kSlots; ++i) {
+      ptx::mbar_init(&sh.queue.full[i], 1);
+      ptx::mbar_init(&sh.queue.empty[i], kWarps - 1);
     }
     sh.abort_flag = 0;
     sh.alive = 0;
@@ -83,84 +86,63 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   ptx::tc_fence_after();
   const uint32_t t_s = sh.tmem, t_dp = t_s + 128, t_dv = t_s + 256, t_dk = t_dv + D;
 
-  Cursor<true> cur;
-  paged::GradRequest rq = {};
-  int r = 0, head = 0, line = 0;
-  uint32_t turn = 0;                                                   // items that this warp has taken
-  auto next = [&]() {
-    const uint32_t slot = turn & 1u, use = turn >> 1;
-    ++turn;
-    const bool here = wait(&sh.queue.full[slot], use);
-    const int item = here ? *static_cast<volatile int*>(&sh.queue.answer[slot]) : INT_MAX;
-    __syncwarp();
-    if (lane == 0) ptx::mbar_arrive(&sh.queue.empty[slot]);
-    return __shfl_sync(0xffffffffu, item, 0);
-  };
-  // row blocks of the item: the first and how many
-  auto blocks = [&](int* first) {
-    int lo, hi;
-    paged::tokens_that_see(a, rq.kv - rq.nq, rq.nq, line * kTile, min(rq.kv, (line + 1) * kTile) - 1, &lo, &hi);
-    *first = lo / p.tpb;
-    return hi > lo ? (hi - 1) / p.tpb - *first + 1 : 0;
-  };
+  Turns turns;
   uint32_t used = 0, blk = 0;                                          // items with blocks, and blocks, so far
   Ring<3> ring;                                                        // the queries' stages
   bool ok = true;
-  int first;
 
   if (warp == kLoads) {
     const Box box(p, lane);
     const uint32_t box_bytes = (uint32_t)p.box_rows * 128u, row_bytes = (uint32_t)block_rows * 128u * C::kHalves;
-    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &rq, &r, &head, &line); item = next()) {
+    Cursor<true> cur;
+    Item it = {};
+    for (int item = blockIdx.x;;) {
+      const bool more = cur.find(p, item, lane, &it);
+      int lo, hi;                                                      // tokens that see any of the keys -> row blocks
+      paged::tokens_that_see(a, it.kv - it.nq, it.nq, it.line * kTile, min(it.kv, (it.line + 1) * kTile) - 1, &lo, &hi);
+      it.first = lo / p.tpb;
+      it.n = !more ? -1 : hi > lo ? (hi - 1) / p.tpb - it.first + 1 : 0;
+      if (!turns.tell(sh.queue, wait, it, lane, &ok) || !more) break;
       const int granted = lane == 0 ? (int)gridDim.x + atomicAdd(p.taken, 1) : 0;
-      const int n = blocks(&first);
       auto load_rows = [&](int i, const CUtensorMap* m, uint64_t* full, uint64_t* empty, uint32_t ph, int to) {
-        ok = ok && wait(empty, ph ^ 1u);
-        ok = __all_sync(0xffffffffu, ok);
+        ok = __all_sync(0xffffffffu, ok && wait(empty, ph ^ 1u));
         if (ok && lane == 0) {
           ptx::mbar_arrive_expect_tx(full, row_bytes);
           for (int h = 0; h < C::kHalves; ++h)
-            ptx::tma_load_4d(smem + to * C::kTileBytes + h * (kTile * 128), m, h * 64, 0, head, rq.q0 + (first + i) * p.tpb, full);
+            ptx::tma_load_4d(smem + to * C::kTileBytes + h * (kTile * 128), m, h * 64, 0, it.head, it.q0 + (it.first + i) * p.tpb, full);
         }
       };
       auto load_q = [&](int i) {
         load_rows(i, &tm_q, &sh.q_full[ring.stage], &sh.q_empty[ring.stage], ring.ph, kQ + ring.stage);
         ring.step();
       };
-      if (n > 0) {
+      if (it.n > 0) {
         int row;
         bool bad = false;
-        const int page = box.page(p, a.block_table + (size_t)r * a.table_stride, line * kTile, rq.kv, C::kHalves, &row, &bad);
+        const int page = box.page(p, a.block_table + (size_t)it.r * a.table_stride, it.line * kTile, it.kv, C::kHalves, &row, &bad);
         load_q(0);
-        ok = ok && wait(&sh.kv_empty, used ^ 1u);
-        ok = __all_sync(0xffffffffu, ok);
+        ok = __all_sync(0xffffffffu, ok && wait(&sh.kv_empty, used ^ 1u));
         if (!ok) break;
         const uint32_t bytes = 2u * box_bytes * (uint32_t)__popc(__ballot_sync(0xffffffffu, page >= 0));
         if (lane == 0) ptx::mbar_arrive_expect_tx(&sh.kv_full, bytes);
         __syncwarp();
         if (page >= 0)
           for (int kv = 0; kv < 2; ++kv)
-            ptx::tma_load_4d(smem + kv * C::kTileBytes + box.half * (kTile * 128) + box.i * box_bytes, kv == 0 ? &tm_k : &tm_v, box.half * 64, head,
-                             row, page, &sh.kv_full);
+            ptx::tma_load_4d(smem + kv * C::kTileBytes + box.half * (kTile * 128) + box.i * box_bytes, kv == 0 ? &tm_k : &tm_v, box.half * 64,
+                             it.head, row, page, &sh.kv_full);
         ++used;
-        for (int i = 0; ok && i < n; ++i) {
+        for (int i = 0; ok && i < it.n; ++i) {
           if (i > 0) load_q(i);
           const uint32_t stage = (blk + i) & 1u;
           load_rows(i, &tm_do, &sh.do_full[stage], &sh.do_empty[stage], (blk + i) >> 1, kDo + stage);
         }
-        blk += n;
+        if (!ok) break;
+        blk += it.n;
       }
-      const uint32_t slot = turn & 1u, use = turn >> 1;
-      ok = ok && wait(&sh.queue.empty[slot], use ^ 1u);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      if (lane == 0) {
-        *static_cast<volatile int*>(&sh.queue.answer[slot]) = granted;
-        ptx::mbar_arrive(&sh.queue.full[slot]);
-      }
+      item = __shfl_sync(0xffffffffu, granted, 0);
     }
     // everything has been given back before the CTA may end (the arrivals are asynchronous)
-    if (used > 0) ok = ok && wait(&sh.kv_empty, used ^ 1u);
+    ok = ok && wait(&sh.kv_empty, used ^ 1u);
     for (uint32_t i = 0; i < 2; ++i) ok = ok && wait(&sh.do_empty[(blk + i) & 1u], ((blk + i) >> 1) ^ 1u);
     for (uint32_t i = 0; i < 3; ++i, ring.step()) ok = ok && wait(&sh.q_empty[ring.stage], ring.ph ^ 1u);
   } else if (warp == kProducts) {
@@ -168,53 +150,56 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     const uint64_t desc = ptx::umma_desc_sw128(base), desc_mn = ptx::umma_desc_sw128_strides(base, kTile * 128, 1024);
     auto lo = [&](int i) { return (uint32_t)desc + i * (C::kTileBytes >> 4); };
     auto lo_mn = [&](int i) { return (uint32_t)desc_mn + i * (C::kTileBytes >> 4); };
+    const uint32_t leads = lane == 0;
+    auto here = [&](uint64_t* bar, uint32_t parity) { return ok = __all_sync(0xffffffffu, wait.spin(bar, parity)); };
     Ring<3> behind;                                                    // the stage of the block whose last product comes next
+    // (the tensor cores take few products ahead: between two of them nothing is waited for that could be waited for earlier)
+    auto queries_here = [&]() { return here(&sh.q_full[ring.stage], ring.ph); };
+    auto gradients_here = [&](uint32_t b) { return here(&sh.do_full[b & 1u], b >> 1); };
     auto scores = [&]() {
-      if (!(ok = wait(&sh.q_full[ring.stage], ring.ph))) return;
-      product_ss<D>(t_s, lo(0), lo(kQ + ring.stage), desc, idesc_s);
-      ptx::umma_commit(&sh.s_full);
+      product_ss<D>(leads, t_s, lo(0), lo(kQ + ring.stage), desc, idesc_s);
+      ptx::umma_commit_if(leads, &sh.s_full);
       ring.step();
     };
     auto d_weights = [&](uint32_t b) {
-      if (!(ok = wait(&sh.do_full[b & 1u], b >> 1))) return;
-      product_ss<D>(t_dp, lo(1), lo(kDo + (b & 1u)), desc, idesc_s);
-      ptx::umma_commit(&sh.dp_full);
+      product_ss<D>(leads, t_dp, lo(1), lo(kDo + (b & 1u)), desc, idesc_s);
+      ptx::umma_commit_if(leads, &sh.dp_full);
     };
     auto work = [&](int n) {
-      if (!(ok = wait(&sh.kv_full, used))) return;
+      if (!queries_here() || !here(&sh.kv_full, used)) return;
       ptx::tc_fence_after();
       scores();
-      if (!ok) return;
+      if (!gradients_here(blk)) return;
       d_weights(blk);
-      if (!ok) return;
-      if (n == 1) ptx::umma_commit(&sh.kv_empty);
+      if (n == 1) ptx::umma_commit_if(leads, &sh.kv_empty);
+      if (!here(&sh.acc_empty, used ^ 1u)) return;
 #pragma unroll 1
       for (int i = 0; i < n; ++i) {
         const uint32_t b = blk + i;
-        if (i == 0 && !(ok = wait(&sh.acc_empty, used ^ 1u))) return;
-        if (!(ok = wait(&sh.p_full, b))) return;
+        const bool more = i + 1 < n;
+        if ((more && !queries_here()) || !here(&sh.p_full, b)) return;
         ptx::tc_fence_after();
-        product_ts(t_dv, t_s, lo_mn(kDo + (b & 1u)), desc_mn, idesc_o, i == 0);
-        ptx::umma_commit(&sh.do_empty[b & 1u]);
-        if (i + 1 < n) scores();
-        if (!ok || !(ok = wait(&sh.ds_full, b))) return;
+        product_ts<64>(leads, t_dv, t_s, lo_mn(kDo + (b & 1u)), desc_mn, idesc_o, i == 0);
+        ptx::umma_commit_if(leads, &sh.do_empty[b & 1u]);
+        if (more) scores();
+        if ((more && !gradients_here(b + 1)) || !here(&sh.ds_full, b)) return;
         ptx::tc_fence_after();
-        product_ts(t_dk, t_dp, lo_mn(kQ + behind.stage), desc_mn, idesc_o, i == 0);
-        ptx::umma_commit(&sh.q_empty[behind.stage]);
+        product_ts<64>(leads, t_dk, t_dp, lo_mn(kQ + behind.stage), desc_mn, idesc_o, i == 0);
+        ptx::umma_commit_if(leads, &sh.q_empty[behind.stage]);
         behind.step();
-        if (i + 1 < n) {
+        if (more) {
           d_weights(b + 1);
-          if (!ok) return;
-          if (i + 2 == n) ptx::umma_commit(&sh.kv_empty);
+          if (i + 2 == n) ptx::umma_commit_if(leads, &sh.kv_empty);
         }
       }
-      ptx::umma_commit(&sh.acc_full);
+      ptx::umma_commit_if(leads, &sh.acc_full);
     };
-    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &rq, &r, &head, &line); item = next()) {
-      const int n = blocks(&first);
+    while (turns.next(sh.queue, wait, &ok)) {
+      const int n = turns.item(sh.queue).n;
+      turns.done(sh.queue, lane);
       if (n == 0) continue;
-      if (lane == 0) work(n);
-      ok = __shfl_sync(0xffffffffu, ok, 0);
+      work(n);
+      if (!ok) break;
       ++used;
       blk += n;
     }
@@ -225,18 +210,21 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       tok[m] = (lane + 32 * m) / p.G;
       g[m] = (lane + 32 * m) % p.G;
     }
-    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &rq, &r, &head, &line); item = next()) {
-      const int n = blocks(&first);
+    while (turns.next(sh.queue, wait, &ok)) {
+      // the blocks' tokens: how many, and how many stand in front of key 0 and see nothing
+      const Item& it = turns.item(sh.queue);
+      const int n = it.n, before = it.first * p.tpb, left = it.nq - before, unseeing = it.nq - it.kv - before;
+      const float2* from = p.g.stats + (long long)(it.q0 + before) * a.Hq + it.head * p.G;
+      turns.done(sh.queue, lane);
       for (int i = 0; ok && i < n; ++i, ++blk) {
-        float2 st[kTile / 32];
+        float2 st[kTile / 32];                                         // (zeros where there is no row, or one that sees no key)
 #pragma unroll
         for (int m = 0; m < kTile / 32; ++m) {
-          const int t = (first + i) * p.tpb + tok[m];
+          const int t = i * p.tpb + tok[m];
           st[m] = make_float2(0.f, 0.f);
-          if (tok[m] < p.tpb && t < rq.nq) st[m] = p.g.stats[(long long)(rq.q0 + t) * a.Hq + head * p.G + g[m]];
+          if (tok[m] < p.tpb && t < left && t >= unseeing) st[m] = from[(long long)t * a.Hq + g[m]];
         }
-        ok = wait(&sh.stat_empty[blk & 1u], (blk >> 1) ^ 1u);
-        ok = __all_sync(0xffffffffu, ok);
+        ok = __all_sync(0xffffffffu, wait(&sh.stat_empty[blk & 1u], (blk >> 1) ^ 1u));
         if (!ok) break;
 #pragma unroll
         for (int m = 0; m < kTile / 32; ++m) {
@@ -249,43 +237,53 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     }
   } else {
     const int part = warp >> 2, key = threadIdx.x & (kTile - 1);       // which half of the rows; this lane's key
-    const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16, half_col = part * 64;
+    const int half_col = part * 64;
+    const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t my_s = t_s + lane_addr + half_col, my_dp = t_dp + lane_addr + half_col;
     const float c = a.scale * paged::kLog2e;
     const uint64_t c2 = ptx::pack2(c, c);
-    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &rq, &r, &head, &line); item = next()) {
-      const int n = blocks(&first), j = line * kTile + key, x0 = rq.kv - rq.nq;
-      const int page = j < rq.kv ? a.block_table[(size_t)r * a.table_stride + j / a.page_size] : 0;
+    while (turns.next(sh.queue, wait, &ok)) {
+      int n, left, rel, rel_end;                                       // blocks, their tokens, those of them that see this lane's key
+      {
+        const Item& it = turns.item(sh.queue);
+        const int j = it.line * kTile + key;
+        n = it.n;
+        left = it.nq - it.first * p.tpb;
+        rel = j - (it.kv - it.nq) - it.first * p.tpb;
+        rel_end = a.window > 0 && j >= a.sinks ? (int)min((long long)rel + a.window, (long long)INT_MAX) : INT_MAX;
+      }
+#pragma unroll 1
       for (int i = 0; i < n; ++i) {
         const uint32_t b = blk + i;
-        const int t0 = (first + i) * p.tpb, rows = min(p.tpb, rq.nq - t0) * p.G;
+        const int t0 = i * p.tpb, rows = min(p.tpb, left - t0) * p.G;
         // rows of the block that see this lane's key: lo .. hi - 1
-        const int lo = min(max(j - x0 - t0, 0), p.tpb) * p.G;
-        int hi = rows;
-        if (a.window > 0 && j >= a.sinks) hi = min(rows, (int)min(max((long long)j + a.window - x0 - t0, 0ll), (long long)p.tpb) * p.G);
-        const bool masked = __any_sync(0xffffffffu, lo > (int)half_col || hi < (int)half_col + 64);
+        const int lo = min(max(rel - t0, 0), p.tpb) * p.G, hi = min(rows, min(max(rel_end - t0, 0), p.tpb) * p.G);
+        const bool masked = __any_sync(0xffffffffu, lo > half_col || hi < half_col + 64);
         const uint32_t see[2] = {bits(lo - half_col, hi - half_col), bits(lo - half_col - 32, hi - half_col - 32)};
-        ok = wait(&sh.s_full, b) && wait(&sh.stat_full[b & 1u], b >> 1);
-        ok = __all_sync(0xffffffffu, ok);
+        // the rows' statistics come before the scores are waited for: loads from shared memory take long beside the products
+        uint64_t w[32];                                                // weights of this lane's key, a pair of rows each
+        ok = wait(&sh.stat_full[b & 1u], b >> 1);
+        const ulonglong2* lse = reinterpret_cast<const ulonglong2*>(&sh.lse[b & 1u][half_col]);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const ulonglong2 l = lse[k];
+          w[2 * k] = l.x;
+          w[2 * k + 1] = l.y;
+        }
+        ok = __all_sync(0xffffffffu, ok && wait(&sh.s_full, b));
         if (!ok) break;
         ptx::tc_fence_after();
-        uint64_t w[32];                                                // weights of this lane's key, a pair of rows each
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           uint32_t v[32], pk[16];
           load32(my_s + 32 * q, v);
-          const ulonglong2* lse = reinterpret_cast<const ulonglong2*>(&sh.lse[b & 1u][half_col + 32 * q]);
+          if (masked) mask32(v, see[q], kMinusInf);
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
-            const ulonglong2 l = lse[k / 2];
             float e0, e1;
-            ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), c2, k & 1 ? l.y : l.x), &e0, &e1);
+            ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), c2, w[16 * q + k]), &e0, &e1);
             e0 = ptx::ex2(e0);
             e1 = ptx::ex2(e1);
-            if (masked) {
-              e0 = (see[q] >> (2 * k)) & 1u ? e0 : 0.f;
-              e1 = (see[q] >> (2 * k + 1)) & 1u ? e1 : 0.f;
-            }
             w[16 * q + k] = ptx::pack2(e0, e1);
             pk[k] = ptx::pack_bf16x2(e0, e1);
           }
@@ -298,33 +296,31 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             clear_rows<D>(tile(kQ + ring.stage), rows, block_rows, threadIdx.x);
             ptx::fence_proxy_async_smem();
           }
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
         }
         ptx::tmem_wait_st();
         ptx::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&sh.p_full);
-        ok = wait(&sh.dp_full, b);
         ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        if (lane == 0) ptx::mbar_arrive(&sh.p_full);
+        const ulonglong2* delta = reinterpret_cast<const ulonglong2*>(&sh.delta[b & 1u][half_col]);
+        ulonglong2 d[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) d[k] = delta[k];
+        ok = __all_sync(0xffffffffu, wait(&sh.dp_full, b));
         if (!ok) break;
         ptx::tc_fence_after();
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           uint32_t v[32], pk[16];
           load32(my_dp + 32 * q, v);
-          const ulonglong2* delta = reinterpret_cast<const ulonglong2*>(&sh.delta[b & 1u][half_col + 32 * q]);
+          if (masked) mask32(v, see[q], 0u);                           // (beside rows that do not exist anything may stand)
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
-            const ulonglong2 d = delta[k / 2];
-            const uint64_t ds = mul2(w[16 * q + k], ptx::add2(ptx::pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), k & 1 ? d.y : d.x));
+            const uint64_t x = ptx::add2(ptx::pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), k & 1 ? d[k / 2].y : d[k / 2].x);
             float e0, e1;
-            ptx::unpack2(ds, &e0, &e1);
-            if (masked) {                                              // (beside rows that do not exist anything may stand)
-              e0 = (see[q] >> (2 * k)) & 1u ? e0 : 0.f;
-              e1 = (see[q] >> (2 * k + 1)) & 1u ? e1 : 0.f;
-            }
+            ptx::unpack2(mul2(w[16 * q + k], x), &e0, &e1);
             pk[k] = ptx::pack_bf16x2(e0, e1);
+            if (q == 0 && (k & 1)) d[k / 2] = delta[8 + k / 2];
           }
           ptx::tmem_st16_async(my_dp + 16 * q, pk);
         }
@@ -339,19 +335,21 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       }
       if (!ok) break;
       // ---- results: values' gradients by one half of the warps, keys' by the other ----
-      __nv_bfloat16* to = static_cast<__nv_bfloat16*>(part == 0 ? p.g.dv : p.g.dk) +
-                          ((long long)rq.k0 + j) * (part == 0 ? p.g.dv_stride : p.g.dk_stride) + head * D;
-      const float by = part == 0 ? 1.f : a.scale;
-      bool odd = page < 0 || page >= a.n_pages;
       if (n > 0) {
-        ok = wait(&sh.acc_full, used);
-        ok = __all_sync(0xffffffffu, ok);
+        ok = __all_sync(0xffffffffu, wait(&sh.acc_full, used));
         if (!ok) break;
         ptx::tc_fence_after();
         ++used;
         blk += n;
       }
-      float bad = 0.f;
+      const Item it = turns.item(sh.queue);
+      const int j = it.line * kTile + key;
+      const int page = j < it.kv ? a.block_table[(size_t)it.r * a.table_stride + j / a.page_size] : 0;
+      const long long stride = part == 0 ? p.g.dv_stride : p.g.dk_stride;
+      const int quad = j & ~3;                                         // the first of the four keys whose columns this lane writes
+      __nv_bfloat16* from = static_cast<__nv_bfloat16*>(part == 0 ? p.g.dv : p.g.dk) + ((long long)it.k0 + quad) * stride + it.head * D;
+      const float by = part == 0 ? 1.f : a.scale;
+      bool finite = true;
 #pragma unroll 1
       for (int q = 0; q < D / 32; ++q) {
         uint32_t v[32];
@@ -361,17 +359,10 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
 #pragma unroll
           for (int k = 0; k < 32; ++k) v[k] = 0u;
         }
+        __nv_bfloat16* to[4];
 #pragma unroll
-        for (int k = 0; k < 32; ++k) bad = fmaf(__uint_as_float(v[k]), 0.f, bad);   // NaN if any is not finite
-        if (j < rq.kv) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            uint32_t x[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = ptx::pack_bf16x2(__uint_as_float(v[8 * k + 2 * e]) * by, __uint_as_float(v[8 * k + 2 * e + 1]) * by);
-            *reinterpret_cast<uint4*>(to + 32 * q + 8 * k) = make_uint4(x[0], x[1], x[2], x[3]);
-          }
-        }
+        for (int m = 0; m < 4; ++m) to[m] = quad + m < it.kv ? from + m * stride + 32 * q : nullptr;
+        finite = store_32_columns(v, by, to, lane) && finite;
       }
       if (n > 0) {
         ptx::tc_fence_before();
@@ -379,16 +370,17 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         if (lane == 0) ptx::mbar_arrive(&sh.acc_empty);
       }
       // a value that is no number, or too large, at a row that another key of the tile sees; a page outside the pool
-      odd = j < rq.kv && (odd || bad != 0.f);
+      const bool odd = j < it.kv && (page < 0 || page >= a.n_pages || !finite);
       __syncwarp();
-      for (uint32_t left = __ballot_sync(0xffffffffu, odd); left != 0u; left &= left - 1u) {
+      for (uint32_t again = __ballot_sync(0xffffffffu, odd); again != 0u; again &= again - 1u) {
         // (0.6 us a row: whoever waits meanwhile starts its limit anew)
-        const int k = line * kTile + (warp & 3) * 32 + __ffs(left) - 1;
+        const int k = it.line * kTile + (warp & 3) * 32 + __ffs(again) - 1;
         if (part == 0)
-          paged::grad_key<__nv_bfloat16, D, false, true>(p.g, r, rq, k, head, lane, &sh.alive);
+          paged::grad_key<__nv_bfloat16, D, false, true>(p.g, it.r, it, k, it.head, lane, &sh.alive);
         else
-          paged::grad_key<__nv_bfloat16, D, true, false>(p.g, r, rq, k, head, lane, &sh.alive);
+          paged::grad_key<__nv_bfloat16, D, true, false>(p.g, it.r, it, k, it.head, lane, &sh.alive);
       }
+      turns.done(sh.queue, lane);
     }
   }
   __syncwarp();

@@ -3,10 +3,12 @@
 // A work item is a block of 128 rows (token, query head of the group) of one (request, key head) with all the key tiles (128 keys)
 // that any of them sees.  One CTA an SM works through items that a counter hands out.  Per tile:
 //     S = Q K^T      P = 2^(c S - lse)      dP = dO V^T      dS = P (dP - delta)      dQ += dS K
-// Two buffers of S, dP and dQ fill the tensor memory (4 x 128 columns at D = 128); dS goes back as bf16 over its own scores, so that
-// the next tile's S and dP are formed while this one's dS is:
+// S, dP, dS (bf16), dQ and Q as an operand fill the tensor memory (512 columns at D = 128; with both operands in shared memory a
+// product takes all of its bandwidth).  The next S and dP are formed as soon as these have been read, dQ behind dS:
 //   * warp 8 loads queries and output gradients once an item, keys through three stages (they are used twice) and values through two;
-//   * warp 9 issues the products;  warps 0-7: a row per lane, half of a tile's keys each.
+//   * warp 9 issues S and dP, warp 10 dQ: a warp that issues is held up until the tensor cores have taken its products, and what
+//     it waits for next should be looked at meanwhile;
+//   * warps 0-7: a row per lane, half of a tile's keys each; P stays in registers.
 #include <climits>
 
 #include "paged_grad_tc.cuh"
@@ -15,10 +17,11 @@ namespace {
 
 using namespace grad_tc;
 
-constexpr int kQWarps = kProducts + 1, kQThreads = kQWarps * 32;     // (rows' statistics are read by their own lanes)
+constexpr int kOutputs = kStats;                                       // the warp that issues dQ (rows' statistics are read by their own lanes)
 
 struct Shared {
-  uint64_t q_full, q_empty, k_full[3], k_empty[3], v_full[2], v_empty[2], s_full[2], ds_full[2], dp_full, dp_empty, acc_full, acc_empty;
+  uint64_t q_full, q_empty, do_full, do_empty, a_full, k_full[3], k_empty[3], v_full[2], v_empty[2], s_full, s_empty, dp_full, dp_empty, ds_full,
+      ds_empty, acc_full, acc_empty;
   Queue queue;
   uint64_t alive;
   int abort_flag;
@@ -26,7 +29,7 @@ struct Shared {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kQThreads, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do, const __grid_constant__ CUtensorMap tm_k,
                const __grid_constant__ CUtensorMap tm_v, const Args p) {
   using C = Cfg<D>;
@@ -45,15 +48,18 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
   const Waits wait = {&sh.abort_flag, &sh.alive, a.err, a.wait_ns};
 
   if (threadIdx.x == 0) {
-    for (uint64_t* b : {&sh.q_full, &sh.q_empty, &sh.dp_full, &sh.acc_full}) ptx::mbar_init(b, 1);
-    for (uint64_t* b : {&sh.dp_empty, &sh.ds_full[0], &sh.ds_full[1], &sh.acc_empty}) ptx::mbar_init(b, kComputeWarps);
+    for (uint64_t* b : {&sh.q_full, &sh.do_full, &sh.do_empty, &sh.s_full, &sh.dp_full, &sh.ds_empty, &sh.acc_full}) ptx::mbar_init(b, 1);
+    for (uint64_t* b : {&sh.q_empty, &sh.a_full, &sh.s_empty, &sh.dp_empty, &sh.ds_full, &sh.acc_empty}) ptx::mbar_init(b, kComputeWarps);
     for (int i = 0; i < 3; ++i) {
       ptx::mbar_init(&sh.k_full[i], 1);
       ptx::mbar_init(&sh.k_empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      for (uint64_t* b : {&sh.v_full[i], &sh.v_empty[i], &sh.s_full[i], &sh.queue.full[i]}) ptx::mbar_init(b, 1);
-      ptx::mbar_init(&sh.queue.empty[i], kQWarps);
+      for (uint64_t* b : {&sh.v_full[i], &sh.v_empty[i]}) ptx::mbar_init(b, 1);
+    }
+    for (int i = 0; i < kSlots; ++i) {
+      ptx::mbar_init(&sh.queue.full[i], 1);
+      ptx::mbar_init(&sh.queue.empty[i], kWarps - 1);
     }
     sh.abort_flag = 0;
     sh.alive = 0;
@@ -72,71 +78,59 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
-  const uint32_t t_s = sh.tmem, t_dp = t_s + 256, t_dq = t_s + 384;    // (S of an odd tile at 128)
+  const uint32_t t_s = sh.tmem, t_dp = t_s + 128, t_ds = t_s + 256, t_q = t_s + 320, t_dq = t_s + 384;
 
-  Cursor<false> cur;
-  paged::GradRequest rq = {};
-  int r = 0, head = 0, line = 0;
-  uint32_t turn = 0;                                                   // items that this warp has taken
-  bool lost = false;                                                   // the item that was left for this one met a bad page
-  auto next = [&]() {
-    const uint32_t slot = turn & 1u, use = turn >> 1;
-    ++turn;
-    const bool here = wait(&sh.queue.full[slot], use);
-    const int item = here ? *static_cast<volatile int*>(&sh.queue.answer[slot]) : INT_MAX;
-    lost = here && *static_cast<volatile bool*>(&sh.queue.lost[slot]);
-    __syncwarp();
-    if (lane == 0) ptx::mbar_arrive(&sh.queue.empty[slot]);
-    return __shfl_sync(0xffffffffu, item, 0);
-  };
-  // the item's key tiles: tile i is i (i < n_sink) or i + skip
-  int n_sink = 0, skip = 0;
-  auto tiles = [&]() {
-    const int x0 = rq.kv - rq.nq, t0 = line * p.tpb, last = x0 + min(rq.nq, t0 + p.tpb) - 1;
-    const int lo = paged::window_begin(x0 + t0, a.window), lo_tile = lo / kTile;
-    n_sink = min((min(a.sinks, lo) + kTile - 1) / kTile, lo_tile);
-    skip = lo_tile - n_sink;
-    return last < 0 ? 0 : last / kTile + 1 - skip;
-  };
-  auto first_key = [&](int i) { return (i < n_sink ? i : i + skip) * kTile; };
+  Turns turns;
   uint32_t used = 0, done = 0;                                         // items with tiles, and tiles, so far
   Ring<3> ring;                                                        // the keys' stages
   bool ok = true;
+  // key tile i of an item: its first tiles reach over the first tokens, the others lie `skip` further
+  auto first_key = [](const Item& it, int i) { return (i < it.first ? i : i + it.skip) * kTile; };
 
   if (warp == kLoads) {
     const Box box(p, lane);
     const uint32_t box_bytes = (uint32_t)p.box_rows * 128u, row_bytes = (uint32_t)(p.tpb * p.G) * 128u * C::kHalves;
-    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &rq, &r, &head, &line); item = next()) {
+    Cursor<false> cur;
+    Item it = {};
+    for (int item = blockIdx.x;;) {
+      const bool more = cur.find(p, item, lane, &it);
+      {
+        const int x0 = it.kv - it.nq, t0 = it.line * p.tpb, last = x0 + min(it.nq, t0 + p.tpb) - 1;
+        const int lo = paged::window_begin(x0 + t0, a.window), lo_tile = lo / kTile;
+        it.first = min((min(a.sinks, lo) + kTile - 1) / kTile, lo_tile);
+        it.skip = lo_tile - it.first;
+        it.n = !more ? -1 : last < 0 ? 0 : last / kTile + 1 - it.skip;
+      }
+      if (!turns.tell(sh.queue, wait, it, lane, &ok) || !more) break;
       const int granted = lane == 0 ? (int)gridDim.x + atomicAdd(p.taken, 1) : 0;
-      const int n = tiles();
       bool bad = false;
-      if (n > 0) {
-        const int32_t* table = a.block_table + (size_t)r * a.table_stride;
-        ok = ok && wait(&sh.q_empty, used ^ 1u);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        if (lane == 0) {
-          ptx::mbar_arrive_expect_tx(&sh.q_full, 2u * row_bytes);
-          for (int h = 0; h < C::kHalves; ++h) {
-            ptx::tma_load_4d(smem + h * (kTile * 128), &tm_q, h * 64, 0, head, rq.q0 + line * p.tpb, &sh.q_full);
-            ptx::tma_load_4d(smem + C::kTileBytes + h * (kTile * 128), &tm_do, h * 64, 0, head, rq.q0 + line * p.tpb, &sh.q_full);
+      if (it.n > 0) {
+        const int32_t* table = a.block_table + (size_t)it.r * a.table_stride;
+        auto rows = [&](int to, const CUtensorMap* m, uint64_t* full, uint64_t* empty) {
+          ok = __all_sync(0xffffffffu, ok && wait(empty, used ^ 1u));
+          if (ok && lane == 0) {
+            ptx::mbar_arrive_expect_tx(full, row_bytes);
+            for (int h = 0; h < C::kHalves; ++h)
+              ptx::tma_load_4d(smem + to * C::kTileBytes + h * (kTile * 128), m, h * 64, 0, it.head, it.q0 + it.line * p.tpb, full);
           }
-        }
+        };
+        rows(0, &tm_q, &sh.q_full, &sh.q_empty);
+        rows(1, &tm_do, &sh.do_full, &sh.do_empty);
+        if (!ok) break;
         ++used;
         int row, next_row = 0;
-        int page = box.page(p, table, first_key(0), rq.kv, C::kHalves, &row, &bad);
-        for (int i = 0; i < n; ++i, ++done) {
+        int page = box.page(p, table, first_key(it, 0), it.kv, C::kHalves, &row, &bad);
+        for (int i = 0; i < it.n; ++i, ++done) {
           int next_page = -1;
-          if (i + 1 < n) next_page = box.page(p, table, first_key(i + 1), rq.kv, C::kHalves, &next_row, &bad);
+          if (i + 1 < it.n) next_page = box.page(p, table, first_key(it, i + 1), it.kv, C::kHalves, &next_row, &bad);
           const uint32_t bytes = box_bytes * (uint32_t)__popc(__ballot_sync(0xffffffffu, page >= 0));
           auto load = [&](const CUtensorMap* m, uint64_t* full, uint64_t* empty, uint32_t ph, int to) {
-            ok = ok && wait(empty, ph ^ 1u);
-            ok = __all_sync(0xffffffffu, ok);
+            ok = __all_sync(0xffffffffu, ok && wait(empty, ph ^ 1u));
             if (!ok) return;
             if (lane == 0) ptx::mbar_arrive_expect_tx(full, bytes);
             __syncwarp();
             if (page >= 0)
-              ptx::tma_load_4d(smem + to * C::kTileBytes + box.half * (kTile * 128) + box.i * box_bytes, m, box.half * 64, head, row, page, full);
+              ptx::tma_load_4d(smem + to * C::kTileBytes + box.half * (kTile * 128) + box.i * box_bytes, m, box.half * 64, it.head, row, page, full);
           };
           load(&tm_k, &sh.k_full[ring.stage], &sh.k_empty[ring.stage], ring.ph, kK + ring.stage);
           load(&tm_v, &sh.v_full[done & 1u], &sh.v_empty[done & 1u], done >> 1, kV + (done & 1u));
@@ -145,95 +139,114 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
           page = next_page;
           row = next_row;
         }
+        if (!ok) break;
       }
-      const uint32_t slot = turn & 1u, use = turn >> 1;
-      ok = ok && wait(&sh.queue.empty[slot], use ^ 1u);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
       bad = __any_sync(0xffffffffu, bad);
-      if (lane == 0) {
-        *static_cast<volatile int*>(&sh.queue.answer[slot]) = granted;
-        *static_cast<volatile bool*>(&sh.queue.lost[slot]) = bad;
-        ptx::mbar_arrive(&sh.queue.full[slot]);
-      }
+      if (bad && lane == 0) static_cast<volatile Item&>(turns.last(sh.queue)).lost = true;   // (before the next item is told)
+      item = __shfl_sync(0xffffffffu, granted, 0);
     }
     // everything has been given back before the CTA may end (the arrivals are asynchronous)
-    ok = ok && wait(&sh.q_empty, used ^ 1u);
+    ok = ok && wait(&sh.q_empty, used ^ 1u) && wait(&sh.do_empty, used ^ 1u);
     for (uint32_t i = 0; i < 2; ++i) ok = ok && wait(&sh.v_empty[(done + i) & 1u], ((done + i) >> 1) ^ 1u);
     for (uint32_t i = 0; i < 3; ++i, ring.step()) ok = ok && wait(&sh.k_empty[ring.stage], ring.ph ^ 1u);
-  } else if (warp == kProducts) {
+  } else if (warp == kProducts || warp == kOutputs) {
     const uint32_t idesc_s = ptx::umma_idesc_bf16(128, 128), idesc_o = ptx::umma_idesc_bf16_b_mn(128, D);
     const uint64_t desc = ptx::umma_desc_sw128(base), desc_mn = ptx::umma_desc_sw128_strides(base, kTile * 128, 1024);
     auto lo = [&](int i) { return (uint32_t)desc + i * (C::kTileBytes >> 4); };
     auto lo_mn = [&](int i) { return (uint32_t)desc_mn + i * (C::kTileBytes >> 4); };
-    Ring<3> behind;                                                    // the stage of the tile whose last product comes next
-    auto scores = [&](uint32_t t) {
-      if (!(ok = wait(&sh.k_full[ring.stage], ring.ph))) return;
-      product_ss<D>(t_s + (t & 1u) * 128, lo(0), lo(kK + ring.stage), desc, idesc_s);
-      ptx::umma_commit(&sh.s_full[t & 1u]);
-      ring.step();
-    };
-    auto d_weights = [&](uint32_t t) {
-      if (!(ok = wait(&sh.v_full[t & 1u], t >> 1)) || !(ok = wait(&sh.dp_empty, t ^ 1u))) return;
-      ptx::tc_fence_after();
-      product_ss<D>(t_dp, lo(1), lo(kV + (t & 1u)), desc, idesc_s);
-      ptx::umma_commit(&sh.dp_full);
-      ptx::umma_commit(&sh.v_empty[t & 1u]);
-    };
-    auto work = [&](int n) {
-      if (!(ok = wait(&sh.q_full, used))) return;
-      scores(done);
-      if (!ok) return;
-      d_weights(done);
-      if (!ok) return;
-      if (n == 1) ptx::umma_commit(&sh.q_empty);
-#pragma unroll 1
-      for (int i = 0; i < n; ++i) {
-        const uint32_t t = done + i;
-        if (i + 1 < n) {
-          scores(t + 1);
-          if (!ok) return;
-          d_weights(t + 1);
-          if (!ok) return;
-          if (i + 2 == n) ptx::umma_commit(&sh.q_empty);
-        }
-        if (i == 0 && !(ok = wait(&sh.acc_empty, used ^ 1u))) return;
-        if (!(ok = wait(&sh.ds_full[t & 1u], t >> 1))) return;         // (the next tile's may come before this is looked at)
-        ptx::tc_fence_after();
-        product_ts(t_dq, t_s + (t & 1u) * 128, lo_mn(kK + behind.stage), desc_mn, idesc_o, i == 0);
-        ptx::umma_commit(&sh.k_empty[behind.stage]);
-        behind.step();
-      }
-      ptx::umma_commit(&sh.acc_full);
-    };
-    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &rq, &r, &head, &line); item = next()) {
-      const int n = tiles();
+    const uint32_t leads = lane == 0;
+    auto here = [&](uint64_t* bar, uint32_t parity) { return ok = __all_sync(0xffffffffu, wait.spin(bar, parity)); };
+    while (turns.next(sh.queue, wait, &ok)) {
+      const int n = turns.item(sh.queue).n;
+      turns.done(sh.queue, lane);
       if (n == 0) continue;
-      if (lane == 0) work(n);
-      ok = __shfl_sync(0xffffffffu, ok, 0);
+      if (warp == kProducts) {
+        if (!here(&sh.a_full, used) || !here(&sh.do_full, used)) break;
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+          const uint32_t t = done + i;
+          if (!here(&sh.k_full[ring.stage], ring.ph) || !here(&sh.s_empty, t ^ 1u)) break;
+          ptx::tc_fence_after();
+          product_ts_k<D>(leads, t_s, t_q, lo(kK + ring.stage), desc, idesc_s);
+          ptx::umma_commit_if(leads, &sh.s_full);
+          ring.step();
+          if (!here(&sh.v_full[t & 1u], t >> 1) || !here(&sh.dp_empty, t ^ 1u)) break;
+          ptx::tc_fence_after();
+          product_ss<D>(leads, t_dp, lo(1), lo(kV + (t & 1u)), desc, idesc_s);
+          ptx::umma_commit_if(leads, &sh.dp_full);
+          ptx::umma_commit_if(leads, &sh.v_empty[t & 1u]);
+        }
+        if (!ok) break;
+        ptx::umma_commit_if(leads, &sh.do_empty);
+      } else {
+        if (!here(&sh.acc_empty, used ^ 1u)) break;
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+          if (!here(&sh.ds_full, done + i)) break;
+          ptx::tc_fence_after();
+          product_ts<32>(leads, t_dq, t_ds, lo_mn(kK + ring.stage), desc_mn, idesc_o, i == 0);
+          ptx::umma_commit_if(leads, &sh.ds_empty);
+          ptx::umma_commit_if(leads, &sh.k_empty[ring.stage]);         // (its S is done, or there were no dS)
+          ring.step();
+        }
+        if (!ok) break;
+        ptx::umma_commit_if(leads, &sh.acc_full);
+      }
       ++used;
       done += n;
     }
   } else {
     const int part = warp >> 2, rr = threadIdx.x & (kTile - 1);        // which half of the keys; this lane's row
-    const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16, half_col = part * 64;
-    const uint32_t my_s = t_s + lane_addr + half_col, my_dp = t_dp + lane_addr + half_col;
+    const int half_col = part * 64;
+    const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t my_s = t_s + lane_addr + half_col, my_dp = t_dp + lane_addr + half_col, my_ds = t_ds + lane_addr + part * 32;
     const float c = a.scale * paged::kLog2e;
     const uint64_t c2 = ptx::pack2(c, c);
     const int my_tok = rr / p.G, my_g = rr % p.G;
-    for (int item = blockIdx.x; ok && cur.find(p, item, lane, &rq, &r, &head, &line);) {
-      const int n = tiles(), tok = line * p.tpb + my_tok;
-      const bool live = my_tok < p.tpb && tok < rq.nq;
-      // position (below 0: sees nothing); a place without a row sees everything, which spares its warp the masks
-      const int x = live ? rq.kv - rq.nq + tok : INT_MAX / 2;
-      const int lo = live ? paged::window_begin(x, a.window) : 0;
-      const long long at = (long long)(rq.q0 + tok) * a.Hq + head * p.G + my_g;
-      const float2 st = live ? p.g.stats[at] : make_float2(0.f, 0.f);
-      const uint64_t lse2 = ptx::pack2(-st.x, -st.x), delta2 = ptx::pack2(-st.y, -st.y);
+    while (turns.next(sh.queue, wait, &ok)) {
+      int n, x, lo, kv, first, skip;
+      uint64_t lse2, delta2;
+      {
+        const Item& it = turns.item(sh.queue);
+        const int tok = it.line * p.tpb + my_tok;
+        const bool live = my_tok < p.tpb && tok < it.nq;
+        n = it.n;
+        kv = it.kv;
+        first = it.first;
+        skip = it.skip;
+        // position (below 0: sees nothing); a place without a row sees everything, which spares its warp the masks
+        x = live ? kv - it.nq + tok : INT_MAX / 2;
+        lo = live ? paged::window_begin(x, a.window) : 0;
+        const bool sees = live && x >= 0;
+        const float2 st = sees ? p.g.stats[(long long)(it.q0 + tok) * a.Hq + it.head * p.G + my_g] : make_float2(0.f, 0.f);
+        lse2 = ptx::pack2(-st.x, -st.x);
+        delta2 = ptx::pack2(-st.y, -st.y);
+      }
+      if (n > 0) {                                                     // half of this lane's row of Q into tensor memory
+        ok = __all_sync(0xffffffffu, wait(&sh.q_full, used));
+        if (!ok) break;
+#pragma unroll
+        for (int k = 0; k < D / 64; ++k) {
+          uint32_t y[16];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int piece = part * (D / 16) + 4 * k + e;
+            ld_shared_v4(tile(0) + rr * 128 + (piece >> 3) * (kTile * 128) + (((piece & 7) ^ (rr & 7)) << 4), &y[4 * e]);
+          }
+          ptx::tmem_st16_async(t_q + lane_addr + part * (D / 4) + 16 * k, y);
+        }
+        ptx::tmem_wait_st();
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          ptx::mbar_arrive(&sh.a_full);
+          ptx::mbar_arrive(&sh.q_empty);
+        }
+      }
+#pragma unroll 1
       for (int i = 0; i < n; ++i) {
         const uint32_t t = done + i;
-        const uint32_t ms = my_s + (t & 1u) * 128;
-        const int k0 = first_key(i) + (int)half_col;
+        const int tile_key = (i < first ? i : i + skip) * kTile, k0 = tile_key + half_col;
         // bit k: this row sees key k0 + 32 q + k
         uint32_t see[2];
 #pragma unroll
@@ -242,15 +255,20 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
           see[q] = bits(INT_MIN, x - j0 + 1) & (bits(lo - j0, 32) | bits(INT_MIN, a.sinks - j0));
         }
         const bool masked = __any_sync(0xffffffffu, (see[0] & see[1]) != 0xffffffffu);
-        ok = wait(&sh.s_full[t & 1u], t >> 1);
-        ok = __all_sync(0xffffffffu, ok);
+        ok = __all_sync(0xffffffffu, wait(&sh.s_full, t));
         if (!ok) break;
         ptx::tc_fence_after();
         uint64_t w[32];                                                // weights of this lane's row, a pair of keys each
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           uint32_t v[32];
-          load32(ms + 32 * q, v);
+          load32(my_s + 32 * q, v);
+          if (q == 1) {                                                // the next tile's may come
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(&sh.s_empty);
+          }
+          if (masked) mask32(v, see[q], kMinusInf);
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
             float e0, e1;
@@ -258,58 +276,59 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
             w[16 * q + k] = ptx::pack2(ptx::ex2(e0), ptx::ex2(e1));
           }
         }
-        if (first_key(i) + kTile > rq.kv) {                            // keys behind the last: whatever the page held before
+        if (tile_key + kTile > kv) {                                   // keys behind the last: whatever the page held before
           ok = wait(&sh.k_full[ring.stage], ring.ph);
           if (ok) {
-            clear_rows<D>(tile(kK + ring.stage), rq.kv - first_key(i), kTile, threadIdx.x);
+            clear_rows<D>(tile(kK + ring.stage), kv - tile_key, kTile, threadIdx.x);
             ptx::fence_proxy_async_smem();
           }
         }
-        ok = ok && wait(&sh.dp_full, t);
-        ok = __all_sync(0xffffffffu, ok);
+        ok = __all_sync(0xffffffffu, ok && wait(&sh.ds_empty, t ^ 1u) && wait(&sh.dp_full, t));
         if (!ok) break;
         ptx::tc_fence_after();
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           uint32_t v[32], pk[16];
           load32(my_dp + 32 * q, v);
-          if (q == 1) {                                                // the next tile's may come
+          if (q == 1) {
             ptx::tc_fence_before();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(&sh.dp_empty);
           }
+          if (masked) mask32(v, see[q], 0u);                           // (beside keys that do not exist anything may stand)
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
-            const uint64_t ds = mul2(w[16 * q + k], ptx::add2(ptx::pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), delta2));
+            const uint64_t y = ptx::add2(ptx::pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), delta2);
             float e0, e1;
-            ptx::unpack2(ds, &e0, &e1);
-            if (masked) {
-              e0 = (see[q] >> (2 * k)) & 1u ? e0 : 0.f;
-              e1 = (see[q] >> (2 * k + 1)) & 1u ? e1 : 0.f;
-            }
+            ptx::unpack2(mul2(w[16 * q + k], y), &e0, &e1);
             pk[k] = ptx::pack_bf16x2(e0, e1);
           }
-          ptx::tmem_st16_async(ms + 16 * q, pk);
+          ptx::tmem_st16_async(my_ds + 16 * q, pk);
         }
         ptx::tmem_wait_st();
         ptx::tc_fence_before();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&sh.ds_full[t & 1u]);
+        if (lane == 0) ptx::mbar_arrive(&sh.ds_full);
         ring.step();
       }
       if (!ok) break;
       // ---- results: half of a row's elements each ----
       if (n > 0) {
-        ok = wait(&sh.acc_full, used);
-        ok = __all_sync(0xffffffffu, ok);
+        ok = __all_sync(0xffffffffu, wait(&sh.acc_full, used));
         if (!ok) break;
         ptx::tc_fence_after();
         ++used;
         done += n;
       }
-      const int row = rq.q0 + tok, q_head = head * p.G + my_g;
-      __nv_bfloat16* to = static_cast<__nv_bfloat16*>(p.g.dq) + (long long)row * p.g.dq_stride + q_head * D + part * (D / 2);
-      float bad = 0.f;
+      const Item it = turns.item(sh.queue);
+      const int tok = it.line * p.tpb + my_tok, row = it.q0 + tok, q_head = it.head * p.G + my_g;
+      const bool live = my_tok < p.tpb && tok < it.nq;
+      __nv_bfloat16* mine = live ? static_cast<__nv_bfloat16*>(p.g.dq) + (long long)row * p.g.dq_stride + q_head * D + part * (D / 2) : nullptr;
+      __nv_bfloat16* to[4];                                            // of the four rows whose columns this lane writes
+#pragma unroll
+      for (int m = 0; m < 4; ++m)
+        to[m] = reinterpret_cast<__nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), (lane & ~3) + m));
+      bool finite = true;
 #pragma unroll 1
       for (int q = 0; q < D / 64; ++q) {
         uint32_t v[32];
@@ -319,18 +338,10 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
 #pragma unroll
           for (int k = 0; k < 32; ++k) v[k] = 0u;
         }
+        finite = store_32_columns(v, a.scale, to, lane) && finite;
 #pragma unroll
-        for (int k = 0; k < 32; ++k) bad = fmaf(__uint_as_float(v[k]), 0.f, bad);   // NaN if any is not finite
-        if (live) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            uint32_t y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              y[e] = ptx::pack_bf16x2(__uint_as_float(v[8 * k + 2 * e]) * a.scale, __uint_as_float(v[8 * k + 2 * e + 1]) * a.scale);
-            *reinterpret_cast<uint4*>(to + 32 * q + 8 * k) = make_uint4(y[0], y[1], y[2], y[3]);
-          }
-        }
+        for (int m = 0; m < 4; ++m)
+          if (to[m] != nullptr) to[m] += 32;
       }
       if (n > 0) {
         ptx::tc_fence_before();
@@ -338,16 +349,18 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         if (lane == 0) ptx::mbar_arrive(&sh.acc_empty);
       }
       __syncwarp();
-      // the answer for the next item tells whether this one's keys were all there: the loads ended long ago
-      const int r_was = r;
-      item = next();
-      const bool odd = live && x >= 0 && (bad != 0.f || lost);
+      // where the next item is told the loads of this one have ended: whether its keys were all there is known
+      ok = __all_sync(0xffffffffu, turns.next_is_told(sh.queue, wait));
+      if (!ok) break;
+      const bool lost = static_cast<const volatile Item&>(turns.item(sh.queue)).lost;
+      const bool odd = live && x >= 0 && (!finite || lost);
       // (0.6 us a key and row: whoever waits meanwhile starts its limit anew; each warp sees to its half of the row's elements)
-      for (uint32_t left = __ballot_sync(0xffffffffu, odd); left != 0u; left &= left - 1u) {
-        const int who = __ffs(left) - 1;
-        paged::grad_row<__nv_bfloat16, D>(p.g, r_was, __shfl_sync(0xffffffffu, row, who), __shfl_sync(0xffffffffu, x, who),
+      for (uint32_t again = __ballot_sync(0xffffffffu, odd); again != 0u; again &= again - 1u) {
+        const int who = __ffs(again) - 1;
+        paged::grad_row<__nv_bfloat16, D>(p.g, it.r, __shfl_sync(0xffffffffu, row, who), __shfl_sync(0xffffffffu, x, who),
                                           __shfl_sync(0xffffffffu, q_head, who), lane, part * (D / 64), (part + 1) * (D / 64), &sh.alive);
       }
+      turns.done(sh.queue, lane);
     }
   }
   __syncwarp();
@@ -369,7 +382,7 @@ int launch(cascade_ctx* ctx, const Args& p, int grid, cudaStream_t s) {
   constexpr int kSmem = smem_bytes<D, Shared>();
   CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_Q, k_paged_grad_q<D>, kSmem));   // (a context has one D)
   KernelScope ks(ctx, K_PAGED_GRAD, s);
-  k_paged_grad_q<D><<<grid, kQThreads, kSmem, s>>>(mq, mo, *mk, *mv, p);
+  k_paged_grad_q<D><<<grid, kThreads, kSmem, s>>>(mq, mo, *mk, *mv, p);
   CASCADE_CUDA_TRY(cudaGetLastError());
   return CASCADE_OK;
 }

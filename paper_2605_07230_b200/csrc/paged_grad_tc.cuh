@@ -44,11 +44,17 @@ struct Args {
   int* taken;                     // [0] items handed out beyond the blocks' own, [1] blocks that are done; zero between launches
 };
 
-// The items that a CTA takes: its own index first, then what the launch's counter gives; the loading warp asks one item ahead.
+// The items that a CTA takes: its own index first, then what the launch's counter gives.  The loading warp finds an item's request
+// and tiles and tells the other warps, at most kSlots items ahead.
+struct Item : paged::GradRequest {
+  int r, head, line;              // request, key head, its tile of keys or block of rows
+  int n, first, skip;             // steps (row blocks or key tiles; -1: no more items), see the passes
+  bool lost;                      // its loads met a page outside the pool: known when the next item is told
+};
+constexpr int kSlots = 4;
 struct Queue {
-  int answer[2];
-  bool lost[2];                   // the item before met a page outside the pool
-  uint64_t full[2], empty[2];
+  Item item[kSlots];
+  uint64_t full[kSlots], empty[kSlots];
 };
 
 // A waiting warp's view of the CTA: where waits give up.
@@ -60,6 +66,42 @@ struct Waits {
   __device__ __forceinline__ bool operator()(uint64_t* bar, uint32_t parity) const {
     return ptx::mbar_wait_short(bar, parity & 1u, abort_flag, err, ns, alive);
   }
+  // Without going to sleep, where the wait lies on the critical path and few poll.
+  __device__ __forceinline__ bool spin(uint64_t* bar, uint32_t parity) const {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (ptx::mbar_test_wait(bar, parity & 1u)) return true;
+    return (*this)(bar, parity);
+  }
+};
+
+// One warp's turns through the queue; false behind the last item, or where a wait gave up.
+struct Turns {
+  uint32_t turn = 0;
+  __device__ __forceinline__ bool next(Queue& q, const Waits& wait, bool* ok) {
+    *ok = __all_sync(0xffffffffu, *ok && wait(&q.full[turn % kSlots], turn / kSlots));
+    return *ok && static_cast<volatile Item&>(q.item[turn % kSlots]).n >= 0;
+  }
+  // (the loading warp's side) false where the wait gave up
+  __device__ __forceinline__ bool tell(Queue& q, const Waits& wait, const Item& it, int lane, bool* ok) {
+    *ok = __all_sync(0xffffffffu, *ok && wait(&q.empty[turn % kSlots], (turn / kSlots) ^ 1u));
+    if (*ok && lane == 0) {
+      q.item[turn % kSlots] = it;
+      ptx::mbar_arrive(&q.full[turn % kSlots]);
+    }
+    ++turn;
+    return *ok;
+  }
+  __device__ __forceinline__ Item& last(Queue& q) const { return q.item[(turn - 1) % kSlots]; }   // the one told last
+  __device__ __forceinline__ bool next_is_told(Queue& q, const Waits& wait) const {
+    return wait(&q.full[(turn + 1) % kSlots], (turn + 1) / kSlots);
+  }
+  __device__ __forceinline__ const Item& item(Queue& q) const { return q.item[turn % kSlots]; }
+  __device__ __forceinline__ void done(Queue& q, int lane) {       // the item is not looked at any more
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(&q.empty[turn % kSlots]);
+    ++turn;
+  }
 };
 
 // Items of the requests in order: kKeys: tiles of keys, else blocks of rows, of every key head; a whole warp walks forward through
@@ -69,8 +111,8 @@ struct Cursor {
   int chunk = -32, lane_items = 0, lane_first = 0, base = 0, total = 0;
   paged::GradRequest lane_rq;
 
-  // -> request and its place in line, or false behind the last
-  __device__ __forceinline__ bool find(const Args& p, int item, int lane, paged::GradRequest* rq, int* r, int* head, int* line) {
+  // -> request, head and line of the item, or false behind the last
+  __device__ __forceinline__ bool find(const Args& p, int item, int lane, Item* it) {
     const PagedAttnArgs& a = p.g.a;
     const int unit = kKeys ? kTile : p.tpb;
     while (chunk < 0 || item >= base + total) {
@@ -92,14 +134,14 @@ struct Cursor {
     const int x = item - base;
     const int who = __ffs(__ballot_sync(0xffffffffu, x >= lane_first && x < lane_first + lane_items)) - 1;
     const int local = x - __shfl_sync(0xffffffffu, lane_first, who);
-    *r = chunk + who;
-    rq->q0 = __shfl_sync(0xffffffffu, lane_rq.q0, who);
-    rq->nq = __shfl_sync(0xffffffffu, lane_rq.nq, who);
-    rq->kv = __shfl_sync(0xffffffffu, lane_rq.kv, who);
-    rq->k0 = __shfl_sync(0xffffffffu, lane_rq.k0, who);
-    const int n = ((kKeys ? rq->kv : rq->nq) + unit - 1) / unit, round = local / a.Hkv;
-    *line = kKeys ? round : n - 1 - round;
-    *head = local - round * a.Hkv;
+    it->r = chunk + who;
+    it->q0 = __shfl_sync(0xffffffffu, lane_rq.q0, who);
+    it->nq = __shfl_sync(0xffffffffu, lane_rq.nq, who);
+    it->kv = __shfl_sync(0xffffffffu, lane_rq.kv, who);
+    it->k0 = __shfl_sync(0xffffffffu, lane_rq.k0, who);
+    const int n = ((kKeys ? it->kv : it->nq) + unit - 1) / unit, round = local / a.Hkv;
+    it->line = kKeys ? round : n - 1 - round;
+    it->head = local - round * a.Hkv;
     return true;
   }
 };
@@ -118,20 +160,37 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
 
 __device__ __forceinline__ uint64_t full_desc(uint32_t lo, uint64_t d) { return (uint64_t)lo | (d & 0xffffffff00000000ull); }
 
+// The products are issued by a whole warp, whose first lane's instructions count (leads != 0): descriptors stay in the registers
+// that the warp shares.
+__device__ __forceinline__ void umma_ts_if(uint32_t leads, uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leads)
+      : "memory");
+}
 // acc[128 x 128] = A B^T, both tiles [128][D] in shared memory (low words of their descriptors).
 template <int D>
-__device__ __forceinline__ void product_ss(uint32_t acc, uint32_t a_lo, uint32_t b_lo, uint64_t desc, uint32_t idesc) {
+__device__ __forceinline__ void product_ss(uint32_t leads, uint32_t acc, uint32_t a_lo, uint32_t b_lo, uint64_t desc, uint32_t idesc) {
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks) {
     const uint32_t off = ((ks >> 2) * (kTile * 128) + (ks & 3) * 32) >> 4;
-    ptx::umma_bf16(acc, full_desc(a_lo + off, desc), full_desc(b_lo + off, desc), idesc, ks != 0);
+    ptx::umma_bf16_if(leads, acc, full_desc(a_lo + off, desc), full_desc(b_lo + off, desc), idesc, ks != 0);
   }
 }
-// acc[128 x D] += A B: A in tensor memory as left by the compute warps (columns 0 .. 31 and 64 .. 95), B a tile [128][D].
-__device__ __forceinline__ void product_ts(uint32_t acc, uint32_t a_tmem, uint32_t b_lo, uint64_t desc, uint32_t idesc, bool first) {
+// acc[128 x 128] = A B^T with A [128][D] in tensor memory (two elements a column), B a tile [128][D].
+template <int D>
+__device__ __forceinline__ void product_ts_k(uint32_t leads, uint32_t acc, uint32_t a_tmem, uint32_t b_lo, uint64_t desc, uint32_t idesc) {
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks)
+    umma_ts_if(leads, acc, a_tmem + ks * 8, full_desc(b_lo + (((ks >> 2) * (kTile * 128) + (ks & 3) * 32) >> 4), desc), idesc, ks != 0);
+}
+// acc[128 x D] += A B with A [128][128] in tensor memory, its halves kGap columns apart, B a tile [128][D].
+template <int kGap>
+__device__ __forceinline__ void product_ts(uint32_t leads, uint32_t acc, uint32_t a_tmem, uint32_t b_lo, uint64_t desc, uint32_t idesc, bool first) {
 #pragma unroll
   for (int ks = 0; ks < kTile / 16; ++ks)
-    ptx::umma_bf16_ts(acc, a_tmem + (ks >> 2) * 64 + (ks & 3) * 8, full_desc(b_lo + ks * (2048 >> 4), desc), idesc, ks != 0 || !first);
+    umma_ts_if(leads, acc, a_tmem + (ks >> 2) * kGap + (ks & 3) * 8, full_desc(b_lo + ks * (2048 >> 4), desc), idesc, ks != 0 || !first);
 }
 
 // 32 columns of tensor memory as 16 pairs (after the wait).
@@ -140,6 +199,53 @@ __device__ __forceinline__ void load32(uint32_t taddr, uint32_t (&v)[32]) {
   ptx::tmem_wait_ld();
 #pragma unroll
   for (int k = 0; k < 32; ++k) asm volatile("" : "+r"(v[k]));   // no use before the wait
+}
+
+__device__ __forceinline__ void ld_shared_v4(uint32_t addr, uint32_t* x) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(addr) : "memory");
+}
+
+// `other` where the bit of a column is not set.
+__device__ __forceinline__ void mask32(uint32_t (&v)[32], uint32_t see, uint32_t other) {
+#pragma unroll
+  for (int k = 0; k < 32; ++k) v[k] = (see >> k) & 1u ? v[k] : other;
+}
+constexpr uint32_t kMinusInf = 0xff800000u;
+
+// 32 columns of a lane's row, times `by`, as bf16: four lanes exchange their 16-byte pieces, so that they write 64 bytes of one
+// row after the other.  to[m]: where the columns of row m of the four go; null: nowhere.  False if a value is not finite.
+__device__ __forceinline__ bool store_32_columns(const uint32_t (&v)[32], float by, __nv_bfloat16* const (&to)[4], int lane) {
+  uint32_t x[4][4];
+  uint64_t bad[2] = {0, 0};
+  const uint64_t by2 = ptx::pack2(by, by);
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const uint64_t y = mul2(ptx::pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), by2);
+    bad[k & 1] = ptx::fma2(y, 0, bad[k & 1]);                         // NaN if any is not finite
+    float lo, hi;
+    ptx::unpack2(y, &lo, &hi);
+    x[k >> 2][k & 3] = ptx::pack_bf16x2(lo, hi);
+  }
+#pragma unroll
+  for (int round = 1; round <= 2; round <<= 1) {                      // 4 x 4 transpose of pieces
+    const bool upper = lane & round;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k & round) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t got = __shfl_xor_sync(0xffffffffu, upper ? x[k][e] : x[k + round][e], round);
+        x[k][e] = upper ? got : x[k][e];
+        x[k + round][e] = upper ? x[k + round][e] : got;
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < 4; ++m)
+    if (to[m] != nullptr) *reinterpret_cast<uint4*>(to[m] + 8 * (lane & 3)) = make_uint4(x[m][0], x[m][1], x[m][2], x[m][3]);
+  float b0, b1;
+  ptx::unpack2(ptx::add2(bad[0], bad[1]), &b0, &b1);
+  return b0 + b1 == 0.f;
 }
 
 // Zeros in rows first .. last - 1 of a tile in shared memory, by the compute warps.
