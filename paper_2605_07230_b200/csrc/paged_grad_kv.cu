@@ -150,52 +150,40 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     const uint64_t desc = ptx::umma_desc_sw128(base), desc_mn = ptx::umma_desc_sw128_strides(base, kTile * 128, 1024);
     auto lo = [&](int i) { return (uint32_t)desc + i * (C::kTileBytes >> 4); };
     auto lo_mn = [&](int i) { return (uint32_t)desc_mn + i * (C::kTileBytes >> 4); };
-    const uint32_t leads = lane == 0;
     auto here = [&](uint64_t* bar, uint32_t parity) { return ok = __all_sync(0xffffffffu, wait.spin(bar, parity)); };
     Ring<3> behind;                                                    // the stage of the block whose last product comes next
-    // (the tensor cores take few products ahead: between two of them nothing is waited for that could be waited for earlier)
-    auto queries_here = [&]() { return here(&sh.q_full[ring.stage], ring.ph); };
-    auto gradients_here = [&](uint32_t b) { return here(&sh.do_full[b & 1u], b >> 1); };
-    auto scores = [&]() {
-      product_ss<D>(leads, t_s, lo(0), lo(kQ + ring.stage), desc, idesc_s);
-      ptx::umma_commit_if(leads, &sh.s_full);
-      ring.step();
-    };
-    auto d_weights = [&](uint32_t b) {
-      product_ss<D>(leads, t_dp, lo(1), lo(kDo + (b & 1u)), desc, idesc_s);
-      ptx::umma_commit_if(leads, &sh.dp_full);
-    };
+    // dV with the next S^T, and dK with the next dP^T, are one piece of code (this warp's instructions are fetched anew each time
+    // beside the others' loops); between two products nothing is waited for that could be waited for earlier.
     auto work = [&](int n) {
-      if (!queries_here() || !here(&sh.kv_full, used)) return;
-      ptx::tc_fence_after();
-      scores();
-      if (!gradients_here(blk)) return;
-      d_weights(blk);
-      if (n == 1) ptx::umma_commit_if(leads, &sh.kv_empty);
-      if (!here(&sh.acc_empty, used ^ 1u)) return;
+      if (!here(&sh.kv_full, used)) return;
 #pragma unroll 1
-      for (int i = 0; i < n; ++i) {
-        const uint32_t b = blk + i;
-        const bool more = i + 1 < n;
-        if ((more && !queries_here()) || !here(&sh.p_full, b)) return;
-        ptx::tc_fence_after();
-        product_ts<64>(leads, t_dv, t_s, lo_mn(kDo + (b & 1u)), desc_mn, idesc_o, i == 0);
-        ptx::umma_commit_if(leads, &sh.do_empty[b & 1u]);
-        if (more) scores();
-        if ((more && !gradients_here(b + 1)) || !here(&sh.ds_full, b)) return;
-        ptx::tc_fence_after();
-        product_ts<64>(leads, t_dk, t_dp, lo_mn(kQ + behind.stage), desc_mn, idesc_o, i == 0);
-        ptx::umma_commit_if(leads, &sh.q_empty[behind.stage]);
-        behind.step();
+      for (int i = -2; i < 2 * n; ++i) {
+        const bool second = i & 1, more = i < 2 * n - 2;
+        const uint32_t b = blk + (i >> 1), next = b + 1;
+        if (more && !here(second ? &sh.do_full[next & 1u] : &sh.q_full[ring.stage], second ? next >> 1 : ring.ph)) return;
+        if (i >= 0) {
+          if (i == 0 && !here(&sh.acc_empty, used ^ 1u)) return;
+          if (!here(second ? &sh.ds_full : &sh.p_full, b)) return;
+          ptx::tc_fence_after();
+          if (elect_one()) {                                           // dV += P^T dO or dK += dS^T Q
+            product_ts<64>(second ? t_dk : t_dv, second ? t_dp : t_s, lo_mn(second ? kQ + behind.stage : kDo + (b & 1u)), desc_mn, idesc_o, i < 2);
+            ptx::umma_commit(second ? &sh.q_empty[behind.stage] : &sh.do_empty[b & 1u]);
+          }
+          if (second) behind.step();
+        }
         if (more) {
-          d_weights(b + 1);
-          if (i + 2 == n) ptx::umma_commit_if(leads, &sh.kv_empty);
+          if (elect_one()) {                                           // S^T = K Q^T or dP^T = V dO^T
+            product_ss<D>(second ? t_dp : t_s, lo(second), lo(second ? kDo + (next & 1u) : kQ + ring.stage), desc, idesc_s);
+            ptx::umma_commit(second ? &sh.dp_full : &sh.s_full);
+            if (i == 2 * n - 3) ptx::umma_commit(&sh.kv_empty);
+          }
+          if (!second) ring.step();
         }
       }
-      ptx::umma_commit_if(leads, &sh.acc_full);
+      if (elect_one()) ptx::umma_commit(&sh.acc_full);
     };
     while (turns.next(sh.queue, wait, &ok)) {
-      const int n = turns.item(sh.queue).n;
+      const int n = __shfl_sync(0xffffffffu, turns.item(sh.queue).n, 0);
       turns.done(sh.queue, lane);
       if (n == 0) continue;
       work(n);

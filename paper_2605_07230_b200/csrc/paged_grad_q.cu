@@ -154,10 +154,9 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     const uint64_t desc = ptx::umma_desc_sw128(base), desc_mn = ptx::umma_desc_sw128_strides(base, kTile * 128, 1024);
     auto lo = [&](int i) { return (uint32_t)desc + i * (C::kTileBytes >> 4); };
     auto lo_mn = [&](int i) { return (uint32_t)desc_mn + i * (C::kTileBytes >> 4); };
-    const uint32_t leads = lane == 0;
     auto here = [&](uint64_t* bar, uint32_t parity) { return ok = __all_sync(0xffffffffu, wait.spin(bar, parity)); };
     while (turns.next(sh.queue, wait, &ok)) {
-      const int n = turns.item(sh.queue).n;
+      const int n = __shfl_sync(0xffffffffu, turns.item(sh.queue).n, 0);
       turns.done(sh.queue, lane);
       if (n == 0) continue;
       if (warp == kProducts) {
@@ -167,30 +166,36 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
           const uint32_t t = done + i;
           if (!here(&sh.k_full[ring.stage], ring.ph) || !here(&sh.s_empty, t ^ 1u)) break;
           ptx::tc_fence_after();
-          product_ts_k<D>(leads, t_s, t_q, lo(kK + ring.stage), desc, idesc_s);
-          ptx::umma_commit_if(leads, &sh.s_full);
+          if (elect_one()) {
+            product_ts_k<D>(t_s, t_q, lo(kK + ring.stage), desc, idesc_s);
+            ptx::umma_commit(&sh.s_full);
+          }
           ring.step();
           if (!here(&sh.v_full[t & 1u], t >> 1) || !here(&sh.dp_empty, t ^ 1u)) break;
           ptx::tc_fence_after();
-          product_ss<D>(leads, t_dp, lo(1), lo(kV + (t & 1u)), desc, idesc_s);
-          ptx::umma_commit_if(leads, &sh.dp_full);
-          ptx::umma_commit_if(leads, &sh.v_empty[t & 1u]);
+          if (elect_one()) {
+            product_ss<D>(t_dp, lo(1), lo(kV + (t & 1u)), desc, idesc_s);
+            ptx::umma_commit(&sh.dp_full);
+            ptx::umma_commit(&sh.v_empty[t & 1u]);
+            if (i + 1 == n) ptx::umma_commit(&sh.do_empty);
+          }
         }
         if (!ok) break;
-        ptx::umma_commit_if(leads, &sh.do_empty);
       } else {
         if (!here(&sh.acc_empty, used ^ 1u)) break;
 #pragma unroll 1
         for (int i = 0; i < n; ++i) {
           if (!here(&sh.ds_full, done + i)) break;
           ptx::tc_fence_after();
-          product_ts<32>(leads, t_dq, t_ds, lo_mn(kK + ring.stage), desc_mn, idesc_o, i == 0);
-          ptx::umma_commit_if(leads, &sh.ds_empty);
-          ptx::umma_commit_if(leads, &sh.k_empty[ring.stage]);         // (its S is done, or there were no dS)
+          if (elect_one()) {
+            product_ts<32>(t_dq, t_ds, lo_mn(kK + ring.stage), desc_mn, idesc_o, i == 0);
+            ptx::umma_commit(&sh.ds_empty);
+            ptx::umma_commit(&sh.k_empty[ring.stage]);                 // (its S is done, or there were no dS)
+            if (i + 1 == n) ptx::umma_commit(&sh.acc_full);
+          }
           ring.step();
         }
         if (!ok) break;
-        ptx::umma_commit_if(leads, &sh.acc_full);
       }
       ++used;
       done += n;

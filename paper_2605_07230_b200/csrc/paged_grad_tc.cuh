@@ -160,37 +160,35 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
 
 __device__ __forceinline__ uint64_t full_desc(uint32_t lo, uint64_t d) { return (uint64_t)lo | (d & 0xffffffff00000000ull); }
 
-// The products are issued by a whole warp, whose first lane's instructions count (leads != 0): descriptors stay in the registers
-// that the warp shares.
-__device__ __forceinline__ void umma_ts_if(uint32_t leads, uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
-      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leads)
-      : "memory");
+// The issuing warps walk their loops as a whole, so that descriptors stay in registers which the warp shares, and one lane (the same
+// each time) issues products and commits: 40 cycles a product of 16 columns where predicated instructions took 51.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t is;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+  return is != 0;
 }
 // acc[128 x 128] = A B^T, both tiles [128][D] in shared memory (low words of their descriptors).
 template <int D>
-__device__ __forceinline__ void product_ss(uint32_t leads, uint32_t acc, uint32_t a_lo, uint32_t b_lo, uint64_t desc, uint32_t idesc) {
+__device__ __forceinline__ void product_ss(uint32_t acc, uint32_t a_lo, uint32_t b_lo, uint64_t desc, uint32_t idesc) {
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks) {
     const uint32_t off = ((ks >> 2) * (kTile * 128) + (ks & 3) * 32) >> 4;
-    ptx::umma_bf16_if(leads, acc, full_desc(a_lo + off, desc), full_desc(b_lo + off, desc), idesc, ks != 0);
+    ptx::umma_bf16(acc, full_desc(a_lo + off, desc), full_desc(b_lo + off, desc), idesc, ks != 0);
   }
 }
 // acc[128 x 128] = A B^T with A [128][D] in tensor memory (two elements a column), B a tile [128][D].
 template <int D>
-__device__ __forceinline__ void product_ts_k(uint32_t leads, uint32_t acc, uint32_t a_tmem, uint32_t b_lo, uint64_t desc, uint32_t idesc) {
+__device__ __forceinline__ void product_ts_k(uint32_t acc, uint32_t a_tmem, uint32_t b_lo, uint64_t desc, uint32_t idesc) {
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks)
-    umma_ts_if(leads, acc, a_tmem + ks * 8, full_desc(b_lo + (((ks >> 2) * (kTile * 128) + (ks & 3) * 32) >> 4), desc), idesc, ks != 0);
+    ptx::umma_bf16_ts(acc, a_tmem + ks * 8, full_desc(b_lo + (((ks >> 2) * (kTile * 128) + (ks & 3) * 32) >> 4), desc), idesc, ks != 0);
 }
 // acc[128 x D] += A B with A [128][128] in tensor memory, its halves kGap columns apart, B a tile [128][D].
 template <int kGap>
-__device__ __forceinline__ void product_ts(uint32_t leads, uint32_t acc, uint32_t a_tmem, uint32_t b_lo, uint64_t desc, uint32_t idesc, bool first) {
+__device__ __forceinline__ void product_ts(uint32_t acc, uint32_t a_tmem, uint32_t b_lo, uint64_t desc, uint32_t idesc, bool first) {
 #pragma unroll
   for (int ks = 0; ks < kTile / 16; ++ks)
-    umma_ts_if(leads, acc, a_tmem + (ks >> 2) * kGap + (ks & 3) * 8, full_desc(b_lo + ks * (2048 >> 4), desc), idesc, ks != 0 || !first);
+    ptx::umma_bf16_ts(acc, a_tmem + (ks >> 2) * kGap + (ks & 3) * 8, full_desc(b_lo + ks * (2048 >> 4), desc), idesc, ks != 0 || !first);
 }
 
 // 32 columns of tensor memory as 16 pairs (after the wait).
