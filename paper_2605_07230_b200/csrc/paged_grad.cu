@@ -149,15 +149,5 @@ extern "C" int cascade_paged_attn_grad(cascade_ctx* ctx, const cascade_paged_cac
   else
     status = wide ? launch_stats<float, 128>(ctx, p, lse, s) : launch_stats<float, 64>(ctx, p, lse, s);
   CASCADE_TRY(status);
-  if (sh.dtype != CASCADE_BF16) return launch_paged_grad_f32(ctx, p, s);
-  grad_tc::Args t;
-  t.g = p;
-  t.G = sh.Hq / sh.Hkv;
-  t.tpb = grad_tc::kTile / t.G;
-  t.box_rows = 8;
-  while (t.box_rows < grad_tc::kTile && a.page_size % (2 * t.box_rows) == 0) t.box_rows *= 2;
-  t.taken = ctx->dev_error + 40;   // (cleared with the error word when the context is made)
-  CASCADE_TRY(launch_paged_grad_kv(ctx, t, s));
-  t.taken += 2;
-  return launch_paged_grad_q(ctx, t, s);
+  return sh.dtype == CASCADE_BF16 ? launch_paged_grad_tc(ctx, p, s) : launch_paged_grad_f32(ctx, p, s);
 }

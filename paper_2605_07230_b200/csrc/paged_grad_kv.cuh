@@ -10,43 +10,32 @@
 //     product that frees a stage) and output gradients through two;
 //   * warp 9 issues the products;  warp 10 brings the rows' statistics;
 //   * warps 0-7: a key per lane, half of a block's rows each; P stays in registers between the two halves of the work.
+#pragma once
 #include <climits>
 
 #include "paged_grad_tc.cuh"
 
-namespace {
+namespace grad_tc {
 
-using namespace grad_tc;
-
-struct Shared {
+struct SharedKv {
   uint64_t kv_full, kv_empty, q_full[3], q_empty[3], do_full[2], do_empty[2], s_full, p_full, dp_full, ds_full, acc_full, acc_empty, stat_full[2],
       stat_empty[2];
   Queue queue;
-  uint64_t alive;
-  int abort_flag;
-  uint32_t tmem;
   __align__(16) float lse[2][kTile], delta[2][kTile];                  // negated
 };
 
+// The whole CTA; `cta` of `n_cta` that begin with this pass, the others (cta >= n_cta) take what its counter hands out.
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
-k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do, const __grid_constant__ CUtensorMap tm_k,
-                const __grid_constant__ CUtensorMap tm_v, const Args p) {
+__device__ __forceinline__ void pass_kv(const CUtensorMap& tm_q, const CUtensorMap& tm_do, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Args& p,
+                                        uint8_t* smem, uint32_t base, uint32_t tmem, const Waits& wait, int cta, int n_cta) {
   using C = Cfg<D>;
-  extern __shared__ __align__(1024) uint8_t smem[];
-  Shared& sh = *reinterpret_cast<Shared*>(smem + C::kTiles * C::kTileBytes);
+  SharedKv& sh = *reinterpret_cast<SharedKv*>(smem + C::kTiles * C::kTileBytes + sizeof(Common));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t base = ptx::smem_u32(smem);
   // tiles: keys, values, queries of three stages, output gradients of two
   constexpr int kQ = 2, kDo = 5;
   auto tile = [&](int i) { return base + i * C::kTileBytes; };
   const PagedAttnArgs& a = p.g.a;
-  if ((base & 1023u) != 0) {                                           // (the same in all threads of all CTAs)
-    if (threadIdx.x == 0) atomicOr(a.err, CASCADE_DEV_ERR_WAIT);
-    return;
-  }
-  const Waits wait = {&sh.abort_flag, &sh.alive, a.err, a.wait_ns};
-
+  int* taken = p.taken + 0;
   if (threadIdx.x == 0) {
     for (uint64_t* b : {&sh.kv_full, &sh.kv_empty, &sh.s_full, &sh.dp_full, &sh.acc_full}) ptx::mbar_init(b, 1);
     for (uint64_t* b : {&sh.p_full, &sh.ds_full, &sh.acc_empty}) ptx::mbar_init(b, kComputeWarps);
@@ -62,8 +51,6 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
       ptx::mbar_init(&sh.queue.full[i], 1);
       ptx::mbar_init(&sh.queue.empty[i], kWarps - 1);
     }
-    sh.abort_flag = 0;
-    sh.alive = 0;
     ptx::fence_mbar_init();
   }
   const int block_rows = p.tpb * p.G;
@@ -71,20 +58,8 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     for (int i = kQ; i < C::kTiles; ++i) clear_rows<D>(tile(i), block_rows, kTile, threadIdx.x);
     ptx::fence_proxy_async_smem();
   }
-  if (warp == kLoads && lane == 0) {
-    ptx::prefetch_tmap(&tm_q);
-    ptx::prefetch_tmap(&tm_do);
-    ptx::prefetch_tmap(&tm_k);
-    ptx::prefetch_tmap(&tm_v);
-  }
-  if (warp == kProducts) {
-    ptx::tmem_alloc(&sh.tmem, 512);
-    ptx::tmem_relinquish();
-  }
-  ptx::tc_fence_before();
   __syncthreads();
-  ptx::tc_fence_after();
-  const uint32_t t_s = sh.tmem, t_dp = t_s + 128, t_dv = t_s + 256, t_dk = t_dv + D;
+  const uint32_t t_s = tmem, t_dp = t_s + 128, t_dv = t_s + 256, t_dk = t_dv + D;
 
   Turns turns;
   uint32_t used = 0, blk = 0;                                          // items with blocks, and blocks, so far
@@ -96,14 +71,15 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     const uint32_t box_bytes = (uint32_t)p.box_rows * 128u, row_bytes = (uint32_t)block_rows * 128u * C::kHalves;
     Cursor<true> cur;
     Item it = {};
-    for (int item = blockIdx.x;;) {
+    for (int item = cta < n_cta ? cta : INT_MIN;;) {
+      if (item == INT_MIN) item = __shfl_sync(0xffffffffu, lane == 0 ? n_cta + atomicAdd(taken, 1) : 0, 0);
       const bool more = cur.find(p, item, lane, &it);
       int lo, hi;                                                      // tokens that see any of the keys -> row blocks
       paged::tokens_that_see(a, it.kv - it.nq, it.nq, it.line * kTile, min(it.kv, (it.line + 1) * kTile) - 1, &lo, &hi);
       it.first = lo / p.tpb;
       it.n = !more ? -1 : hi > lo ? (hi - 1) / p.tpb - it.first + 1 : 0;
       if (!turns.tell(sh.queue, wait, it, lane, &ok) || !more) break;
-      const int granted = lane == 0 ? (int)gridDim.x + atomicAdd(p.taken, 1) : 0;
+      const int granted = lane == 0 ? n_cta + atomicAdd(taken, 1) : 0;
       auto load_rows = [&](int i, const CUtensorMap* m, uint64_t* full, uint64_t* empty, uint32_t ph, int to) {
         ok = __all_sync(0xffffffffu, ok && wait(empty, ph ^ 1u));
         if (ok && lane == 0) {
@@ -150,7 +126,7 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     const uint64_t desc = ptx::umma_desc_sw128(base), desc_mn = ptx::umma_desc_sw128_strides(base, kTile * 128, 1024);
     auto lo = [&](int i) { return (uint32_t)desc + i * (C::kTileBytes >> 4); };
     auto lo_mn = [&](int i) { return (uint32_t)desc_mn + i * (C::kTileBytes >> 4); };
-    auto here = [&](uint64_t* bar, uint32_t parity) { return ok = __all_sync(0xffffffffu, wait.spin(bar, parity)); };
+    auto here = [&](uint64_t* bar, uint32_t parity) { return ok = __all_sync(0xffffffffu, wait(bar, parity)); };
     Ring<3> behind;                                                    // the stage of the block whose last product comes next
     // dV with the next S^T, and dK with the next dP^T, are one piece of code (this warp's instructions are fetched anew each time
     // beside the others' loops); between two products nothing is waited for that could be waited for earlier.
@@ -268,11 +244,10 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
           if (masked) mask32(v, see[q], kMinusInf);
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
+            const uint64_t x = ptx::fma2(ptx::pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), c2, w[16 * q + k]);
+            w[16 * q + k] = k % 3 == 1 ? pow2<true>(x) : pow2<false>(x);
             float e0, e1;
-            ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), c2, w[16 * q + k]), &e0, &e1);
-            e0 = ptx::ex2(e0);
-            e1 = ptx::ex2(e1);
-            w[16 * q + k] = ptx::pack2(e0, e1);
+            ptx::unpack2(w[16 * q + k], &e0, &e1);
             pk[k] = ptx::pack_bf16x2(e0, e1);
           }
           ptx::tmem_st16_async(my_s + 16 * q, pk);
@@ -364,9 +339,9 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         // (0.6 us a row: whoever waits meanwhile starts its limit anew)
         const int k = it.line * kTile + (warp & 3) * 32 + __ffs(again) - 1;
         if (part == 0)
-          paged::grad_key<__nv_bfloat16, D, false, true>(p.g, it.r, it, k, it.head, lane, &sh.alive);
+          paged::grad_key<__nv_bfloat16, D, false, true>(p.g, it.r, it, k, it.head, lane, wait.alive);
         else
-          paged::grad_key<__nv_bfloat16, D, true, false>(p.g, it.r, it, k, it.head, lane, &sh.alive);
+          paged::grad_key<__nv_bfloat16, D, true, false>(p.g, it.r, it, k, it.head, lane, wait.alive);
       }
       turns.done(sh.queue, lane);
     }
@@ -376,34 +351,13 @@ k_paged_grad_kv(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
-  if (threadIdx.x == 0 && atomicAdd(p.taken + 1, 1) == (int)gridDim.x - 1) p.taken[0] = p.taken[1] = 0;
-  if (warp == kProducts) ptx::tmem_dealloc(t_s, 512);
+  if (threadIdx.x == 0)                                                // (the other pass lays its own barriers out here)
+    for (uint64_t* b = reinterpret_cast<uint64_t*>(&sh); b < reinterpret_cast<uint64_t*>(&sh.queue); ++b) inval(b);
+  if (threadIdx.x < kSlots) {
+    inval(&sh.queue.full[threadIdx.x]);
+    inval(&sh.queue.empty[threadIdx.x]);
+  }
+  __syncthreads();
 }
 
-template <int D>
-int launch(cascade_ctx* ctx, const Args& p, int grid, cudaStream_t s) {
-  const PagedAttnArgs& a = p.g.a;
-  CUtensorMap mq, mo;
-  const CUtensorMap *mk = page_map(ctx, p, D, a.k), *mv = page_map(ctx, p, D, a.v);
-  if (mk == nullptr || mv == nullptr || !row_map(&mq, p, D, a.q, a.q_stride) || !row_map(&mo, p, D, p.g.d_out, (long long)a.Hq * D))
-    return CASCADE_ERR_CUDA;
-  constexpr int kSmem = smem_bytes<D, Shared>();
-  CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_KV, k_paged_grad_kv<D>, kSmem));   // (a context has one D)
-  KernelScope ks(ctx, K_PAGED_GRAD, s);
-  k_paged_grad_kv<D><<<grid, kThreads, kSmem, s>>>(mq, mo, *mk, *mv, p);
-  CASCADE_CUDA_TRY(cudaGetLastError());
-  return CASCADE_OK;
-}
-
-}  // namespace
-
-int launch_paged_grad_kv(cascade_ctx* ctx, const grad_tc::Args& p, cudaStream_t s) {
-  const PagedAttnArgs& a = p.g.a;
-  // no more items than this: a request's tiles are at most ceil(keys / 128)
-  const long long tiles = (long long)p.g.n_kv / kTile + a.n_req, by_length = (long long)a.n_req * ((a.max_kv + kTile - 1) / kTile);
-  const long long items = (tiles < by_length ? tiles : by_length) * a.Hkv;
-  if (items > INT_MAX / 2) return CASCADE_ERR_UNSUPPORTED_SHAPE;
-  if (items == 0) return CASCADE_OK;
-  const int grid = (int)(items < ctx->sm_count ? items : ctx->sm_count);
-  return ctx->shape.D == 128 ? launch<128>(ctx, p, grid, s) : launch<64>(ctx, p, grid, s);
-}
+}  // namespace grad_tc

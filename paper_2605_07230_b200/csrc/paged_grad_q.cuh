@@ -9,44 +9,33 @@
 //   * warp 9 issues S and dP, warp 10 dQ: a warp that issues is held up until the tensor cores have taken its products, and what
 //     it waits for next should be looked at meanwhile;
 //   * warps 0-7: a row per lane, half of a tile's keys each; P stays in registers.
+#pragma once
 #include <climits>
 
 #include "paged_grad_tc.cuh"
 
-namespace {
-
-using namespace grad_tc;
+namespace grad_tc {
 
 constexpr int kOutputs = kStats;                                       // the warp that issues dQ (rows' statistics are read by their own lanes)
 
-struct Shared {
+struct SharedQ {
   uint64_t q_full, q_empty, do_full, do_empty, a_full, k_full[3], k_empty[3], v_full[2], v_empty[2], s_full, s_empty, dp_full, dp_empty, ds_full,
       ds_empty, acc_full, acc_empty;
   Queue queue;
-  uint64_t alive;
-  int abort_flag;
-  uint32_t tmem;
 };
 
+// The whole CTA; `cta` of `n_cta` that begin with this pass, the others (cta >= n_cta) take what its counter hands out.
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
-k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do, const __grid_constant__ CUtensorMap tm_k,
-               const __grid_constant__ CUtensorMap tm_v, const Args p) {
+__device__ __forceinline__ void pass_q(const CUtensorMap& tm_q, const CUtensorMap& tm_do, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const Args& p,
+                                        uint8_t* smem, uint32_t base, uint32_t tmem, const Waits& wait, int cta, int n_cta) {
   using C = Cfg<D>;
-  extern __shared__ __align__(1024) uint8_t smem[];
-  Shared& sh = *reinterpret_cast<Shared*>(smem + C::kTiles * C::kTileBytes);
+  SharedQ& sh = *reinterpret_cast<SharedQ*>(smem + C::kTiles * C::kTileBytes + sizeof(Common));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t base = ptx::smem_u32(smem);
   // tiles: queries, output gradients, keys of three stages, values of two
   constexpr int kK = 2, kV = 5;
   auto tile = [&](int i) { return base + i * C::kTileBytes; };
   const PagedAttnArgs& a = p.g.a;
-  if ((base & 1023u) != 0) {                                           // (the same in all threads of all CTAs)
-    if (threadIdx.x == 0) atomicOr(a.err, CASCADE_DEV_ERR_WAIT);
-    return;
-  }
-  const Waits wait = {&sh.abort_flag, &sh.alive, a.err, a.wait_ns};
-
+  int* taken = p.taken + 1;
   if (threadIdx.x == 0) {
     for (uint64_t* b : {&sh.q_full, &sh.do_full, &sh.do_empty, &sh.s_full, &sh.dp_full, &sh.ds_empty, &sh.acc_full}) ptx::mbar_init(b, 1);
     for (uint64_t* b : {&sh.q_empty, &sh.a_full, &sh.s_empty, &sh.dp_empty, &sh.ds_full, &sh.acc_empty}) ptx::mbar_init(b, kComputeWarps);
@@ -61,24 +50,10 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
       ptx::mbar_init(&sh.queue.full[i], 1);
       ptx::mbar_init(&sh.queue.empty[i], kWarps - 1);
     }
-    sh.abort_flag = 0;
-    sh.alive = 0;
     ptx::fence_mbar_init();
   }
-  if (warp == kLoads && lane == 0) {
-    ptx::prefetch_tmap(&tm_q);
-    ptx::prefetch_tmap(&tm_do);
-    ptx::prefetch_tmap(&tm_k);
-    ptx::prefetch_tmap(&tm_v);
-  }
-  if (warp == kProducts) {
-    ptx::tmem_alloc(&sh.tmem, 512);
-    ptx::tmem_relinquish();
-  }
-  ptx::tc_fence_before();
   __syncthreads();
-  ptx::tc_fence_after();
-  const uint32_t t_s = sh.tmem, t_dp = t_s + 128, t_ds = t_s + 256, t_q = t_s + 320, t_dq = t_s + 384;
+  const uint32_t t_s = tmem, t_dp = t_s + 128, t_ds = t_s + 256, t_q = t_s + 320, t_dq = t_s + 384;
 
   Turns turns;
   uint32_t used = 0, done = 0;                                         // items with tiles, and tiles, so far
@@ -92,7 +67,8 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     const uint32_t box_bytes = (uint32_t)p.box_rows * 128u, row_bytes = (uint32_t)(p.tpb * p.G) * 128u * C::kHalves;
     Cursor<false> cur;
     Item it = {};
-    for (int item = blockIdx.x;;) {
+    for (int item = cta < n_cta ? cta : INT_MIN;;) {
+      if (item == INT_MIN) item = __shfl_sync(0xffffffffu, lane == 0 ? n_cta + atomicAdd(taken, 1) : 0, 0);
       const bool more = cur.find(p, item, lane, &it);
       {
         const int x0 = it.kv - it.nq, t0 = it.line * p.tpb, last = x0 + min(it.nq, t0 + p.tpb) - 1;
@@ -102,7 +78,7 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
         it.n = !more ? -1 : last < 0 ? 0 : last / kTile + 1 - it.skip;
       }
       if (!turns.tell(sh.queue, wait, it, lane, &ok) || !more) break;
-      const int granted = lane == 0 ? (int)gridDim.x + atomicAdd(p.taken, 1) : 0;
+      const int granted = lane == 0 ? n_cta + atomicAdd(taken, 1) : 0;
       bool bad = false;
       if (it.n > 0) {
         const int32_t* table = a.block_table + (size_t)it.r * a.table_stride;
@@ -146,7 +122,7 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
       item = __shfl_sync(0xffffffffu, granted, 0);
     }
     // everything has been given back before the CTA may end (the arrivals are asynchronous)
-    ok = ok && wait(&sh.q_empty, used ^ 1u) && wait(&sh.do_empty, used ^ 1u);
+    ok = ok && wait(&sh.q_empty, used ^ 1u) && wait(&sh.do_empty, used ^ 1u) && wait(&sh.ds_empty, done ^ 1u);
     for (uint32_t i = 0; i < 2; ++i) ok = ok && wait(&sh.v_empty[(done + i) & 1u], ((done + i) >> 1) ^ 1u);
     for (uint32_t i = 0; i < 3; ++i, ring.step()) ok = ok && wait(&sh.k_empty[ring.stage], ring.ph ^ 1u);
   } else if (warp == kProducts || warp == kOutputs) {
@@ -154,7 +130,7 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
     const uint64_t desc = ptx::umma_desc_sw128(base), desc_mn = ptx::umma_desc_sw128_strides(base, kTile * 128, 1024);
     auto lo = [&](int i) { return (uint32_t)desc + i * (C::kTileBytes >> 4); };
     auto lo_mn = [&](int i) { return (uint32_t)desc_mn + i * (C::kTileBytes >> 4); };
-    auto here = [&](uint64_t* bar, uint32_t parity) { return ok = __all_sync(0xffffffffu, wait.spin(bar, parity)); };
+    auto here = [&](uint64_t* bar, uint32_t parity) { return ok = __all_sync(0xffffffffu, wait(bar, parity)); };
     while (turns.next(sh.queue, wait, &ok)) {
       const int n = __shfl_sync(0xffffffffu, turns.item(sh.queue).n, 0);
       turns.done(sh.queue, lane);
@@ -276,9 +252,8 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
           if (masked) mask32(v, see[q], kMinusInf);
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
-            float e0, e1;
-            ptx::unpack2(ptx::fma2(ptx::pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), c2, lse2), &e0, &e1);
-            w[16 * q + k] = ptx::pack2(ptx::ex2(e0), ptx::ex2(e1));
+            const uint64_t y = ptx::fma2(ptx::pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), c2, lse2);
+            w[16 * q + k] = k % 3 == 1 ? pow2<true>(y) : pow2<false>(y);
           }
         }
         if (tile_key + kTile > kv) {                                   // keys behind the last: whatever the page held before
@@ -363,7 +338,7 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
       for (uint32_t again = __ballot_sync(0xffffffffu, odd); again != 0u; again &= again - 1u) {
         const int who = __ffs(again) - 1;
         paged::grad_row<__nv_bfloat16, D>(p.g, it.r, __shfl_sync(0xffffffffu, row, who), __shfl_sync(0xffffffffu, x, who),
-                                          __shfl_sync(0xffffffffu, q_head, who), lane, part * (D / 64), (part + 1) * (D / 64), &sh.alive);
+                                          __shfl_sync(0xffffffffu, q_head, who), lane, part * (D / 64), (part + 1) * (D / 64), wait.alive);
       }
       turns.done(sh.queue, lane);
     }
@@ -373,33 +348,13 @@ k_paged_grad_q(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
-  if (threadIdx.x == 0 && atomicAdd(p.taken + 1, 1) == (int)gridDim.x - 1) p.taken[0] = p.taken[1] = 0;
-  if (warp == kProducts) ptx::tmem_dealloc(t_s, 512);
+  if (threadIdx.x == 0)                                                // (the other pass lays its own barriers out here)
+    for (uint64_t* b = reinterpret_cast<uint64_t*>(&sh); b < reinterpret_cast<uint64_t*>(&sh.queue); ++b) inval(b);
+  if (threadIdx.x < kSlots) {
+    inval(&sh.queue.full[threadIdx.x]);
+    inval(&sh.queue.empty[threadIdx.x]);
+  }
+  __syncthreads();
 }
 
-template <int D>
-int launch(cascade_ctx* ctx, const Args& p, int grid, cudaStream_t s) {
-  const PagedAttnArgs& a = p.g.a;
-  CUtensorMap mq, mo;
-  const CUtensorMap *mk = page_map(ctx, p, D, a.k), *mv = page_map(ctx, p, D, a.v);
-  if (mk == nullptr || mv == nullptr || !row_map(&mq, p, D, a.q, a.q_stride) || !row_map(&mo, p, D, p.g.d_out, (long long)a.Hq * D))
-    return CASCADE_ERR_CUDA;
-  constexpr int kSmem = smem_bytes<D, Shared>();
-  CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_Q, k_paged_grad_q<D>, kSmem));   // (a context has one D)
-  KernelScope ks(ctx, K_PAGED_GRAD, s);
-  k_paged_grad_q<D><<<grid, kThreads, kSmem, s>>>(mq, mo, *mk, *mv, p);
-  CASCADE_CUDA_TRY(cudaGetLastError());
-  return CASCADE_OK;
-}
-
-}  // namespace
-
-int launch_paged_grad_q(cascade_ctx* ctx, const grad_tc::Args& p, cudaStream_t s) {
-  const PagedAttnArgs& a = p.g.a;
-  // no more items than this: a request's blocks are at most ceil(tokens / tpb)
-  const long long blocks = (long long)a.n_tok / p.tpb + a.n_req, by_length = (long long)a.n_req * ((a.max_q + p.tpb - 1) / p.tpb);
-  const long long items = (blocks < by_length ? blocks : by_length) * a.Hkv;
-  if (items > INT_MAX / 2) return CASCADE_ERR_UNSUPPORTED_SHAPE;
-  const int grid = (int)(items < ctx->sm_count ? items : ctx->sm_count);
-  return ctx->shape.D == 128 ? launch<128>(ctx, p, grid, s) : launch<64>(ctx, p, grid, s);
-}
+}  // namespace grad_tc

@@ -1,0 +1,106 @@
+// The gradient of the attention over a paged cache on the tensor cores (bf16): keys' and queries' passes side by side in one launch.
+//
+// A CTA an SM; most begin with the keys' pass, the rest with the queries' (a step of 128 x 128 takes 4.1 and 2.9 thousand cycles).
+// Where there are many items a CTA that finds no more goes on with the other pass.
+#include "paged_grad_kv.cuh"
+#include "paged_grad_q.cuh"
+
+namespace {
+
+using namespace grad_tc;
+
+template <int D>
+constexpr int kSmem = Cfg<D>::kTiles * Cfg<D>::kTileBytes + (int)sizeof(Common) +
+                      (int)(sizeof(SharedKv) > sizeof(SharedQ) ? sizeof(SharedKv) : sizeof(SharedQ));
+static_assert(kSmem<128> <= 232448, "shared memory of a CTA");
+static_assert(sizeof(Common) % 16 == 0, "alignment of what follows");
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+k_paged_grad_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do, const __grid_constant__ CUtensorMap tm_k,
+                const __grid_constant__ CUtensorMap tm_v, const Args p) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  Common& sh = *reinterpret_cast<Common*>(smem + Cfg<D>::kTiles * Cfg<D>::kTileBytes);
+  const uint32_t base = ptx::smem_u32(smem);
+  if ((base & 1023u) != 0) {                                           // (the same in all threads of all CTAs)
+    if (threadIdx.x == 0) atomicOr(p.g.a.err, CASCADE_DEV_ERR_WAIT);
+    return;
+  }
+  const int warp = threadIdx.x >> 5;
+  const Waits wait = {&sh.abort_flag, &sh.alive, p.g.a.err, p.g.a.wait_ns};
+  if (threadIdx.x == 0) {
+    sh.abort_flag = 0;
+    sh.alive = 0;
+    ptx::prefetch_tmap(&tm_q);
+    ptx::prefetch_tmap(&tm_do);
+    ptx::prefetch_tmap(&tm_k);
+    ptx::prefetch_tmap(&tm_v);
+  }
+  if (warp == kProducts) {
+    ptx::tmem_alloc(&sh.tmem, 512);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = sh.tmem;
+  const bool keys_first = (int)blockIdx.x < p.n_cta_keys;
+  const int n_q = (int)gridDim.x - p.n_cta_keys;
+#pragma unroll 1
+  for (int k = 0; k < (p.both ? 2 : 1) && !*wait.abort_flag; ++k) {
+    const bool keys = keys_first == (k == 0);
+    const int cta = k != 0 ? INT_MAX : keys ? (int)blockIdx.x : (int)blockIdx.x - p.n_cta_keys;
+    if (keys)
+      pass_kv<D>(tm_q, tm_do, tm_k, tm_v, p, smem, base, tmem, wait, cta, p.n_cta_keys);
+    else
+      pass_q<D>(tm_q, tm_do, tm_k, tm_v, p, smem, base, tmem, wait, cta, n_q);
+  }
+  if (threadIdx.x == 0 && atomicAdd(p.taken + 2, 1) == (int)gridDim.x - 1) p.taken[0] = p.taken[1] = p.taken[2] = 0;
+  if (warp == kProducts) ptx::tmem_dealloc(tmem, 512);
+}
+
+template <int D>
+int launch(cascade_ctx* ctx, const Args& p, int grid, cudaStream_t s) {
+  const PagedAttnArgs& a = p.g.a;
+  CUtensorMap mq, mo;
+  const CUtensorMap *mk = page_map(ctx, p, D, a.k), *mv = page_map(ctx, p, D, a.v);
+  if (mk == nullptr || mv == nullptr || !row_map(&mq, p, D, a.q, a.q_stride) || !row_map(&mo, p, D, p.g.d_out, (long long)a.Hq * D))
+    return CASCADE_ERR_CUDA;
+  CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_KV, k_paged_grad_tc<D>, kSmem<D>));   // (a context has one D)
+  KernelScope ks(ctx, K_PAGED_GRAD, s);
+  k_paged_grad_tc<D><<<grid, kThreads, kSmem<D>, s>>>(mq, mo, *mk, *mv, p);
+  CASCADE_CUDA_TRY(cudaGetLastError());
+  return CASCADE_OK;
+}
+
+// No more items than this: a request's tiles are at most ceil(length / unit).
+long long most_items(const PagedAttnArgs& a, long long total, int most, int unit) {
+  const long long pieces = total / unit + a.n_req, by_length = (long long)a.n_req * ((most + unit - 1) / unit);
+  return (pieces < by_length ? pieces : by_length) * a.Hkv;
+}
+
+}  // namespace
+
+int launch_paged_grad_tc(cascade_ctx* ctx, const PagedGradArgs& g, cudaStream_t s) {
+  const PagedAttnArgs& a = g.a;
+  Args p;
+  p.g = g;
+  p.G = a.Hq / a.Hkv;
+  p.tpb = kTile / p.G;
+  p.box_rows = 8;
+  while (p.box_rows < kTile && a.page_size % (2 * p.box_rows) == 0) p.box_rows *= 2;
+  p.taken = ctx->dev_error + 40;   // (cleared with the error word when the context is made)
+  const long long keys = most_items(a, g.n_kv, a.max_kv, kTile), rows = most_items(a, a.n_tok, a.max_q, p.tpb), sms = ctx->sm_count;
+  if (keys > INT_MAX / 2 || rows > INT_MAX / 2) return CASCADE_ERR_UNSUPPORTED_SHAPE;
+  // all items at once if there are no more than SMs; else the SMs in proportion to the passes' time
+  if (keys + rows <= sms) {
+    p.n_cta_keys = (int)keys;
+  } else {
+    const long long share = (sms * 41 * keys + (41 * keys + 29 * rows) / 2) / (41 * keys + 29 * rows), most = keys < sms - 1 ? keys : sms - 1;
+    p.n_cta_keys = (int)(keys == 0 ? 0 : share < 1 ? 1 : share > most ? most : share);
+  }
+  const long long left = sms - p.n_cta_keys;
+  const int grid = p.n_cta_keys + (int)(rows < left ? rows : left);
+  p.both = keys + rows > 4 * sms;
+  return ctx->shape.D == 128 ? launch<128>(ctx, p, grid, s) : launch<64>(ctx, p, grid, s);
+}

@@ -19,12 +19,13 @@ struct Cfg {
   static constexpr int kTileBytes = kTile * D * 2;
   static constexpr int kTiles = 7;
 };
-// Shared memory: the tiles, then what S holds.  The tiles' swizzle wants 1024-byte boundaries, which dynamic shared memory has
-// where a kernel has no other; a kernel that finds it elsewhere reports and leaves.
-template <int D, typename S>
-constexpr int smem_bytes() {
-  return Cfg<D>::kTiles * Cfg<D>::kTileBytes + (int)sizeof(S);
-}
+// Shared memory: the tiles, what both passes share, then a pass's own.  The tiles' swizzle wants 1024-byte boundaries, which dynamic
+// shared memory has where a kernel has no other; a kernel that finds it elsewhere reports and leaves.
+struct Common {
+  uint64_t alive;
+  int abort_flag;
+  uint32_t tmem;
+};
 
 // Place of the next use in a ring of kN stages, and its parity.
 template <int kN>
@@ -41,7 +42,9 @@ struct Ring {
 struct Args {
   PagedGradArgs g;
   int G, tpb, box_rows;           // query heads a key head; tokens per row block; rows of a page box
-  int* taken;                     // [0] items handed out beyond the blocks' own, [1] blocks that are done; zero between launches
+  int n_cta_keys;                 // CTAs that begin with the keys' pass
+  bool both;                      // a CTA whose pass has no more items goes on with the other
+  int* taken;                     // items of either pass handed out beyond the CTAs' own, CTAs that are done; zero between launches
 };
 
 // The items that a CTA takes: its own index first, then what the launch's counter gives.  The loading warp finds an item's request
@@ -65,13 +68,6 @@ struct Waits {
   uint64_t ns;
   __device__ __forceinline__ bool operator()(uint64_t* bar, uint32_t parity) const {
     return ptx::mbar_wait_short(bar, parity & 1u, abort_flag, err, ns, alive);
-  }
-  // Without going to sleep, where the wait lies on the critical path and few poll.
-  __device__ __forceinline__ bool spin(uint64_t* bar, uint32_t parity) const {
-#pragma unroll 1
-    for (int i = 0; i < 64; ++i)
-      if (ptx::mbar_test_wait(bar, parity & 1u)) return true;
-    return (*this)(bar, parity);
   }
 };
 
@@ -158,6 +154,29 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   return r;
 }
 
+// 2^x of a pair.  kPoly: on the multiply-add units, 1 + r (c1 + r (c2 + r (c3 + r c4))) with r = x - round(x) in [-1/2, 1/2] (least
+// largest error of that form: 2.9e-6 relative, where the weights are rounded to 2^-9), times 2^round(x); below -127 exactly 0, no
+// number stays none.  A third of the weights goes there: 16 exponentials a cycle and SM take 1024 cycles a 128 x 128 tile.
+template <bool kPoly>
+__device__ __forceinline__ uint64_t pow2(uint64_t x) {
+  float x0, x1;
+  ptx::unpack2(x, &x0, &x1);
+  if (!kPoly) return ptx::pack2(ptx::ex2(x0), ptx::ex2(x1));
+  auto both = [](float v) { return ptx::pack2(v, v); };
+  asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x0));       // -127
+  asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x1));
+  x = ptx::pack2(x0, x1);
+  const uint64_t t = ptx::add2(x, both(12582912.f));       // 1.5 2^23: the integer part in the last bits
+  const uint64_t r = ptx::fma2(ptx::add2(t, both(-12582912.f)), both(-1.f), x);
+  uint64_t y = ptx::fma2(both(0.009582853f), r, both(0.055906426f));
+  y = ptx::fma2(y, r, both(0.24024099f));
+  y = ptx::fma2(y, r, both(0.69312418f));
+  y = ptx::fma2(y, r, both(1.f));
+  float t0, t1;
+  ptx::unpack2(t, &t0, &t1);
+  return mul2(y, ptx::pack2(__int_as_float(__float_as_int(t0) * (1 << 23) + 0x3f800000), __int_as_float(__float_as_int(t1) * (1 << 23) + 0x3f800000)));
+}
+
 __device__ __forceinline__ uint64_t full_desc(uint32_t lo, uint64_t d) { return (uint64_t)lo | (d & 0xffffffff00000000ull); }
 
 // The issuing warps walk their loops as a whole, so that descriptors stay in registers which the warp shares, and one lane (the same
@@ -199,6 +218,7 @@ __device__ __forceinline__ void load32(uint32_t taddr, uint32_t (&v)[32]) {
   for (int k = 0; k < 32; ++k) asm volatile("" : "+r"(v[k]));   // no use before the wait
 }
 
+__device__ __forceinline__ void inval(uint64_t* bar) { asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(ptx::smem_u32(bar)) : "memory"); }
 __device__ __forceinline__ void ld_shared_v4(uint32_t addr, uint32_t* x) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(addr) : "memory");
 }
@@ -290,6 +310,5 @@ inline const CUtensorMap* page_map(cascade_ctx* ctx, const Args& p, int D, const
 
 }  // namespace grad_tc
 
-// paged_grad_kv.cu, paged_grad_q.cu: the two passes on the tensor cores (bf16).
-int launch_paged_grad_kv(cascade_ctx* ctx, const grad_tc::Args& p, cudaStream_t s);
-int launch_paged_grad_q(cascade_ctx* ctx, const grad_tc::Args& p, cudaStream_t s);
+// paged_grad_tc.cu: both passes in one launch (bf16).
+int launch_paged_grad_tc(cascade_ctx* ctx, const PagedGradArgs& g, cudaStream_t s);
