@@ -4,96 +4,209 @@
 //     q_i = exp(t_i / T) / sum_j exp(t_j / T)      (or exp(t_i / T - target_lse): the target's mass outside is left out)
 //     loss = - w sum_i q_i log softmax(d / T)[id_i] = w (Q log Z + sum_i q_i (m - d_id) / T)
 //     grad = (w / T) (Q softmax(d / T) - sum_i q_i e_id)
-// with m the row's maximum, Z = sum_v exp((d_v - m) / T), Q = sum_i q_i.  Every term of the loss is positive, so nothing cancels.
+// with m the row's maximum, Z = sum_v exp((d_v - m) / T), Q = sum_i q_i.
+//
+// Both are memory-bound and walk over a row once.  The loss looks the drafter's logits of the stored tokens up behind the row, from the
+// L2.  (In front of it 292 to 322 us for 4608 rows of 65536 where this takes 262, since memory gives 64 bytes for 4; from shared memory,
+// as the gradient does it, 494 us: too much work an element.)  The gradient goes in stretches: the stored entries that fall into one
+// go into shared memory at their tokens' places, then the logits, already requested, are worked on beside them.
 #include "cascade_internal.h"
 #include "ptx_paged.cuh"
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kMaxSplits = 8;       // CTAs of one row (a cluster)
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kMaxSplits = 8;       // CTAs of one row of the loss (a cluster)
+constexpr int kBatch = 4;           // pieces a thread of a stretch
 
 // Rows are walked in pieces of 16 bytes from the 16-byte boundary at or in front of their first element: element v of the row
-// is place v + lead.  A piece that is not wholly inside is read and written element by element.
+// is place v + lead.  The pieces that lie wholly inside are `first` .. `last` - 1; what is left at both ends goes element by element.
 template <typename E>
 struct Row {
   static constexpr int kVec = 16 / (int)sizeof(E);
-  int lead, V;
-  __device__ __forceinline__ Row(const E* row, int v) : lead((int)((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(E))), V(v) {}
-  __device__ __forceinline__ int pieces() const { return (V + lead + kVec - 1) / kVec; }
-  __device__ __forceinline__ bool whole(int piece) const { return piece * kVec >= lead && (piece + 1) * kVec <= V + lead; }
+  int lead, first, last, V, head, tail;                    // (elements in front of `head` and from `tail` on are the ends)
+  __device__ __forceinline__ Row(const E* row, int v)
+      : lead((int)((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(E))), first(lead > 0), last(max((v + lead) / kVec, first)), V(v),
+        head(min(first * kVec - lead, v)), tail(max(last * kVec - lead, head)) {}
+  // i = 0 .. 2 kVec - 1: an element of the ends, V or more for none
+  __device__ __forceinline__ int edge(int i) const { return i >= kVec ? tail + i - kVec : i < head ? i : V; }
 };
 
-__device__ __forceinline__ void unpack(const uint4& r, float (&x)[4]) {
-  x[0] = __uint_as_float(r.x);
-  x[1] = __uint_as_float(r.y);
-  x[2] = __uint_as_float(r.z);
-  x[3] = __uint_as_float(r.w);
+// The values of a piece as pairs.
+__device__ __forceinline__ void unpack(const uint4& r, uint64_t (&x)[2]) {
+  x[0] = (uint64_t)r.y << 32 | r.x;
+  x[1] = (uint64_t)r.w << 32 | r.z;
 }
-__device__ __forceinline__ void unpack(const uint4& r, float (&x)[8]) {
+__device__ __forceinline__ void unpack(const uint4& r, uint64_t (&x)[4]) {
   const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = ptx::pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+}
+__device__ __forceinline__ uint4 pack(const uint64_t (&x)[2]) {
+  return make_uint4((uint32_t)x[0], (uint32_t)(x[0] >> 32), (uint32_t)x[1], (uint32_t)(x[1] >> 32));
+}
+__device__ __forceinline__ uint4 pack(const uint64_t (&x)[4]) {
+  uint32_t w[4];
+#pragma unroll
   for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    float lo, hi;
+    ptx::unpack2(x[i], &lo, &hi);
+    w[i] = ptx::pack_bf16x2(lo, hi);
   }
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ uint4 pack(const float (&x)[4]) {
-  return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-}
-__device__ __forceinline__ uint4 pack(const float (&x)[8]) {
-  return make_uint4(ptx::pack_bf16x2(x[0], x[1]), ptx::pack_bf16x2(x[2], x[3]), ptx::pack_bf16x2(x[4], x[5]), ptx::pack_bf16x2(x[6], x[7]));
+__device__ __forceinline__ uint64_t both(float x) { return ptx::pack2(x, x); }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ uint32_t bits_of(const float* p) { return __float_as_uint(*p); }
+__device__ __forceinline__ uint32_t bits_of(const __nv_bfloat16* p) { return *reinterpret_cast<const uint16_t*>(p); }
 __device__ __forceinline__ void from_float(float* p, float x) { *p = x; }
 __device__ __forceinline__ void from_float(__nv_bfloat16* p, float x) { *p = __float2bfloat16(x); }
 
-// One piece; places outside the row get `fill`.
-template <typename E>
-__device__ __forceinline__ void load_piece(const E* row, const Row<E>& r, int piece, float fill, float (&x)[Row<E>::kVec]) {
-  const int v0 = piece * Row<E>::kVec - r.lead;
-  if (r.whole(piece)) {
-    unpack(*reinterpret_cast<const uint4*>(row + v0), x);
-  } else {
+// A thread's pieces of the stretch that begins at piece p0.
+template <typename E, int kThreads>
+__device__ __forceinline__ void load_stretch(const E* d, int lead, bool aligned, int p0, int last, uint4 (&raw)[kBatch]) {
+  constexpr int kVec = Row<E>::kVec;
 #pragma unroll
-    for (int i = 0; i < Row<E>::kVec; ++i) x[i] = v0 + i >= 0 && v0 + i < r.V ? to_float(row[v0 + i]) : fill;
+  for (int b = 0; b < kBatch; ++b) {
+    const int p = p0 + b * kThreads + (int)threadIdx.x;
+    if (p >= last) break;
+    if (aligned) {
+      raw[b] = __ldg(reinterpret_cast<const uint4*>(d - lead) + p);
+    } else {
+      const E* x = d + (p * kVec - lead);
+      uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) w[i * (int)sizeof(E) / 4] |= bits_of(x + i) << (i * (int)sizeof(E) % 4 * 8);
+      raw[b] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
   }
 }
 
-// Running maximum and sum of exponentials relative to it (an empty one: -inf, 0).
+// What is stored of a position: the first entries of a thread stay in registers.
+template <int kThreads, int kHold>
+struct Stored {
+  const float* top;
+  const int32_t* ids;
+  int n, V, token[kHold];
+  float value[kHold];                                      // logits, then weights
+  __device__ __forceinline__ Stored(const float* t, const int32_t* i, int count, int v) : top(t), ids(i), n(count), V(v) {
+#pragma unroll
+    for (int k = 0; k < kHold; ++k) {
+      const int at = k * kThreads + (int)threadIdx.x;
+      token[k] = at < n ? ids[at] : -1;
+      value[k] = at < n ? top[at] : -INFINITY;
+    }
+#pragma unroll
+    for (int k = 0; k < kHold; ++k)
+      if (token[k] < 0 || token[k] >= V) {
+        token[k] = -1;
+        value[k] = -INFINITY;
+      }
+  }
+  template <typename F>
+  __device__ __forceinline__ void each_more(F&& f) const { // the entries beyond those
+    for (int at = kHold * kThreads + (int)threadIdx.x; at < n; at += kThreads) {
+      const int v = ids[at];
+      if (v >= 0 && v < V) f(v, top[at]);
+    }
+  }
+  // s_q[place] = the weight of the token there, for the places of a stretch (base: its first token) and, with `ends`, the elements at
+  // the row's ends behind them.  Ends with a barrier; the next call wants one in front of it.
+  template <typename W>
+  __device__ __forceinline__ void scatter(float* s_q, int* s_twice, int base, int places, bool ends, int head, int tail, int vec, W&& weight) const {
+    const int tid = threadIdx.x, slots = places + (ends ? 2 * vec : 0);
+    auto place = [&](int v) {
+      const int in = v - base;
+      if (v < 0 || v >= V) return -1;
+      if (in >= 0 && in < places) return in;
+      return !ends ? -1 : v < head ? places + v : v >= tail ? places + vec + v - tail : -1;
+    };
+    for (int i = tid; i < slots / 4; i += kThreads) reinterpret_cast<float4*>(s_q)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (tid == 0) *s_twice = 0;
+    __syncthreads();
+    auto put = [&](int at, float w) {
+      if (at >= 0 && atomicExch(&s_q[at], w) != 0.f) *s_twice = 1;
+    };
+#pragma unroll
+    for (int k = 0; k < kHold; ++k) put(place(token[k]), value[k]);
+    each_more([&](int v, float t) {
+      const int at = place(v);
+      if (at >= 0) put(at, weight(t));
+    });
+    __syncthreads();
+    if (*s_twice) {                                        // a token more than once: its entries in order, by the thread that owns it
+      for (int i = tid; i < slots; i += kThreads) s_q[i] = 0.f;
+      __syncthreads();
+      for (int at = 0; at < n; ++at) {
+        const int in = place(ids[at]);
+        if (in >= 0 && in % kThreads == tid) s_q[in] += weight(top[at]);
+      }
+      __syncthreads();
+    }
+  }
+};
+
+// Running maximum m and sum of 2^(c x - c m) with c m rounded once (an empty one: -inf, 0).
 struct Soft {
   float m, z;
 };
-__device__ __forceinline__ float scaled(float x, float m, float c) { return ptx::ex2((x - m) * c); }
+__device__ __forceinline__ float reference(float m, float c) { return m == -INFINITY ? 0.f : m * c; }
+__device__ __forceinline__ float scaled(float x, float ref, float c) { return ptx::ex2(fmaf(x, c, -ref)); }
 __device__ __forceinline__ Soft join(const Soft& a, const Soft& b, float c) {
-  const float m = fmaxf(a.m, b.m);
-  const float wa = a.m == -INFINITY ? 1.f : scaled(a.m, m, c), wb = b.m == -INFINITY ? 1.f : scaled(b.m, m, c);
+  const float m = fmaxf(a.m, b.m), ref = reference(m, c);
+  const float wa = a.m == -INFINITY ? 1.f : ptx::ex2(reference(a.m, c) - ref), wb = b.m == -INFINITY ? 1.f : ptx::ex2(reference(b.m, c) - ref);
   return {m, a.z * wa + b.z * wb};     // (the sum of an empty part is 0, or NaN by a value that was no number)
 }
-template <int kN>
-__device__ __forceinline__ void add(Soft& s, const float (&x)[kN], float c) {
-  float m = x[0];
-#pragma unroll
-  for (int i = 1; i < kN; ++i) m = fmaxf(m, x[i]);
+// `ref` = reference(s.m, c) goes along.
+__device__ __forceinline__ void raise(Soft& s, float& ref, float m, float c) {
   if (m > s.m) {
-    s.z *= s.m == -INFINITY ? 1.f : scaled(s.m, m, c);
+    const float to = m * c;
+    if (s.m != -INFINITY) s.z *= ptx::ex2(ref - to);
     s.m = m;
+    ref = to;
   }
-  const float ref = s.m == -INFINITY ? 0.f : s.m;
-#pragma unroll
-  for (int i = 0; i < kN; ++i) s.z += scaled(x[i], ref, c);
 }
-
-template <int kThreads>
-__device__ __forceinline__ Soft block_join(Soft s, float c, Soft* red) {
+template <int kN>
+__device__ __forceinline__ void add(Soft& s, float& ref, const uint64_t (&x)[kN], float c) {
+  float m = -INFINITY;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) s = join(s, {__shfl_xor_sync(0xffffffffu, s.m, o), __shfl_xor_sync(0xffffffffu, s.z, o)}, c);
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
-  __syncthreads();
-  s = red[0];
-  for (int i = 1; i < kThreads / 32; ++i) s = join(s, red[i], c);
+  for (int i = 0; i < kN; ++i) {
+    float a, b;
+    ptx::unpack2(x[i], &a, &b);
+    m = fmaxf(m, fmaxf(a, b));
+  }
+  raise(s, ref, m, c);
+  const uint64_t cc = both(c), minus = both(-ref);
+  uint64_t sum = 0;
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    float a, b;
+    ptx::unpack2(ptx::fma2(x[i], cc, minus), &a, &b);
+    sum = ptx::add2(sum, ptx::pack2(ptx::ex2(a), ptx::ex2(b)));
+  }
+  float a, b;
+  ptx::unpack2(sum, &a, &b);
+  s.z += a + b;
+}
+__device__ __forceinline__ Soft warp_join(Soft s, float c, int lanes) {
+  for (int o = lanes / 2; o > 0; o >>= 1) s = join(s, {__shfl_xor_sync(0xffffffffu, s.m, o), __shfl_xor_sync(0xffffffffu, s.z, o)}, c);
   return s;
+}
+template <int kThreads>
+__device__ __forceinline__ float block_max(float x, float* red) {
+  constexpr int kWarps = kThreads / 32;
+  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = x;
+  __syncthreads();
+  x = red[threadIdx.x & (kWarps - 1)];
+  for (int o = kWarps / 2; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
 }
 
 struct LossArgs {
@@ -106,18 +219,28 @@ struct LossArgs {
   float temperature, tau, raised;
 };
 
-// One row a cluster of `splits` CTAs.  Memory-bound: the row, the stored logits and the hidden states are read once, the drafter's
-// logits of the stored tokens again from the L2.
+// One row a cluster of `splits` CTAs, a share of the row and of the stored entries each.
 template <typename E, int kThreads>
-__global__ void __launch_bounds__(kThreads) k_distill_loss(const LossArgs a) {
-  constexpr int kVec = Row<E>::kVec, kBatch = 4, kHold = 4;
-  __shared__ Soft red_d[kThreads / 32], red_t[kThreads / 32];
-  __shared__ __align__(16) float4 s_soft[kMaxSplits];      // (m, Z, m_t, Z_t) of every CTA of the row
-  __shared__ double s_part[kMaxSplits][5];                 // its sums: q (m - d), q, and the three of the cosine
-  __shared__ double s_red[kThreads / 32][5];
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : 2) k_distill_loss(const LossArgs a) {
+  constexpr int kVec = Row<E>::kVec, kHold = 4, kWarps = kThreads / 32, kPieces = kBatch * kThreads;
+  __shared__ float s_max[kWarps];
+  __shared__ Soft s_warp[kWarps];
+  __shared__ double s_sum[kWarps][5];
+  __shared__ __align__(16) float4 s_soft[kMaxSplits];      // (m, Z, largest stored logit) of every CTA of the row
+  __shared__ double s_part[kMaxSplits][5];                 // its sums: q d, q, and the three of the cosine
+  asm volatile("griddepcontrol.launch_dependents;");       // (the kernel that adds the losses up waits for this one's end itself)
   const int row = blockIdx.x / a.splits, rank = blockIdx.x % a.splits, tid = threadIdx.x;
   const float c = kLog2e / a.temperature, inv_t = 1.f / a.temperature;
-  const int seq = a.seq == nullptr ? 0 : a.seq[row];
+  const int seq = a.seq == nullptr ? 0 : a.seq[row], seq_next = a.seq == nullptr ? 0 : row + 1 < a.K ? a.seq[row + 1] : -1;
+  // what comes first of everything is requested at once, padding's too
+  const E* d = static_cast<const E*>(a.draft) + row * a.stride;
+  const Row<E> r(d, a.V);
+  const int share = (r.last - r.first + a.splits - 1) / a.splits, last = min(r.last, r.first + (rank + 1) * share);
+  int p = r.first + rank * share;
+  uint4 raw[kBatch];
+  load_stretch<E, kThreads>(d, r.lead, true, p, last, raw);
+  const int per = (a.n + a.splits - 1) / a.splits, i0 = min(a.n, rank * per);
+  Stored<kThreads, kHold> stored(a.top + (long long)row * a.n + i0, a.ids + (long long)row * a.n + i0, min(a.n - i0, per), a.V);
   if (seq < 0) {                                           // (the same in every CTA of the cluster)
     if (rank == 0 && tid == 0) {
       a.loss[row] = 0.f;
@@ -125,131 +248,132 @@ __global__ void __launch_bounds__(kThreads) k_distill_loss(const LossArgs a) {
     }
     return;
   }
-  const E* d = static_cast<const E*>(a.draft) + row * a.stride;
-  const float* top = a.top + (long long)row * a.n;
-  const int32_t* ids = a.ids + (long long)row * a.n;
-  // the stored entries of this CTA: the first few of a thread stay in registers
-  const int per = (a.n + a.splits - 1) / a.splits, i0 = min(a.n, rank * per), i1 = min(a.n, i0 + per);
-  float t[kHold];
-  int id[kHold];
-#pragma unroll
-  for (int i = 0; i < kHold; ++i) {
-    const int at = i0 + i * kThreads + tid;
-    id[i] = at < i1 ? ids[at] : -1;
-    t[i] = at < i1 ? top[at] : -INFINITY;
-    if (id[i] < 0 || id[i] >= a.V) {
-      id[i] = -1;
-      t[i] = -INFINITY;
+  if (a.splits > 1) ptx::cluster_arrive();                 // (waited for before anything is written to another CTA)
+  // the sums of the cosine with the next position's hidden state (64 bits: it may lie next to the threshold)
+  double sum[5] = {0.0, 0.0, 0.0, 0.0, 0.0};
+  const bool pair = a.feat != nullptr && row + 1 < a.K && seq_next == seq;
+  if (pair) {
+    const float *fa = a.feat + (long long)row * a.h, *fb = fa + a.h;
+    auto term = [&](float x, float y) {
+      const double u = x, v = y;
+      sum[2] += u * v;
+      sum[3] += u * u;
+      sum[4] += v * v;
+    };
+    const int step = a.splits * kThreads, from = rank * kThreads + tid;
+    if ((a.h & 3) == 0 && (reinterpret_cast<uintptr_t>(a.feat) & 15u) == 0) {
+      const float4 *va = reinterpret_cast<const float4*>(fa), *vb = reinterpret_cast<const float4*>(fb);
+#pragma unroll 4
+      for (int i = from; i < a.h / 4; i += step) {
+        const float4 x = va[i], y = vb[i];
+        term(x.x, y.x);
+        term(x.y, y.y);
+        term(x.z, y.z);
+        term(x.w, y.w);
+      }
+    } else {
+#pragma unroll 4
+      for (int i = from; i < a.h; i += step) term(fa[i], fb[i]);
     }
   }
-  auto each_more = [&](auto&& f) {                         // the others
-    for (int at = i0 + kHold * kThreads + tid; at < i1; at += kThreads) {
-      const int v = ids[at];
-      if (v >= 0 && v < a.V) f(v, top[at]);
-    }
-  };
   // the row
-  const Row<E> r(d, a.V);
-  const int pieces = r.pieces(), share = (pieces + a.splits - 1) / a.splits, p1 = min(pieces, (rank + 1) * share);
   Soft sd = {-INFINITY, 0.f};
-  for (int p = rank * share + tid; p < p1; p += kBatch * kThreads) {
-    float x[kBatch][kVec];
+  float ref_d = 0.f;
+  if (rank == 0 && tid < 2 * kVec && r.edge(tid) < a.V) {
+    const uint64_t one[1] = {ptx::pack2(to_float(d[r.edge(tid)]), -INFINITY)};
+    add(sd, ref_d, one, c);
+  }
+  for (; p < last; p += kPieces) {
+    uint4 now[kBatch];
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) now[b] = raw[b];
+    load_stretch<E, kThreads>(d, r.lead, true, p + kPieces, last, raw);
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
-      if (p + b * kThreads < p1) {
-        load_piece(d, r, p + b * kThreads, -INFINITY, x[b]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) x[b][i] = -INFINITY;
-      }
-    }
-#pragma unroll
-    for (int b = 0; b < kBatch; ++b) add(sd, x[b], c);
-  }
-  Soft st = {-INFINITY, 0.f};
-  if (a.target_lse == nullptr) {
-    add(st, t, c);
-    each_more([&](int, float x) {
-      const float one[1] = {x};
-      add(st, one, c);
-    });
-  }
-  sd = block_join<kThreads>(sd, c, red_d);
-  st = block_join<kThreads>(st, c, red_t);
-  if (a.splits > 1) {
-    ptx::cluster_arrive();
-    ptx::cluster_wait();                                   // all CTAs have started
-    if (tid < a.splits)
-      ptx::st_cluster_v4(ptx::map_to_cta(ptx::smem_u32(&s_soft[rank]), tid), make_float4(sd.m, sd.z, st.m, st.z));
-    __syncwarp();
-    ptx::cluster_arrive();
-    ptx::cluster_wait();
-    sd = {s_soft[0].x, s_soft[0].y};
-    st = {s_soft[0].z, s_soft[0].w};
-    for (int i = 1; i < a.splits; ++i) {
-      sd = join(sd, {s_soft[i].x, s_soft[i].y}, c);
-      st = join(st, {s_soft[i].z, s_soft[i].w}, c);
+      if (p + b * kThreads + tid >= last) break;
+      uint64_t x[kVec / 2];
+      unpack(now[b], x);
+      add(sd, ref_d, x, c);
     }
   }
-  // sums over the stored entries (64 bits: few of them), and those of the cosine with the next position's hidden state
+  // the drafter's logits of the stored tokens, from the L2
+  float dv[kHold];
+#pragma unroll
+  for (int k = 0; k < kHold; ++k) dv[k] = stored.token[k] >= 0 ? to_float(d[stored.token[k]]) : 0.f;
   const bool given = a.target_lse != nullptr;
-  const float t_lse = given ? a.target_lse[row] : 0.f, t_ref = st.m == -INFINITY ? 0.f : st.m;
-  double sum[5] = {0.0, 0.0, 0.0, 0.0, 0.0};
-  auto entry = [&](int v, float x) {
-    const float q = given ? ptx::ex2(fmaf(x, inv_t, -t_lse) * kLog2e) : scaled(x, t_ref, c);
-    if (q != 0.f) {
-      sum[0] += (double)(q * (sd.m - to_float(d[v])));
+  const float t_lse = given ? a.target_lse[row] : 0.f;
+  float most = -INFINITY;
+  if (!given) {
+#pragma unroll
+    for (int k = 0; k < kHold; ++k) most = fmaxf(most, stored.value[k]);
+    stored.each_more([&](int, float t) { most = fmaxf(most, t); });
+    most = block_max<kThreads>(most, s_max);
+  }
+  // sums over the entries (64 bits: few of them, and maximum times weight less weight times logit cancels)
+  const float ref_t = reference(most, c);
+  auto entry = [&](float t, float y) {
+    const float q = given ? ptx::ex2(fmaf(t, inv_t, -t_lse) * kLog2e) : scaled(t, ref_t, c);
+    if (q != 0.f) {                                        // (a token that weighs nothing may have -inf)
+      sum[0] += (double)q * (double)y;
       sum[1] += (double)q;
     }
   };
 #pragma unroll
-  for (int i = 0; i < kHold; ++i)
-    if (id[i] >= 0) entry(id[i], t[i]);
-  each_more(entry);
-  const bool pair = a.feat != nullptr && row + 1 < a.K && (a.seq == nullptr || a.seq[row + 1] == seq);
-  if (pair) {
-    const float *fa = a.feat + (long long)row * a.h, *fb = fa + a.h;
-    for (int i = rank * kThreads + tid; i < a.h; i += a.splits * kThreads) {
-      const double x = fa[i], y = fb[i];
-      sum[2] += x * y;
-      sum[3] += x * x;
-      sum[4] += y * y;
-    }
-  }
+  for (int k = 0; k < kHold; ++k)
+    if (stored.token[k] >= 0) entry(stored.value[k], dv[k]);
+  stored.each_more([&](int v, float t) { entry(t, to_float(d[v])); });
+  sd = warp_join(sd, c, 32);
 #pragma unroll
-  for (int i = 0; i < 5; ++i) {
+  for (int i = 0; i < 5; ++i)
     for (int o = 16; o > 0; o >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
-    if ((tid & 31) == 0) s_red[tid >> 5][i] = sum[i];
+  if ((tid & 31) == 0) {
+    s_warp[tid >> 5] = sd;
+#pragma unroll
+    for (int i = 0; i < 5; ++i) s_sum[tid >> 5][i] = sum[i];
   }
   __syncthreads();
-  if (tid < 5) {
-    double x = 0.0;
-    for (int w = 0; w < kThreads / 32; ++w) x += s_red[w][tid];
-    if (a.splits > 1) {
-      const uint32_t to = ptx::map_to_cta(ptx::smem_u32(&s_part[rank][tid]), 0);
-      asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to), "d"(x) : "memory");
-    } else {
-      s_part[0][tid] = x;
+  if (a.splits > 1) ptx::cluster_wait();                   // all CTAs have started
+  if (tid < 32) {
+    sd = warp_join(s_warp[tid & (kWarps - 1)], c, kWarps);
+    const uint32_t to = a.splits > 1 ? ptx::map_to_cta(ptx::smem_u32(&s_part[rank][tid < 5 ? tid : 0]), 0) : ptx::smem_u32(&s_part[0][tid < 5 ? tid : 0]);
+    if (tid < 5) {
+      double y = 0.0;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) y += s_sum[w][tid];
+      asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to), "d"(y) : "memory");
     }
+    if (tid == 5)
+      ptx::st_cluster_v4(a.splits > 1 ? ptx::map_to_cta(ptx::smem_u32(&s_soft[rank]), 0) : ptx::smem_u32(&s_soft[0]), make_float4(sd.m, sd.z, most, 0.f));
+    __syncwarp();
   }
   if (a.splits > 1) {
     __syncwarp();
     ptx::cluster_arrive();
     ptx::cluster_wait();
-  } else {
-    __syncthreads();
   }
   if (rank == 0 && tid == 0) {
-    double x[5] = {0.0, 0.0, 0.0, 0.0, 0.0};
-    for (int s = 0; s < a.splits; ++s)
-      for (int i = 0; i < 5; ++i) x[i] += s_part[s][i];
-    const float w = pair && x[2] / (sqrt(x[3]) * sqrt(x[4])) >= (double)a.tau ? a.raised : 1.f;
-    const double log_z = log((double)sd.z), z_t = given ? 1.0 : x[1];
-    const bool any = x[1] != 0.0;                          // something stored weighs something (or is no number)
-    const double mass = given ? x[1] : any ? x[1] / z_t : 0.0;
-    const double ce = any ? mass * log_z + x[0] / z_t * (double)inv_t : 0.0;
+    double y[5] = {0.0, 0.0, 0.0, 0.0, 0.0};
+    most = s_soft[0].z;
+    for (int s = 1; s < a.splits; ++s) most = fmaxf(most, s_soft[s].z);
+    for (int s = 0; s < a.splits; ++s) {
+      const float4 x = s_soft[s];
+      sd = s == 0 ? Soft{x.x, x.y} : join(sd, {x.x, x.y}, c);
+      // (a CTA's weights are by its own largest entry)
+      const double by = given || a.splits == 1 || x.z == -INFINITY ? 1.0 : (double)exp2f(reference(x.z, c) - reference(most, c));
+      for (int i = 0; i < 5; ++i) y[i] += i < 2 ? by * s_part[s][i] : s_part[s][i];
+    }
+    // cosine >= tau, squared with its sign
+    const double bound = (double)a.tau * fabs((double)a.tau) * (y[3] * y[4]);
+    const float w = pair && y[3] * y[4] > 0.0 && y[2] * fabs(y[2]) >= bound ? a.raised : 1.f;
+    // log sum exp((d - m) / T): what c m was rounded by comes back
+    const double log_z = (double)logf(sd.z) + ((double)reference(sd.m, c) - (double)sd.m * c) * (double)kLn2;
+    const bool any = y[1] != 0.0;                          // something stored weighs something (or is no number)
+    const double mass = given ? y[1] : any ? y[1] / y[1] : 0.0, gap = (double)sd.m * y[1] - y[0];
+    const double ce = any ? mass * log_z + (given ? gap : gap / y[1]) * (double)inv_t : 0.0;
     a.loss[row] = (float)(w * ce);
-    const float lse_t = given ? t_lse : any ? (float)((double)t_ref * inv_t + log(z_t)) : 0.f;
+    const float lse_t = given ? t_lse
+                        : any ? (float)((double)most * inv_t + (double)logf((float)y[1]) + ((double)reference(most, c) - (double)most * c) * (double)kLn2)
+                              : 0.f;
     reinterpret_cast<float4*>(a.saved)[row] = make_float4((float)((double)sd.m * inv_t + log_z), lse_t, (float)mass, w);
   }
 }
@@ -257,6 +381,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_loss(const LossArgs a) {
 // total = sum of n values, in a fixed order.
 __global__ void __launch_bounds__(1024) k_distill_total(const float* __restrict__ x, int n, float* __restrict__ out) {
   __shared__ double s_warp[32];
+  asm volatile("griddepcontrol.wait;" ::: "memory");       // the losses are there
   double s = 0.0;
   for (int i = threadIdx.x; i < n; i += 1024) s += (double)x[i];
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -279,109 +404,67 @@ struct GradArgs {
   float temperature, scale;
 };
 
-// A row, or one of `splits` parts of it, a CTA, in stretches of kStretch places: the stored entries of a stretch go into shared
-// memory, then one pass reads the drafter's logits and writes the gradient.  Memory-bound.
-template <typename E, int kThreads, int kStretch>
-__global__ void __launch_bounds__(kThreads) k_distill_grad(const GradArgs a) {
-  constexpr int kVec = Row<E>::kVec, kBatch = kStretch / kVec / kThreads, kHold = 4;
-  __shared__ __align__(16) float s_q[kStretch];
+// A row, or one of `splits` parts of it, a CTA.
+template <typename E, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : 2) k_distill_grad(const GradArgs a) {
+  constexpr int kVec = Row<E>::kVec, kHold = 4, kPieces = kBatch * kThreads;
+  extern __shared__ __align__(16) float s_q[];             // [places of a stretch, then the elements at the row's ends]
   __shared__ int s_twice;
   const int row = blockIdx.x / a.splits, part = blockIdx.x % a.splits, tid = threadIdx.x;
   // (row by row the logits may be where the gradient goes: every element is read before the same thread writes it)
   const E* d = static_cast<const E*>(a.draft) + row * a.stride;
   E* g = static_cast<E*>(a.grad) + row * a.grad_stride;
   const float4 saved = reinterpret_cast<const float4*>(a.saved)[row];      // lse, target lse, Q, weight
-  const float inv_t = 1.f / a.temperature;
-  const float f = saved.w * (a.up == nullptr ? 1.f : a.up[row]) * a.scale * inv_t;
-  const Row<E> r(g, a.V);
-  const bool same = r.lead == Row<E>(d, a.V).lead;         // both rows have their 16-byte boundaries at the same elements
-  const int pieces = r.pieces(), share = ((pieces + a.splits - 1) / a.splits + 31) / 32 * 32;
-  const int first = min(pieces, part * share), last = min(pieces, first + share);
-  auto store = [&](int piece, const float (&x)[kVec]) {
-    const int v0 = piece * kVec - r.lead;
-    if (r.whole(piece)) {
-      *reinterpret_cast<uint4*>(g + v0) = pack(x);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kVec; ++i)
-        if (v0 + i >= 0 && v0 + i < r.V) from_float(g + v0 + i, x[i]);
-    }
-  };
-  if (f == 0.f) {                                          // padding: nothing of the row is looked at
-    float zero[kVec];
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) zero[i] = 0.f;
-    for (int p = first + tid; p < last; p += kThreads) store(p, zero);
+  const float up = a.up == nullptr ? 1.f : a.up[row], inv_t = 1.f / a.temperature;
+  const Row<E> r(g, a.V);                                  // (logits with other boundaries are read element by element)
+  const bool aligned = r.lead == Row<E>(d, a.V).lead;
+  const int share = ((r.last - r.first + a.splits - 1) / a.splits + 31) / 32 * 32;
+  const int first = min(r.last, r.first + part * share), last = min(r.last, first + share);
+  uint4* to = reinterpret_cast<uint4*>(g - r.lead);
+  const int edge = part == 0 && tid < 2 * kVec ? r.edge(tid) : a.V;        // (the first part's)
+  // what comes first is requested at once, padding's too
+  uint4 raw[kBatch];
+  load_stretch<E, kThreads>(d, r.lead, aligned, first, last, raw);
+  Stored<kThreads, kHold> stored(a.top + (long long)row * a.n, a.ids + (long long)row * a.n, a.n, a.V);
+  const float f = saved.w * up * a.scale * inv_t;
+  if (f == 0.f) {                                          // padding: zeros, whatever the row holds
+    for (int p = first + tid; p < last; p += kThreads) to[p] = make_uint4(0, 0, 0, 0);
+    if (edge < a.V) from_float(g + edge, 0.f);
     return;
   }
-  const float* top = a.top + (long long)row * a.n;
-  const int32_t* ids = a.ids + (long long)row * a.n;
   auto weight = [&](float t) { return ptx::ex2(fmaf(t, inv_t, -saved.y) * kLog2e); };
-  int place[kHold];
-  float q[kHold];
 #pragma unroll
-  for (int i = 0; i < kHold; ++i) {
-    const int at = i * kThreads + tid, v = at < a.n ? ids[at] : -1;
-    place[i] = v >= 0 && v < a.V ? v + r.lead : -1;
-    q[i] = place[i] >= 0 ? weight(top[at]) : 0.f;
-  }
-  if (tid == 0) s_twice = 0;
-  for (int p0 = first; p0 < last; p0 += kStretch / kVec) {
-    const int base = p0 * kVec, n_piece = min(last - p0, kStretch / kVec);
-    float x[kBatch][kVec];
-#pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      const int p = b * kThreads + tid;
-      if (p < n_piece) {
-        if (same) {
-          load_piece(d, r, p0 + p, 0.f, x[b]);
-        } else {
-          const int v0 = (p0 + p) * kVec - r.lead;
-#pragma unroll
-          for (int i = 0; i < kVec; ++i) x[b][i] = v0 + i >= 0 && v0 + i < a.V ? to_float(d[v0 + i]) : 0.f;
-        }
-      }
-    }
-    for (int i = tid; i < kStretch / 4; i += kThreads) reinterpret_cast<float4*>(s_q)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    __syncthreads();
-    auto put = [&](int at, float w) {
-      const int in = at - base;
-      if (in >= 0 && in < n_piece * kVec && atomicExch(&s_q[in], w) != 0.f) s_twice = 1;
-    };
-#pragma unroll
-    for (int i = 0; i < kHold; ++i)
-      if (place[i] >= 0) put(place[i], q[i]);
-    for (int at = kHold * kThreads + tid; at < a.n; at += kThreads) {
-      const int v = ids[at];
-      if (v >= 0 && v < a.V) put(v + r.lead, weight(top[at]));
-    }
-    __syncthreads();
-    if (s_twice) {                                         // a token more than once: its entries in order, by the thread that owns it
-      for (int i = tid; i < kStretch; i += kThreads) s_q[i] = 0.f;
-      __syncthreads();
-      for (int at = 0; at < a.n; ++at) {
-        const int v = ids[at], in = v + r.lead - base;
-        if (v >= 0 && v < a.V && in >= 0 && in < n_piece * kVec && in % kThreads == tid) s_q[in] += weight(top[at]);
-      }
-      __syncthreads();
-      if (tid == 0) s_twice = 0;
-    }
+  for (int k = 0; k < kHold; ++k) stored.value[k] = weight(stored.value[k]);
+  const uint64_t scale2 = both(inv_t), lse2 = both(-saved.x), log2e2 = both(kLog2e), mass2 = both(saved.z * f), minus2 = both(-f);
+  for (int p0 = first;; p0 += kPieces) {
+    // (requested here and not one stretch ahead: 387 us for 4608 rows of 65536, ahead 420 us; reads and writes in turn suit the memory)
+    if (p0 != first) load_stretch<E, kThreads>(d, r.lead, aligned, p0, last, raw);
+    const int n_piece = max(0, min(kPieces, last - p0));
+    const bool ends = part == 0 && p0 == first;
+    stored.scatter(s_q, &s_twice, p0 * kVec - r.lead, n_piece * kVec, ends, r.head, r.tail, kVec, weight);
+    if (ends && edge < a.V)
+      from_float(g + edge, saved.z * f * ptx::ex2(fmaf(to_float(d[edge]), inv_t, -saved.x) * kLog2e) - f * s_q[n_piece * kVec + tid]);
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
-      const int p = b * kThreads + tid;
-      if (p < n_piece) {
-        float y[kVec];
+      const int at = b * kThreads + tid;
+      if (at >= n_piece) break;
+      uint64_t x[kVec / 2];
+      unpack(raw[b], x);
+      const ulonglong2* sq = reinterpret_cast<const ulonglong2*>(&s_q[at * kVec]);
 #pragma unroll
-        for (int i = 0; i < kVec; ++i)
-          y[i] = f * fmaf(saved.z, ptx::ex2(fmaf(x[b][i], inv_t, -saved.x) * kLog2e), -s_q[p * kVec + i]);
-        store(p0 + p, y);
+      for (int i = 0; i < kVec / 2; ++i) {
+        float lo, hi;
+        ptx::unpack2(mul2(ptx::fma2(x[i], scale2, lse2), log2e2), &lo, &hi);
+        const ulonglong2 qq = sq[i / 2];
+        x[i] = ptx::fma2(ptx::pack2(ptx::ex2(lo), ptx::ex2(hi)), mass2, mul2(i & 1 ? qq.y : qq.x, minus2));
       }
+      __stcs(to + p0 + at, pack(x));
     }
+    if (p0 + kPieces >= last) break;
     __syncthreads();
   }
 }
 
-constexpr int kLossThreads = 512, kGradThreads = 512, kStretch = 8192;
 constexpr int kMostValues = INT32_MAX - 65535;      // tokens and stored entries of a row: indexes stay in 32 bits beyond the last one
 constexpr long long kMostStride = 1ll << 40;
 
@@ -391,19 +474,43 @@ int sm_count() {
   return n;
 }
 
+// Few rows are shared out until every SM has some, in parts of at least 4 pieces a thread of 128; short parts take 256 threads instead
+// of 512, so that more of them are on an SM at once.  Shared memory: the places of a stretch and the row's ends.
+template <typename E>
+int plan(int K, int V, int* splits, int* threads, int* smem) {
+  constexpr int kVec = 16 / (int)sizeof(E);
+  const int sms = sm_count(), pieces = V / kVec;
+  if (sms <= 0) return CASCADE_ERR_CUDA;
+  *splits = 1;
+  while (*splits * 4 * 128 < pieces && (long long)K * *splits * 2 <= 4 * sms) *splits *= 2;
+  if ((long long)K * *splits > INT32_MAX) return CASCADE_ERR_UNSUPPORTED_SHAPE;
+  const int part = cascade_detail::ceil_div(pieces, *splits) + 32;
+  *threads = part <= kBatch * 256 ? 256 : 512;
+  *smem = ((part < kBatch * *threads ? part : kBatch * *threads) * kVec + 2 * kVec) * (int)sizeof(float);
+  return CASCADE_OK;
+}
+template <typename F>
+int allow_smem(F* f, int bytes) {
+  if (bytes > 40 * 1024) CASCADE_CUDA_TRY(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  return CASCADE_OK;
+}
+
 template <typename E>
 int launch_loss(const LossArgs& in, cudaStream_t s) {
   LossArgs a = in;
   const int sms = sm_count();
   if (sms <= 0) return CASCADE_ERR_CUDA;
-  // few rows: as many CTAs a row as fill the SMs, each with two batches of loads a thread at least
+  // few rows are shared out until every SM has some.  Long rows take 512 threads: no more than two rows an SM are then at work, and
+  // the stored tokens' logits are still in the L2 at their ends (4608 rows of 262144 bytes: 262 us, with 256 threads 307 us); of short
+  // rows more are wanted (1153 of 20014 bytes: 18.5 us, with 512 threads 26.5 us)
   const long long bytes = (long long)a.V * sizeof(E);
   a.splits = 1;
-  while (a.splits < kMaxSplits && (long long)a.K * a.splits * 2 <= 2 * sms && bytes >= (long long)a.splits * kLossThreads * 64) a.splits *= 2;
+  while (a.splits < kMaxSplits && bytes >= a.splits * 8192ll && (long long)a.K * a.splits * 2 <= 4 * sms) a.splits *= 2;
   if ((long long)a.K * a.splits > INT32_MAX) return CASCADE_ERR_UNSUPPORTED_SHAPE;
+  const bool small = bytes / a.splits <= 65536;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(a.K * a.splits));
-  cfg.blockDim = dim3(kLossThreads);
+  cfg.blockDim = dim3(small ? 256 : 512);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -411,20 +518,19 @@ int launch_loss(const LossArgs& in, cudaStream_t s) {
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  CASCADE_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_distill_loss<E, kLossThreads>, a));
+  auto* f = small ? k_distill_loss<E, 256> : k_distill_loss<E, 512>;
+  CASCADE_CUDA_TRY(cudaLaunchKernelEx(&cfg, f, a));
   return CASCADE_OK;
 }
 
 template <typename E>
 int launch_grad(const GradArgs& in, cudaStream_t s) {
   GradArgs a = in;
-  const int sms = sm_count();
-  if (sms <= 0) return CASCADE_ERR_CUDA;
-  const int stretches = cascade_detail::ceil_div(a.V, kStretch);
-  a.splits = 1;
-  while (a.splits * 2 <= stretches * 2 && (long long)a.K * a.splits * 2 <= 3 * sms) a.splits *= 2;
-  if ((long long)a.K * a.splits > INT32_MAX) return CASCADE_ERR_UNSUPPORTED_SHAPE;
-  k_distill_grad<E, kGradThreads, kStretch><<<a.K * a.splits, kGradThreads, 0, s>>>(a);
+  int threads, smem;
+  CASCADE_TRY(plan<E>(a.K, a.V, &a.splits, &threads, &smem));
+  auto* f = threads == 256 ? k_distill_grad<E, 256> : k_distill_grad<E, 512>;
+  CASCADE_TRY(allow_smem(f, smem));
+  f<<<a.K * a.splits, threads, smem, s>>>(a);
   CASCADE_CUDA_TRY(cudaGetLastError());
   return CASCADE_OK;
 }
@@ -488,8 +594,16 @@ extern "C" int cascade_distill_loss(const void* draft_logits, int32_t logits_dty
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   CASCADE_TRY(logits_dtype == CASCADE_BF16 ? launch_loss<__nv_bfloat16>(a, s) : launch_loss<float>(a, s));
   if (total_out != nullptr) {
-    k_distill_total<<<1, 1024, 0, s>>>(loss_out, K, total_out);
-    CASCADE_CUDA_TRY(cudaGetLastError());
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(1);
+    cfg.blockDim = dim3(1024);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // it starts beside the losses' kernel and waits for its end
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    CASCADE_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_distill_total, (const float*)loss_out, (int)K, total_out));
   }
   return CASCADE_OK;
 }

@@ -13,8 +13,8 @@ bool aligned4(const P*... p) {
 int check_current_device(const cascade_ctx* ctx);
 
 // Bits of cascade_ctx.paged_configured.
-enum : uint32_t { PAGED_CFG_TABLES = 1, PAGED_CFG_ATTN_TC = 2, PAGED_CFG_SAMPLE = 4, PAGED_CFG_SAMPLE_BF16 = 8, PAGED_CFG_GRAD_KV = 16,
-                 PAGED_CFG_GRAD_Q = 32 };
+enum : uint32_t { PAGED_CFG_TABLES = 1, PAGED_CFG_ATTN_TC = 2, PAGED_CFG_SAMPLE = 4, PAGED_CFG_SAMPLE_BF16 = 8, PAGED_CFG_GRAD_TC = 16,
+                 PAGED_CFG_GRAD_F32 = 32 };
 // Lets kernel `f` use `bytes` of dynamic shared memory, once per context and bit.
 template <typename F>
 int configure_smem(cascade_ctx* ctx, uint32_t bit, F* f, int bytes) {

@@ -149,9 +149,9 @@ __device__ __forceinline__ void store_out(float* to, long long stride, const uin
   }
 }
 
+// A tile of keys.
 template <int D>
-__global__ void __launch_bounds__(kThreads) k_paged_grad_kv_f32(const PagedGradArgs p) {
-  extern __shared__ __align__(16) float smem[];
+__device__ __forceinline__ void keys_pass(const PagedGradArgs& p, float* smem) {
   __shared__ uint8_t there[kT];
   __shared__ uint32_t odd[2];
   const Tile<D> t(smem);
@@ -204,9 +204,9 @@ __global__ void __launch_bounds__(kThreads) k_paged_grad_kv_f32(const PagedGradA
     if (odd[key >> 5] >> (key & 31) & 1u) paged::grad_key<float, D>(p, r, rq, k_first + key, kh, threadIdx.x % 32);
 }
 
+// A block of rows.
 template <int D>
-__global__ void __launch_bounds__(kThreads) k_paged_grad_q_f32(const PagedGradArgs p) {
-  extern __shared__ __align__(16) float smem[];
+__device__ __forceinline__ void rows_pass(const PagedGradArgs& p, float* smem) {
   __shared__ uint8_t there[kT];
   __shared__ uint32_t odd[2];
   const Tile<D> t(smem);
@@ -270,20 +270,24 @@ __global__ void __launch_bounds__(kThreads) k_paged_grad_q_f32(const PagedGradAr
 }
 
 template <int D>
+__global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) k_paged_grad_f32(const PagedGradArgs p) {
+  extern __shared__ __align__(16) float smem[];
+  if (blockIdx.z == 0)
+    keys_pass<D>(p, smem);
+  else
+    rows_pass<D>(p, smem);
+}
+
+template <int D>
 int launch(cascade_ctx* ctx, const PagedGradArgs& p, cudaStream_t s) {
   const PagedAttnArgs& a = p.a;
   const int G = a.Hq / a.Hkv;
   const long long kv_blocks = ((long long)a.max_kv + kT - 1) / kT * a.Hkv, q_blocks = ((long long)a.max_q * G + kT - 1) / kT * a.Hkv;
-  if (kv_blocks > INT_MAX || q_blocks > INT_MAX) return CASCADE_ERR_UNSUPPORTED_SHAPE;
-  CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_KV, k_paged_grad_kv_f32<D>, Cfg<D>::kSmem));
-  CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_Q, k_paged_grad_q_f32<D>, Cfg<D>::kSmem));
-  if (kv_blocks > 0) {
-    KernelScope ks(ctx, K_PAGED_GRAD, s);
-    k_paged_grad_kv_f32<D><<<dim3((unsigned)kv_blocks, a.n_req), kThreads, Cfg<D>::kSmem, s>>>(p);
-    CASCADE_CUDA_TRY(cudaGetLastError());
-  }
+  const long long blocks = kv_blocks > q_blocks ? kv_blocks : q_blocks;
+  if (blocks > INT_MAX) return CASCADE_ERR_UNSUPPORTED_SHAPE;
+  CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_F32, k_paged_grad_f32<D>, Cfg<D>::kSmem));   // (a context has one D)
   KernelScope ks(ctx, K_PAGED_GRAD, s);
-  k_paged_grad_q_f32<D><<<dim3((unsigned)q_blocks, a.n_req), kThreads, Cfg<D>::kSmem, s>>>(p);
+  k_paged_grad_f32<D><<<dim3((unsigned)blocks, a.n_req, 2), kThreads, Cfg<D>::kSmem, s>>>(p);
   CASCADE_CUDA_TRY(cudaGetLastError());
   return CASCADE_OK;
 }

@@ -66,7 +66,7 @@ int launch(cascade_ctx* ctx, const Args& p, int grid, cudaStream_t s) {
   const CUtensorMap *mk = page_map(ctx, p, D, a.k), *mv = page_map(ctx, p, D, a.v);
   if (mk == nullptr || mv == nullptr || !row_map(&mq, p, D, a.q, a.q_stride) || !row_map(&mo, p, D, p.g.d_out, (long long)a.Hq * D))
     return CASCADE_ERR_CUDA;
-  CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_KV, k_paged_grad_tc<D>, kSmem<D>));   // (a context has one D)
+  CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_TC, k_paged_grad_tc<D>, kSmem<D>));   // (a context has one D)
   KernelScope ks(ctx, K_PAGED_GRAD, s);
   k_paged_grad_tc<D><<<grid, kThreads, kSmem<D>, s>>>(mq, mo, *mk, *mv, p);
   CASCADE_CUDA_TRY(cudaGetLastError());
