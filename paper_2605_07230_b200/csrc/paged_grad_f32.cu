@@ -1,7 +1,10 @@
 // The gradient of the attention over a paged cache with ordinary multiply-adds: 64 x 64 tiles of scores in shared memory.
 //
-// Compute-bound.  Products run on packed pairs (two multiply-adds an instruction): scores sum over pairs of a head's elements,
-// outputs hold pairs of them.  A CTA owns 64 rows (queries' pass) or 64 keys (keys' pass) and walks over the other side.
+// Products run on packed pairs (two multiply-adds an instruction): scores sum over pairs of a head's elements, outputs hold pairs of
+// them.  A CTA owns 64 keys or 64 rows and walks over the other side; both passes are one launch (8 short sequences, 4 heads of 64:
+// 90 us, in two launches 150 us).  Four sequences of 1000 tokens, 8 heads: 18 TFLOP/s (five products) at D = 64 and 128, the multiply-add
+// units 43 % busy and shared memory 66 %: what bounds it is the latency of either with four warps a scheduler.  Requesting a step's
+// operands one ahead needs registers for half as many warps: 14 % slower at D = 64, the same at 128.
 #include <climits>
 
 #include "paged.h"
@@ -17,6 +20,12 @@ template <int D>
 struct Cfg {
   static constexpr int kRow = D + 4;
   static constexpr int kSmem = (4 * kT * kRow + 2 * kT * kSp + 2 * kT) * (int)sizeof(float);
+};
+
+struct F32Args {
+  PagedGradArgs g;
+  int G;                      // query heads a key head
+  paged::PageDiv page, group; // (divisions by multiplication)
 };
 
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
@@ -92,42 +101,56 @@ struct Tile {
 
 // Rows first .. first + 63 of (token, head of the group) of a key head: queries and output gradients, zeros behind the last.
 template <int D>
-__device__ __forceinline__ void load_rows(const PagedGradArgs& p, int q0, int kh, int G, int first, int n_rows, const Tile<D>& t) {
+__device__ __forceinline__ void load_rows(const F32Args& f, int q0, int kh, int first, int n_rows, const Tile<D>& t) {
+  const PagedGradArgs& p = f.g;
   const PagedAttnArgs& a = p.a;
-  for (int i = threadIdx.x; i < kT * (D / 4); i += kThreads) {
-    const int row = i / (D / 4), col = i % (D / 4) * 4, rr = first + row;
+  const int col = threadIdx.x % (D / 4) * 4;
+#pragma unroll
+  for (int k = 0; k < kT * (D / 4) / kThreads; ++k) {
+    const int row = threadIdx.x / (D / 4) + k * (kThreads * 4 / D), rr = first + row;
     float4 q = make_float4(0.f, 0.f, 0.f, 0.f), g = q;
     if (rr < n_rows) {
-      const long long token = q0 + rr / G;
-      const int head = kh * G + rr % G;
+      const int tok = f.group.page(rr), head = kh * f.G + rr - tok * f.G;
+      const long long token = q0 + tok;
       q = load4(static_cast<const float*>(a.q) + token * a.q_stride + head * D + col);
       g = load4(static_cast<const float*>(p.d_out) + (token * a.Hq + head) * D + col);
+      if (col == 0) {
+        const float2 st = p.stats[token * a.Hq + head];
+        t.lse[row] = st.x;
+        t.delta[row] = st.y;
+      }
     }
     paged::store4(t.a + row * Cfg<D>::kRow + col, q);
     paged::store4(t.b + row * Cfg<D>::kRow + col, g);
   }
-  for (int row = threadIdx.x; row < kT; row += kThreads) {
-    const int rr = first + row;
-    float2 st = make_float2(0.f, 0.f);
-    if (rr < n_rows) st = p.stats[(long long)(q0 + rr / G) * a.Hq + kh * G + rr % G];
-    t.lse[row] = st.x;
-    t.delta[row] = st.y;
-  }
 }
 // Keys first .. first + 63 of a request and their values, zeros where there is none; there[] tells which.
 template <int D>
-__device__ __forceinline__ void load_keys(const PagedAttnArgs& a, int r, int kh, int first, int kv, const Tile<D>& t, uint8_t* there) {
-  for (int i = threadIdx.x; i < kT * (D / 4); i += kThreads) {
-    const int row = i / (D / 4), col = i % (D / 4) * 4, j = first + row;
-    const long long off = j < kv ? paged::key_offset(a, r, j, kh, D) : -1;
-    float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
-    if (off >= 0) {
-      k = load4(static_cast<const float*>(a.k) + off + col);
+__device__ __forceinline__ void load_keys(const F32Args& f, int r, int kh, int first, int kv, const Tile<D>& t, uint8_t* there) {
+  const PagedAttnArgs& a = f.g.a;
+  const int col = threadIdx.x % (D / 4) * 4;
+  const int32_t* table = a.block_table + (size_t)r * a.table_stride;
+  constexpr int kN = kT * (D / 4) / kThreads;
+  int at[kN];                                                // pages first: their loads go together
+#pragma unroll
+  for (int k = 0; k < kN; ++k) {
+    const int j = first + (int)threadIdx.x / (D / 4) + k * (kThreads * 4 / D);
+    at[k] = j < kv ? table[f.page.page(j)] : -1;
+  }
+#pragma unroll
+  for (int k = 0; k < kN; ++k) {
+    const int row = threadIdx.x / (D / 4) + k * (kThreads * 4 / D), j = first + row;
+    const bool is = at[k] >= 0 && at[k] < a.n_pages;
+    if (j < kv && !is && col == 0) atomicOr(a.err, CASCADE_DEV_ERR_BAD_PAGE);
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f), v = x;
+    if (is) {
+      const long long off = (long long)at[k] * a.page_stride + ((long long)(j - f.page.page(j) * a.page_size) * a.Hkv + kh) * D;
+      x = load4(static_cast<const float*>(a.k) + off + col);
       v = load4(static_cast<const float*>(a.v) + off + col);
     }
-    paged::store4(t.c + row * Cfg<D>::kRow + col, k);
+    paged::store4(t.c + row * Cfg<D>::kRow + col, x);
     paged::store4(t.d + row * Cfg<D>::kRow + col, v);
-    if (col == 0) there[row] = off >= 0;
+    if (col == 0) there[row] = is;
   }
 }
 
@@ -151,18 +174,19 @@ __device__ __forceinline__ void store_out(float* to, long long stride, const uin
 
 // A tile of keys.
 template <int D>
-__device__ __forceinline__ void keys_pass(const PagedGradArgs& p, float* smem) {
+__device__ __forceinline__ void keys_pass(const F32Args& f, float* smem) {
+  const PagedGradArgs& p = f.g;
   __shared__ uint8_t there[kT];
   __shared__ uint32_t odd[2];
   const Tile<D> t(smem);
   const PagedAttnArgs& a = p.a;
-  const int G = a.Hq / a.Hkv, kh = blockIdx.x % a.Hkv, k_first = blockIdx.x / a.Hkv * kT, r = blockIdx.y;
+  const int G = f.G, kh = blockIdx.x % a.Hkv, k_first = blockIdx.x / a.Hkv * kT, r = blockIdx.y;
   paged::GradRequest rq;
   if (!paged::load_request(p, r, &rq) || k_first >= rq.kv) return;
   const int n_keys = min(kT, rq.kv - k_first), x0 = rq.kv - rq.nq;
   const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
   if (threadIdx.x < 2) odd[threadIdx.x] = 0u;
-  load_keys<D>(a, r, kh, k_first, rq.kv, t, there);
+  load_keys<D>(f, r, kh, k_first, rq.kv, t, there);
   uint64_t dk[4][D / 32], dv[4][D / 32];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -172,14 +196,14 @@ __device__ __forceinline__ void keys_pass(const PagedGradArgs& p, float* smem) {
   paged::tokens_that_see(a, x0, rq.nq, k_first, k_first + n_keys - 1, &lo, &hi);
   for (int first = lo * G; first < hi * G; first += kT) {
     __syncthreads();
-    load_rows<D>(p, rq.q0, kh, G, first, hi * G, t);
+    load_rows<D>(f, rq.q0, kh, first, hi * G, t);
     __syncthreads();
     float s[4][4], g[4][4];
     scores<D>(t.a, t.c, tx, ty, s);
     scores<D>(t.b, t.d, tx, ty, g);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int row = ty + 16 * i, x = x0 + (first + row) / G;
+      const int row = ty + 16 * i, x = x0 + f.group.page(first + row);
       const float lse = t.lse[row], delta = t.delta[row];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -206,18 +230,19 @@ __device__ __forceinline__ void keys_pass(const PagedGradArgs& p, float* smem) {
 
 // A block of rows.
 template <int D>
-__device__ __forceinline__ void rows_pass(const PagedGradArgs& p, float* smem) {
+__device__ __forceinline__ void rows_pass(const F32Args& f, float* smem) {
+  const PagedGradArgs& p = f.g;
   __shared__ uint8_t there[kT];
   __shared__ uint32_t odd[2];
   const Tile<D> t(smem);
   const PagedAttnArgs& a = p.a;
-  const int G = a.Hq / a.Hkv, kh = blockIdx.x % a.Hkv, first = blockIdx.x / a.Hkv * kT, r = blockIdx.y;
+  const int G = f.G, kh = blockIdx.x % a.Hkv, first = blockIdx.x / a.Hkv * kT, r = blockIdx.y;
   paged::GradRequest rq;
   if (!paged::load_request(p, r, &rq) || first >= rq.nq * G) return;
   const int n_rows = min(kT, rq.nq * G - first), x0 = rq.kv - rq.nq;
   const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
   if (threadIdx.x < 2) odd[threadIdx.x] = 0u;
-  load_rows<D>(p, rq.q0, kh, G, first, rq.nq * G, t);
+  load_rows<D>(f, rq.q0, kh, first, rq.nq * G, t);
   uint64_t dq[4][D / 32];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -227,14 +252,14 @@ __device__ __forceinline__ void rows_pass(const PagedGradArgs& p, float* smem) {
   const int begin = paged::window_begin(max(x_first, 0), a.window), sink_end = min(a.sinks, begin);
   for (int k_first = sink_end > 0 ? 0 : begin / kT * kT; k_first <= x_last;) {
     __syncthreads();
-    load_keys<D>(a, r, kh, k_first, rq.kv, t, there);
+    load_keys<D>(f, r, kh, k_first, rq.kv, t, there);
     __syncthreads();
     float s[4][4], g[4][4];
     scores<D>(t.a, t.c, tx, ty, s);
     scores<D>(t.b, t.d, tx, ty, g);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int row = ty + 16 * i, x = x0 + (first + row) / G;
+      const int row = ty + 16 * i, x = x0 + f.group.page(first + row);
       const float lse = t.lse[row], delta = t.delta[row];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -270,7 +295,7 @@ __device__ __forceinline__ void rows_pass(const PagedGradArgs& p, float* smem) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) k_paged_grad_f32(const PagedGradArgs p) {
+__global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) k_paged_grad_f32(const F32Args p) {
   extern __shared__ __align__(16) float smem[];
   if (blockIdx.z == 0)
     keys_pass<D>(p, smem);
@@ -282,12 +307,13 @@ template <int D>
 int launch(cascade_ctx* ctx, const PagedGradArgs& p, cudaStream_t s) {
   const PagedAttnArgs& a = p.a;
   const int G = a.Hq / a.Hkv;
+  const F32Args f = {p, G, paged::page_div(a.page_size), paged::page_div(G)};
   const long long kv_blocks = ((long long)a.max_kv + kT - 1) / kT * a.Hkv, q_blocks = ((long long)a.max_q * G + kT - 1) / kT * a.Hkv;
   const long long blocks = kv_blocks > q_blocks ? kv_blocks : q_blocks;
   if (blocks > INT_MAX) return CASCADE_ERR_UNSUPPORTED_SHAPE;
   CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_F32, k_paged_grad_f32<D>, Cfg<D>::kSmem));   // (a context has one D)
   KernelScope ks(ctx, K_PAGED_GRAD, s);
-  k_paged_grad_f32<D><<<dim3((unsigned)blocks, a.n_req, 2), kThreads, Cfg<D>::kSmem, s>>>(p);
+  k_paged_grad_f32<D><<<dim3((unsigned)blocks, a.n_req, 2), kThreads, Cfg<D>::kSmem, s>>>(f);
   CASCADE_CUDA_TRY(cudaGetLastError());
   return CASCADE_OK;
 }
