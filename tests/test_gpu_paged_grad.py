@@ -200,6 +200,37 @@ def test_many_requests_some_without_tokens(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_len,kv_len", [([4], [0]), ([3, 0, 0], [0, 0, 7]), ([0, 0], [0, 5])])
+def test_requests_without_keys_or_rows(q_len, kv_len, dtype):
+    Call(q_len, kv_len, 2, 1, 64, dtype, pad=1).run().check()
+
+
+def test_more_items_than_a_launch_holds_at_once():
+    """Several items a block, and blocks that go on with the other pass; the same bits every time."""
+    rng = np.random.default_rng(3)
+    q = rng.integers(1, 280, 30).tolist()
+    c = Call(q, [n + int(rng.integers(0, 60)) for n in q], 20, 20, 64, seed=16).run()
+    c.check()
+    first = [t.clone() for r in range(30) for t in c.got(r)]
+    for _ in range(3):
+        c.backward()
+    c.ctx.check()
+    assert all(torch.equal(a, b) for a, b in zip(first, [t for r in range(30) for t in c.got(r)]))
+
+
+def test_long_sums_key_by_key_beside_short_waits():
+    """A value that is no number has most keys of a long sequence summed again: no wait gives up meanwhile."""
+    c = Call([1500], [1500], 4, 2, 128, seed=17)
+    c.forward()
+    c.d_out[1400, 0, 3] = float("nan")
+    c.ctx.set_wait_limit(3_000_000)
+    c.backward()
+    c.ctx.check()
+    got = c.got(0)
+    assert got[2][:1401, 0].isnan().any(-1).all() and got[2][1401:].isfinite().all() and got[2][:, 1].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_steep_scores(dtype):
     """Weights near 0 and 1 (scores of a size of a hundred)."""
     Call([200], [200], 2, 1, 128, dtype, size=3.5, seed=11).run().check()
