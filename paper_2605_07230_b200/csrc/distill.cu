@@ -489,12 +489,6 @@ int plan(int K, int V, int* splits, int* threads, int* smem) {
   *smem = ((part < kBatch * *threads ? part : kBatch * *threads) * kVec + 2 * kVec) * (int)sizeof(float);
   return CASCADE_OK;
 }
-template <typename F>
-int allow_smem(F* f, int bytes) {
-  if (bytes > 40 * 1024) CASCADE_CUDA_TRY(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
-  return CASCADE_OK;
-}
-
 template <typename E>
 int launch_loss(const LossArgs& in, cudaStream_t s) {
   LossArgs a = in;
@@ -529,7 +523,9 @@ int launch_grad(const GradArgs& in, cudaStream_t s) {
   int threads, smem;
   CASCADE_TRY(plan<E>(a.K, a.V, &a.splits, &threads, &smem));
   auto* f = threads == 256 ? k_distill_grad<E, 256> : k_distill_grad<E, 512>;
-  CASCADE_TRY(allow_smem(f, smem));
+  // (the most that any call of this kernel asks for: calls of other threads may lie between this and the launch)
+  CASCADE_CUDA_TRY(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                        (kBatch * threads + 2) * (16 / (int)sizeof(E)) * (int)sizeof(float)));
   f<<<a.K * a.splits, threads, smem, s>>>(a);
   CASCADE_CUDA_TRY(cudaGetLastError());
   return CASCADE_OK;
@@ -537,13 +533,16 @@ int launch_grad(const GradArgs& in, cudaStream_t s) {
 
 bool off(const void* p, unsigned align) { return (reinterpret_cast<uintptr_t>(p) & (align - 1)) != 0; }
 
-bool meets(const void* a, long long a_bytes, const void* b, long long b_bytes) {
+bool meets(const void* a, uintptr_t a_bytes, const void* b, uintptr_t b_bytes) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return a != nullptr && b != nullptr && x < y + b_bytes && y < x + a_bytes;
 }
 
-// Bytes from the first to the last element of K rows of V elements.
-long long span(int K, int V, long long stride, int es) { return ((K - 1) * stride + V) * es; }
+// Bytes from the first to the last element of K rows of n elements (more than any memory has counts as 2^62).
+uintptr_t span(int K, int n, long long stride, int es) {
+  const __int128 bytes = ((__int128)(K - 1) * stride + n) * es;
+  return bytes < 1ll << 62 ? (uintptr_t)bytes : (uintptr_t)1 << 62;
+}
 
 }  // namespace
 
@@ -564,10 +563,10 @@ extern "C" int cascade_distill_loss(const void* draft_logits, int32_t logits_dty
     return CASCADE_ERR_INVALID_ARG;
   const struct {
     const void* at;
-    long long bytes;
-  } in[] = {{draft_logits, span(K, V, row_stride, es)}, {top_logits, 4ll * K * n_top}, {top_ids, 4ll * K * n_top}, {target_lse, 4ll * K},
-            {feat, 4ll * K * h}, {seq, 4ll * K}},
-    out[] = {{loss_out, 4ll * K}, {saved_out, 16ll * K}, {total_out, 4}};
+    uintptr_t bytes;
+  } in[] = {{draft_logits, span(K, V, row_stride, es)}, {top_logits, span(K, n_top, n_top, 4)}, {top_ids, span(K, n_top, n_top, 4)},
+            {target_lse, span(K, 1, 1, 4)}, {feat, span(K, h, h, 4)}, {seq, span(K, 1, 1, 4)}},
+    out[] = {{loss_out, span(K, 1, 1, 4)}, {saved_out, span(K, 4, 4, 4)}, {total_out, 4}};
   for (int i = 0; i < 3; ++i) {
     for (const auto& x : in)
       if (meets(out[i].at, out[i].bytes, x.at, x.bytes)) return CASCADE_ERR_INVALID_ARG;
@@ -621,10 +620,11 @@ extern "C" int cascade_distill_grad(const void* draft_logits, int32_t logits_dty
   const int es = logits_dtype == CASCADE_BF16 ? 2 : 4;
   if (off(draft_logits, es) || off(grad_out, es) || off(top_logits, 4) || off(top_ids, 4) || off(saved, 16) || off(grad_loss, 4))
     return CASCADE_ERR_INVALID_ARG;
-  const long long bytes = span(K, V, grad_stride, es);
+  const uintptr_t bytes = span(K, V, grad_stride, es), stored = span(K, n_top, n_top, 4);
   const bool in_place = grad_out == draft_logits && (grad_stride == row_stride || K == 1);
-  if ((!in_place && meets(grad_out, bytes, draft_logits, span(K, V, row_stride, es))) || meets(grad_out, bytes, top_logits, 4ll * K * n_top) ||
-      meets(grad_out, bytes, top_ids, 4ll * K * n_top) || meets(grad_out, bytes, saved, 16ll * K) || meets(grad_out, bytes, grad_loss, 4ll * K))
+  if ((!in_place && meets(grad_out, bytes, draft_logits, span(K, V, row_stride, es))) || meets(grad_out, bytes, top_logits, stored) ||
+      meets(grad_out, bytes, top_ids, stored) || meets(grad_out, bytes, saved, span(K, 4, 4, 4)) ||
+      meets(grad_out, bytes, grad_loss, span(K, 1, 1, 4)))
     return CASCADE_ERR_INVALID_ARG;
   GradArgs a;
   a.draft = draft_logits;

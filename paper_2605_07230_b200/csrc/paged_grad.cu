@@ -54,12 +54,15 @@ int launch_stats(cascade_ctx* ctx, const PagedGradArgs& p, const float* lse, cud
 struct Rows {
   const void* at;
   int64_t n, stride, width;
-  int64_t span() const { return n == 0 ? 0 : (n - 1) * stride + width; }
+  uintptr_t span() const {                                             // (more than any memory has counts as 2^62)
+    const __int128 bytes = n == 0 ? 0 : (__int128)(n - 1) * stride + width;
+    return bytes < (int64_t)1 << 62 ? (uintptr_t)bytes : (uintptr_t)1 << 62;
+  }
 };
 // Whether two of them share a byte; rows that lie between each other may have one common stride.
 bool meet(const Rows& a, const Rows& b) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
-  if (a.n == 0 || b.n == 0 || x >= y + (uintptr_t)b.span() || y >= x + (uintptr_t)a.span()) return false;
+  if (a.n == 0 || b.n == 0 || x >= y + b.span() || y >= x + a.span()) return false;
   if (a.stride != b.stride) return true;
   const int64_t d = (int64_t)(y > x ? (y - x) % a.stride : (a.stride - (x - y) % a.stride) % a.stride);   // b's rows behind a's
   return d < a.width || d + b.width > a.stride;
@@ -95,7 +98,9 @@ extern "C" int cascade_paged_attn_grad(cascade_ctx* ctx, const cascade_paged_cac
                           {dv, n_kv, dv_stride * es, kv_row * es}, {scratch, 1, 1, (int64_t)n_tok * sh.Hq * 8}};
   const int64_t pool = ((int64_t)(cache->n_pages - 1) * cache->page_stride + (int64_t)cache->page_size * kv_row) * es;
   const Rows inputs[] = {{q, n_tok, q_stride * es, q_row * es}, {out, 1, 1, n_tok * q_row * es}, {d_out, 1, 1, n_tok * q_row * es},
-                         {lse, 1, 1, (int64_t)n_tok * sh.Hq * 4}, {cache->k_pages, 1, 1, pool}, {cache->v_pages, 1, 1, pool}};
+                         {lse, 1, 1, (int64_t)n_tok * sh.Hq * 4}, {cache->k_pages, 1, 1, pool}, {cache->v_pages, 1, 1, pool},
+                         {cache->block_table, n_req, (int64_t)cache->table_stride * 4, (int64_t)cache->table_stride * 4},
+                         {q_begin, 1, 1, (n_req + 1ll) * 4}, {kv_len, 1, 1, n_req * 4ll}, {k_begin, k_begin != nullptr, 1, n_req * 4ll}};
   for (int i = 0; i < 4; ++i) {
     for (const Rows& x : inputs)
       if (meet(outputs[i], x)) return CASCADE_ERR_INVALID_ARG;

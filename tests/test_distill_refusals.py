@@ -30,7 +30,9 @@ NAN, INF = float("nan"), float("inf")
                                 dict(saved=AT["saved"] + 8), dict(loss=AT["loss"] + 1), dict(seq=AT["seq"] + 2), dict(total=AT["total"] + 2),
                                 dict(loss=AT["draft"] + 4 * (K * V - 1)), dict(saved=AT["top"]), dict(total=AT["loss"] + 4 * (K - 1)),
                                 dict(saved=AT["loss"]), dict(loss=AT["feat"] + 4 * K * H - 4), dict(total=AT["seq"]),
-                                dict(loss=AT["lse"])])
+                                dict(loss=AT["lse"]),
+                                # rows farther apart than 64 bits count: they meet what lies behind
+                                dict(K=2**31 - 1, stride=2**40, total=None)])
 def test_loss_refuses(kw):
     assert loss(**kw) == cb.ERR_INVALID_ARG
 

@@ -58,7 +58,11 @@ def test_alignment_to_4_bytes(name):
                                 dict(dv=AT["v_pages"] + 5 * 16 * KV_ROW), dict(scratch=AT["dq"]), dict(dq=AT["d_out"]),
                                 # one stacked gradient whose parts overlap by one element
                                 dict(dq_stride=512, dk_stride=512, dv_stride=512, dk=AT["dq"] + ROW - 16),
-                                dict(dq_stride=512, dk_stride=512, dv_stride=512, dk=AT["dq"] + 1024 - KV_ROW + 16)])
+                                dict(dq_stride=512, dk_stride=512, dv_stride=512, dk=AT["dq"] + 1024 - KV_ROW + 16),
+                                dict(dq=AT["q_begin"]), dict(dk=AT["kv_len"] - KV_ROW), dict(scratch=AT["k_begin"]),
+                                dict(dv=AT["table"] + 16),
+                                # rows farther apart than 64 bits count
+                                dict(n_kv=2**31 - 1, dk_stride=2**40)])
 def test_overlaps(kw):
     assert call(**kw) == cb.ERR_INVALID_ARG
 
