@@ -16,29 +16,31 @@
 
 namespace {
 
-constexpr int kOwn = 128, kStep = 64;
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
+constexpr int kOwn = 128;
+constexpr int kComputeWarps = 8, kProducts = kComputeWarps;            // the last warp issues products
+// A launch's 168 registers a thread are dealt out anew: 224 for the eight warps that compute, 56 for four of which one is at work.
+constexpr int kThreads = (kComputeWarps + 4) * 32;
 
 template <int D>
 struct Cfg {
-  static constexpr bool kShare = D == 128;               // X1 and X2 take turns in one place, Y1 and Y2 have one place each
-  static constexpr int kOwnPart = kOwn * D * 2, kOwnTile = 3 * kOwnPart;        // bytes
-  static constexpr int kStepPart = kStep * D * 2, kStepTile = 3 * kStepPart;
-  static constexpr int kX2 = kShare ? 0 : kOwnTile, kY = kShare ? kOwnTile : 2 * kOwnTile;
-  static constexpr int kTiles = kY + (kShare ? 2 : 4) * kStepTile;
+  static constexpr int kStep = D == 64 ? 64 : 32;                                // lines walked over at a time
+  static constexpr int kCols = kStep / 2;                                        // of them a thread's
+  static constexpr int kLinesAtOnce = kComputeWarps * 32 * 8 / D, kN = kStep / kLinesAtOnce;   // loads: 8 elements a thread of kN lines
+  // bytes: h and m of X1 and X2, two buffers of h, m, l of Y1 and Y2
+  static constexpr int kOwnPart = kOwn * D * 2, kStepPart = kStep * D * 2, kStepTile = 3 * kStepPart;
+  static constexpr int kX2 = 2 * kOwnPart, kY = 4 * kOwnPart, kTiles = kY + 4 * kStepTile;
+  // columns of the tensor memory: S and dP (P and dS as operands, 3 kStep / 2 columns, over them), results, l of X1 and X2
+  static constexpr int kS = 0, kDp = 2 * kStep, kOut = 4 * kStep, kXl = 384;
+  static_assert(kOut + 2 * D <= kXl && kXl + D <= 512, "tensor memory");
 };
-// columns of the tensor memory: S, dP (dS as an operand over them), P as an operand, results
-constexpr int kS = 0, kDp = 64, kDsOp = 0, kPOp = 128, kOut = 224;
-static_assert(kOut + 2 * 128 <= 512, "tensor memory");
 
 struct Shared {
-  uint64_t s_full, dp_full, out_full, alive;
+  uint64_t s_full, dp_full, out_full, p_full, ds_full, y_full, alive;
   int abort_flag;
   uint32_t tmem;
   uint32_t odd[kOwn / 32];                               // own lines with a result that is not finite
-  float2 stats[2][kStep];                                // of the rows walked over
-  uint8_t there[2][kStep], own_there[kOwn];              // keys whose pages are in the pool
+  __align__(16) float lse[2][64], delta[2][64];          // of the rows walked over
+  uint8_t there[2][64], own_there[kOwn];                 // keys whose pages are in the pool
 };
 
 struct F32Args {
@@ -47,21 +49,24 @@ struct F32Args {
   paged::PageDiv page, group; // (divisions by multiplication)
 };
 
-// Lines of one (request, key head): keys and values, or queries and output gradients (of rows (token, head) up to `end`).
+// Lines of one (request, key head): keys and values, or queries and output gradients (of rows (token, head)), up to `end`.
+template <bool kKeys>
 struct Lines {
   const F32Args& f;
   const int32_t* table;
   int head, q0, end;
+  __device__ __forceinline__ int page(int j) const { return kKeys && j < end ? table[f.page.page(j)] : -1; }
   // -> where line j's elements are; false: there is none (zeros)
-  template <bool kKeys>
-  __device__ __forceinline__ bool find(int j, int D, const float** first, const float** second) const {
+  __device__ __forceinline__ bool find(int j, int page, int D, const float** first, const float** second) const {
     const PagedGradArgs& p = f.g;
     const PagedAttnArgs& a = p.a;
     if (j >= end) return false;
     if (kKeys) {
-      const int in = f.page.page(j), page = table[in];
-      if (page < 0 || page >= a.n_pages) return false;
-      const long long off = (long long)page * a.page_stride + ((long long)(j - in * a.page_size) * a.Hkv + head) * D;
+      if (page < 0 || page >= a.n_pages) {
+        atomicOr(a.err, CASCADE_DEV_ERR_BAD_PAGE);
+        return false;
+      }
+      const long long off = (long long)page * a.page_stride + ((long long)(j - f.page.page(j) * a.page_size) * a.Hkv + head) * D;
       *first = static_cast<const float*>(a.k) + off;
       *second = static_cast<const float*>(a.v) + off;
     } else {
@@ -87,15 +92,15 @@ __device__ __forceinline__ void split2(float x0, float x1, uint32_t* h, uint32_t
   *l = ptx::pack_bf16x2(x0, x1);
 }
 // Eight elements of a line -> their 16 bytes of the three parts.
-__device__ __forceinline__ void store_parts(uint32_t at, int part_bytes, const float4& x, const float4& y) {
+__device__ __forceinline__ void store_parts(uint32_t h_at, uint32_t m_at, uint32_t l_at, const float4& x, const float4& y) {
   uint32_t h[4], m[4], l[4];
   split2(x.x, x.y, &h[0], &m[0], &l[0]);
   split2(x.z, x.w, &h[1], &m[1], &l[1]);
   split2(y.x, y.y, &h[2], &m[2], &l[2]);
   split2(y.z, y.w, &h[3], &m[3], &l[3]);
-  ptx::st_shared_v4(at, h[0], h[1], h[2], h[3]);
-  ptx::st_shared_v4(at + part_bytes, m[0], m[1], m[2], m[3]);
-  ptx::st_shared_v4(at + 2 * part_bytes, l[0], l[1], l[2], l[3]);
+  ptx::st_shared_v4(h_at, h[0], h[1], h[2], h[3]);
+  ptx::st_shared_v4(m_at, m[0], m[1], m[2], m[3]);
+  ptx::st_shared_v4(l_at, l[0], l[1], l[2], l[3]);
 }
 // Place of the 16 bytes `chunk` of a line in a tile whose rows are swizzled over 128 bytes.
 template <int kLines>
@@ -104,62 +109,67 @@ __device__ __forceinline__ uint32_t place(int line, int chunk) {
 }
 
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ void ld_shared_v4(uint32_t addr, uint32_t* x) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(addr) : "memory");
+}
 __device__ __forceinline__ bool elect_one() {
   uint32_t is;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
   return is != 0;
 }
 __device__ __forceinline__ uint64_t plus(uint64_t desc, uint32_t bytes) { return desc + (bytes >> 4); }
-// The six terms, the smallest first: parts of A and of B.
-__device__ __forceinline__ int part_a(int term) { return (0x001102 >> (4 * term)) & 15; }   // l h m m h h
-__device__ __forceinline__ int part_b(int term) { return (0x010120 >> (4 * term)) & 15; }   // h l m h m h
+// The terms from the smallest to the largest, l h, h l, m m, m h, h m, h h: the parts of A and of B.
+__device__ __forceinline__ int part_a(int term) { return (0x001102 >> (4 * term)) & 15; }
+__device__ __forceinline__ int part_b(int term) { return (0x010120 >> (4 * term)) & 15; }
 
-// acc[128 x 64] = X Y^T
+// acc[128 x kStep] = X Y^T, h and m of X in shared memory, l in the tensor memory
 template <int D>
-__device__ __forceinline__ void scores(uint32_t acc, uint32_t x, uint32_t y) {
+__device__ __forceinline__ void scores(uint32_t acc, uint32_t x, uint32_t xl, uint32_t y) {
+  constexpr int kStep = Cfg<D>::kStep;
   const uint32_t idesc = ptx::umma_idesc_bf16(kOwn, kStep);
   const uint64_t dx = ptx::umma_desc_sw128(x), dy = ptx::umma_desc_sw128(y);
+  auto own = [](int ks) { return (ks >> 2) * (kOwn * 128) + (ks & 3) * 32; };
+  auto other = [](int ks) { return (ks >> 2) * (kStep * 128) + (ks & 3) * 32; };
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) ptx::umma_bf16_ts(acc, xl + ks * 8, plus(dy, other(ks)), idesc, ks != 0);
 #pragma unroll 1
-  for (int t = 0; t < 6; ++t) {
+  for (int t = 1; t < 6; ++t) {
     const uint64_t a = plus(dx, part_a(t) * Cfg<D>::kOwnPart), b = plus(dy, part_b(t) * Cfg<D>::kStepPart);
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
-      ptx::umma_bf16(acc, plus(a, (ks >> 2) * (kOwn * 128) + (ks & 3) * 32), plus(b, (ks >> 2) * (kStep * 128) + (ks & 3) * 32), idesc,
-                     ks != 0 || t != 0);
+    for (int ks = 0; ks < D / 16; ++ks) ptx::umma_bf16(acc, plus(a, own(ks)), plus(b, other(ks)), idesc, 1);
   }
 }
-// acc[128 x D] = W Y with W [128][64] in the tensor memory, 32 columns a part
+// acc[128 x D] = W Y with W [128][kStep] in the tensor memory, kStep / 2 columns a part
 template <int D>
 __device__ __forceinline__ void results(uint32_t acc, uint32_t w, uint32_t y) {
+  constexpr int kStep = Cfg<D>::kStep;
   const uint32_t idesc = ptx::umma_idesc_bf16_b_mn(kOwn, D);
   const uint64_t dy = ptx::umma_desc_sw128_strides(y, kStep * 128, 1024);
 #pragma unroll 1
   for (int t = 0; t < 6; ++t) {
     const uint64_t b = plus(dy, part_b(t) * Cfg<D>::kStepPart);
 #pragma unroll
-    for (int ks = 0; ks < kStep / 16; ++ks) ptx::umma_bf16_ts(acc, w + part_a(t) * 32 + ks * 8, plus(b, ks * 2048), idesc, ks != 0 || t != 0);
+    for (int ks = 0; ks < kStep / 16; ++ks)
+      ptx::umma_bf16_ts(acc, w + part_a(t) * (kStep / 2) + ks * 8, plus(b, ks * 2048), idesc, ks != 0 || t != 0);
   }
 }
 
-// 32 columns (after the wait).
-__device__ __forceinline__ void load32(uint32_t taddr, float (&v)[32]) {
-  uint32_t r[32];
-  ptx::tmem_ld32_async(taddr, r);
-  ptx::tmem_wait_ld();
+// Columns of the tensor memory (after the wait).
+__device__ __forceinline__ void load(uint32_t taddr, float (&v)[16]) { ptx::tmem_ld16(taddr, v); }
+__device__ __forceinline__ void load(uint32_t taddr, float (&v)[32]) { ptx::tmem_ld32(taddr, v); }
+// Weights of a lane as an operand's columns of each part, `gap` columns apart.
+template <int kCols>
+__device__ __forceinline__ void store_operand(uint32_t taddr, int gap, const float (&w)[kCols]) {
+  uint32_t x[3][kCols / 2];
 #pragma unroll
-  for (int k = 0; k < 32; ++k) {
-    asm volatile("" : "+r"(r[k]));                                     // no use before the wait
-    v[k] = __uint_as_float(r[k]);
+  for (int k = 0; k < kCols / 2; ++k) split2(w[2 * k], w[2 * k + 1], &x[0][k], &x[1][k], &x[2][k]);
+#pragma unroll
+  for (int part = 0; part < 3; ++part) {
+    if (kCols == 32)
+      ptx::tmem_st16_async(taddr + part * gap, x[part]);
+    else
+      ptx::tmem_st8_async(taddr + part * gap, x[part]);
   }
-}
-// 32 weights of a lane as an operand's 16 columns of each part.
-__device__ __forceinline__ void store_operand(uint32_t taddr, const float (&w)[32]) {
-  uint32_t h[16], m[16], l[16];
-#pragma unroll
-  for (int k = 0; k < 16; ++k) split2(w[2 * k], w[2 * k + 1], &h[k], &m[k], &l[k]);
-  ptx::tmem_st16_async(taddr, h);
-  ptx::tmem_st16_async(taddr + 32, m);
-  ptx::tmem_st16_async(taddr + 64, l);
   ptx::tmem_wait_st();
 }
 // Bits lo .. hi - 1 of a word.
@@ -168,10 +178,14 @@ __device__ __forceinline__ uint32_t bits(int lo, int hi) {
   return below(hi) & ~below(lo);
 }
 
-// One CTA's tile of keys (kKeys) or block of rows.
+// One CTA's tile of keys (kKeys) or block of rows.  Per step:
+//   warps 0-7   | loads of the next step   P   results of the last step added up   next step into shared memory   dS
+//   products    | last dK or dQ   dP                                               dV   next S
+// Every wait of a compute warp is made, in vain too, so that the two warps of 32 lines stay beside each other.
 template <int D, bool kKeys>
 __device__ __forceinline__ void pass(const F32Args& f, uint8_t* smem, Shared& sh) {
   using C = Cfg<D>;
+  constexpr int kStep = C::kStep, kCols = C::kCols, kN = C::kN, kAtOnce = C::kLinesAtOnce;
   const PagedGradArgs& p = f.g;
   const PagedAttnArgs& a = p.a;
   const int G = f.G, head = blockIdx.x % a.Hkv, r = blockIdx.y;
@@ -202,102 +216,164 @@ __device__ __forceinline__ void pass(const F32Args& f, uint8_t* smem, Shared& sh
     at += kStep;
     return kKeys || at < sink_end ? at : max(at, begin);
   };
-  const int32_t* table = a.block_table + (size_t)r * a.table_stride;
-  const Lines mine = {f, table, head, rq.q0, lines}, others = {f, table, head, rq.q0, kKeys ? end : rq.kv};
-
-  const uint32_t base = ptx::smem_u32(smem);
-  const int chunk = tid % (D / 8), line0 = tid / (D / 8);              // a thread's 8 elements of every kThreads / (D / 8)-th line
-  constexpr int kLinesAtOnce = kThreads * 8 / D;
-  // X1 and X2, or one of them
-  auto load_own = [&](bool one, bool two) {
-#pragma unroll 4
-    for (int line = line0; line < kOwn; line += kLinesAtOnce) {
-      const float *x1 = nullptr, *x2 = nullptr;
-      const bool is = mine.find<kKeys>(first + line, D, &x1, &x2);
-      const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (kKeys && one && chunk == 0) {
-        sh.own_there[line] = is;
-        if (!is && first + line < lines) atomicOr(a.err, CASCADE_DEV_ERR_BAD_PAGE);
-      }
-      const uint32_t at = base + place<kOwn>(line, chunk);
-      if (one) store_parts(at, C::kOwnPart, is ? load4(x1 + 8 * chunk) : zero, is ? load4(x1 + 8 * chunk + 4) : zero);
-      if (two) store_parts(at + C::kX2, C::kOwnPart, is ? load4(x2 + 8 * chunk) : zero, is ? load4(x2 + 8 * chunk + 4) : zero);
-    }
-  };
-  constexpr int kN = kStep / kLinesAtOnce;
-  float4 y[kN][4];                                                     // a step's elements on their way: Y1, Y2
-  auto request = [&](int at, int buf) {
-#pragma unroll
-    for (int k = 0; k < kN; ++k) {
-      const int line = line0 + k * kLinesAtOnce;
-      const float *y1 = nullptr, *y2 = nullptr;
-      const bool is = others.find<!kKeys>(at + line, D, &y1, &y2);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[k][e] = is ? load4((e < 2 ? y1 : y2) + 8 * chunk + 4 * (e & 1)) : make_float4(0.f, 0.f, 0.f, 0.f);
-      if (chunk != 0) continue;
-      if (kKeys) {
-        float2 st = make_float2(0.f, 0.f);
-        if (is) {
-          const int tok = f.group.page(at + line);
-          st = p.stats[(long long)(rq.q0 + tok) * a.Hq + head * G + at + line - tok * G];
-        }
-        sh.stats[buf][line] = st;
-      } else {
-        sh.there[buf][line] = is;
-        if (!is && at + line < rq.kv) atomicOr(a.err, CASCADE_DEV_ERR_BAD_PAGE);
-      }
-    }
-  };
-  auto y_tile = [&](int buf, int which) { return base + C::kY + ((C::kShare ? 0 : 2 * buf) + which) * C::kStepTile; };
-  auto put = [&](int buf) {
-#pragma unroll
-    for (int k = 0; k < kN; ++k)
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        store_parts(y_tile(buf, e) + place<kStep>(line0 + k * kLinesAtOnce, chunk), C::kStepPart, y[k][2 * e], y[k][2 * e + 1]);
-  };
-
   if (tid == 0) {
     for (uint64_t* b : {&sh.s_full, &sh.dp_full, &sh.out_full}) ptx::mbar_init(b, 1);
+    for (uint64_t* b : {&sh.p_full, &sh.ds_full, &sh.y_full}) ptx::mbar_init(b, kComputeWarps);
     ptx::fence_mbar_init();
     sh.abort_flag = 0;
     sh.alive = 0;
   }
   if (tid < kOwn / 32) sh.odd[tid] = 0u;
-  if (warp == 0) {
+  if (warp == kProducts) {
     ptx::tmem_alloc(&sh.tmem, 512);
     ptx::tmem_relinquish();
   }
-  if (walk < end) request(walk, 0);
-  load_own(true, !C::kShare);
-  if (walk < end) put(0);
-  ptx::fence_proxy_async_smem();
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
-  const uint32_t tmem = sh.tmem;
-  auto wait = [&](uint64_t* bar, uint32_t parity) { return ptx::mbar_wait_short(bar, parity & 1u, &sh.abort_flag, a.err, a.wait_ns, &sh.alive); };
-  auto issue_scores = [&](int buf, bool one, bool two) {
-    if (warp != 0 || !elect_one()) return;
-    if (one) {
-      scores<D>(tmem + kS, base, y_tile(buf, 0));
-      ptx::umma_commit(&sh.s_full);
-    }
-    if (two) {
-      scores<D>(tmem + kDp, base + C::kX2, y_tile(buf, 1));
-      ptx::umma_commit(&sh.dp_full);
-    }
-  };
-  // all threads' stores to shared or tensor memory are there and all their loads done, for the products that warp 0 issues next
-  auto meet = [&](bool ok) {
-    ptx::tc_fence_before();
-    ok = __syncthreads_and(ok);
+  const uint32_t tmem = sh.tmem, base = ptx::smem_u32(smem);
+  auto y_tile = [&](int buf, int which) { return base + C::kY + (2 * buf + which) * C::kStepTile; };
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    const bool ok = __all_sync(0xffffffffu, ptx::mbar_wait_short(bar, parity & 1u, &sh.abort_flag, a.err, a.wait_ns, &sh.alive));
     ptx::tc_fence_after();
     return ok;
   };
+  bool ok = true;
 
+  if (warp >= kComputeWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    int at = warp == kProducts ? walk : end, buf = 0;
+    if (at < end && (ok = wait(&sh.y_full, 0)) && elect_one()) {
+      scores<D>(tmem + C::kS, base, tmem + C::kXl, y_tile(0, 0));
+      ptx::umma_commit(&sh.s_full);
+      scores<D>(tmem + C::kDp, base + C::kX2, tmem + C::kXl + D / 2, y_tile(0, 1));
+      ptx::umma_commit(&sh.dp_full);
+    }
+    for (int i = 0; ok && at < end; ++i, buf ^= 1) {
+      at = next(at);
+      const bool more = at < end;
+      if (!(ok = wait(&sh.p_full, i))) break;
+      if (kKeys && elect_one()) results<D>(tmem + C::kOut + D, tmem + C::kS, y_tile(buf, 1));
+      if (more) {
+        if (!(ok = wait(&sh.y_full, i + 1))) break;
+        if (elect_one()) {
+          scores<D>(tmem + C::kS, base, tmem + C::kXl, y_tile(buf ^ 1, 0));
+          ptx::umma_commit(&sh.s_full);
+        }
+      }
+      if (!(ok = wait(&sh.ds_full, i))) break;
+      if (elect_one()) {
+        results<D>(tmem + C::kOut, tmem + C::kDp, y_tile(buf, 0));
+        ptx::umma_commit(&sh.out_full);
+        if (more) {
+          scores<D>(tmem + C::kDp, base + C::kX2, tmem + C::kXl + D / 2, y_tile(buf ^ 1, 1));
+          ptx::umma_commit(&sh.dp_full);
+        }
+      }
+    }
+    __syncwarp();
+    if (!__syncthreads_and(ok)) __nanosleep(1000000);                  // products still in flight
+    __syncthreads();
+    ptx::tc_fence_after();
+    if (warp == kProducts) ptx::tmem_dealloc(tmem, 512);
+    return;
+  }
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+
+  const int32_t* table = a.block_table + (size_t)r * a.table_stride;
+  const Lines<kKeys> mine = {f, table, head, rq.q0, lines};
+  const Lines<!kKeys> others = {f, table, head, rq.q0, kKeys ? end : rq.kv};
+  auto all = [] { asm volatile("bar.sync 1, %0;" ::"n"(kComputeWarps * 32) : "memory"); };          // the compute warps
+  auto both = [&] { asm volatile("bar.sync %0, 64;" ::"r"(2 + (warp & 3)) : "memory"); };            // the two warps of 32 lines
+  const int chunk = tid % (D / 8), line0 = tid / (D / 8);              // a thread's 8 elements of lines line0, line0 + kAtOnce, ...
+  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+  float4 y[kN][4];                                                     // a step's elements on their way: Y1, Y2
+  float2 st[kN];                                                       // its rows' statistics, or whether its keys are there
+  int page[kN];                                                        // the pages of the step after that
+  auto pages = [&](int at) {
+#pragma unroll
+    for (int k = 0; k < kN; ++k) page[k] = others.page(at + line0 + k * kAtOnce);
+  };
+  auto request = [&](int at) {
+#pragma unroll
+    for (int k = 0; k < kN; ++k) {
+      const int j = at + line0 + k * kAtOnce;
+      const float *y1 = nullptr, *y2 = nullptr;
+      const bool is = others.find(j, page[k], D, &y1, &y2);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[k][e] = is ? load4((e < 2 ? y1 : y2) + 8 * chunk + 4 * (e & 1)) : zero;
+      st[k] = make_float2(is, 0.f);
+      if (kKeys && is && chunk == 0) {
+        const int tok = f.group.page(j);
+        st[k] = p.stats[(long long)(rq.q0 + tok) * a.Hq + head * G + j - tok * G];
+      }
+    }
+  };
+  auto put = [&](int buf) {
+#pragma unroll
+    for (int k = 0; k < kN; ++k) {
+      const int line = line0 + k * kAtOnce;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t at = y_tile(buf, e) + place<kStep>(line, chunk);
+        store_parts(at, at + C::kStepPart, at + 2 * C::kStepPart, y[k][2 * e], y[k][2 * e + 1]);
+      }
+      if (chunk != 0) continue;
+      if (kKeys)
+        sh.lse[buf][line] = st[k].x, sh.delta[buf][line] = st[k].y;
+      else
+        sh.there[buf][line] = st[k].x != 0.f;
+    }
+    ptx::fence_proxy_async_smem();
+    ptx::tc_fence_before();
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(&sh.y_full);
+  };
+
+  // ---- X1 and X2; their l by way of the steps' place into the tensor memory ----
   const int half = warp >> 2, mine_line = tid & (kOwn - 1), n_mine = first + mine_line;
-  const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16, at_lane = tmem + lane_addr;
+  const uint32_t at_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+  constexpr int kOwnN = kOwn / kAtOnce;
+  int own_page[kOwnN];
+#pragma unroll
+  for (int k = 0; k < kOwnN; ++k) own_page[k] = mine.page(first + line0 + k * kAtOnce);
+  pages(walk);
+#pragma unroll
+  for (int k0 = 0; k0 < kOwnN; k0 += 2) {
+    float4 x[2][4];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int line = line0 + (k0 + k) * kAtOnce;
+      const float *x1 = nullptr, *x2 = nullptr;
+      const bool is = mine.find(first + line, own_page[k0 + k], D, &x1, &x2);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[k][e] = is ? load4((e < 2 ? x1 : x2) + 8 * chunk + 4 * (e & 1)) : zero;
+      if (kKeys && chunk == 0) sh.own_there[line] = is;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t at = base + place<kOwn>(line0 + (k0 + k) * kAtOnce, chunk);
+        store_parts(at + e * C::kX2, at + e * C::kX2 + C::kOwnPart, at + C::kY + e * C::kOwnPart, x[k][2 * e], x[k][2 * e + 1]);
+      }
+  }
+  if (walk < end) {
+    request(walk);
+    pages(next(walk));
+  }
+  all();
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+#pragma unroll
+    for (int q = 0; q < D / 64; ++q) {
+      uint32_t l[16];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        ld_shared_v4(base + C::kY + e * C::kOwnPart + place<kOwn>(mine_line, half * (D / 16) + 4 * q + k), l + 4 * k);
+      ptx::tmem_st16_async(at_lane + C::kXl + e * (D / 2) + half * (D / 4) + 16 * q, l);
+    }
+  ptx::tmem_wait_st();
   // rows [see_lo, see_hi) see this lane's key, or this lane's row at position x sees the keys from x_begin to x and the first ones
   int see_lo = 0, see_hi = 0, x = -1, x_begin = 0;
   float lse = 0.f, delta = 0.f;
@@ -312,124 +388,134 @@ __device__ __forceinline__ void pass(const F32Args& f, uint8_t* smem, Shared& sh
     const int tok = f.group.page(n_mine);
     x = x0 + tok;
     x_begin = paged::window_begin(x, a.window);
-    const float2 st = p.stats[(long long)(rq.q0 + tok) * a.Hq + head * G + n_mine - tok * G];
-    lse = st.x;
-    delta = st.y;
+    const float2 mine_stats = p.stats[(long long)(rq.q0 + tok) * a.Hq + head * G + n_mine - tok * G];
+    lse = mine_stats.x;
+    delta = mine_stats.y;
   }
+  all();                                                               // (the l are read)
+  if (walk < end) put(0);
+
   float out[kKeys ? 2 : 1][D / 2];                                     // this lane's half of the columns: dK or dQ, dV
 #pragma unroll
   for (int o = 0; o < (kKeys ? 2 : 1); ++o)
 #pragma unroll
     for (int k = 0; k < D / 2; ++k) out[o][k] = 0.f;
-
-  bool ok = true;
-  if (walk < end) issue_scores(0, true, !C::kShare);
-  int buf = 0;
+  int buf = 0, steps = 0;
+  auto add = [&] {                                                     // the results of the step before
+    ok = wait(&sh.out_full, steps - 1) && ok;
+#pragma unroll
+    for (int o = 0; o < (kKeys ? 2 : 1); ++o)
+#pragma unroll
+      for (int q = 0; q < D / 32; ++q) {
+        float z[16];
+        load(at_lane + C::kOut + o * D + half * (D / 2) + 16 * q, z);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) out[o][16 * q + k] += z[k];
+      }
+  };
 #pragma unroll 1
-  for (int at = walk, i = 0; at < end; ++i) {
-    const int then = next(at), col = at + half * 32;
+  for (int at = walk; at < end; ++steps, buf ^= 1) {
+    const int col = at + half * kCols;
+    at = next(at);
+    const bool more = at < end;
+    if (more) {
+      request(at);
+      pages(next(at));
+    }
+    ok = wait(&sh.y_full, steps) && ok;                                    // (statistics and marks of this step)
     uint32_t see;
     if (kKeys) {
       see = bits(see_lo - col, see_hi - col);
     } else {
-      const uint32_t there = __ballot_sync(0xffffffffu, sh.there[buf][half * 32 + lane]);
+      const uint32_t there = __ballot_sync(0xffffffffu, lane < kCols && sh.there[buf][half * kCols + lane % kCols]);
       see = there & bits(0, x + 1 - col) & (bits(x_begin - col, 32) | bits(0, a.sinks - col));
     }
-    if (!C::kShare && then < end) request(then, buf ^ 1);
+    // (loads and weights of unseen pairs too: a branch a pair took 3400 cycles a step)
+    float lses[kCols], deltas[kCols];
+    auto stats = [&](const float* from, float (&to)[kCols]) {
+#pragma unroll
+      for (int k = 0; k < kCols; k += 4) *reinterpret_cast<float4*>(to + k) = load4(from + half * kCols + k);
+    };
+    if (kKeys) stats(sh.lse[buf], lses);
     // ---- P ----
-    float w[32], v[32];
-    ok = wait(&sh.s_full, i) && ok;
-    ptx::tc_fence_after();
-    __syncwarp();
-    load32(at_lane + kS + 32 * half, v);
-    const float2* stats = &sh.stats[buf][half * 32];
+    float w[kCols], v[kCols];
+    ok = wait(&sh.s_full, steps) && ok;
+    load(at_lane + C::kS + half * kCols, v);
+    if (kKeys) {
+      ptx::tc_fence_before();
+      both();                                                          // (S is read: P goes over it)
+      ptx::tc_fence_after();
+    }
 #pragma unroll
-    for (int k = 0; k < 32; ++k) w[k] = (see >> k) & 1u ? paged::grad_weight<float>(v[k], a.scale, kKeys ? stats[k].x : lse) : 0.f;
-    if (kKeys) store_operand(at_lane + kPOp + 16 * half, w);
-    if (C::kShare) {
-      load_own(false, true);
-      ptx::fence_proxy_async_smem();
+    for (int k = 0; k < kCols; ++k) {
+      const float weight = paged::grad_weight<float>(v[k], a.scale, kKeys ? lses[k] : lse);
+      w[k] = (see >> k) & 1u ? weight : 0.f;
     }
-    if (kKeys || C::kShare) {
-      ok = meet(ok);
-      if (!ok) break;
-      if (C::kShare) issue_scores(buf, false, true);
-      if (kKeys && warp == 0 && elect_one()) results<D>(tmem + kOut + D, tmem + kPOp, y_tile(buf, 1));
-    }
+    if (steps > 0) add();
+    if (kKeys) store_operand(at_lane + C::kS + half * (kCols / 2), kStep / 2, w);
+    ptx::tc_fence_before();
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(&sh.p_full);
+    if (more) put(buf ^ 1);
     // ---- dS ----
-    ok = wait(&sh.dp_full, i) && ok;
+    if (kKeys) stats(sh.delta[buf], deltas);
+    ok = wait(&sh.dp_full, steps) && ok;
+    load(at_lane + C::kDp + half * kCols, v);
+    ptx::tc_fence_before();
+    both();
     ptx::tc_fence_after();
-    __syncwarp();
-    load32(at_lane + kDp + 32 * half, v);
 #pragma unroll
-    for (int k = 0; k < 32; ++k) w[k] = (see >> k) & 1u ? w[k] * (v[k] - (kKeys ? stats[k].y : delta)) : 0.f;
-    ok = meet(ok);                                                     // (S and dP are read: dS goes over them)
-    if (!ok) break;
-    store_operand(at_lane + kDsOp + 16 * half, w);
-    ok = meet(ok);
-    if (warp == 0 && elect_one()) {
-      results<D>(tmem + kOut, tmem + kDsOp, y_tile(buf, 0));
-      ptx::umma_commit(&sh.out_full);
+    for (int k = 0; k < kCols; ++k) {
+      const float ds = w[k] * (v[k] - (kKeys ? deltas[k] : delta));
+      w[k] = (see >> k) & 1u ? ds : 0.f;
     }
-    if (!C::kShare && then < end) {                                    // the next step's products queue up behind
-      put(buf ^ 1);
-      ptx::fence_proxy_async_smem();
-      meet(true);
-      issue_scores(buf ^ 1, true, true);
-    }
-    // ---- results ----
-    ok = wait(&sh.out_full, i) && ok;
-    ptx::tc_fence_after();
+    store_operand(at_lane + C::kDp + half * (kCols / 2), kStep / 2, w);
+    ptx::tc_fence_before();
     __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(&sh.ds_full);
+  }
+  if (steps > 0) add();
+  ptx::tc_fence_before();
+  __syncwarp();
+  if (__syncthreads_and(ok)) {
+    // ---- 32 columns of a warp's lines at a time, by way of the steps' place: 128 bytes of a row by 8 lanes ----
+    const uint32_t stage = base + C::kY + warp * 4096;
+    float bad = 0.f;
 #pragma unroll
     for (int o = 0; o < (kKeys ? 2 : 1); ++o)
 #pragma unroll
       for (int q = 0; q < D / 64; ++q) {
-        load32(at_lane + kOut + o * D + half * (D / 2) + 32 * q, v);
-#pragma unroll
-        for (int k = 0; k < 32; ++k) out[o][32 * q + k] += v[k];
-      }
-    at = then;
-    if (C::kShare && at < end) {
-      request(at, buf ^ 1);
-      load_own(true, false);
-      put(buf ^ 1);
-      ptx::fence_proxy_async_smem();
-      ok = meet(ok);
-      if (!ok) break;
-      issue_scores(buf ^ 1, true, false);
-    }
-    buf ^= 1;
-  }
-  if (!__syncthreads_and(ok)) {
-    __nanosleep(1000000);                                              // products still in flight
-  } else {
-    if (mine_line < n_own) {
-      float* to[2];
-      if (kKeys) {
-        const long long row = (long long)rq.k0 + n_mine;
-        to[0] = static_cast<float*>(p.dk) + row * p.dk_stride + head * D;
-        to[1] = static_cast<float*>(p.dv) + row * p.dv_stride + head * D;
-      } else {
-        const int tok = f.group.page(n_mine);
-        to[0] = static_cast<float*>(p.dq) + (long long)(rq.q0 + tok) * p.dq_stride + (head * G + n_mine - tok * G) * D;
-      }
-      float bad = 0.f;
-#pragma unroll
-      for (int o = 0; o < (kKeys ? 2 : 1); ++o) {
         const float by = o == 0 ? a.scale : 1.f;
 #pragma unroll
-        for (int k = 0; k < D / 2; k += 4) {
-          const float4 z = make_float4(out[o][k] * by, out[o][k + 1] * by, out[o][k + 2] * by, out[o][k + 3] * by);
-          bad += out[o][k] * 0.f + out[o][k + 1] * 0.f + out[o][k + 2] * 0.f + out[o][k + 3] * 0.f;
-          paged::store4(to[o] + half * (D / 2) + k, z);
+        for (int k = 0; k < 8; ++k) {
+          const float* z = &out[o][32 * q + 4 * k];
+          bad += z[0] * 0.f + z[1] * 0.f + z[2] * 0.f + z[3] * 0.f;
+          ptx::st_shared_v4(stage + lane * 128 + ((k ^ (lane & 7)) << 4), __float_as_uint(z[0] * by), __float_as_uint(z[1] * by),
+                            __float_as_uint(z[2] * by), __float_as_uint(z[3] * by));
         }
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int line = 4 * k + (lane >> 3), j = first + (warp & 3) * 32 + line;
+          uint32_t z[4];
+          ld_shared_v4(stage + line * 128 + (((lane & 7) ^ (line & 7)) << 4), z);
+          if (j >= lines) continue;
+          float* to;
+          if (kKeys) {
+            const long long row = (long long)rq.k0 + j;
+            to = o == 0 ? static_cast<float*>(p.dk) + row * p.dk_stride + head * D : static_cast<float*>(p.dv) + row * p.dv_stride + head * D;
+          } else {
+            const int tok = f.group.page(j);
+            to = static_cast<float*>(p.dq) + (long long)(rq.q0 + tok) * p.dq_stride + (head * G + j - tok * G) * D;
+          }
+          *reinterpret_cast<uint4*>(to + half * (D / 2) + 32 * q + 4 * (lane & 7)) = make_uint4(z[0], z[1], z[2], z[3]);
+        }
+        __syncwarp();
       }
-      if (bad != 0.f) atomicOr(&sh.odd[mine_line >> 5], 1u << (mine_line & 31));
-    }
-    __syncthreads();
+    if (bad != 0.f && mine_line < n_own) atomicOr(&sh.odd[mine_line >> 5], 1u << (mine_line & 31));
+    all();
     // (a value that is no number, or too large, at a line that another line of the tile sees)
-    for (int line = warp; line < n_own; line += kWarps) {
+    for (int line = warp; line < n_own; line += kComputeWarps) {
       if (!(sh.odd[line >> 5] >> (line & 31) & 1u)) continue;
       const int j = first + line, tok = j / G;
       if (kKeys)
@@ -438,10 +524,7 @@ __device__ __forceinline__ void pass(const F32Args& f, uint8_t* smem, Shared& sh
         paged::grad_row<float, D>(p, r, rq.q0 + tok, x0 + tok, head * G + j - tok * G, lane);
     }
   }
-  ptx::tc_fence_before();
   __syncthreads();
-  ptx::tc_fence_after();
-  if (warp == 0) ptx::tmem_dealloc(tmem, 512);
 }
 
 template <int D>
