@@ -5,10 +5,16 @@
 // so that what the tensor cores' additions cut off counts at the size of hh alone; products of one step start from zero and are added
 // up in registers.
 //
-// A CTA owns 128 keys, or 128 rows (token, query head of the group), and walks over the other side 64 at a time:
+// A CTA owns 128 keys, or 128 rows (token, query head of the group), and walks over the other side 64 (D = 64) or 32 lines at a time:
 //     S = X1 Y1^T    P = exp(c S - lse)    dP = X2 Y2^T    dS = P (dP - delta)        keys: dV += P Y2, dK += dS Y1;  rows: dQ += dS Y1
 // with X1, X2 its own keys and values (queries and output gradients), Y1, Y2 the others'.  A lane of the tensor memory is one of its
-// own lines, so all that a thread sums belongs to one line.  P and dS are the products' operands from the tensor memory.
+// own lines, so all that a thread sums belongs to one line.  P and dS are the products' operands from the tensor memory, where the l
+// of X1 and X2 stay too (there is no room for them beside two steps of Y).  Both passes are one launch.
+//
+// 8 sequences of 47 to 450 tokens, 4 heads of 64: 31 us (64 x 64 tiles of multiply-adds: 90 us).  4 of 1000 tokens, 8 heads: 141 us at
+// D = 64, 289 us at 128, 71 TFLOP/s of the five products that have to be (multiply-adds: 18); 42 products of that size are formed for
+// them, 600 TFLOP/s.  A step of 64 takes 5600 cycles where its 96 products, issued one by one, take 4300; loads, splits and weights of
+// the next step lie beside them.
 #include <climits>
 
 #include "paged.h"
@@ -18,7 +24,8 @@ namespace {
 
 constexpr int kOwn = 128;
 constexpr int kComputeWarps = 8, kProducts = kComputeWarps;            // the last warp issues products
-// A launch's 168 registers a thread are dealt out anew: 224 for the eight warps that compute, 56 for four of which one is at work.
+// A launch's 168 registers a thread are dealt out anew: 224 for the eight warps that compute, 56 for four of which one is at work
+// (nine warps of 168: 38 and 156 us for the two cases above that take 31 and 141).
 constexpr int kThreads = (kComputeWarps + 4) * 32;
 
 template <int D>
@@ -338,6 +345,10 @@ __device__ __forceinline__ void pass(const F32Args& f, uint8_t* smem, Shared& sh
 #pragma unroll
   for (int k = 0; k < kOwnN; ++k) own_page[k] = mine.page(first + line0 + k * kAtOnce);
   pages(walk);
+  if (walk < end) {
+    request(walk);
+    pages(next(walk));
+  }
 #pragma unroll
   for (int k0 = 0; k0 < kOwnN; k0 += 2) {
     float4 x[2][4];
@@ -357,10 +368,6 @@ __device__ __forceinline__ void pass(const F32Args& f, uint8_t* smem, Shared& sh
         const uint32_t at = base + place<kOwn>(line0 + (k0 + k) * kAtOnce, chunk);
         store_parts(at + e * C::kX2, at + e * C::kX2 + C::kOwnPart, at + C::kY + e * C::kOwnPart, x[k][2 * e], x[k][2 * e + 1]);
       }
-  }
-  if (walk < end) {
-    request(walk);
-    pages(next(walk));
   }
   all();
 #pragma unroll
@@ -478,50 +485,55 @@ __device__ __forceinline__ void pass(const F32Args& f, uint8_t* smem, Shared& sh
   ptx::tc_fence_before();
   __syncwarp();
   if (__syncthreads_and(ok)) {
-    // ---- 32 columns of a warp's lines at a time, by way of the steps' place: 128 bytes of a row by 8 lanes ----
-    const uint32_t stage = base + C::kY + warp * 4096;
+    // ---- by way of the own lines' place, 32 columns of a warp's lines at a time: 128 bytes of a row by 8 lanes ----
+    constexpr int kParts = (kKeys ? 2 : 1) * (D / 64);
+    static_assert(kComputeWarps * kParts * 4096 <= C::kY, "place of results");
+    const uint32_t stage = base + warp * (kParts * 4096);
     float bad = 0.f;
 #pragma unroll
-    for (int o = 0; o < (kKeys ? 2 : 1); ++o)
+    for (int part = 0; part < kParts; ++part)
 #pragma unroll
-      for (int q = 0; q < D / 64; ++q) {
-        const float by = o == 0 ? a.scale : 1.f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float* z = &out[o][32 * q + 4 * k];
-          bad += z[0] * 0.f + z[1] * 0.f + z[2] * 0.f + z[3] * 0.f;
-          ptx::st_shared_v4(stage + lane * 128 + ((k ^ (lane & 7)) << 4), __float_as_uint(z[0] * by), __float_as_uint(z[1] * by),
-                            __float_as_uint(z[2] * by), __float_as_uint(z[3] * by));
-        }
-        __syncwarp();
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int line = 4 * k + (lane >> 3), j = first + (warp & 3) * 32 + line;
-          uint32_t z[4];
-          ld_shared_v4(stage + line * 128 + (((lane & 7) ^ (line & 7)) << 4), z);
-          if (j >= lines) continue;
-          float* to;
-          if (kKeys) {
-            const long long row = (long long)rq.k0 + j;
-            to = o == 0 ? static_cast<float*>(p.dk) + row * p.dk_stride + head * D : static_cast<float*>(p.dv) + row * p.dv_stride + head * D;
-          } else {
-            const int tok = f.group.page(j);
-            to = static_cast<float*>(p.dq) + (long long)(rq.q0 + tok) * p.dq_stride + (head * G + j - tok * G) * D;
-          }
-          *reinterpret_cast<uint4*>(to + half * (D / 2) + 32 * q + 4 * (lane & 7)) = make_uint4(z[0], z[1], z[2], z[3]);
-        }
-        __syncwarp();
+      for (int k = 0; k < 8; ++k) {
+        const float* z = &out[part / (D / 64)][part % (D / 64) * 32 + 4 * k];
+        const float by = part < D / 64 ? a.scale : 1.f;
+        bad += z[0] * 0.f + z[1] * 0.f + z[2] * 0.f + z[3] * 0.f;
+        ptx::st_shared_v4(stage + part * 4096 + lane * 128 + ((k ^ (lane & 7)) << 4), __float_as_uint(z[0] * by), __float_as_uint(z[1] * by),
+                          __float_as_uint(z[2] * by), __float_as_uint(z[3] * by));
       }
+    __syncwarp();
+#pragma unroll 2
+    for (int k = 0; k < 8; ++k) {
+      const int line = 4 * k + (lane >> 3), j = first + (warp & 3) * 32 + line;
+      if (j >= lines) continue;
+      float* to[2];
+      if (kKeys) {
+        const long long row = (long long)rq.k0 + j;
+        to[0] = static_cast<float*>(p.dk) + row * p.dk_stride + head * D;
+        to[1] = static_cast<float*>(p.dv) + row * p.dv_stride + head * D;
+      } else {
+        const int tok = f.group.page(j);
+        to[0] = static_cast<float*>(p.dq) + (long long)(rq.q0 + tok) * p.dq_stride + (head * G + j - tok * G) * D;
+      }
+#pragma unroll
+      for (int part = 0; part < kParts; ++part) {
+        uint32_t z[4];
+        ld_shared_v4(stage + part * 4096 + line * 128 + (((lane & 7) ^ (line & 7)) << 4), z);
+        *reinterpret_cast<uint4*>(to[part / (D / 64)] + half * (D / 2) + part % (D / 64) * 32 + 4 * (lane & 7)) = make_uint4(z[0], z[1], z[2], z[3]);
+      }
+    }
     if (bad != 0.f && mine_line < n_own) atomicOr(&sh.odd[mine_line >> 5], 1u << (mine_line & 31));
     all();
     // (a value that is no number, or too large, at a line that another line of the tile sees)
-    for (int line = warp; line < n_own; line += kComputeWarps) {
-      if (!(sh.odd[line >> 5] >> (line & 31) & 1u)) continue;
-      const int j = first + line, tok = j / G;
-      if (kKeys)
-        paged::grad_key<float, D>(p, r, rq, j, head, lane);
-      else
-        paged::grad_row<float, D>(p, r, rq.q0 + tok, x0 + tok, head * G + j - tok * G, lane);
+    if ((sh.odd[0] | sh.odd[1] | sh.odd[2] | sh.odd[3]) != 0u) {
+#pragma unroll 1
+      for (int line = warp; line < n_own; line += kComputeWarps) {
+        if (!(sh.odd[line >> 5] >> (line & 31) & 1u)) continue;
+        const int j = first + line, tok = j / G;
+        if (kKeys)
+          paged::grad_key<float, D>(p, r, rq, j, head, lane);
+        else
+          paged::grad_row<float, D>(p, r, rq.q0 + tok, x0 + tok, head * G + j - tok * G, lane);
+      }
     }
   }
   __syncthreads();
