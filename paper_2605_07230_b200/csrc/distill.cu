@@ -18,6 +18,7 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kMaxSplits = 8;       // CTAs of one row of the loss (a cluster)
 constexpr int kBatch = 4;           // pieces a thread of a stretch
+constexpr int kHold = 4;            // stored entries that a thread holds in registers
 
 // Rows are walked in pieces of 16 bytes from the 16-byte boundary at or in front of their first element: element v of the row
 // is place v + lead.  The pieces that lie wholly inside are `first` .. `last` - 1; what is left at both ends goes element by element.
@@ -89,7 +90,7 @@ __device__ __forceinline__ void load_stretch(const E* d, int lead, bool aligned,
 }
 
 // What is stored of a position: the first entries of a thread stay in registers.
-template <int kThreads, int kHold>
+template <int kThreads>
 struct Stored {
   const float* top;
   const int32_t* ids;
@@ -221,8 +222,8 @@ struct LossArgs {
 
 // One row a cluster of `splits` CTAs, a share of the row and of the stored entries each.
 template <typename E, int kThreads>
-__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : 2) k_distill_loss(const LossArgs a) {
-  constexpr int kVec = Row<E>::kVec, kHold = 4, kWarps = kThreads / 32, kPieces = kBatch * kThreads;
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_distill_loss(const LossArgs a) {
+  constexpr int kVec = Row<E>::kVec, kWarps = kThreads / 32, kPieces = kBatch * kThreads;
   __shared__ float s_max[kWarps];
   __shared__ Soft s_warp[kWarps];
   __shared__ double s_sum[kWarps][5];
@@ -240,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : 2) k_distill_l
   uint4 raw[kBatch];
   load_stretch<E, kThreads>(d, r.lead, true, p, last, raw);
   const int per = (a.n + a.splits - 1) / a.splits, i0 = min(a.n, rank * per);
-  Stored<kThreads, kHold> stored(a.top + (long long)row * a.n + i0, a.ids + (long long)row * a.n + i0, min(a.n - i0, per), a.V);
+  Stored<kThreads> stored(a.top + (long long)row * a.n + i0, a.ids + (long long)row * a.n + i0, min(a.n - i0, per), a.V);
   if (seq < 0) {                                           // (the same in every CTA of the cluster)
     if (rank == 0 && tid == 0) {
       a.loss[row] = 0.f;
@@ -406,8 +407,8 @@ struct GradArgs {
 
 // A row, or one of `splits` parts of it, a CTA.
 template <typename E, int kThreads>
-__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : 2) k_distill_grad(const GradArgs a) {
-  constexpr int kVec = Row<E>::kVec, kHold = 4, kPieces = kBatch * kThreads;
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_distill_grad(const GradArgs a) {
+  constexpr int kVec = Row<E>::kVec, kPieces = kBatch * kThreads;
   extern __shared__ __align__(16) float s_q[];             // [places of a stretch, then the elements at the row's ends]
   __shared__ int s_twice;
   const int row = blockIdx.x / a.splits, part = blockIdx.x % a.splits, tid = threadIdx.x;
@@ -425,7 +426,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : 2) k_distill_g
   // what comes first is requested at once, padding's too
   uint4 raw[kBatch];
   load_stretch<E, kThreads>(d, r.lead, aligned, first, last, raw);
-  Stored<kThreads, kHold> stored(a.top + (long long)row * a.n, a.ids + (long long)row * a.n, a.n, a.V);
+  Stored<kThreads> stored(a.top + (long long)row * a.n, a.ids + (long long)row * a.n, a.n, a.V);
   const float f = saved.w * up * a.scale * inv_t;
   if (f == 0.f) {                                          // padding: zeros, whatever the row holds
     for (int p = first + tid; p < last; p += kThreads) to[p] = make_uint4(0, 0, 0, 0);
@@ -474,10 +475,13 @@ int sm_count() {
   return n;
 }
 
-// Few rows are shared out until every SM has some, in parts of at least 4 pieces a thread of 128; short parts take 256 threads instead
-// of 512, so that more of them are on an SM at once.  Shared memory: the places of a stretch and the row's ends.
+// Few rows are shared out until every SM has some, in parts of at least 4 pieces a thread of 128.  A part goes over all of its row's
+// stored entries, once a stretch, so that it takes as many threads as hold them in registers (4608 rows of 16384, 2000 entries: 512
+// threads 126 us, 256 171 us, 128 268 us).  128 threads are for many parts with few entries, of which more are on an SM at once
+// (1153 bf16 rows of 10007, 333 entries: 14.5 us, 256 threads 18.4 us; 300 rows: 256 threads 14 us, 128 16 us; 4608 rows of 262144
+// bytes: 370 us, 128 380 us).  Shared memory: the places of a stretch and the row's ends.
 template <typename E>
-int plan(int K, int V, int* splits, int* threads, int* smem) {
+int plan(int K, int V, int n, int* splits, int* threads, int* smem) {
   constexpr int kVec = 16 / (int)sizeof(E);
   const int sms = sm_count(), pieces = V / kVec;
   if (sms <= 0) return CASCADE_ERR_CUDA;
@@ -485,26 +489,35 @@ int plan(int K, int V, int* splits, int* threads, int* smem) {
   while (*splits * 4 * 128 < pieces && (long long)K * *splits * 2 <= 4 * sms) *splits *= 2;
   if ((long long)K * *splits > INT32_MAX) return CASCADE_ERR_UNSUPPORTED_SHAPE;
   const int part = cascade_detail::ceil_div(pieces, *splits) + 32;
-  *threads = part <= kBatch * 256 ? 256 : 512;
+  *threads = n > kHold * 256 ? 512 : n > kHold * 128 || (long long)K * *splits <= 4 * sms || part > 8192 + 32 ? 256 : 128;
   *smem = ((part < kBatch * *threads ? part : kBatch * *threads) * kVec + 2 * kVec) * (int)sizeof(float);
   return CASCADE_OK;
 }
+
 template <typename E>
 int launch_loss(const LossArgs& in, cudaStream_t s) {
   LossArgs a = in;
   const int sms = sm_count();
   if (sms <= 0) return CASCADE_ERR_CUDA;
-  // few rows are shared out until every SM has some.  Long rows take 512 threads: no more than two rows an SM are then at work, and
-  // the stored tokens' logits are still in the L2 at their ends (4608 rows of 262144 bytes: 262 us, with 256 threads 307 us); of short
-  // rows more are wanted (1153 of 20014 bytes: 18.5 us, with 512 threads 26.5 us)
+  // few rows are shared out until every SM has some
   const long long bytes = (long long)a.V * sizeof(E);
   a.splits = 1;
   while (a.splits < kMaxSplits && bytes >= a.splits * 8192ll && (long long)a.K * a.splits * 2 <= 4 * sms) a.splits *= 2;
   if ((long long)a.K * a.splits > INT32_MAX) return CASCADE_ERR_UNSUPPORTED_SHAPE;
-  const bool small = bytes / a.splits <= 65536;
+  // Many parts take 128 threads, more of them being on an SM at once (1153 bf16 rows of 10007, 333 entries: 14.4 us, 256 threads
+  // 18.4 us), unless there are more stored entries than they hold in registers and the part is long: the logits of the entries
+  // should still be in the L2 at its end, so that fewer rows are to be under way (4608 rows of 262144 bytes, 2000 entries: 512 threads
+  // 261 us, 256 303 us, 128 344 us; 1000 entries: 249, 244, 264 us).  A few hundred rows leave room for 256 (300 rows of 65536, 400
+  // entries: 20 us, 128 threads 23 us).
+  const long long part = bytes / a.splits;
+  const int n = (a.n + a.splits - 1) / a.splits;
+  const int threads = a.splits == 1 && a.K <= 4 * sms                                         ? 256
+                      : n <= kHold * 128 || (part <= 65536 && a.splits == 1)                    ? 128
+                      : n <= kHold * 256 || part <= 131072                                    ? 256
+                                                                                              : 512;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(a.K * a.splits));
-  cfg.blockDim = dim3(small ? 256 : 512);
+  cfg.blockDim = dim3(threads);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -512,7 +525,7 @@ int launch_loss(const LossArgs& in, cudaStream_t s) {
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  auto* f = small ? k_distill_loss<E, 256> : k_distill_loss<E, 512>;
+  auto* f = threads == 128 ? k_distill_loss<E, 128> : threads == 256 ? k_distill_loss<E, 256> : k_distill_loss<E, 512>;
   CASCADE_CUDA_TRY(cudaLaunchKernelEx(&cfg, f, a));
   return CASCADE_OK;
 }
@@ -521,8 +534,8 @@ template <typename E>
 int launch_grad(const GradArgs& in, cudaStream_t s) {
   GradArgs a = in;
   int threads, smem;
-  CASCADE_TRY(plan<E>(a.K, a.V, &a.splits, &threads, &smem));
-  auto* f = threads == 256 ? k_distill_grad<E, 256> : k_distill_grad<E, 512>;
+  CASCADE_TRY(plan<E>(a.K, a.V, a.n, &a.splits, &threads, &smem));
+  auto* f = threads == 128 ? k_distill_grad<E, 128> : threads == 256 ? k_distill_grad<E, 256> : k_distill_grad<E, 512>;
   // (the most that any call of this kernel asks for: calls of other threads may lie between this and the launch)
   CASCADE_CUDA_TRY(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                         (kBatch * threads + 2) * (16 / (int)sizeof(E)) * (int)sizeof(float)));
