@@ -78,7 +78,7 @@ __device__ __forceinline__ void load_stretch(const E* d, int lead, bool aligned,
     const int p = p0 + b * kThreads + (int)threadIdx.x;
     if (p >= last) break;
     if (aligned) {
-      raw[b] = __ldg(reinterpret_cast<const uint4*>(d - lead) + p);
+      raw[b] = reinterpret_cast<const uint4*>(d - lead)[p];
     } else {
       const E* x = d + (p * kVec - lead);
       uint32_t w[4] = {0, 0, 0, 0};
