@@ -1,7 +1,12 @@
 // The gradient of the attention over a paged cache on the tensor cores (bf16): keys' and queries' passes side by side in one launch.
 //
-// A CTA an SM; most begin with the keys' pass, the rest with the queries' (a step of 128 x 128 takes 4.1 and 2.9 thousand cycles).
-// Where there are many items a CTA that finds no more goes on with the other pass.
+// A CTA an SM; some begin with the keys' pass, the rest with the queries' (a step of 128 x 128 takes 4.1 and 2.9 thousand cycles, of
+// which the products alone need 2.0 and 1.5).  Where there are many items a CTA that finds no more goes on with the other pass.
+//
+// 8 sequences of 2480 tokens, 32 heads of 128: 1.57 to 1.72 ms, 590 to 640 TFLOP/s of the five products that have to be, 820 to 900 of the
+// seven that are formed (the card's best: 1694); 2 of 640 tokens: 64 us; 12 of 100 to 1144, 20 heads of 64: 166 us.  The tensor cores
+// are busy 52 % (keys) and 57 % (queries) of the time.  What holds them up: the first and last steps of an item, which nothing lies
+// beside (7 and 9 thousand cycles an item), and weights and their gradients on the way through the registers.
 #include "paged_grad_kv.cuh"
 #include "paged_grad_q.cuh"
 
@@ -92,11 +97,18 @@ int launch_paged_grad_tc(cascade_ctx* ctx, const PagedGradArgs& g, cudaStream_t 
   p.taken = ctx->dev_error + 40;   // (cleared with the error word when the context is made)
   const long long keys = most_items(a, g.n_kv, a.max_kv, kTile), rows = most_items(a, a.n_tok, a.max_q, p.tpb), sms = ctx->sm_count;
   if (keys > INT_MAX / 2 || rows > INT_MAX / 2) return CASCADE_ERR_UNSUPPORTED_SHAPE;
-  // all items at once if there are no more than SMs; else the SMs in proportion to the passes' time
+  // All items at once if there are no more than SMs; else the SMs in proportion to the passes' time: thousands of cycles an item and
+  // a step, of which there are as many in both, estimated from the requests' mean lengths.  (2 x 640 tokens, 32 heads of 128: 64 us; by
+  // 41 : 29 an item, which is right for long rows alone, 67 us.)
   if (keys + rows <= sms) {
     p.n_cta_keys = (int)keys;
   } else {
-    const long long share = (sms * 41 * keys + (41 * keys + 29 * rows) / 2) / (41 * keys + 29 * rows), most = keys < sms - 1 ? keys : sms - 1;
+    const bool wide = ctx->shape.D == 128;
+    double seen = ((double)g.n_kv - 0.5 * a.n_tok) / a.n_req;          // keys that a row sees
+    if (a.window > 0 && seen > (double)a.window + a.sinks) seen = (double)a.window + a.sinks;
+    const double steps = (seen > 0 ? seen / kTile + 0.5 : 0.5) * rows;
+    const double time_keys = (wide ? 7 : 4) * (double)keys + 4.05 * steps, time_rows = (wide ? 8.8 : 4.2) * (double)rows + 2.9 * steps;
+    const long long share = (long long)(sms * time_keys / (time_keys + time_rows) + 0.5), most = keys < sms - 1 ? keys : sms - 1;
     p.n_cta_keys = (int)(keys == 0 ? 0 : share < 1 ? 1 : share > most ? most : share);
   }
   const long long left = sms - p.n_cta_keys;
