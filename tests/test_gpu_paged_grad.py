@@ -114,7 +114,8 @@ class Call:
     def tolerance(self, r, size, want):
         """A score is off by its D roundings of terms that sum to at most S (in 32 bits, a tensor core's additions counted twice),
         its exponential by that, by its argument's three roundings and by 2^-22 of its own; the weight's gradient by D roundings of
-        its parts; both go to the operands' type for a product, and n terms are added.  One rounding of the result."""
+        its parts; both go to the operands' type for a product (half a step, and a hundredth of one for an exponential that is off by
+        3e-6), and n terms are added.  One rounding of the result."""
         (q, g, o, lse), k, v = self.request(r)
         if not len(q) or not len(k):
             return [torch.zeros_like(w) for w in want]
