@@ -156,5 +156,5 @@ __device__ void grad_key(const PagedGradArgs& p, int r, const GradRequest& rq, i
 
 }  // namespace paged
 
-// paged_grad_f32.cu: tiles in shared memory, packed fp32 multiply-adds (the fp32 type).
+// paged_grad_f32.cu: the fp32 type, three bf16 parts a number.
 int launch_paged_grad_f32(cascade_ctx* ctx, const PagedGradArgs& p, cudaStream_t s);
