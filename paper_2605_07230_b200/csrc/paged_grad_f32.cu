@@ -560,7 +560,8 @@ int launch(cascade_ctx* ctx, const PagedGradArgs& p, cudaStream_t s) {
   const PagedAttnArgs& a = p.a;
   const int G = a.Hq / a.Hkv;
   const F32Args f = {p, G, paged::page_div(a.page_size), paged::page_div(G)};
-  const long long kv_blocks = ((long long)a.max_kv + kOwn - 1) / kOwn * a.Hkv, q_blocks = ((long long)a.max_q * G + kOwn - 1) / kOwn * a.Hkv;
+  const int max_kv = a.max_kv < p.n_kv ? a.max_kv : p.n_kv;            // (longer requests are left out)
+  const long long kv_blocks = ((long long)max_kv + kOwn - 1) / kOwn * a.Hkv, q_blocks = ((long long)a.max_q * G + kOwn - 1) / kOwn * a.Hkv;
   const long long blocks = kv_blocks > q_blocks ? kv_blocks : q_blocks;
   if (blocks > INT_MAX) return CASCADE_ERR_UNSUPPORTED_SHAPE;
   CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_F32, k_paged_grad_f32<D>, kSmem));   // (a context has one D)

@@ -232,6 +232,43 @@ def test_long_sums_key_by_key_beside_short_waits():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_bounds_far_above_the_lengths_change_nothing(dtype):
+    c = Call([70, 1, 0, 133], [70, 40, 9, 300], 4, 2, 64, dtype, seed=18).run()
+    first = [t.clone() for r in range(4) for t in c.got(r)]
+    c.max_q, c.max_kv = 1 << 20, c.table.shape[1] * 16 * 1000
+    c.backward()
+    c.ctx.check()
+    assert all(torch.equal(a, b) for a, b in zip(first, [t for r in range(4) for t in c.got(r)]))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_fp32_numbers_of_all_sizes(D):
+    """Values and output gradients of 2^-40 to 2^40: every element keeps its own 24 bits."""
+    c = Call([150], [190], 2, 1, D, "f32", seed=19)
+    rng = np.random.default_rng(20)
+    power = lambda t: t.mul_(torch.as_tensor(2.0 ** rng.integers(-40, 41, tuple(t.shape)).astype(np.float32), device=G.DEV))   # noqa: E731
+    power(c.v_pages)
+    power(c.d_out)
+    c.run().check()
+
+
+def test_calls_of_both_types_side_by_side():
+    calls = [Call([400], [400], 8, 8, 128, "bf16", seed=21), Call([300], [300], 4, 4, 64, "f32", seed=22), Call([200, 90], [200, 90], 4, 4, 128, "f32", seed=23)]
+    for c in calls:
+        c.forward()
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for c, s in zip(calls, streams):
+            with torch.cuda.stream(s):
+                c.backward()
+    torch.cuda.synchronize()
+    for c in calls:
+        c.ctx.check()
+        c.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_steep_scores(dtype):
     """Weights near 0 and 1 (scores of a size of a hundred)."""
     Call([200], [200], 2, 1, 128, dtype, size=3.5, seed=11).run().check()
