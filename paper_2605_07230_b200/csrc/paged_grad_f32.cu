@@ -53,6 +53,7 @@ struct Shared {
 struct F32Args {
   PagedGradArgs g;
   int G;                      // query heads a key head
+  int split_keys, split_rows; // CTAs (a cluster) that share the walk of a tile in either pass
   paged::PageDiv page, group; // (divisions by multiplication)
 };
 
@@ -185,7 +186,14 @@ __device__ __forceinline__ uint32_t bits(int lo, int hi) {
   return below(hi) & ~below(lo);
 }
 
-// One CTA's tile of keys (kKeys) or block of rows.  Per step:
+__device__ __forceinline__ void cluster_meet() {
+  __syncwarp();
+  ptx::cluster_arrive();
+  ptx::cluster_wait();
+}
+
+// One CTA's tile of keys (kKeys) or block of rows; of a cluster of `splits` each takes every splits-th step, and their results
+// are added up by pairs, pairs of pairs and so on.  Per step:
 //   warps 0-7   | loads of the next step   P   results of the last step added up   next step into shared memory   dS
 //   products    | last dK or dQ   dP                                               dV   next S
 // Every wait of a compute warp is made, in vain too, so that the two warps of 32 lines stay beside each other.
@@ -195,12 +203,13 @@ __device__ __forceinline__ void pass(const F32Args& f, uint8_t* smem, Shared& sh
   constexpr int kStep = C::kStep, kCols = C::kCols, kN = C::kN, kAtOnce = C::kLinesAtOnce;
   const PagedGradArgs& p = f.g;
   const PagedAttnArgs& a = p.a;
-  const int G = f.G, head = blockIdx.x % a.Hkv, r = blockIdx.y;
+  const int splits = kKeys ? f.split_keys : f.split_rows, rank = blockIdx.x % splits, tile = blockIdx.x / splits;
+  const int G = f.G, head = tile % a.Hkv, r = blockIdx.y;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   paged::GradRequest rq;
   if (!paged::load_request(p, r, &rq)) return;
   const int x0 = rq.kv - rq.nq, lines = kKeys ? rq.kv : rq.nq * G;
-  int own = blockIdx.x / a.Hkv;                                        // the longest first: keys in order, rows from the end
+  int own = tile / a.Hkv;                                        // the longest first: keys in order, rows from the end
   if (!kKeys) own = (lines + kOwn - 1) / kOwn - 1 - own;
   const int first = own * kOwn;
   if (first < 0 || first >= lines) return;
@@ -219,10 +228,15 @@ __device__ __forceinline__ void pass(const F32Args& f, uint8_t* smem, Shared& sh
     walk = sink_end > 0 ? 0 : begin;
     end = x0 + (first + n_own - 1) / G + 1;
   }
-  auto next = [&](int at) {
+  auto step = [&](int at) {
     at += kStep;
     return kKeys || at < sink_end ? at : max(at, begin);
   };
+  auto next = [&](int at) {
+    for (int i = 0; i < splits && at < end; ++i) at = step(at);
+    return at;
+  };
+  for (int i = 0; i < rank && walk < end; ++i) walk = step(walk);
   if (tid == 0) {
     for (uint64_t* b : {&sh.s_full, &sh.dp_full, &sh.out_full}) ptx::mbar_init(b, 1);
     for (uint64_t* b : {&sh.p_full, &sh.ds_full, &sh.y_full}) ptx::mbar_init(b, kComputeWarps);
@@ -280,6 +294,7 @@ __device__ __forceinline__ void pass(const F32Args& f, uint8_t* smem, Shared& sh
     }
     __syncwarp();
     if (!__syncthreads_and(ok)) __nanosleep(1000000);                  // products still in flight
+    for (int n = 1; n < splits; n *= 2) cluster_meet(), cluster_meet();
     __syncthreads();
     ptx::tc_fence_after();
     if (warp == kProducts) ptx::tmem_dealloc(tmem, 512);
@@ -484,7 +499,34 @@ __device__ __forceinline__ void pass(const F32Args& f, uint8_t* smem, Shared& sh
   if (steps > 0) add();
   ptx::tc_fence_before();
   __syncwarp();
-  if (__syncthreads_and(ok)) {
+  ok = __syncthreads_and(ok);
+  if (splits > 1) {
+    constexpr int kValues = (kKeys ? 2 : 1) * (D / 2);
+    static_assert(kValues * kComputeWarps * 32 * 4 <= C::kY, "place of another CTA's results");
+    for (int n = 1; n < splits; n *= 2) {
+      cluster_meet();                                                  // the place is free: products are done, results of before added up
+      if (rank % (2 * n) == n) {
+        const uint32_t to = ptx::map_to_cta(base, rank - n) + tid * 16;
+#pragma unroll
+        for (int k = 0; k < kValues; k += 4) {
+          const float* z = &out[k / (D / 2)][k % (D / 2)];
+          ptx::st_cluster_v4(to + k * (kComputeWarps * 32 * 4), make_float4(z[0], z[1], z[2], z[3]));
+        }
+      }
+      cluster_meet();
+      if (rank % (2 * n) == 0) {
+#pragma unroll
+        for (int k = 0; k < kValues; k += 4) {
+          uint32_t z[4];
+          ld_shared_v4(base + tid * 16 + k * (kComputeWarps * 32 * 4), z);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) out[k / (D / 2)][k % (D / 2) + e] += __uint_as_float(z[e]);
+        }
+      }
+    }
+    all();                                                             // (the results go the same way)
+  }
+  if (ok && rank == 0) {
     // ---- by way of the own lines' place, 32 columns of a warp's lines at a time: 128 bytes of a row by 8 lanes ----
     constexpr int kParts = (kKeys ? 2 : 1) * (D / 64);
     static_assert(kComputeWarps * kParts * 4096 <= C::kY, "place of results");
@@ -559,15 +601,48 @@ int launch(cascade_ctx* ctx, const PagedGradArgs& p, cudaStream_t s) {
   static_assert(kSmem <= 232448, "shared memory of a CTA");
   const PagedAttnArgs& a = p.a;
   const int G = a.Hq / a.Hkv;
-  const F32Args f = {p, G, paged::page_div(a.page_size), paged::page_div(G)};
+  F32Args f = {p, G, 1, 1, paged::page_div(a.page_size), paged::page_div(G)};
   const int max_kv = a.max_kv < p.n_kv ? a.max_kv : p.n_kv;            // (longer requests are left out)
   const long long kv_blocks = ((long long)max_kv + kOwn - 1) / kOwn * a.Hkv, q_blocks = ((long long)a.max_q * G + kOwn - 1) / kOwn * a.Hkv;
   const long long blocks = kv_blocks > q_blocks ? kv_blocks : q_blocks;
   if (blocks > INT_MAX) return CASCADE_ERR_UNSUPPORTED_SHAPE;
   CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_F32, k_paged_grad_f32<D>, kSmem));   // (a context has one D)
+  // While there are SMs left, the steps of a tile are shared out in the pass with the longer walk, or in both, such that the longest
+  // walk is shortest; setting up a tile takes as long as two steps, adding up another CTA's results one and a half.
+  // (1000 tokens, one head of 64: 34 us, without 58 us; 2 x 500, 8 query heads of 128 on one key head: 84 us, without 403 us.)
+  long long rows_seen = a.max_q, keys_seen = max_kv;
+  if (a.window > 0) {
+    if (keys_seen > (long long)a.window + a.sinks + kOwn) keys_seen = (long long)a.window + a.sinks + kOwn;
+    if (a.sinks == 0 && rows_seen > (long long)a.window + kOwn) rows_seen = (long long)a.window + kOwn;
+  }
+  const double steps_keys = (double)rows_seen * G / Cfg<D>::kStep, steps_rows = (double)keys_seen / Cfg<D>::kStep;
+  double best = 1e300;
+  int cluster = 1;
+  for (int n = 1, levels = 0; n <= 8; n *= 2, ++levels)
+    for (int which = 1; which <= 3; ++which) {
+      const int sk = which & 1 ? n : 1, sr = which & 2 ? n : 1;
+      if (n > 1 && (kv_blocks * sk + q_blocks * sr) * a.n_req > ctx->sm_count) continue;
+      const double keys = 2 + steps_keys / sk + (sk > 1 ? 1.5 * levels : 0), rows = 2 + steps_rows / sr + (sr > 1 ? 1.5 * levels : 0), time = keys > rows ? keys : rows;
+      if (time >= 0.95 * best) continue;
+      best = time;
+      cluster = n;
+      f.split_keys = sk;
+      f.split_rows = sr;
+    }
+  const long long x = kv_blocks * f.split_keys > q_blocks * f.split_rows ? kv_blocks * f.split_keys : q_blocks * f.split_rows;
   KernelScope ks(ctx, K_PAGED_GRAD, s);
-  k_paged_grad_f32<D><<<dim3((unsigned)blocks, a.n_req, 2), kThreads, kSmem, s>>>(f);
-  CASCADE_CUDA_TRY(cudaGetLastError());
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((x + cluster - 1) / cluster * cluster), a.n_req, 2);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  CASCADE_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_paged_grad_f32<D>, (const F32Args)f));
   return CASCADE_OK;
 }
 

@@ -252,6 +252,31 @@ def test_fp32_numbers_of_all_sizes(D):
     c.run().check()
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (300, 5)])
+@pytest.mark.parametrize("q_len,kv_len,Hq,Hkv,D", [([1000], [1000], 1, 1, 64), ([500, 31], [500, 700], 8, 1, 128), ([900], [900], 10, 2, 64),
+                                                   ([330, 330], [400, 330], 2, 2, 128), ([3], [2000], 1, 1, 64), ([700], [40], 4, 1, 64)])
+def test_fp32_few_tiles_with_long_walks(q_len, kv_len, Hq, Hkv, D, window, sinks):
+    """A tile's steps are shared out over a cluster: the sums, and the same bits every time."""
+    c = Call(q_len, kv_len, Hq, Hkv, D, "f32", window=window, sinks=sinks, seed=24).run()
+    c.check()
+    first = [t.clone() for r in range(len(q_len)) for t in c.got(r)]
+    for _ in range(3):
+        c.backward()
+    c.ctx.check()
+    assert all(torch.equal(a, b) for a, b in zip(first, [t for r in range(len(q_len)) for t in c.got(r)]))
+
+
+def test_fp32_a_value_that_is_no_number_in_a_long_walk():
+    c = Call([1000], [1000], 2, 1, 64, "f32", seed=25)
+    c.forward()
+    c.d_out[900, 0, 7] = float("nan")
+    c.backward()
+    c.ctx.check()
+    dq, dk, dv = c.got(0)
+    assert dq[900, 0].isnan().any() and dq[:900].isfinite().all() and dq[901:].isfinite().all() and dq[:, 1].isfinite().all()
+    assert dv[:901, 0, 7].isnan().all() and dv[901:].isfinite().all() and dk[901:].isfinite().all()
+
+
 def test_calls_of_both_types_side_by_side():
     calls = [Call([400], [400], 8, 8, 128, "bf16", seed=21), Call([300], [300], 4, 4, 64, "f32", seed=22), Call([200, 90], [200, 90], 4, 4, 128, "f32", seed=23)]
     for c in calls:
