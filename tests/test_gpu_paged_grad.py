@@ -417,6 +417,23 @@ def test_requests_outside_what_was_given_are_left_out(dtype):
     spoiled(rows_of_the_pass)
 
 
+@pytest.mark.parametrize("q_len,H,D,dtype", [([90, 200], 4, 128, "f32"), ([1000], 1, 64, "f32"), ([90, 200], 4, 64, "bf16")])
+def test_a_context_whose_first_call_is_recorded(q_len, H, D, dtype):
+    c = Call(q_len, q_len, H, H, D, dtype, seed=26)
+    c.forward()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.backward()
+    graph.replay()
+    torch.cuda.synchronize()
+    c.ctx.check()
+    c.check()
+    first = [t.clone() for r in range(len(q_len)) for t in c.got(r)]
+    c.backward()
+    assert all(torch.equal(a, b) for a, b in zip(first, [t for r in range(len(q_len)) for t in c.got(r)]))
+
+
 def test_recorded_and_replayed_on_another_stream():
     c = Call([90, 200], [90, 200], 4, 4, 128, seed=12)
     c.forward()
