@@ -11,6 +11,9 @@
 //     product that frees a stage) and output gradients through two;
 //   * warp 9 issues the products;  warp 10 brings the rows' statistics;
 //   * warps 0-7: a key per lane, half of a block's rows each; P stays in registers between the two halves of the work.
+//
+// Few items with many row blocks (many query heads on one key head) are shared out: a cluster of `split` CTAs takes an item, a stretch of
+// its blocks each, and adds up its results by pairs, pairs of pairs and so on, in the tensor memory of the first.
 #pragma once
 #include <climits>
 
@@ -24,6 +27,48 @@ struct SharedKv {
   Queue queue;
   __align__(16) float lse[2][kTile], delta[2][kTile];                  // negated
 };
+
+// The results `acc` (a lane's columns in tensor memory; none yet: zeros) of a cluster's CTAs added up by pairs, by way of the tiles'
+// place.  (A function of its own: beside the rest it costs registers.)
+template <int D>
+__device__ __noinline__ void join(uint32_t acc, uint32_t base, uint32_t place, int split, int rank, bool any) {
+#pragma unroll 1
+  for (int m = 1; m < split; m *= 2) {
+    cluster_meet();                                                    // everywhere the products are done with the tiles
+    if (rank % (2 * m) == m) {
+      const uint32_t to = ptx::map_to_cta(base, rank - m) + place;
+#pragma unroll 1
+      for (int q = 0; q < D / 32; ++q) {
+        uint32_t v[32];
+        load32(acc + 32 * q, v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          auto z = [&](int e) { return any ? __uint_as_float(v[4 * k + e]) : 0.f; };
+          ptx::st_cluster_v4(to + (q * 8 + k) * (kTile * 16), make_float4(z(0), z(1), z(2), z(3)));
+        }
+      }
+    }
+    cluster_meet();
+    if (rank % (2 * m) == 0) {
+#pragma unroll 1
+      for (int q = 0; q < D / 32; ++q) {
+        uint32_t v[32];
+        load32(acc + 32 * q, v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          uint32_t z[4];
+          ld_shared_v4(base + place + (q * 8 + k) * (kTile * 16), z);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[4 * k + e] = __float_as_uint((any ? __uint_as_float(v[4 * k + e]) : 0.f) + __uint_as_float(z[e]));
+        }
+        ptx::tmem_st16_async(acc + 32 * q, v);
+        ptx::tmem_st16_async(acc + 32 * q + 16, v + 16);
+        ptx::tmem_wait_st();
+      }
+      any = true;
+    }
+  }
+}
 
 // The whole CTA; `cta` of `n_cta` that begin with this pass, the others (cta >= n_cta) take what its counter hands out.
 template <int D>
@@ -62,6 +107,8 @@ __device__ __forceinline__ void pass_kv(const CUtensorMap& tm_q, const CUtensorM
   __syncthreads();
   const uint32_t t_s = tmem, t_dp = t_s + 128, t_dv = t_s + 256, t_dk = t_dv + D;
 
+  const int rank = blockIdx.x % p.split;
+  bool joined = p.split == 1;
   Turns turns;
   uint32_t used = 0, blk = 0;                                          // items with blocks, and blocks, so far
   Ring<3> ring;                                                        // the queries' stages
@@ -74,11 +121,17 @@ __device__ __forceinline__ void pass_kv(const CUtensorMap& tm_q, const CUtensorM
     Item it = {};
     for (int item = cta < n_cta ? cta : INT_MIN;;) {
       if (item == INT_MIN) item = __shfl_sync(0xffffffffu, lane == 0 ? n_cta + atomicAdd(taken, 1) : 0, 0);
-      const bool more = cur.find(p, item, lane, &it);
+      // (a cluster has one item, whatever the requests' ranges)
+      const bool more = cur.find(p, item, lane, &it) && (p.split == 1 || item < n_cta);
       int lo, hi;                                                      // tokens that see any of the keys -> row blocks
       paged::tokens_that_see(a, it.kv - it.nq, it.nq, it.line * kTile, min(it.kv, (it.line + 1) * kTile) - 1, &lo, &hi);
       it.first = lo / p.tpb;
       it.n = !more ? -1 : hi > lo ? (hi - 1) / p.tpb - it.first + 1 : 0;
+      if (p.split > 1 && more) {
+        const int each = (it.n + p.split - 1) / p.split, skip = min(it.n, rank * each);
+        it.first += skip;
+        it.n = min(it.n - skip, each);
+      }
       if (!turns.tell(sh.queue, wait, it, lane, &ok) || !more) break;
       const int granted = lane == 0 ? n_cta + atomicAdd(taken, 1) : 0;
       auto load_rows = [&](int i, const CUtensorMap* m, uint64_t* full, uint64_t* empty, uint32_t ph, int to) {
@@ -306,6 +359,15 @@ __device__ __forceinline__ void pass_kv(const CUtensorMap& tm_q, const CUtensorM
         ++used;
         blk += n;
       }
+      if (p.split > 1) {
+        joined = true;
+        join<D>((part == 0 ? t_dv : t_dk) + lane_addr, base, (part * (D / 32) * 8 * kTile + key) * 16, p.split, rank, n > 0);
+        if (rank != 0) {
+          turns.done(sh.queue, lane);
+          continue;
+        }
+        n = 1;
+      }
       const Item it = turns.item(sh.queue);
       const int j = it.line * kTile + key;
       const int page = j < it.kv ? a.block_table[(size_t)it.r * a.table_stride + j / a.page_size] : 0;
@@ -347,6 +409,8 @@ __device__ __forceinline__ void pass_kv(const CUtensorMap& tm_q, const CUtensorM
       turns.done(sh.queue, lane);
     }
   }
+  if (warp >= kComputeWarps || !joined)
+    for (int m = 1; m < p.split; m *= 2) cluster_meet(), cluster_meet();
   __syncwarp();
   if (*wait.abort_flag) __nanosleep(1000000);                          // copies still in flight
   ptx::tc_fence_before();

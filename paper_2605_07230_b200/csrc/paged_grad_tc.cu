@@ -54,9 +54,9 @@ k_paged_grad_tc(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
 #pragma unroll 1
   for (int k = 0; k < (p.both ? 2 : 1) && !*wait.abort_flag; ++k) {
     const bool keys = keys_first == (k == 0);
-    const int cta = k != 0 ? INT_MAX : keys ? (int)blockIdx.x : (int)blockIdx.x - p.n_cta_keys;
+    const int cta = k != 0 ? INT_MAX : keys ? (int)blockIdx.x / p.split : (int)blockIdx.x - p.n_cta_keys;
     if (keys)
-      pass_kv<D>(tm_q, tm_do, tm_k, tm_v, p, smem, base, tmem, wait, cta, p.n_cta_keys);
+      pass_kv<D>(tm_q, tm_do, tm_k, tm_v, p, smem, base, tmem, wait, cta, p.n_cta_keys / p.split);
     else
       pass_q<D>(tm_q, tm_do, tm_k, tm_v, p, smem, base, tmem, wait, cta, n_q);
   }
@@ -73,8 +73,18 @@ int launch(cascade_ctx* ctx, const Args& p, int grid, cudaStream_t s) {
     return CASCADE_ERR_CUDA;
   CASCADE_TRY(configure_smem(ctx, PAGED_CFG_GRAD_TC, k_paged_grad_tc<D>, kSmem<D>));   // (a context has one D)
   KernelScope ks(ctx, K_PAGED_GRAD, s);
-  k_paged_grad_tc<D><<<grid, kThreads, kSmem<D>, s>>>(mq, mo, *mk, *mv, p);
-  CASCADE_CUDA_TRY(cudaGetLastError());
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem<D>;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = p.split;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  CASCADE_CUDA_TRY(cudaLaunchKernelEx(&cfg, k_paged_grad_tc<D>, mq, mo, *mk, *mv, p));
   return CASCADE_OK;
 }
 
@@ -100,19 +110,40 @@ int launch_paged_grad_tc(cascade_ctx* ctx, const PagedGradArgs& g, cudaStream_t 
   // All items at once if there are no more than SMs; else the SMs in proportion to the passes' time: thousands of cycles an item and
   // a step, of which there are as many in both, estimated from the requests' mean lengths.  (2 x 640 tokens, 32 heads of 128: 64 us; by
   // 41 : 29 an item, which is right for long rows alone, 67 us.)
+  const bool wide = ctx->shape.D == 128;
+  double seen = ((double)g.n_kv - 0.5 * a.n_tok) / a.n_req;            // keys that a row sees
+  if (a.window > 0 && seen > (double)a.window + a.sinks) seen = (double)a.window + a.sinks;
+  const double steps = (seen > 0 ? seen / kTile + 0.5 : 0.5) * rows, item_keys = wide ? 7 : 4, item_rows = wide ? 8.8 : 4.2;
+  const double time_keys = item_keys * (double)keys + 4.05 * steps, time_rows = item_rows * (double)rows + 2.9 * steps;
   if (keys + rows <= sms) {
     p.n_cta_keys = (int)keys;
   } else {
-    const bool wide = ctx->shape.D == 128;
-    double seen = ((double)g.n_kv - 0.5 * a.n_tok) / a.n_req;          // keys that a row sees
-    if (a.window > 0 && seen > (double)a.window + a.sinks) seen = (double)a.window + a.sinks;
-    const double steps = (seen > 0 ? seen / kTile + 0.5 : 0.5) * rows;
-    const double time_keys = (wide ? 7 : 4) * (double)keys + 4.05 * steps, time_rows = (wide ? 8.8 : 4.2) * (double)rows + 2.9 * steps;
     const long long share = (long long)(sms * time_keys / (time_keys + time_rows) + 0.5), most = keys < sms - 1 ? keys : sms - 1;
     p.n_cta_keys = (int)(keys == 0 ? 0 : share < 1 ? 1 : share > most ? most : share);
   }
+  // Few tiles of keys with many row blocks each: the blocks of a tile are shared out where that shortens the longest walk or wait by a
+  // tenth.  Adding up another CTA's results takes 16 (D = 64: 8) thousand cycles.  (2 x 500 tokens, 8 query heads of 128 on one key
+  // head: 40 us, without 74 us; 2000 tokens, 8 heads of 64 on one: 68 us, without 198 us.)
+  p.split = 1;
+  if (keys > 0) {
+    double blocks = (double)((a.max_q + p.tpb - 1) / p.tpb);
+    if (a.window > 0 && a.sinks == 0 && blocks > ((double)a.window + kTile) / p.tpb + 1) blocks = ((double)a.window + kTile) / p.tpb + 1;
+    const double row_item = item_rows + 2.9 * (a.window > 0 && (double)a.max_kv > (double)a.window + a.sinks ? ((double)a.window + a.sinks) / kTile + 1
+                                                                                                             : (double)a.max_kv / kTile);
+    auto longest = [](double x, double y) { return x > y ? x : y; };
+    double best = 0.9 * longest(longest(item_keys + 4.05 * blocks, row_item), (time_keys + time_rows) / sms);
+    for (int n = 2, levels = 1; n <= 8 && keys * n < sms; n *= 2, ++levels) {
+      const long long for_rows = rows < sms - keys * n ? rows : sms - keys * n;
+      const double time = longest(longest(item_keys + 4.05 * blocks / n + levels * (wide ? 16 : 8), row_item), time_rows / for_rows);
+      if (time >= best) continue;
+      best = time;
+      p.split = n;
+      p.n_cta_keys = (int)keys * n;
+    }
+  }
   const long long left = sms - p.n_cta_keys;
-  const int grid = p.n_cta_keys + (int)(rows < left ? rows : left);
-  p.both = keys + rows > 4 * sms;
+  int grid = p.n_cta_keys + (int)(rows < left ? rows : left);
+  grid = (grid + p.split - 1) / p.split * p.split;                     // (whole clusters; the last ones may find no rows)
+  p.both = p.split == 1 && keys + rows > 4 * sms;
   return ctx->shape.D == 128 ? launch<128>(ctx, p, grid, s) : launch<64>(ctx, p, grid, s);
 }

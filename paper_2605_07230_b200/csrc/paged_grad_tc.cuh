@@ -43,6 +43,7 @@ struct Args {
   PagedGradArgs g;
   int G, tpb, box_rows;           // query heads a key head; tokens per row block; rows of a page box
   int n_cta_keys;                 // CTAs that begin with the keys' pass
+  int split;                      // of them (a cluster) share the row blocks of an item
   bool both;                      // a CTA whose pass has no more items goes on with the other
   int* taken;                     // items of either pass handed out beyond the CTAs' own, CTAs that are done; zero between launches
 };
@@ -59,6 +60,12 @@ struct Queue {
   Item item[kSlots];
   uint64_t full[kSlots], empty[kSlots];
 };
+
+__device__ __forceinline__ void cluster_meet() {
+  __syncwarp();
+  ptx::cluster_arrive();
+  ptx::cluster_wait();
+}
 
 // A waiting warp's view of the CTA: where waits give up.
 struct Waits {

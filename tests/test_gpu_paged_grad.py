@@ -254,10 +254,12 @@ def test_fp32_numbers_of_all_sizes(D):
 
 @pytest.mark.parametrize("window,sinks", [(0, 0), (300, 5)])
 @pytest.mark.parametrize("q_len,kv_len,Hq,Hkv,D", [([1000], [1000], 1, 1, 64), ([500, 31], [500, 700], 8, 1, 128), ([900], [900], 10, 2, 64),
-                                                   ([330, 330], [400, 330], 2, 2, 128), ([3], [2000], 1, 1, 64), ([700], [40], 4, 1, 64)])
-def test_fp32_few_tiles_with_long_walks(q_len, kv_len, Hq, Hkv, D, window, sinks):
+                                                   ([330, 330], [400, 330], 2, 2, 128), ([3], [2000], 1, 1, 64), ([700], [40], 4, 1, 64),
+                                                   ([2000], [2000], 8, 1, 64), ([300, 0, 260], [310, 0, 290], 32, 1, 128)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_few_tiles_with_long_walks(q_len, kv_len, Hq, Hkv, D, window, sinks, dtype):
     """A tile's steps are shared out over a cluster: the sums, and the same bits every time."""
-    c = Call(q_len, kv_len, Hq, Hkv, D, "f32", window=window, sinks=sinks, seed=24).run()
+    c = Call(q_len, kv_len, Hq, Hkv, D, dtype, window=window, sinks=sinks, seed=24).run()
     c.check()
     first = [t.clone() for r in range(len(q_len)) for t in c.got(r)]
     for _ in range(3):
@@ -266,8 +268,9 @@ def test_fp32_few_tiles_with_long_walks(q_len, kv_len, Hq, Hkv, D, window, sinks
     assert all(torch.equal(a, b) for a, b in zip(first, [t for r in range(len(q_len)) for t in c.got(r)]))
 
 
-def test_fp32_a_value_that_is_no_number_in_a_long_walk():
-    c = Call([1000], [1000], 2, 1, 64, "f32", seed=25)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_value_that_is_no_number_in_a_long_walk(dtype):
+    c = Call([1000], [1000], 8, 1, 64, dtype, seed=25)
     c.forward()
     c.d_out[900, 0, 7] = float("nan")
     c.backward()
