@@ -7,8 +7,8 @@
 // with m the row's maximum, Z = sum_v exp((d_v - m) / T), Q = sum_i q_i.
 //
 // Both are memory-bound and walk over a row once.  The loss looks the drafter's logits of the stored tokens up behind the row, from the
-// L2.  (In front of it 292 to 322 us for 4608 rows of 65536 where this takes 262, since memory gives 64 bytes for 4; from shared memory,
-// as the gradient does it, 494 us: too much work an element.)  The gradient goes in stretches: the stored entries that fall into one
+// L1 or L2.  (In front of it 292 to 322 us for 4608 rows of 65536 where this takes 245, since memory gives 64 bytes for 4; from shared
+// memory, as the gradient does it, 494 us: too much work an element.)  The gradient goes in stretches: the stored entries that fall into one
 // go into shared memory at their tokens' places, then the logits, already requested, are worked on beside them.
 #include "cascade_internal.h"
 #include "ptx_paged.cuh"
@@ -506,8 +506,8 @@ int launch_loss(const LossArgs& in, cudaStream_t s) {
   if ((long long)a.K * a.splits > INT32_MAX) return CASCADE_ERR_UNSUPPORTED_SHAPE;
   // Many parts take 128 threads, more of them being on an SM at once (1153 bf16 rows of 10007, 333 entries: 14.4 us, 256 threads
   // 18.4 us), unless there are more stored entries than they hold in registers and the part is long: the logits of the entries
-  // should still be in the L2 at its end, so that fewer rows are to be under way (4608 rows of 262144 bytes, 2000 entries: 512 threads
-  // 261 us, 256 303 us, 128 344 us; 1000 entries: 249, 244, 264 us).  A few hundred rows leave room for 256 (300 rows of 65536, 400
+  // should still be in the L1 or L2 at its end, so that fewer rows are to be under way (4608 rows of 262144 bytes, 2000 entries: 512
+  // threads 245 us, 256 295 us, 128 334 us; 1000 entries, by loads past the L1: 249, 244, 264 us).  A few hundred rows leave room for 256 (300 rows of 65536, 400
   // entries: 20 us, 128 threads 23 us).
   const long long part = bytes / a.splits;
   const int n = (a.n + a.splits - 1) / a.splits;
