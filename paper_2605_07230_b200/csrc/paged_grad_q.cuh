@@ -333,7 +333,8 @@ __device__ __forceinline__ void pass_q(const CUtensorMap& tm_q, const CUtensorMa
       ok = __all_sync(0xffffffffu, turns.next_is_told(sh.queue, wait));
       if (!ok) break;
       const bool lost = static_cast<const volatile Item&>(turns.item(sh.queue)).lost;
-      const bool odd = live && x >= 0 && (!finite || lost);
+      // (rows that see no key too: beside a key that holds no number their zeros became none)
+      const bool odd = live && (!finite || lost);
       // (0.6 us a key and row: whoever waits meanwhile starts its limit anew; each warp sees to its half of the row's elements)
       for (uint32_t again = __ballot_sync(0xffffffffu, odd); again != 0u; again &= again - 1u) {
         const int who = __ffs(again) - 1;
