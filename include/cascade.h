@@ -578,7 +578,8 @@ int cascade_drafter_loss(const float* target_logits, const float* draft_logits, 
  *   draft_logits [K,V] float (logits_dtype CASCADE_F32) or bf16 (CASCADE_BF16), rows row_stride elements apart (>= V, at most
  *     2^40), aligned to the element; V, n_top <= 2^31 - 65536 (CASCADE_ERR_UNSUPPORTED_SHAPE)
  *   top_logits [K,n_top] float, top_ids [K,n_top] int32: in any order; an id outside [0,V) marks a place without an entry, a
- *     token given more than once adds up.  A position none of whose entries weighs anything has loss and gradient 0.
+ *     token given more than once adds up.  An entry less than 2^-126 of the largest (target_lse: of 1) weighs nothing, whatever the
+ *     drafter's logit of its token.  A position none of whose entries weighs anything has loss and gradient 0.
  *   saved_out [K,4] float, 16-byte aligned: log-sum-exp of d / T, that of the target, Q_k, w_k: what the gradient needs
  *   total_out [1] float or NULL: sum of loss_out, in a fixed order
  *   grad_loss [K] float or NULL (1); scale: finite

@@ -199,6 +199,12 @@ __device__ __forceinline__ Soft warp_join(Soft s, float c, int lanes) {
   for (int o = lanes / 2; o > 0; o >>= 1) s = join(s, {__shfl_xor_sync(0xffffffffu, s.m, o), __shfl_xor_sync(0xffffffffu, s.z, o)}, c);
   return s;
 }
+// The largest of `lanes` values that are -inf as a rule.
+__device__ __forceinline__ float most_left_out(float x, int lanes) {
+  if (__any_sync(0xffffffffu, x != -INFINITY))
+    for (int o = lanes / 2; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
 template <int kThreads>
 __device__ __forceinline__ float block_max(float x, float* red) {
   constexpr int kWarps = kThreads / 32;
@@ -227,7 +233,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_distill_loss(cons
   __shared__ float s_max[kWarps];
   __shared__ Soft s_warp[kWarps];
   __shared__ double s_sum[kWarps][5];
-  __shared__ __align__(16) float4 s_soft[kMaxSplits];      // (m, Z, largest stored logit) of every CTA of the row
+  __shared__ float s_out[kWarps];
+  __shared__ __align__(16) float4 s_soft[kMaxSplits];      // (m, Z, largest stored logit, largest left out) of every CTA of the row
   __shared__ double s_part[kMaxSplits][5];                 // its sums: q d, q, and the three of the cosine
   asm volatile("griddepcontrol.launch_dependents;");       // (the kernel that adds the losses up waits for this one's end itself)
   const int row = blockIdx.x / a.splits, rank = blockIdx.x % a.splits, tid = threadIdx.x;
@@ -310,12 +317,17 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_distill_loss(cons
     stored.each_more([&](int, float t) { most = fmaxf(most, t); });
     most = block_max<kThreads>(most, s_max);
   }
-  // sums over the entries (64 bits: few of them, and maximum times weight less weight times logit cancels)
+  // sums over the entries (64 bits: few of them, and maximum times weight less weight times logit cancels); of the entries whose token
+  // the drafter leaves out (-inf) the largest logit: whether it weighs anything goes by the largest of the whole row
+  auto weight = [&](float t, float ref) { return given ? ptx::ex2(fmaf(t, inv_t, -t_lse) * kLog2e) : scaled(t, ref, c); };
   const float ref_t = reference(most, c);
+  float left_out = -INFINITY;
   auto entry = [&](float t, float y) {
-    const float q = given ? ptx::ex2(fmaf(t, inv_t, -t_lse) * kLog2e) : scaled(t, ref_t, c);
+    const float q = weight(t, ref_t);
     if (q != 0.f) {                                        // (a token that weighs nothing may have -inf)
-      sum[0] += (double)q * (double)y;
+      const bool out = y == -INFINITY;
+      left_out = fmaxf(left_out, out ? t : -INFINITY);
+      sum[0] += (double)q * (double)(out ? 0.f : y);
       sum[1] += (double)q;
     }
   };
@@ -324,11 +336,13 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_distill_loss(cons
     if (stored.token[k] >= 0) entry(stored.value[k], dv[k]);
   stored.each_more([&](int v, float t) { entry(t, to_float(d[v])); });
   sd = warp_join(sd, c, 32);
+  left_out = most_left_out(left_out, 32);
 #pragma unroll
   for (int i = 0; i < 5; ++i)
     for (int o = 16; o > 0; o >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
   if ((tid & 31) == 0) {
     s_warp[tid >> 5] = sd;
+    s_out[tid >> 5] = left_out;
 #pragma unroll
     for (int i = 0; i < 5; ++i) s_sum[tid >> 5][i] = sum[i];
   }
@@ -336,6 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_distill_loss(cons
   if (a.splits > 1) ptx::cluster_wait();                   // all CTAs have started
   if (tid < 32) {
     sd = warp_join(s_warp[tid & (kWarps - 1)], c, kWarps);
+    left_out = most_left_out(s_out[tid & (kWarps - 1)], kWarps);
     const uint32_t to = a.splits > 1 ? ptx::map_to_cta(ptx::smem_u32(&s_part[rank][tid < 5 ? tid : 0]), 0) : ptx::smem_u32(&s_part[0][tid < 5 ? tid : 0]);
     if (tid < 5) {
       double y = 0.0;
@@ -344,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_distill_loss(cons
       asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to), "d"(y) : "memory");
     }
     if (tid == 5)
-      ptx::st_cluster_v4(a.splits > 1 ? ptx::map_to_cta(ptx::smem_u32(&s_soft[rank]), 0) : ptx::smem_u32(&s_soft[0]), make_float4(sd.m, sd.z, most, 0.f));
+      ptx::st_cluster_v4(a.splits > 1 ? ptx::map_to_cta(ptx::smem_u32(&s_soft[rank]), 0) : ptx::smem_u32(&s_soft[0]), make_float4(sd.m, sd.z, most, left_out));
     __syncwarp();
   }
   if (a.splits > 1) {
@@ -355,7 +370,11 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_distill_loss(cons
   if (rank == 0 && tid == 0) {
     double y[5] = {0.0, 0.0, 0.0, 0.0, 0.0};
     most = s_soft[0].z;
-    for (int s = 1; s < a.splits; ++s) most = fmaxf(most, s_soft[s].z);
+    left_out = s_soft[0].w;
+    for (int s = 1; s < a.splits; ++s) {
+      most = fmaxf(most, s_soft[s].z);
+      left_out = fmaxf(left_out, s_soft[s].w);
+    }
     for (int s = 0; s < a.splits; ++s) {
       const float4 x = s_soft[s];
       sd = s == 0 ? Soft{x.x, x.y} : join(sd, {x.x, x.y}, c);
@@ -363,6 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_distill_loss(cons
       const double by = given || a.splits == 1 || x.z == -INFINITY ? 1.0 : (double)exp2f(reference(x.z, c) - reference(most, c));
       for (int i = 0; i < 5; ++i) y[i] += i < 2 ? by * s_part[s][i] : s_part[s][i];
     }
+    if (left_out != -INFINITY && weight(left_out, reference(most, c)) != 0.f) y[0] = -INFINITY;
     // cosine >= tau, squared with its sign
     const double bound = (double)a.tau * fabs((double)a.tau) * (y[3] * y[4]);
     const float w = pair && y[3] * y[4] > 0.0 && y[2] * fabs(y[2]) >= bound ? a.raised : 1.f;

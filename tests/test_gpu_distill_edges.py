@@ -1,0 +1,52 @@
+"""GPU: the loss from stored logits and its gradient where weights vanish and values are no numbers."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import train_oracle as TO
+from tests import gpu_util as G
+from tests.test_gpu_distill import Step, check_grad, check_loss, dev, make
+
+pytestmark = pytest.mark.gpu
+
+FEW, MANY = 3, 700                                                   # rows shared out over several blocks, and a block each
+
+
+def falling(rng, K, V, n, T, gap):
+    """Rows whose stored logits fall from entry to entry, the last of them `gap` (over T) below the first; the drafter leaves the
+    last one's token out."""
+    ids = np.stack([rng.permutation(V)[:n] for _ in range(K)]).astype(np.int32)
+    top = np.repeat((-np.linspace(0, 1, n) ** 3 * gap * T).astype(np.float32)[None], K, 0)
+    draft = rng.normal(0, 2 * T, (K, V)).astype(np.float32)
+    draft[np.arange(K), ids[:, -1]] = -np.inf
+    return draft, top, ids
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("K", [FEW, MANY])
+@pytest.mark.parametrize("T", [0.05, 1.0])
+@pytest.mark.parametrize("V,n", [(16384, 64), (16384, 2000), (40001, 9)])
+def test_an_entry_without_weight_at_a_logit_of_minus_infinity(V, n, T, K, dtype):
+    """The gap lies past what 64 bits hold: the entry weighs nothing by any count."""
+    draft, top, ids = falling(np.random.default_rng(n), K, V, n, T, 900.0)
+    s = Step(draft, top, ids, dtype, temperature=T)
+    s.forward()
+    with np.errstate(invalid="ignore"):
+        check_loss(s, TO.distill_loss(s.host, top, ids, temperature=T), T)
+    assert s.loss.isfinite().all() and s.total.isfinite().all()
+
+
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("gap", [70.0, 84.0, 90.0, 140.0, 200.0])
+def test_which_entries_weigh_something_does_not_depend_on_the_number_of_rows(gap, given):
+    """Weights of 2^-101 and 2^-121, and what lies below 2^-126 and counts as none."""
+    V, n, T = 16384, 64, 1.0
+    draft, top, ids = falling(np.random.default_rng(5), MANY, V, n, T, gap)
+    lse = np.full(MANY, np.log(np.exp(top[0].astype(np.float64)).sum()), np.float32) if given else None
+    losses = []
+    for K in (FEW, MANY):
+        s = Step(draft[:K], top[:K], ids[:K], target_lse=None if lse is None else lse[:K])
+        s.forward()
+        losses.append(s.loss[:FEW].cpu().numpy())
+    weighs = gap < 87                                                # 126 ln 2 = 87.3, with the log-sum-exp (2.6) in front or not
+    assert not np.isnan(losses).any() and (np.isinf(losses) == weighs).all(), losses
