@@ -579,14 +579,15 @@ int cascade_drafter_loss(const float* target_logits, const float* draft_logits, 
  *     2^40), aligned to the element; V, n_top <= 2^31 - 65536 (CASCADE_ERR_UNSUPPORTED_SHAPE)
  *   top_logits [K,n_top] float, top_ids [K,n_top] int32: in any order; an id outside [0,V) marks a place without an entry, a
  *     token given more than once adds up.  An entry less than 2^-126 of the largest (target_lse: of 1) weighs nothing, whatever the
- *     drafter's logit of its token.  A position none of whose entries weighs anything has loss and gradient 0.
+ *     drafter's logit of its token.  A position none of whose entries weighs anything has loss and gradient 0,
+ *     whatever its logits hold.
  *   saved_out [K,4] float, 16-byte aligned: log-sum-exp of d / T, that of the target, Q_k, w_k: what the gradient needs
  *   total_out [1] float or NULL: sum of loss_out, in a fixed order
  *   grad_loss [K] float or NULL (1); scale: finite
  *   grad_out [K,V] of the logits' type, rows grad_stride apart; may be draft_logits itself (same stride): the gradient then
  *     replaces the logits.  Where scale * grad_loss[k] * w_k is 0 the row is zeros.  But for that no output overlaps another or
  *     an input (CASCADE_ERR_INVALID_ARG).
- * A logit that is no number, or +inf, makes its position's loss and gradient NaN; one of -inf has p = 0.
+ * Elsewhere a logit that is no number, or +inf, makes its position's loss and gradient NaN; one of -inf has p = 0.
  * Sums and statistics are 32 bits (the sums over stored entries and of the cosine 64); a bf16 gradient is rounded once.
  * The same call leaves the same bits every time.  No context is needed and nothing is allocated; one kernel each, and one for
  * total_out.  Errors: CASCADE_ERR_INVALID_ARG (null pointers, sizes < 1, 1e-30 <= temperature <= 1e30 not met, c <= 0, NaN

@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_distill_grad(cons
   load_stretch<E, kThreads>(d, r.lead, aligned, first, last, raw);
   Stored<kThreads> stored(a.top + (long long)row * a.n, a.ids + (long long)row * a.n, a.n, a.V);
   const float f = saved.w * up * a.scale * inv_t;
-  if (f == 0.f) {                                          // padding: zeros, whatever the row holds
+  if (f == 0.f || saved.z == 0.f) {                        // padding, or no entry weighs anything: zeros, whatever the row holds
     for (int p = first + tid; p < last; p += kThreads) to[p] = make_uint4(0, 0, 0, 0);
     if (edge < a.V) from_float(g + edge, 0.f);
     return;

@@ -50,3 +50,20 @@ def test_which_entries_weigh_something_does_not_depend_on_the_number_of_rows(gap
         losses.append(s.loss[:FEW].cpu().numpy())
     weighs = gap < 87                                                # 126 ln 2 = 87.3, with the log-sum-exp (2.6) in front or not
     assert not np.isnan(losses).any() and (np.isinf(losses) == weighs).all(), losses
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [500, 65536])
+def test_a_position_without_weight_has_a_gradient_of_zeros_whatever_its_logits_hold(V, dtype):
+    K, n = 5, 50
+    _, draft, top, ids, _, _ = make(21, K, V, n)
+    ids[0], top[1], ids[2] = -1, -np.inf, V
+    draft[0, 7], draft[1, V - 1], draft[2, 3], draft[3, 4] = np.nan, np.inf, -np.inf, np.nan
+    s = Step(draft, top, ids, dtype)
+    s.forward()
+    assert not s.loss[:3].any() and s.loss[3].isnan() and s.loss[4] > 0
+    s.backward()
+    assert not s.grad[:3].any() and not s.grad[:3].isnan().any() and s.grad[3].isnan().all()
+    check_grad_row = TO.distill_grad(s.host[4:], top[4:], ids[4:], s.saved[4:].cpu().numpy())
+    # p and q are off by at most 2^-18 here (exponents of at most 30 with two roundings), and rounded once
+    assert np.abs(s.grad[4:].float().cpu().numpy() - check_grad_row).max() <= np.abs(check_grad_row).max() * (2.0**-8 + 2.0**-18)
