@@ -574,13 +574,13 @@ int cascade_drafter_loss(const float* target_logits, const float* draft_logits, 
  *     grad_out[k] = scale * grad_loss[k] * w_k / T * (Q_k p - sum_i q_i e_(id_i)),   Q_k = sum_i q_i
  * w_k = c where feat[k] and feat[k+1] converge (cosine >= tau_seq) and belong to one sequence, else 1; feat NULL: 1 everywhere.
  * seq [K] int32 or NULL (one sequence): the sequence a position belongs to; negative: padding, whose loss, gradient and saved
- * row are zeros whatever its logits hold.
+ * row are zeros whatever its logits and its grad_loss hold.
  *   draft_logits [K,V] float (logits_dtype CASCADE_F32) or bf16 (CASCADE_BF16), rows row_stride elements apart (>= V, at most
  *     2^40), aligned to the element; V, n_top <= 2^31 - 65536 (CASCADE_ERR_UNSUPPORTED_SHAPE)
  *   top_logits [K,n_top] float, top_ids [K,n_top] int32: in any order; an id outside [0,V) marks a place without an entry, a
- *     token given more than once adds up.  An entry less than 2^-126 of the largest (target_lse: of 1) weighs nothing, whatever the
- *     drafter's logit of its token.  A position none of whose entries weighs anything has loss and gradient 0,
- *     whatever its logits hold.
+ *     token given more than once adds up.  An entry that would weigh less than 2^-126 of the largest (with target_lse: of 1) weighs
+ *     nothing, whatever the drafter's logit of its token.  A position none of whose entries weighs anything has loss and
+ *     gradient 0, whatever its logits and its grad_loss hold.
  *   saved_out [K,4] float, 16-byte aligned: log-sum-exp of d / T, that of the target, Q_k, w_k: what the gradient needs
  *   total_out [1] float or NULL: sum of loss_out, in a fixed order
  *   grad_loss [K] float or NULL (1); scale: finite

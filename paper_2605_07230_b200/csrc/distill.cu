@@ -448,7 +448,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_distill_grad(cons
   load_stretch<E, kThreads>(d, r.lead, aligned, first, last, raw);
   Stored<kThreads> stored(a.top + (long long)row * a.n, a.ids + (long long)row * a.n, a.n, a.V);
   const float f = saved.w * up * a.scale * inv_t;
-  if (f == 0.f || saved.z == 0.f) {                        // padding, or no entry weighs anything: zeros, whatever the row holds
+  // padding, or no entry weighs anything: zeros, whatever the row holds and whatever comes back from above
+  if (f == 0.f || saved.w == 0.f || saved.z == 0.f) {
     for (int p = first + tid; p < last; p += kThreads) to[p] = make_uint4(0, 0, 0, 0);
     if (edge < a.V) from_float(g + edge, 0.f);
     return;

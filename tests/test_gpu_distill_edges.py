@@ -67,3 +67,21 @@ def test_a_position_without_weight_has_a_gradient_of_zeros_whatever_its_logits_h
     check_grad_row = TO.distill_grad(s.host[4:], top[4:], ids[4:], s.saved[4:].cpu().numpy())
     # p and q are off by at most 2^-18 here (exponents of at most 30 with two roundings), and rounded once
     assert np.abs(s.grad[4:].float().cpu().numpy() - check_grad_row).max() <= np.abs(check_grad_row).max() * (2.0**-8 + 2.0**-18)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("up", [np.nan, np.inf])
+def test_padding_has_a_gradient_of_zeros_whatever_comes_back_from_above(up, dtype):
+    K, V = 6, 3001
+    _, draft, top, ids, _, _ = make(22, K, V, 30)
+    draft[2] = np.nan
+    seq, back = np.array([0, 0, -1, -1, 1, 1]), np.array([1.0, 0.5, up, up, 2.0, up], np.float32)
+    s = Step(draft, top, ids, dtype, seq=seq)
+    s.forward()
+    s.backward(grad_loss=dev(back))
+    assert not s.grad[2:4].any() and not s.grad[2:4].isnan().any()
+    assert s.grad[[0, 1, 4]].isfinite().all() and not s.grad[5].isfinite().all()
+    whole = s.host, s.grad, s.top, s.ids
+    s.host, s.grad, s.top, s.ids = s.host[:2], s.grad[:2], s.top[:2], s.ids[:2]
+    check_grad(s, s.saved[:2].cpu().numpy(), back[:2], 1.0, dtype=dtype)
+    s.host, s.grad, s.top, s.ids = whole
