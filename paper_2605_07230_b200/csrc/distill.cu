@@ -383,9 +383,9 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_distill_loss(cons
       for (int i = 0; i < 5; ++i) y[i] += i < 2 ? by * s_part[s][i] : s_part[s][i];
     }
     if (left_out != -INFINITY && weight(left_out, reference(most, c)) != 0.f) y[0] = -INFINITY;
-    // cosine >= tau, squared with its sign
-    const double bound = (double)a.tau * fabs((double)a.tau) * (y[3] * y[4]);
-    const float w = pair && y[3] * y[4] > 0.0 && y[2] * fabs(y[2]) >= bound ? a.raised : 1.f;
+    // cosine >= tau, squared with its sign (zeros and infinities have no cosine)
+    const double squares = y[3] * y[4], bound = (double)a.tau * fabs((double)a.tau) * squares;
+    const float w = pair && squares > 0.0 && squares < (double)INFINITY && y[2] * fabs(y[2]) >= bound ? a.raised : 1.f;
     // log sum exp((d - m) / T): what c m was rounded by comes back
     const double log_z = (double)logf(sd.z) + ((double)reference(sd.m, c) - (double)sd.m * c) * (double)kLn2;
     const bool any = y[1] != 0.0;                          // something stored weighs something (or is no number)

@@ -85,3 +85,19 @@ def test_padding_has_a_gradient_of_zeros_whatever_comes_back_from_above(up, dtyp
     s.host, s.grad, s.top, s.ids = s.host[:2], s.grad[:2], s.top[:2], s.ids[:2]
     check_grad(s, s.saved[:2].cpu().numpy(), back[:2], 1.0, dtype=dtype)
     s.host, s.grad, s.top, s.ids = whole
+
+
+@pytest.mark.parametrize("h", [8, 33])
+def test_hidden_states_without_a_direction_do_not_converge(h):
+    """Infinities, values that are no numbers, zeros: their cosine is no number."""
+    K, V, n = 12, 200, 10
+    _, draft, top, ids, _, rng = make(23, K, V, n)
+    feat = np.repeat(rng.standard_normal((1, h)), K, 0).astype(np.float32)
+    feat[1, 3], feat[4, 0], feat[6, 2], feat[9] = np.inf, -np.inf, np.nan, 0.0
+    for tau in (-0.5, 0.5):
+        s = Step(draft, top, ids, feat=feat, tau_seq=tau, c=3.0)
+        s.forward()
+        with np.errstate(invalid="ignore"):
+            ref = TO.distill_loss(s.host, top, ids, feat=feat, tau=tau, c=3.0)
+        assert ref[1][:, 3].tolist() == [1, 1, 3, 1, 1, 1, 1, 3, 1, 1, 3, 1]
+        check_loss(s, ref)
