@@ -11,6 +11,7 @@
 // memory, as the gradient does it, 494 us: too much work an element.)  The gradient goes in stretches: the stored entries that fall into one
 // go into shared memory at their tokens' places, then the logits, already requested, are worked on beside them.
 #include "cascade_internal.h"
+#include "overlap.h"
 #include "ptx_paged.cuh"
 
 namespace {
@@ -567,16 +568,10 @@ int launch_grad(const GradArgs& in, cudaStream_t s) {
 
 bool off(const void* p, unsigned align) { return (reinterpret_cast<uintptr_t>(p) & (align - 1)) != 0; }
 
-bool meets(const void* a, uintptr_t a_bytes, const void* b, uintptr_t b_bytes) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return a != nullptr && b != nullptr && x < y + b_bytes && y < x + a_bytes;
-}
-
-// Bytes from the first to the last element of K rows of n elements (more than any memory has counts as 2^62).
-uintptr_t span(int K, int n, long long stride, int es) {
-  const __int128 bytes = ((__int128)(K - 1) * stride + n) * es;
-  return bytes < 1ll << 62 ? (uintptr_t)bytes : (uintptr_t)1 << 62;
-}
+using cascade_detail::Rows;
+// K rows of n elements of `es` bytes, `stride` elements apart (none where nothing is given).
+Rows rows(const void* at, int64_t K, int64_t n, int64_t stride, int es) { return {at, at != nullptr ? K : 0, stride * es, n * es}; }
+Rows dense(const void* at, int64_t K, int64_t n) { return rows(at, K, n, n, 4); }
 
 }  // namespace
 
@@ -595,17 +590,14 @@ extern "C" int cascade_distill_loss(const void* draft_logits, int32_t logits_dty
   if (off(draft_logits, es) || off(top_logits, 4) || off(top_ids, 4) || off(target_lse, 4) || off(feat, 4) || off(seq, 4) ||
       off(loss_out, 4) || off(saved_out, 16) || off(total_out, 4))
     return CASCADE_ERR_INVALID_ARG;
-  const struct {
-    const void* at;
-    uintptr_t bytes;
-  } in[] = {{draft_logits, span(K, V, row_stride, es)}, {top_logits, span(K, n_top, n_top, 4)}, {top_ids, span(K, n_top, n_top, 4)},
-            {target_lse, span(K, 1, 1, 4)}, {feat, span(K, h, h, 4)}, {seq, span(K, 1, 1, 4)}},
-    out[] = {{loss_out, span(K, 1, 1, 4)}, {saved_out, span(K, 4, 4, 4)}, {total_out, 4}};
+  const Rows in[] = {rows(draft_logits, K, V, row_stride, es), dense(top_logits, K, n_top), dense(top_ids, K, n_top),
+                     dense(target_lse, K, 1), dense(feat, K, h), dense(seq, K, 1)},
+             out[] = {dense(loss_out, K, 1), dense(saved_out, K, 4), dense(total_out, 1, 1)};
   for (int i = 0; i < 3; ++i) {
-    for (const auto& x : in)
-      if (meets(out[i].at, out[i].bytes, x.at, x.bytes)) return CASCADE_ERR_INVALID_ARG;
+    for (const Rows& x : in)
+      if (meet(out[i], x)) return CASCADE_ERR_INVALID_ARG;
     for (int j = 0; j < i; ++j)
-      if (meets(out[i].at, out[i].bytes, out[j].at, out[j].bytes)) return CASCADE_ERR_INVALID_ARG;
+      if (meet(out[i], out[j])) return CASCADE_ERR_INVALID_ARG;
   }
   LossArgs a;
   a.draft = draft_logits;
@@ -654,12 +646,11 @@ extern "C" int cascade_distill_grad(const void* draft_logits, int32_t logits_dty
   const int es = logits_dtype == CASCADE_BF16 ? 2 : 4;
   if (off(draft_logits, es) || off(grad_out, es) || off(top_logits, 4) || off(top_ids, 4) || off(saved, 16) || off(grad_loss, 4))
     return CASCADE_ERR_INVALID_ARG;
-  const uintptr_t bytes = span(K, V, grad_stride, es), stored = span(K, n_top, n_top, 4);
+  const Rows out = rows(grad_out, K, V, grad_stride, es), logits = rows(draft_logits, K, V, row_stride, es);
   const bool in_place = grad_out == draft_logits && (grad_stride == row_stride || K == 1);
-  if ((!in_place && meets(grad_out, bytes, draft_logits, span(K, V, row_stride, es))) || meets(grad_out, bytes, top_logits, stored) ||
-      meets(grad_out, bytes, top_ids, stored) || meets(grad_out, bytes, saved, span(K, 4, 4, 4)) ||
-      meets(grad_out, bytes, grad_loss, span(K, 1, 1, 4)))
-    return CASCADE_ERR_INVALID_ARG;
+  if (!in_place && meet(out, logits)) return CASCADE_ERR_INVALID_ARG;
+  for (const Rows& x : {dense(top_logits, K, n_top), dense(top_ids, K, n_top), dense(saved, K, 4), dense(grad_loss, K, 1)})
+    if (meet(out, x)) return CASCADE_ERR_INVALID_ARG;
   GradArgs a;
   a.draft = draft_logits;
   a.top = top_logits;

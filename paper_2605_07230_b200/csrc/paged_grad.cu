@@ -1,10 +1,13 @@
 // The gradient of the attention over a paged cache: checks, the rows' statistics, and the choice of kernels.
 #include <climits>
 
+#include "overlap.h"
 #include "paged.h"
 #include "paged_grad_tc.cuh"
 
 namespace {
+
+using cascade_detail::Rows;
 
 constexpr int kMaxGroup = 128;               // query heads a key head: they share a row block
 constexpr int kMaxKeys = INT32_MAX - 65535;  // so that a key's index rounded up to a tile stays in 32 bits
@@ -48,24 +51,6 @@ int launch_stats(cascade_ctx* ctx, const PagedGradArgs& p, const float* lse, cud
   k_paged_grad_stats<E, D><<<(unsigned)(blocks < most ? blocks : most), kThreads, 0, s>>>(p, lse);
   CASCADE_CUDA_TRY(cudaGetLastError());
   return CASCADE_OK;
-}
-
-// `n` rows of `width` bytes that start `stride` bytes apart.
-struct Rows {
-  const void* at;
-  int64_t n, stride, width;
-  uintptr_t span() const {                                             // (more than any memory has counts as 2^62)
-    const __int128 bytes = n == 0 ? 0 : (__int128)(n - 1) * stride + width;
-    return bytes < (int64_t)1 << 62 ? (uintptr_t)bytes : (uintptr_t)1 << 62;
-  }
-};
-// Whether two of them share a byte; rows that lie between each other may have one common stride.
-bool meet(const Rows& a, const Rows& b) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
-  if (a.n == 0 || b.n == 0 || x >= y + b.span() || y >= x + a.span()) return false;
-  if (a.stride != b.stride) return true;
-  const int64_t d = (int64_t)(y > x ? (y - x) % a.stride : (a.stride - (x - y) % a.stride) % a.stride);   // b's rows behind a's
-  return d < a.width || d + b.width > a.stride;
 }
 
 }  // namespace

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from oracle import train_oracle as TO
+from paper_2605_07230_b200 import binding as cb
 from tests import gpu_util as G
 from tests.test_gpu_distill import Step, check_grad, check_loss, dev, make
 
@@ -101,3 +102,21 @@ def test_hidden_states_without_a_direction_do_not_converge(h):
             ref = TO.distill_loss(s.host, top, ids, feat=feat, tau=tau, c=3.0)
         assert ref[1][:, 3].tolist() == [1, 1, 3, 1, 1, 1, 1, 3, 1, 1, 3, 1]
         check_loss(s, ref)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("K,V", [(7, 1003), (300, 65), (1, 129)])
+def test_gradient_rows_between_the_logits_rows(K, V, dtype):
+    """Logits and gradients as halves of one buffer's rows, either first."""
+    _, draft, top, ids, _, _ = make(24, K, V, 20)
+    for first in (0, 1):
+        s = Step(draft, top, ids, dtype)
+        rows = torch.full((K, 2, V + 3), float("nan"), device=G.DEV, dtype=s.draft.dtype)
+        rows[:, first, :V] = s.draft
+        s.draft, s.grad = rows[:, first, :V], rows[:, 1 - first, :V]
+        s.forward()
+        s.backward()
+        check_grad(s, s.saved.cpu().numpy(), None, 1.0, dtype=dtype)
+        assert np.array_equal(s.draft.float().cpu().numpy(), s.host) and rows[:, :, V:].isnan().all()
+    with pytest.raises(cb.CascadeError):                             # by one element into the logits
+        cb.cascade_distill_grad(rows[:, 0, :V], s.top, s.ids, s.saved, rows.view(K, -1)[:, V - 1: 2 * V - 1])
