@@ -8,6 +8,7 @@
 // five, but no atomics, no fp32 copy of dQ and the same bits every time.
 #pragma once
 #include "paged_attn.cuh"
+#include "paged_range.h"
 
 struct PagedGradArgs {
   PagedAttnArgs a;             // (a.out is read)
@@ -36,12 +37,6 @@ __device__ __forceinline__ bool load_request(const PagedGradArgs& p, int r, Grad
   return ok;
 }
 
-// Tokens of a request (first position x0, nq of them) that see any of the keys k_first .. k_last: [*lo, *hi).
-__device__ __forceinline__ void tokens_that_see(const PagedAttnArgs& a, int x0, int nq, int k_first, int k_last, int* lo, int* hi) {
-  *lo = max(0, k_first - x0);
-  *hi = nq;
-  if (a.window > 0 && k_first >= a.sinks) *hi = (int)min((long long)nq, (long long)k_last + a.window - x0);
-}
 __device__ __forceinline__ bool sees(const PagedAttnArgs& a, int x, int j) {
   return j <= x && (a.window == 0 || j >= window_begin(x, a.window) || j < a.sinks);
 }

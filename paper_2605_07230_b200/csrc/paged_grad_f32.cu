@@ -218,10 +218,7 @@ __device__ __forceinline__ void pass(const F32Args& f, uint8_t* smem, Shared& sh
   // what is walked over: rows [walk, end) that see any of the keys, or keys up to the last that a row sees
   int walk, end, begin = 0, sink_end = 0;
   if (kKeys) {
-    int lo, hi;
-    paged::tokens_that_see(a, x0, rq.nq, first, first + n_own - 1, &lo, &hi);
-    walk = lo * G;
-    end = hi * G;
+    paged::rows_that_see(a, x0, rq.nq, G, first, first + n_own - 1, &walk, &end);
   } else {
     begin = paged::window_begin(max(x0 + first / G, 0), a.window) / kStep * kStep;
     sink_end = min(a.sinks, begin);
@@ -400,12 +397,7 @@ __device__ __forceinline__ void pass(const F32Args& f, uint8_t* smem, Shared& sh
   int see_lo = 0, see_hi = 0, x = -1, x_begin = 0;
   float lse = 0.f, delta = 0.f;
   if (kKeys) {
-    if (mine_line < n_own && sh.own_there[mine_line]) {
-      int lo, hi;
-      paged::tokens_that_see(a, x0, rq.nq, n_mine, n_mine, &lo, &hi);
-      see_lo = lo * G;
-      see_hi = hi * G;
-    }
+    if (mine_line < n_own && sh.own_there[mine_line]) paged::rows_that_see(a, x0, rq.nq, G, n_mine, n_mine, &see_lo, &see_hi);
   } else if (mine_line < n_own) {
     const int tok = f.group.page(n_mine);
     x = x0 + tok;
