@@ -120,3 +120,48 @@ def test_gradient_rows_between_the_logits_rows(K, V, dtype):
         assert np.array_equal(s.draft.float().cpu().numpy(), s.host) and rows[:, :, V:].isnan().all()
     with pytest.raises(cb.CascadeError):                             # by one element into the logits
         cb.cascade_distill_grad(rows[:, 0, :V], s.top, s.ids, s.saved, rows.view(K, -1)[:, V - 1: 2 * V - 1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("K,V,n", [(5, 100, 300), (20000, 9, 4), (2, 300001, 700), (4000, 1031, 257)])
+def test_more_entries_than_tokens_and_more_rows_than_blocks_at_once(K, V, n, dtype):
+    rng = np.random.default_rng(V)
+    draft = rng.normal(0, 2, (K, V)).astype(np.float32)
+    ids = rng.integers(-1, V + 1, (K, n)).astype(np.int32)           # given several times, and places without an entry
+    top = rng.normal(0, 2, (K, n)).astype(np.float32)
+    s = Step(draft, top, ids, dtype)
+    s.forward()
+    some = np.unique(np.linspace(0, K - 1, 60).astype(int))
+    at = torch.as_tensor(some, device=G.DEV)
+    total, losses = float(s.total), s.loss.double().cpu().numpy()
+    s.host, s.loss, s.top, s.ids = s.host[some], s.loss[at], s.top[at], s.ids[at]
+    kept, whole = s.saved, s.total.clone()
+    s.saved, s.total = s.saved[at], s.loss.double().sum().float()
+    check_loss(s, TO.distill_loss(s.host, top[some], ids[some]))
+    assert abs(total - losses.sum()) <= 2.0**-23 * losses.sum()
+    s.saved, s.total, s.top, s.ids = kept, whole, dev(top), dev(ids, torch.int32)
+    s.backward()
+    got = s.grad[at].float().cpu().numpy()
+    want = TO.distill_grad(s.host, top[some], ids[some], kept[at].cpu().numpy())
+    # a token's weights, at most n of them that add up to 1: (n + 4) roundings of 32 bits; exponents of at most 64 rounded three times
+    tol = (n + 4 + 3 * 64 + 8) * 2.0**-24 + (2.0**-8 if dtype == "bf16" else 0) * np.abs(want)
+    assert (np.abs(got - want) <= tol).all(), np.abs(got - want).max()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_arrays_that_begin_at_any_number(dtype):
+    """Hidden states, entries and losses 4 bytes behind a boundary of 16."""
+    K, V, n, h = 9, 501, 33, 16
+    _, draft, top, ids, feat, _ = make(25, K, V, n, h)
+    s = Step(draft, top, ids, dtype, feat=feat, target_lse=np.full(K, 20.0, np.float32), seq=np.zeros(K), tau_seq=0.6)
+    def shift(t):
+        store = torch.zeros(t.numel() + 1, device=G.DEV, dtype=t.dtype)
+        store[1:] = t.reshape(-1)
+        return store[1:].view(t.shape)
+    s.top, s.ids, s.loss, s.total = (shift(t) for t in (s.top, s.ids, s.loss, s.total))
+    for name in ("feat", "target_lse", "seq"):
+        s.kw[name] = shift(s.kw[name])
+    s.forward()
+    check_loss(s, TO.distill_loss(s.host, top, ids, target_lse=np.full(K, 20.0), feat=feat, seq=np.zeros(K), tau=0.6))
+    s.backward(grad_loss=shift(torch.ones(K, device=G.DEV)))
+    check_grad(s, s.saved.cpu().numpy(), np.ones(K), 1.0, dtype=dtype)
