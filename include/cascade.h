@@ -513,8 +513,8 @@ int cascade_paged_attn(cascade_ctx* ctx, const cascade_paged_cache* cache, int32
  * do not see it, a key's.  Keys of a page outside the pool count as not seen, by rows that are summed again key by key
  * (CASCADE_ERR_BAD_PAGE); their dk and dv are zeros.  A row or key whose result is not finite is summed again the same way.
  * Statistics, sums and accumulators are fp32.  bf16: weights and their gradients (P, dS) are rounded to bf16 for their products, the
- * weights being right to 3e-6 before.  fp32: a product counts to 2^-25 of its size (three bf16 parts a number).  The same call leaves
- * the same bits every time. */
+ * weights before being right to 3e-6 + 1.2e-7 (|score| + |lse|), beside what a score's 32-bit sum leaves.  fp32: a product counts to
+ * 2^-24 of its size (three bf16 parts a number).  The same call leaves the same bits every time. */
 int cascade_paged_attn_grad(cascade_ctx* ctx, const cascade_paged_cache* cache, int32_t n_req, int32_t n_tok, const void* q,
                             int64_t q_stride, const int32_t* q_begin, const int32_t* kv_len, int32_t max_q, int32_t max_kv,
                             int32_t window, int32_t sinks, float softmax_scale, const void* out, const float* lse,
@@ -588,7 +588,9 @@ int cascade_drafter_loss(const float* target_logits, const float* draft_logits, 
  *     replaces the logits.  Where scale * grad_loss[k] * w_k is 0 the row is zeros.  But for that no output overlaps another or
  *     an input (CASCADE_ERR_INVALID_ARG).
  * Elsewhere a logit that is no number, or +inf, makes its position's loss and gradient NaN; one of -inf has p = 0.
- * Sums and statistics are 32 bits (the sums over stored entries and of the cosine 64); a bf16 gradient is rounded once.
+ * Sums and statistics are 32 bits (the sums over stored entries and of the cosine 64); a bf16 gradient is rounded once.  The
+ * gradient's p and q come from the saved 32-bit sums: relative to their size they are right to 4e-7 + 2.4e-7 (|d| + |lse|), logits
+ * and sums over T, so that a temperature far below the logits' size costs them bits.
  * The same call leaves the same bits every time.  No context is needed and nothing is allocated; one kernel each, and one for
  * total_out.  Errors: CASCADE_ERR_INVALID_ARG (null pointers, sizes < 1, 1e-30 <= temperature <= 1e30 not met, c <= 0, NaN
  * threshold). */

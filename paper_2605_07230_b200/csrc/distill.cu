@@ -7,7 +7,7 @@
 // with m the row's maximum, Z = sum_v exp((d_v - m) / T), Q = sum_i q_i.
 //
 // Both are memory-bound and walk over a row once.  The loss looks the drafter's logits of the stored tokens up behind the row, from the
-// L1 or L2.  (In front of it 292 to 322 us for 4608 rows of 65536 where this takes 245, since memory gives 64 bytes for 4; from shared
+// L1 or L2.  (In front of it 292 to 322 us for 4608 rows of 65536 where this takes 246, since memory gives 64 bytes for 4; from shared
 // memory, as the gradient does it, 494 us: too much work an element.)  The gradient goes in stretches: the stored entries that fall into one
 // go into shared memory at their tokens' places, then the logits, already requested, are worked on beside them.
 #include "cascade_internal.h"
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) k_distill_loss(cons
       add(sd, ref_d, x, c);
     }
   }
-  // the drafter's logits of the stored tokens, from the L2
+  // the drafter's logits of the stored tokens, from the L1 or L2
   float dv[kHold];
 #pragma unroll
   for (int k = 0; k < kHold; ++k) dv[k] = stored.token[k] >= 0 ? to_float(d[stored.token[k]]) : 0.f;
@@ -526,11 +526,11 @@ int launch_loss(const LossArgs& in, cudaStream_t s) {
   a.splits = 1;
   while (a.splits < kMaxSplits && bytes >= a.splits * 8192ll && (long long)a.K * a.splits * 2 <= 4 * sms) a.splits *= 2;
   if ((long long)a.K * a.splits > INT32_MAX) return CASCADE_ERR_UNSUPPORTED_SHAPE;
-  // Many parts take 128 threads, more of them being on an SM at once (1153 bf16 rows of 10007, 333 entries: 14.4 us, 256 threads
-  // 18.4 us), unless there are more stored entries than they hold in registers and the part is long: the logits of the entries
-  // should still be in the L1 or L2 at its end, so that fewer rows are to be under way (4608 rows of 262144 bytes, 2000 entries: 512
-  // threads 245 us, 256 295 us, 128 334 us; 1000 entries, by loads past the L1: 249, 244, 264 us).  A few hundred rows leave room for 256 (300 rows of 65536, 400
-  // entries: 20 us, 128 threads 23 us).
+  // Many parts take 128 threads, more of them being on an SM at once (1153 bf16 rows of 10007, 300 entries: 16 us, 256 threads 21 us),
+  // unless there are more stored entries than they hold in registers and the part is long: the logits of the entries should still be in
+  // the L1 or L2 at its end, so that fewer rows are to be under way (4608 rows of 262144 bytes, 2000 entries: 512 threads 243 us, 256
+  // 288 us, 128 336 us; 1000 entries: 233, 222, 257 us; rows of 131072 bytes, 2000 entries: 172, 157, 203 us; of 65536 bytes: 123, 113,
+  // 113 us).  A few hundred rows leave room for 256 (400 rows of 65536, 300 entries: 27 us, 128 threads 35 us).
   const long long part = bytes / a.splits;
   const int n = (a.n + a.splits - 1) / a.splits;
   const int threads = a.splits == 1 && a.K <= 4 * sms                                         ? 256

@@ -1,7 +1,7 @@
 // The gradient of the attention over a paged cache in 32 bits, on the tensor cores.
 //
-// A 32-bit number is the sum of three bf16 numbers h + m + l (8 bits each, to the last bit); of a product's nine terms the six from
-// 2^-18 up are formed, ll, ml and lm are left out (2^-26 of the product).  A product's terms go into the accumulator the smallest first,
+// A 32-bit number is the sum of three bf16 numbers h + m + l (8 bits each, to the last bit: m up to 2^-8 of it, l up to 2^-17); of a
+// product's nine terms six are formed, ll, ml and lm are left out (2^-24 of the product).  They go into the accumulator the smallest first,
 // so that what the tensor cores' additions cut off counts at the size of hh alone; products of one step start from zero and are added
 // up in registers.
 //

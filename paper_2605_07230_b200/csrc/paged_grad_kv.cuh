@@ -4,7 +4,7 @@
 // see any of them.  One CTA an SM works through items that a counter hands out.  With rows on the columns, per block:
 //     S^T = K Q^T      P^T = 2^(c S^T - lse)      dP^T = V dO^T      dS^T = P^T (dP^T - delta)      dV += P^T dO      dK += dS^T Q
 // S^T, dP^T, dV and dK fill the tensor memory (4 x 128 columns at D = 128); P^T and dS^T go back as bf16 over their own scores
-// and are the products' operand from there (both operands have one type: 2^-9 of a weight, which leaves an error of 0.0024 of the
+// and are the products' operand from there (both operands have one type: 2^-8 of a weight at most, which leaves an error of 0.0024 of the
 // results' size where results rounded once have 0.0017).  The products of one block alternate with the next block's scores:
 //     dV, S^T of the next block  beside the computation of dS^T;   dK, dP^T of the next block  beside that of P^T
 //   * warp 8 loads keys and values once an item, queries through three stages (the next block's are wanted right behind the

@@ -4,9 +4,9 @@
 // which the products alone need 2.0 and 1.5).  Where there are many items a CTA that finds no more goes on with the other pass.
 //
 // 8 sequences of 2480 tokens, 32 heads of 128: 1.57 to 1.72 ms, 590 to 640 TFLOP/s of the five products that have to be, 820 to 900 of the
-// seven that are formed (the card's best: 1694); 2 of 640 tokens: 64 us; 12 of 100 to 1144, 20 heads of 64: 166 us.  The tensor cores
-// are busy 52 % (keys) and 57 % (queries) of the time.  What holds them up: the first and last steps of an item, which nothing lies
-// beside (7 and 9 thousand cycles an item), and weights and their gradients on the way through the registers.
+// seven that are formed (the card's best: 1694); 2 of 640 tokens: 63 us; 12 of 100 to 1144, 20 heads of 64: 168 us.  On 2 sequences of
+// 2480 tokens (393 us) the tensor cores are busy 53 % of the time.  What holds them up: the first and last steps of an item, which nothing
+// lies beside (7 and 9 thousand cycles an item), and weights and their gradients on the way through the registers.
 #include "paged_grad_kv.cuh"
 #include "paged_grad_q.cuh"
 

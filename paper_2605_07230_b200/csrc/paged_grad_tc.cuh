@@ -162,7 +162,7 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
 }
 
 // 2^x of a pair.  kPoly: on the multiply-add units, 1 + r (c1 + r (c2 + r (c3 + r c4))) with r = x - round(x) in [-1/2, 1/2] (least
-// largest error of that form: 2.9e-6 relative, where the weights are rounded to 2^-9), times 2^round(x); below -127 exactly 0, no
+// largest error of that form: 2.9e-6 relative, where the weights are rounded to 2^-8), times 2^round(x); below -127 exactly 0, no
 // number stays none.  A third of the weights goes there: 16 exponentials a cycle and SM take 1024 cycles a 128 x 128 tile.
 template <bool kPoly>
 __device__ __forceinline__ uint64_t pow2(uint64_t x) {
